@@ -7,7 +7,8 @@ the points of each cell are summed. The work runs in libbevpool.so
 (hand-written HIP for gfx950) behind the C ABI of include/bevpool.h. This
 package is the thin binding: ``_binding`` mirrors the C calls one to one, and
 ``Plan`` adds torch tensor plumbing (device memory and the current stream
-only). There is no CPU fallback. A missing library raises ImportError.
+only). ``group_norm_act``, ``cross_attention`` and ``dropout_add`` are the
+operators of a model that reads the pooled map (include/bevmap.h). There is no CPU fallback. A missing library raises ImportError.
 """
 from __future__ import annotations
 
@@ -22,6 +23,7 @@ from ._binding import (BEVPOOL_BF16, BEVPOOL_F16, BEVPOOL_F32, BEVPOOL_MAX, BEVP
                        bevpool_plan, bevpool_plan_destroy, bevpool_plan_export,
                        bevpool_plan_import, bevpool_associate_noalloc, bevpool_plan_slabs,
                        bevpool_plan_info_get, bevpool_version)
+from .map_ops import cross_attention, dropout_add, group_norm_act
 
 __all__ = [
     "Plan", "SlabPlan", "bev_pool", "BevpoolError", "bevpool_plan", "bevpool_forward", "bevpool_forward_ex",
@@ -31,6 +33,7 @@ __all__ = [
     "bevpool_plan_export", "bevpool_plan_import", "bevpool_plan_destroy", "bevpool_last_error", "bevpool_version",
     "bevpool_geometry", "geometry_of", "BEVPOOL_F32", "BEVPOOL_BF16", "BEVPOOL_F16",
     "bevpool_associate_noalloc", "associate_noalloc", "bevpool_plan_slabs",
+    "group_norm_act", "cross_attention", "dropout_add",
 ]
 
 _GEOM_FIELDS = [f for f, _ in bevpool_geometry._fields_]

@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(HERE, "libbevpool.so")
 # measurement probe for bench.py --floor (not part of the pooling library)
 FLOOR_SOURCE = "floor.hip"
 FLOOR_LIB_PATH = os.path.join(HERE, "libbevpool_floor.so")
-SOURCES = ["bevpool.hip", "plan.hip", "forward.hip", "backward.hip", "layout.hip"]
+SOURCES = ["bevpool.hip", "plan.hip", "forward.hip", "backward.hip", "layout.hip",
+           "mapops.hip", "norm.hip", "dropout.hip", "attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -112,7 +112,7 @@ extern "C" {
 
 const char *bevpool_last_error(void) { return g_last_error; }
 
-int32_t bevpool_version(void) { return 200; }  // 0.2.0: bevpool_forward_ex
+int32_t bevpool_version(void) { return 300; }  // 0.3.0: bevmap.h
 
 namespace {
 // Sizes and parameters of a geometry (both plan constructors).

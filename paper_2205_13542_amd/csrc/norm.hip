@@ -1,0 +1,589 @@
+// Group norm with an activation, channels last, and its gradients
+// (bevmap_group_norm, bevmap_group_norm_backward).
+//
+// Both directions are two passes over the frame, a sum and an apply, and are
+// bound by memory. In the sum pass a workgroup takes a chunk of rows of one frame;
+// a thread keeps to V neighbouring channels and walks the chunk's rows, so that a
+// wave reads whole stretches of rows whatever a group's width, and forms its
+// channels' statistics in registers. Statistics travel as (mean, sum of squared
+// deviations) and are joined by
+//   mean = sum n_i mean_i / n,  M2 = sum M2_i + sum n_i (mean_i - mean)^2,
+// so a large common offset costs no precision. In the apply pass every workgroup
+// joins the chunks' statistics of its frame (they are few, and in cache) and
+// then streams rows.
+#include "mapops.h"
+
+namespace bevmap {
+namespace {
+
+constexpr int kNormBlock = 256;
+constexpr int kNormRows = 4;        // rows that a thread has in flight
+constexpr int kMergeLanes = 16;     // lanes that join one group's parts
+constexpr int kWgradChannels = 16;  // channels of a workgroup that sums weight gradients
+
+struct NormArgs {
+    const void *x, *dy, *weight, *bias;
+    void *y, *dx, *dweight, *dbias;
+    float *mean, *rstd;             // [B][G]
+    float2 *parts;                  // [B][chunks][G]
+    float *channel_sums;            // backward: [B][chunks][2][C]
+    int64_t ldx;
+    int32_t batch, rows, C, G, per; // per: channels of a group
+    int32_t chunk, n_chunks;        // rows of a chunk, chunks of a frame
+    int32_t apply_rows, n_apply;    // the same for the apply pass
+    int32_t y_dtype, w_dtype, act;
+    float eps;
+};
+
+__device__ __forceinline__ float activate(float z, int act) {
+    switch (act) {
+        case BEVMAP_ACT_RELU: return z < 0.0f ? 0.0f : z;
+        case BEVMAP_ACT_SILU: return z / (1.0f + __expf(-z));
+        case BEVMAP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+        default: return z;
+    }
+}
+
+__device__ __forceinline__ float slope(float z, int act) {
+    switch (act) {
+        case BEVMAP_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+        case BEVMAP_ACT_SILU: {
+            const float s = 1.0f / (1.0f + __expf(-z));
+            return s * (1.0f + z * (1.0f - s));
+        }
+        case BEVMAP_ACT_GELU:
+            return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * __expf(-0.5f * z * z) * 0.39894228f;
+        default: return 1.0f;
+    }
+}
+
+__device__ __forceinline__ float weight_at(const void *w, int c, int dtype, float none) {
+    float v = none;
+    if (w) load_any<1>(w, c, dtype, &v);
+    return v;
+}
+
+__device__ __forceinline__ float lane_sum(float v) {     // over kMergeLanes lanes
+#pragma unroll
+    for (int m = 1; m < kMergeLanes; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Columns of a block of vectors: thread -> (row lane, vector).
+struct Columns {
+    int vectors, lanes;   // vectors of this block, row lanes that walk it
+    int lane, vec;        // of this thread; lane >= lanes: idle
+};
+__device__ __forceinline__ Columns columns(int first, int n_vec) {
+    Columns c;
+    c.vectors = min(kNormBlock, n_vec - first);
+    c.lanes = kNormBlock / c.vectors;
+    c.lane = threadIdx.x / c.vectors;
+    c.vec = first + threadIdx.x - c.lane * c.vectors;
+    return c;
+}
+
+// Statistics of a chunk of rows: parts[b][chunk][g] = (mean, M2).
+template <int DT, int V>
+__global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
+    using T = typename Num<DT>::T;
+    extern __shared__ float lds[];
+    float *ch_mean = lds, *ch_m2 = lds + a.C;             // [C] each
+    float *th = lds + 2 * a.C;                            // [2][lanes][V * vectors]
+    const int b = blockIdx.y, r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const int n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
+    for (int first = 0; first < n_vec; first += kNormBlock) {
+        const Columns c = columns(first, n_vec);
+        float mean[V], m2[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f;
+        int n = 0;
+        if (c.lane < c.lanes) {
+            const T *p = x + c.vec * V;
+            int r = r0 + c.lane;
+            for (; r + (kNormRows - 1) * c.lanes < r1; r += kNormRows * c.lanes) {
+                float v[kNormRows][V];
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) load_n<T, V>(p + int64_t(r + k * c.lanes) * a.ldx, v[k]);
+                // join kNormRows values of each channel to the n before them
+                const float share = float(kNormRows) / float(n + kNormRows), both = float(n) * share;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float m = 0.0f, q = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kNormRows; ++k) m += v[k][i];
+                    m *= 1.0f / kNormRows;
+#pragma unroll
+                    for (int k = 0; k < kNormRows; ++k) q = fmaf(v[k][i] - m, v[k][i] - m, q);
+                    const float d = m - mean[i];
+                    mean[i] = fmaf(d, share, mean[i]);
+                    m2[i] += fmaf(d * d, both, q);
+                }
+                n += kNormRows;
+            }
+            for (; r < r1; r += c.lanes) {
+                float v[V];
+                load_n<T, V>(p + int64_t(r) * a.ldx, v);
+                const float share = 1.0f / float(n + 1), both = float(n) * share;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = v[i] - mean[i];
+                    mean[i] = fmaf(d, share, mean[i]);
+                    m2[i] = fmaf(d * d, both, m2[i]);
+                }
+                ++n;
+            }
+        }
+        const int width = c.vectors * V;                  // channels of this block of columns
+        if (c.lane < c.lanes) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                th[c.lane * width + (c.vec - first) * V + i] = mean[i];
+                th[(c.lanes + c.lane) * width + (c.vec - first) * V + i] = m2[i];
+            }
+        }
+        __syncthreads();
+        // join the row lanes; lane l walked ceil((rows - l) / lanes) rows
+        const int rows = r1 - r0;
+        for (int i = threadIdx.x; i < width; i += kNormBlock) {
+            float m = 0.0f, q = 0.0f;
+            for (int l = 0; l < c.lanes; ++l) m += th[l * width + i] * float((rows - l + c.lanes - 1) / c.lanes);
+            m /= float(rows);
+            for (int l = 0; l < c.lanes; ++l) {
+                const float d = th[l * width + i] - m;
+                q += th[(c.lanes + l) * width + i] + d * d * float((rows - l + c.lanes - 1) / c.lanes);
+            }
+            ch_mean[first * V + i] = m;
+            ch_m2[first * V + i] = q;
+        }
+        __syncthreads();
+    }
+    // join a group's channels, all of equal counts
+    const int lane = threadIdx.x % kMergeLanes;
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+        const int g = g0 + threadIdx.x / kMergeLanes;
+        float m = 0.0f, q = 0.0f;
+        if (g < a.G)
+            for (int c = lane; c < a.per; c += kMergeLanes) m += ch_mean[g * a.per + c];
+        m = lane_sum(m) / float(a.per);
+        if (g < a.G)
+            for (int c = lane; c < a.per; c += kMergeLanes) {
+                const float d = ch_mean[g * a.per + c] - m;
+                q += ch_m2[g * a.per + c] + d * d * float(r1 - r0);
+            }
+        q = lane_sum(q);
+        if (g < a.G && lane == 0) a.parts[(int64_t(b) * a.n_chunks + blockIdx.x) * a.G + g] = make_float2(m, q);
+    }
+}
+
+// Joins the chunks' statistics of frame b: group g's mean and rstd to LDS.
+__device__ __forceinline__ void join_chunks(const NormArgs &a, int b, float *mean, float *rstd, bool write) {
+    const int lane = threadIdx.x % kMergeLanes;
+    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
+    const float total = float(a.rows);
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+        const int g = g0 + threadIdx.x / kMergeLanes;
+        float m = 0.0f, q = 0.0f;
+        if (g < a.G)
+            for (int k = lane; k < a.n_chunks; k += kMergeLanes)
+                m += parts[int64_t(k) * a.G + g].x * float(min(a.chunk, a.rows - k * a.chunk));
+        m = lane_sum(m) / total;
+        if (g < a.G)
+            for (int k = lane; k < a.n_chunks; k += kMergeLanes) {
+                const float2 p = parts[int64_t(k) * a.G + g];
+                const float d = p.x - m;
+                q += p.y + d * d * (float(min(a.chunk, a.rows - k * a.chunk)) * float(a.per));
+            }
+        q = lane_sum(q);
+        if (g < a.G && lane == 0) {
+            const float rs = 1.0f / sqrtf(q / (total * float(a.per)) + a.eps);
+            mean[g] = m;
+            rstd[g] = rs;
+            if (write) {
+                a.mean[int64_t(b) * a.G + g] = m;
+                a.rstd[int64_t(b) * a.G + g] = rs;
+            }
+        }
+    }
+    __syncthreads();
+}
+
+template <int DT, int V>
+__global__ __launch_bounds__(kNormBlock) void k_norm_apply(NormArgs a) {
+    using T = typename Num<DT>::T;
+    extern __shared__ float lds[];
+    float *mean = lds, *rstd = lds + a.G;
+    const int b = blockIdx.y, r0 = blockIdx.x * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
+    join_chunks(a, b, mean, rstd, blockIdx.x == 0);
+    const int n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
+    const int64_t out0 = int64_t(b) * a.rows * a.C;
+    for (int first = 0; first < n_vec; first += kNormBlock) {
+        const Columns c = columns(first, n_vec);
+        if (c.lane >= c.lanes) continue;
+        float mu[V], mul[V], add[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int ch = c.vec * V + i, g = ch / a.per;
+            mu[i] = mean[g];
+            mul[i] = rstd[g] * weight_at(a.weight, ch, a.w_dtype, 1.0f);
+            add[i] = weight_at(a.bias, ch, a.w_dtype, 0.0f);
+        }
+        for (int r = r0 + c.lane; r < r1; r += kNormRows * c.lanes) {
+            float v[kNormRows][V];
+#pragma unroll
+            for (int k = 0; k < kNormRows; ++k)
+                if (r + k * c.lanes < r1) load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
+#pragma unroll
+            for (int k = 0; k < kNormRows; ++k) {
+                if (r + k * c.lanes >= r1) break;
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[k][i] = activate(fmaf(v[k][i] - mu[i], mul[i], add[i]), a.act);
+                store_any<V>(a.y, out0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, v[k]);
+            }
+        }
+    }
+}
+
+// Per channel sums over a chunk of dz and dz * xh, with dz = dy act'(z); and per
+// group those sums with the channels' weights: parts = (sum e, sum e xh), e = dz w.
+template <int DT, int V>
+__global__ __launch_bounds__(kNormBlock) void k_norm_grad_sum(NormArgs a) {
+    using T = typename Num<DT>::T;
+    extern __shared__ float lds[];
+    float *ch_sum = lds, *ch_dot = lds + a.C;
+    float *th = lds + 2 * a.C;
+    const int b = blockIdx.y, r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const int n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
+    const int64_t dy0 = int64_t(b) * a.rows * a.C;
+    float *sums = a.channel_sums + (int64_t(b) * a.n_chunks + blockIdx.x) * 2 * a.C;
+    for (int first = 0; first < n_vec; first += kNormBlock) {
+        const Columns c = columns(first, n_vec);
+        const int width = c.vectors * V;
+        if (c.lane < c.lanes) {
+            float mu[V], rs[V], w[V], add[V], sum[V], dot[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int ch = c.vec * V + i, g = ch / a.per;
+                mu[i] = a.mean[int64_t(b) * a.G + g];
+                rs[i] = a.rstd[int64_t(b) * a.G + g];
+                w[i] = weight_at(a.weight, ch, a.w_dtype, 1.0f);
+                add[i] = weight_at(a.bias, ch, a.w_dtype, 0.0f);
+                sum[i] = dot[i] = 0.0f;
+            }
+            for (int r = r0 + c.lane; r < r1; r += kNormRows * c.lanes) {
+                float v[kNormRows][V], d[kNormRows][V];
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k)
+                    if (r + k * c.lanes < r1) {
+                        load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
+                        load_any<V>(a.dy, dy0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, d[k]);
+                    }
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) {
+                    if (r + k * c.lanes >= r1) break;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float xh = (v[k][i] - mu[i]) * rs[i];
+                        const float dz = d[k][i] * slope(fmaf(xh, w[i], add[i]), a.act);
+                        sum[i] += dz;
+                        dot[i] = fmaf(dz, xh, dot[i]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                th[c.lane * width + (c.vec - first) * V + i] = sum[i];
+                th[(c.lanes + c.lane) * width + (c.vec - first) * V + i] = dot[i];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < width; i += kNormBlock) {
+            float s = 0.0f, d = 0.0f;
+            for (int l = 0; l < c.lanes; ++l) {
+                s += th[l * width + i];
+                d += th[(c.lanes + l) * width + i];
+            }
+            const int ch = first * V + i;
+            sums[ch] = s;
+            sums[a.C + ch] = d;
+            const float w = weight_at(a.weight, ch, a.w_dtype, 1.0f);
+            ch_sum[ch] = s * w;
+            ch_dot[ch] = d * w;
+        }
+        __syncthreads();
+    }
+    const int lane = threadIdx.x % kMergeLanes;
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+        const int g = g0 + threadIdx.x / kMergeLanes;
+        float s = 0.0f, d = 0.0f;
+        if (g < a.G)
+            for (int c = lane; c < a.per; c += kMergeLanes) {
+                s += ch_sum[g * a.per + c];
+                d += ch_dot[g * a.per + c];
+            }
+        s = lane_sum(s);
+        d = lane_sum(d);
+        if (g < a.G && lane == 0) a.parts[(int64_t(b) * a.n_chunks + blockIdx.x) * a.G + g] = make_float2(s, d);
+    }
+}
+
+// Weight gradients of kWgradChannels channels: the chunks' sums of all frames.
+__device__ __forceinline__ void weight_gradients(const NormArgs &a, int block, float *lds) {
+    const int ch = block * kWgradChannels + threadIdx.x % kWgradChannels;
+    const int lane = threadIdx.x / kWgradChannels, lanes = kNormBlock / kWgradChannels;
+    const int64_t n = int64_t(a.batch) * a.n_chunks;
+    float s = 0.0f, d = 0.0f;
+    if (ch < a.C)
+        for (int64_t k = lane; k < n; k += lanes) {
+            s += a.channel_sums[k * 2 * a.C + ch];
+            d += a.channel_sums[k * 2 * a.C + a.C + ch];
+        }
+    lds[threadIdx.x] = s;
+    lds[kNormBlock + threadIdx.x] = d;
+    __syncthreads();
+    if (lane == 0 && ch < a.C) {
+        s = d = 0.0f;
+        for (int l = 0; l < lanes; ++l) {
+            s += lds[l * kWgradChannels + threadIdx.x];
+            d += lds[kNormBlock + l * kWgradChannels + threadIdx.x];
+        }
+        if (a.dbias) store_any<1>(a.dbias, ch, a.w_dtype, &s);
+        if (a.dweight) store_any<1>(a.dweight, ch, a.w_dtype, &d);
+    }
+}
+
+// dx = rstd (e - mean(e) - xh mean(e xh)). The grid's last workgroups of frame 0
+// sum the weight gradients.
+template <int DT, int V>
+__global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
+    using T = typename Num<DT>::T;
+    extern __shared__ float lds[];
+    const int b = blockIdx.y;
+    if (int(blockIdx.x) >= a.n_apply) {
+        if (b == 0) weight_gradients(a, blockIdx.x - a.n_apply, lds);
+        return;
+    }
+    float *m1 = lds, *m2 = lds + a.G;
+    const int r0 = blockIdx.x * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
+    const int lane = threadIdx.x % kMergeLanes;
+    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+        const int g = g0 + threadIdx.x / kMergeLanes;
+        float s = 0.0f, d = 0.0f;
+        if (g < a.G)
+            for (int k = lane; k < a.n_chunks; k += kMergeLanes) {
+                const float2 p = parts[int64_t(k) * a.G + g];
+                s += p.x;
+                d += p.y;
+            }
+        s = lane_sum(s);
+        d = lane_sum(d);
+        if (g < a.G && lane == 0) {
+            const float inv = 1.0f / (float(a.rows) * float(a.per));
+            m1[g] = s * inv;
+            m2[g] = d * inv;
+        }
+    }
+    __syncthreads();
+    const int n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
+    T *dx = static_cast<T *>(a.dx) + int64_t(b) * a.rows * a.C;
+    const int64_t dy0 = int64_t(b) * a.rows * a.C;
+    for (int first = 0; first < n_vec; first += kNormBlock) {
+        const Columns c = columns(first, n_vec);
+        if (c.lane >= c.lanes) continue;
+        float mu[V], rs[V], w[V], add[V], e1[V], e2[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int ch = c.vec * V + i, g = ch / a.per;
+            mu[i] = a.mean[int64_t(b) * a.G + g];
+            rs[i] = a.rstd[int64_t(b) * a.G + g];
+            w[i] = weight_at(a.weight, ch, a.w_dtype, 1.0f);
+            add[i] = weight_at(a.bias, ch, a.w_dtype, 0.0f);
+            e1[i] = m1[g];
+            e2[i] = m2[g];
+        }
+        for (int r = r0 + c.lane; r < r1; r += kNormRows * c.lanes) {
+            float v[kNormRows][V], d[kNormRows][V];
+#pragma unroll
+            for (int k = 0; k < kNormRows; ++k)
+                if (r + k * c.lanes < r1) {
+                    load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
+                    load_any<V>(a.dy, dy0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, d[k]);
+                }
+#pragma unroll
+            for (int k = 0; k < kNormRows; ++k) {
+                if (r + k * c.lanes >= r1) break;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float xh = (v[k][i] - mu[i]) * rs[i];
+                    const float e = d[k][i] * slope(fmaf(xh, w[i], add[i]), a.act) * w[i];
+                    v[k][i] = rs[i] * (e - e1[i] - xh * e2[i]);
+                }
+                store_n<T, V>(dx + int64_t(r + k * c.lanes) * a.C + c.vec * V, v[k]);
+            }
+        }
+    }
+}
+
+constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
+constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
+constexpr int kMinRows = 16;        // rows of a chunk at least
+
+int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
+
+void split(const bevmap_norm &n, NormArgs *a) {
+    const int per_frame = kSumGrid / (n.batch < kSumGrid ? n.batch : kSumGrid);
+    a->chunk = ceil_div(n.pixels, per_frame);
+    if (a->chunk < kMinRows) a->chunk = kMinRows;
+    a->n_chunks = ceil_div(n.pixels, a->chunk);
+    const int apply = kApplyGrid / (n.batch < kApplyGrid ? n.batch : kApplyGrid);
+    a->apply_rows = ceil_div(n.pixels, apply);
+    if (a->apply_rows < kMinRows) a->apply_rows = kMinRows;
+    a->n_apply = ceil_div(n.pixels, a->apply_rows);
+}
+
+NormArgs fill(const bevmap_norm &n, const void *x, const void *weight, const void *bias, void *workspace) {
+    NormArgs a{};
+    a.x = x;
+    a.weight = weight;
+    a.bias = bias;
+    a.ldx = n.row_stride;
+    a.batch = n.batch;
+    a.rows = n.pixels;
+    a.C = n.channels;
+    a.G = n.groups;
+    a.per = n.channels / n.groups;
+    a.y_dtype = n.y_dtype;
+    a.w_dtype = n.weight_dtype;
+    a.act = n.act;
+    a.eps = n.eps;
+    split(n, &a);
+    a.parts = static_cast<float2 *>(workspace);
+    a.channel_sums = reinterpret_cast<float *>(a.parts + int64_t(n.batch) * a.n_chunks * n.groups);
+    return a;
+}
+
+// Elements of an access: the widest of 16 bytes of x and less that divides the
+// channels and that every tensor's alignment allows.
+int vector_of(const bevmap_norm &n, const void *x, const void *y, const void *dx) {
+    for (int v = n.x_dtype == BEVPOOL_F32 ? 4 : 8; v > 1; v >>= 1)
+        if (n.channels % v == 0 && aligned_for(x, n.row_stride, n.x_dtype, v) && aligned_for(y, 0, n.y_dtype, v) &&
+            (!dx || aligned_for(dx, 0, n.x_dtype, v)))
+            return v;
+    return 1;
+}
+
+// Bytes of LDS: two floats a channel, and two for each thread's V channels.
+size_t sum_lds(const NormArgs &a, int v) { return (2 * size_t(a.C) + 2 * size_t(kNormBlock) * v) * sizeof(float); }
+
+// Raises a kernel's limit of dynamic LDS where it needs more than the default.
+template <class K>
+int allow_lds(K kernel, size_t bytes) {
+    if (bytes > 64 * 1024)
+        BEVPOOL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                        hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)));
+    return BEVPOOL_OK;
+}
+
+template <int DT, int V>
+int forward(const NormArgs &a, hipStream_t stream) {
+    const size_t lds = sum_lds(a, V);
+    if (int rc = allow_lds(k_norm_sum<DT, V>, lds)) return rc;
+    hipLaunchKernelGGL((k_norm_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kNormBlock), lds, stream, a);
+    BEVPOOL_HIP(hipGetLastError());
+    const size_t lds2 = 2 * size_t(a.G) * sizeof(float);
+    if (int rc = allow_lds(k_norm_apply<DT, V>, lds2)) return rc;
+    hipLaunchKernelGGL((k_norm_apply<DT, V>), dim3(a.n_apply, a.batch), dim3(kNormBlock), lds2, stream, a);
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+template <int DT, int V>
+int backward(const NormArgs &a, hipStream_t stream) {
+    const size_t lds = sum_lds(a, V);
+    if (int rc = allow_lds(k_norm_grad_sum<DT, V>, lds)) return rc;
+    hipLaunchKernelGGL((k_norm_grad_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kNormBlock), lds, stream, a);
+    BEVPOOL_HIP(hipGetLastError());
+    const size_t lds2 = size_t(a.G > kNormBlock ? a.G : kNormBlock) * 2 * sizeof(float);
+    if (int rc = allow_lds(k_norm_grad_apply<DT, V>, lds2)) return rc;
+    const int extra = a.dweight || a.dbias ? ceil_div(a.C, kWgradChannels) : 0;
+    hipLaunchKernelGGL((k_norm_grad_apply<DT, V>), dim3(a.n_apply + extra, a.batch), dim3(kNormBlock), lds2, stream,
+                       a);
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+template <int DT>
+int dispatch(const NormArgs &a, int v, bool back, hipStream_t stream) {
+    switch (v) {
+        case 8:
+            if constexpr (DT != BEVPOOL_F32) return back ? backward<DT, 8>(a, stream) : forward<DT, 8>(a, stream);
+        case 4: return back ? backward<DT, 4>(a, stream) : forward<DT, 4>(a, stream);
+        case 2: return back ? backward<DT, 2>(a, stream) : forward<DT, 2>(a, stream);
+        default: return back ? backward<DT, 1>(a, stream) : forward<DT, 1>(a, stream);
+    }
+}
+
+int dispatch(int dtype, const NormArgs &a, int v, bool back, hipStream_t stream) {
+    switch (dtype) {
+        case BEVPOOL_F32: return dispatch<BEVPOOL_F32>(a, v, back, stream);
+        case BEVPOOL_BF16: return dispatch<BEVPOOL_BF16>(a, v, back, stream);
+        default: return dispatch<BEVPOOL_F16>(a, v, back, stream);
+    }
+}
+
+__global__ void k_zero_weights(void *a, void *b, int n, int dtype) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    const float zero = 0.0f;
+    if (i < n && a) store_any<1>(a, i, dtype, &zero);
+    if (i < n && b) store_any<1>(b, i, dtype, &zero);
+}
+
+}  // namespace
+}  // namespace bevmap
+
+using namespace bevmap;
+
+int64_t bevmap_norm_workspace_bytes(const bevmap_norm &n, bool backward) {
+    if (n.batch == 0 || n.pixels == 0) return 0;
+    NormArgs a{};
+    split(n, &a);
+    const int64_t chunks = int64_t(n.batch) * a.n_chunks;
+    return chunks * n.groups * int64_t(sizeof(float2)) +
+           (backward ? chunks * 2 * n.channels * int64_t(sizeof(float)) : 0);
+}
+
+int bevmap_launch_norm(const bevmap_norm &n, const void *x, const void *weight, const void *bias, void *y,
+                       float *mean, float *rstd, void *workspace, hipStream_t stream) {
+    if (n.batch == 0 || n.pixels == 0) return BEVPOOL_OK;
+    NormArgs a = fill(n, x, weight, bias, workspace);
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    return dispatch(n.x_dtype, a, vector_of(n, x, y, nullptr), false, stream);
+}
+
+int bevmap_launch_norm_backward(const bevmap_norm &n, const void *grad_y, const void *x, const void *weight,
+                                const void *bias, const float *mean, const float *rstd, void *grad_x,
+                                void *grad_weight, void *grad_bias, void *workspace, hipStream_t stream) {
+    if (n.batch == 0 || n.pixels == 0) {
+        if (grad_weight || grad_bias) {
+            hipLaunchKernelGGL(k_zero_weights, dim3(ceil_div(n.channels, kNormBlock)), dim3(kNormBlock), 0, stream,
+                               grad_weight, grad_bias, n.channels, n.weight_dtype);
+            BEVPOOL_HIP(hipGetLastError());
+        }
+        return BEVPOOL_OK;
+    }
+    NormArgs a = fill(n, x, weight, bias, workspace);
+    a.dy = grad_y;
+    a.dx = grad_x;
+    a.dweight = grad_weight;
+    a.dbias = grad_bias;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    return dispatch(n.x_dtype, a, vector_of(n, x, grad_y, grad_x), true, stream);
+}

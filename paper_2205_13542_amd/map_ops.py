@@ -1,0 +1,331 @@
+"""Operators of the model that reads a pooled map, channels last, with gradients.
+
+    normed = group_norm_act(bev, groups=8, weight=w, bias=b, act="silu", out_dtype=torch.bfloat16)
+    heard  = cross_attention(q, k, v, key_mask=seen)       # queries ask the map's cells
+    tokens = dropout_add(heard, 0.1, seed, step, residual=tokens)
+
+Each runs in libbevpool.so (include/bevmap.h) on the current stream of its
+inputs' device, and is differentiable. Temporaries come from torch's allocator.
+There is no CPU form: tensors elsewhere are refused with a BevpoolError, as
+are types and layouts that a call does not take (nothing is copied silently).
+"""
+from __future__ import annotations
+
+import math
+
+from . import _binding, _map_binding
+from ._binding import BevpoolError
+
+_ACTS = {"none": _map_binding.BEVMAP_ACT_NONE, "relu": _map_binding.BEVMAP_ACT_RELU,
+         "silu": _map_binding.BEVMAP_ACT_SILU, "gelu": _map_binding.BEVMAP_ACT_GELU}
+
+
+def _refuse(message, code=_binding.BEVPOOL_ERR_INVALID_ARG):
+    raise BevpoolError(code, message)
+
+
+_CODES = None
+
+
+def _code(dtype) -> int:
+    global _CODES
+    if _CODES is None:
+        import torch
+        _CODES = {torch.float32: _binding.BEVPOOL_F32, torch.bfloat16: _binding.BEVPOOL_BF16,
+                  torch.float16: _binding.BEVPOOL_F16}
+    code = _CODES.get(dtype)
+    if code is None:
+        _refuse(f"dtype {dtype}", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
+    return code
+
+
+def _row_stride(t):
+    """Elements from row to row (of the last dimension) if rows are evenly
+    spaced and their elements adjacent, else None."""
+    if t.is_contiguous():
+        return t.shape[-1] if t.dim() else 1
+    shape, strides = t.shape, t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        return None
+    step = expect = None
+    for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if size == 1:
+            continue
+        if step is None:
+            step = stride
+        elif stride != expect:
+            return None
+        expect = stride * size
+    return shape[-1] if step is None else step if step >= shape[-1] else None
+
+
+def _on(device, *tensors):
+    """Refuses tensors that are not all on one GPU."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            _refuse("all tensors must be on one device")
+    if device.type != "cuda":
+        _refuse("inputs must be device tensors")
+
+
+class _Current:
+    """Makes a device current and knows its current stream (an int)."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        self.stream = torch.cuda.current_stream(device).cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _ptr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
+    import torch
+    if x.dim() < 2:
+        _refuse("x must have a batch and a channel dimension")
+    _on(x.device, x, weight, bias)
+    if act not in _ACTS:
+        _refuse(f"act {act!r}")
+    C = x.shape[-1]
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None and (tuple(t.shape) != (C,) or not t.is_contiguous()):
+            _refuse(f"{name} must be a contiguous tensor of {C} elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        _refuse("weight and bias must share a dtype", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
+    stride = _row_stride(x)
+    if stride is None:
+        _refuse("rows of x must be evenly spaced, their channels adjacent")
+    w_like = weight if weight is not None else bias
+    norm = _map_binding.bevmap_norm(
+        x.shape[0], math.prod(x.shape[1:-1]), C, groups, stride, eps, _ACTS[act], _code(x.dtype),
+        _code(out_dtype or x.dtype), _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
+    size = _map_binding.bevmap_group_norm_workspace(norm, False)
+    y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+    stats = torch.empty((2, x.shape[0], groups), dtype=torch.float32, device=x.device)
+    space = torch.empty(size, dtype=torch.uint8, device=x.device)
+    mean = stats.data_ptr()
+    with _Current(x.device) as stream:
+        _map_binding.bevmap_group_norm(norm, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean,
+                                       mean + 4 * x.shape[0] * groups, space.data_ptr(), size, stream)
+    return y, stats, norm
+
+
+def _norm_backward(norm, stats, dy, x, weight, bias, want_weight, want_bias):
+    import torch
+    size = _map_binding.bevmap_group_norm_workspace(norm, True)
+    dy = dy.contiguous()
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw = torch.empty_like(weight) if want_weight else None
+    db = torch.empty_like(bias) if want_bias else None
+    space = torch.empty(size, dtype=torch.uint8, device=x.device)
+    mean = stats.data_ptr()
+    with _Current(x.device) as stream:
+        _map_binding.bevmap_group_norm_backward(norm, dy.data_ptr(), x.data_ptr(), _ptr(weight), _ptr(bias), mean,
+                                                mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw),
+                                                _ptr(db), space.data_ptr(), size, stream)
+    return dx, dw, db
+
+
+def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
+    import torch
+    _on(q.device, q, k, v, key_lengths, key_mask)
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        _refuse("q, k and v must be 4-D", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+    B, N, H, D = q.shape
+    M, K = k.shape[1], k.shape[2]
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit",
+                _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+    if q.dtype != k.dtype or q.dtype != v.dtype:
+        _refuse("q, k and v must share a dtype", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if D > 1 and (qs[3] != 1 or ks[3] != 1 or vs[3] != 1):
+        _refuse("the channels of q, k and v must be adjacent")
+    if key_lengths is not None:
+        if tuple(key_lengths.shape) != (B,) or not key_lengths.is_contiguous():
+            _refuse(f"key_lengths must be a contiguous tensor of {B} elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+        if key_lengths.dtype != torch.int32:
+            _refuse("key_lengths must be int32", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
+    mask_batch = 0
+    if key_mask is not None:
+        if tuple(key_mask.shape) != (B, M) or (M > 1 and key_mask.stride(1) != 1):
+            _refuse(f"key_mask must be [{B}][{M}] with adjacent elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+        if key_mask.dtype not in (torch.bool, torch.uint8):
+            _refuse("key_mask must be bool", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
+        mask_batch = key_mask.stride(0)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D) if D else 1.0
+    attend = _map_binding.bevmap_attend(B, N, M, H, K, D, _code(q.dtype), scale, *qs[:3], *ks[:3], *vs[:3],
+                                        mask_batch)
+    size = _map_binding.bevmap_attention_workspace(attend, False)
+    out = torch.empty((B, N, H, D), dtype=q.dtype, device=q.device)
+    low = torch.empty_like(out) if train and q.dtype != torch.float32 else None
+    lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device) if train else None
+    space = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+    with _Current(q.device) as stream:
+        _map_binding.bevmap_attention(attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lengths),
+                                      _ptr(key_mask), out.data_ptr(), _ptr(low), _ptr(lse), _ptr(space), size,
+                                      stream)
+    return out, low, lse, attend
+
+
+def _attend_backward(attend, dout, q, k, v, key_lengths, key_mask, out, low, lse):
+    import torch
+    size = _map_binding.bevmap_attention_workspace(attend, True)
+    dout = dout.contiguous()
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    space = torch.empty(size, dtype=torch.uint8, device=q.device)
+    with _Current(q.device) as stream:
+        _map_binding.bevmap_attention_backward(attend, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                               _ptr(key_lengths), _ptr(key_mask), out.data_ptr(), _ptr(low),
+                                               lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                               space.data_ptr(), size, stream)
+    return dq, dk, dv
+
+
+def _dropout(x, threshold, seed, offset, residual):
+    import torch
+    _on(x.device, x, residual)
+    stride = _row_stride(x)
+    residual_stride = 0 if residual is None else _row_stride(residual)
+    if stride is None or residual_stride is None:
+        _refuse("rows of x and residual must be evenly spaced, their elements adjacent")
+    if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
+        _refuse("residual must have the shape and dtype of x", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    columns = x.shape[-1] if x.dim() else 1
+    rows = x.numel() // columns if columns else 0
+    with _Current(x.device) as stream:
+        _map_binding.bevmap_dropout(x.data_ptr(), stride, _ptr(residual), residual_stride, y.data_ptr(), rows,
+                                    columns, _code(x.dtype), threshold, seed, offset, stream)
+    return y
+
+
+_FUNCTIONS = None
+
+
+def _functions():
+    global _FUNCTIONS
+    if _FUNCTIONS is not None:
+        return _FUNCTIONS
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _GroupNormAct(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
+            y, stats, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
+            ctx.save_for_backward(x, weight, bias, stats)
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            x, weight, bias, stats = ctx.saved_tensors
+            need = ctx.needs_input_grad
+            dx, dw, db = _norm_backward(ctx.norm, stats, dy, x, weight, bias, need[1], need[2])
+            return dx if need[0] else None, dw, db, None, None, None, None
+
+    class _CrossAttention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, scale, key_lengths, key_mask):
+            out, low, lse, ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
+            ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
+            return out
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dout):
+            q, k, v, key_lengths, key_mask, out, low, lse = ctx.saved_tensors
+            grads = _attend_backward(ctx.attend, dout, q, k, v, key_lengths, key_mask, out, low, lse)
+            return *(g if n else None for g, n in zip(grads, ctx.needs_input_grad)), None, None, None
+
+    class _DropoutAdd(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, residual, threshold, seed, offset):
+            ctx.draw = threshold, seed, offset
+            return _dropout(x, threshold, seed, offset, residual)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            dx = None
+            if ctx.needs_input_grad[0]:
+                dx = _dropout(dy if _row_stride(dy) is not None else dy.contiguous(), *ctx.draw, None)
+            return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
+
+    _FUNCTIONS = _GroupNormAct, _CrossAttention, _DropoutAdd
+    return _FUNCTIONS
+
+
+def _learns(*tensors) -> bool:
+    import torch
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", out_dtype=None):
+    """Group norm over a map with an activation, channels last: x [B][...][C]
+    (fp32, bf16 or fp16), contiguous or a channel slice of a wider map; returns
+    a contiguous map of out_dtype (x's by default).
+
+    Channel c belongs to group c // (C // groups); mean and biased variance are
+    those of a sample's group over all its cells; y = act(weight * (x - mean) /
+    sqrt(variance + eps) + bias), act "none", "relu", "silu" or "gelu" (through
+    erf). weight, bias: [C] of one dtype, or None. Statistics are fp32, y is
+    rounded once. Differentiable in x, weight and bias."""
+    if _learns(x, weight, bias):
+        return _functions()[0].apply(x, weight, bias, groups, eps, act, out_dtype)
+    return _norm_forward(x, groups, weight, bias, eps, act, out_dtype)[0]
+
+
+def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
+    """Attention of queries to an encoder's states of another length.
+
+    q [B][N][H][D], k and v [B][M][K][D] (fp32, bf16 or fp16, one dtype; any
+    strides but for adjacent channels, so views of a packed projection do); H
+    is a multiple of K, and head h reads key head h // (H // K); D at most 128.
+    Returns [B][N][H][D], contiguous: softmax(scale * q k^T) v, scale by default
+    1 / sqrt(D).
+
+    key_lengths: int32 [B], states j >= key_lengths[b] are not in use (values
+    are clamped to [0, M]). key_mask: bool [B][M], states with False are not in
+    use. States not in use may hold anything, NaN too; they do not reach the
+    output, and their gradients are 0. A query without a state in use gets 0.
+    Few queries over many states (one token in serving) are split over the
+    states. Differentiable in q, k and v, bitwise reproducible."""
+    if _learns(q, k, v):
+        return _functions()[1].apply(q, k, v, scale, key_lengths, key_mask)
+    return _attend_forward(q, k, v, scale, key_lengths, key_mask, False)[0]
+
+
+def dropout_add(x, p, seed, offset=0, residual=None):
+    """residual + dropout(x), the mask drawn from (seed, offset) and the element's
+    index in x and never stored.
+
+    x (fp32, bf16 or fp16), contiguous or with evenly spaced rows; residual alike
+    or None. p in [0, 1] is placed to the nearest 1 / 65536, and kept elements
+    are scaled by one over the placed keep probability. seed, offset: integers
+    in [0, 2^64); a step that needs another mask takes another offset (a HIP
+    graph that captured the call draws the same mask in each replay).
+    Differentiable in x and residual: the backward draws the mask again."""
+    if not 0.0 <= p <= 1.0:
+        _refuse(f"p={p} is outside [0, 1]")
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        _refuse("seed and offset must be in [0, 2^64)")
+    threshold = int(65536 * p + 0.5)
+    if _learns(x, residual):
+        return _functions()[2].apply(x, residual, threshold, seed, offset)
+    return _dropout(x, threshold, seed, offset, residual)

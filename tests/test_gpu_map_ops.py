@@ -1,0 +1,621 @@
+"""The map operators on the GPU against plain implementations in 64 bits.
+
+Tolerances are elementwise bounds, formed from the reference's own sums of
+magnitudes before anything runs: a value rounded to its type is off by at most
+u |value| (u, the unit roundoff of 24, 8 and 11 significant bits, is 2^-24,
+2^-8 and 2^-11 for fp32, bf16 and fp16; below fp16's normal range by 2^-25), and each fp32 sum by a small
+multiple of 2^-24 times the sum of magnitudes of what it adds.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def bev(torch):
+    import paper_2205_13542_amd as bev
+    bev._map_binding.load()
+    return bev
+
+
+def _dtype(torch, name):
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def _u(name):
+    return {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[name]
+
+
+def _tiny(name):
+    """Half the spacing of the type's subnormal numbers."""
+    return {"f32": 0.0, "bf16": 0.0, "f16": 2.0 ** -25}[name]
+
+
+def _check(what, got, ref, tol):
+    got = got.double()
+    assert got.shape == ref.shape, what
+    bad = ~((got - ref).abs() <= tol)
+    assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} off, worst "
+                           f"{float(((got - ref).abs() / tol.clamp(min=1e-300)).max()):.3g} of the bound")
+
+
+# ---------------------------------------------------------------- group norm
+
+def _norm_reference(torch, x, groups, w, b, eps, act, dy, k):
+    """y, gradients and their bounds; k counts the fp32 roundings of a sum's chain."""
+    B, C = x.shape[0], x.shape[-1]
+    shape = x.shape
+    x = x.double().reshape(B, -1, groups, C // groups)
+    w, b = (t.double().view(groups, -1) for t in (w, b))
+    mean = x.mean((1, 3), keepdim=True)
+    var = (x - mean).pow(2).mean((1, 3), keepdim=True)
+    rstd = 1 / torch.sqrt(var + eps)
+    xh = (x - mean) * rstd
+    z = xh * w + b
+    # mean is off by k U32 mean(|x|), x - mean by that and its rounding, rstd by k U32 of itself and by
+    # the square of the mean's error, which is smaller still
+    far = (x.abs().mean((1, 3), keepdim=True) * rstd)
+    dxh = k * U32 * (xh.abs() + far)
+    dz_ = dxh * w.abs() + 3 * U32 * (z.abs() + b.abs())
+    phi = torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    cdf = 0.5 * torch.erfc(-z / math.sqrt(2))
+    sig = torch.sigmoid(z)
+    y, slope, bend = {"none": (z, torch.ones_like(z), 0.0), "relu": (z.clamp(min=0), (z > 0).double(), 0.0),
+                      "silu": (z * sig, sig * (1 + z * (1 - sig)), 0.5),
+                      "gelu": (z * cdf, cdf + z * phi, 0.8)}[act]
+    # an activation's own evaluation: a few roundings of magnitudes up to 1 + |z|, exponents of up to z^2
+    own = 8 * U32 * (1 + z.abs()) * (1 if act in ("silu", "gelu") else 0)
+    y_tol = 1.2 * dz_ + own * z.abs().clamp(max=1) + 2 * U32 * y.abs()
+    out = {"y": (y.reshape(shape), y_tol.reshape(shape))}
+    if dy is None:
+        return out
+    dy = dy.double().view_as(x)
+    dslope = bend * dz_ + own * (1 + z.abs())
+    if act == "relu":
+        dslope = (z.abs() <= dz_).double()      # the slope may be either
+    e0 = dy * slope
+    e0_tol = dy.abs() * dslope + 2 * U32 * e0.abs()
+    dw, db = (e0 * xh).sum((0, 1)), e0.sum((0, 1))
+    dw_tol = (e0_tol * (xh.abs() + dxh) + e0.abs() * dxh + k * U32 * (e0 * xh).abs()).sum((0, 1))
+    db_tol = (e0_tol + k * U32 * e0.abs()).sum((0, 1))
+    e, e_tol = e0 * w, e0_tol * w.abs() + U32 * (e0 * w).abs()
+    m1, m2 = e.mean((1, 3), keepdim=True), (e * xh).mean((1, 3), keepdim=True)
+    m1_tol = (e_tol + k * U32 * e.abs()).mean((1, 3), keepdim=True)
+    m2_tol = (e_tol * xh.abs() + e.abs() * dxh + k * U32 * (e * xh).abs()).mean((1, 3), keepdim=True)
+    dx = rstd * (e - m1 - xh * m2)
+    dx_tol = rstd * (e_tol + m1_tol + xh.abs() * m2_tol + dxh * m2.abs()
+                     + k * U32 * (e.abs() + m1.abs() + (xh * m2).abs()))
+    out.update(dx=(dx.reshape(shape), dx_tol.reshape(shape)), dw=(dw.view(C), dw_tol.view(C)),
+               db=(db.view(C), db_tol.view(C)))
+    return out
+
+
+NORM_CASES = [
+    # shape, groups, channels left of a slice, x, y, weights, act, offset of x
+    ((1, 1, 1, 1), 1, 0, "f32", "f32", "f32", "none", 0.0),
+    ((1, 4, 4, 8), 8, 0, "f32", "f32", "f32", "relu", 0.0),
+    ((2, 37, 29, 66), 11, 7, "f32", "f32", "f32", "gelu", 0.0),
+    ((1, 60, 61, 80), 8, 0, "f32", "bf16", "f32", "silu", 0.5),
+    ((3, 33, 80), 5, 0, "bf16", "bf16", "bf16", "silu", 0.0),
+    ((2, 19, 23, 72), 9, 8, "f16", "f16", "f16", "gelu", 1.0),
+    ((5, 7, 24), 3, 0, "f16", "f32", "f32", "none", 0.0),
+    ((4, 30), 6, 0, "f32", "f16", "bf16", "silu", 0.0),
+    ((2, 5, 6, 1030), 10, 2, "bf16", "bf16", "f32", "relu", 0.0),     # more vectors of two than threads
+    ((1, 3, 8192), 2, 0, "f32", "f32", "f32", "silu", 0.0),           # the most channels
+    ((1, 40, 40, 16), 16, 0, "f32", "f32", "f32", "gelu", 1000.0),    # mean far above the deviation
+    ((17, 11, 3, 32), 4, 0, "bf16", "f32", "f32", "gelu", -3.0),
+    ((1, 50000, 4), 2, 1, "f32", "f32", "f32", "silu", 0.0),
+]
+
+
+def _norm_inputs(torch, shape, groups, extra, xdt, ydt, wdt, offset, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    wide = torch.randn((*shape[:-1], shape[-1] + extra), generator=gen, device="cuda")
+    x = (wide + offset).to(_dtype(torch, xdt))[..., extra:]
+    w = (1 + 0.3 * torch.randn(shape[-1], generator=gen, device="cuda")).to(_dtype(torch, wdt))
+    b = (0.3 * torch.randn(shape[-1], generator=gen, device="cuda")).to(_dtype(torch, wdt))
+    dy = torch.randn(shape, generator=gen, device="cuda").to(_dtype(torch, ydt))
+    return x, w, b, dy
+
+
+@pytest.mark.parametrize("shape,groups,extra,xdt,ydt,wdt,act,offset", NORM_CASES)
+def test_group_norm(torch, bev, shape, groups, extra, xdt, ydt, wdt, act, offset):
+    print(f"[norm] {shape} groups={groups} +{extra} {xdt}->{ydt} {wdt} {act}", flush=True)
+    x, w, b, dy = _norm_inputs(torch, shape, groups, extra, xdt, ydt, wdt, offset)
+    x, w, b = (t.detach().requires_grad_() for t in (x, w, b))
+    y = bev.group_norm_act(x, groups, w, b, act=act, out_dtype=_dtype(torch, ydt))
+    assert y.is_contiguous() and y.dtype == _dtype(torch, ydt)
+    dx, dw, db = torch.autograd.grad(y, (x, w, b), dy)
+    with torch.no_grad():
+        # chains: up to 64 values in a thread, then lanes, channels and chunks by tens
+        ref = _norm_reference(torch, x, groups, w, b, 1e-5, act, dy, k=128)
+        for name, got, dt in (("y", y, ydt), ("dx", dx, xdt), ("dw", dw, wdt), ("db", db, wdt)):
+            r, tol = ref[name]
+            _check(name, got, r, tol + _u(dt) * (r.abs() + tol) + _tiny(dt) + 1e-35)
+        again = bev.group_norm_act(x, groups, w, b, act=act, out_dtype=_dtype(torch, ydt))
+        assert torch.equal(again, y)
+
+
+def test_group_norm_without_weights_and_partial_gradients(torch, bev):
+    x, w, b, dy = _norm_inputs(torch, (2, 9, 8, 24), 3, 0, "f32", "f32", "f32", 0.0)
+    ones, zeros = torch.ones_like(w), torch.zeros_like(b)
+    assert torch.equal(bev.group_norm_act(x, 3), bev.group_norm_act(x, 3, ones, zeros))
+    assert torch.equal(bev.group_norm_act(x, 3, w), bev.group_norm_act(x, 3, w, zeros))
+    w.requires_grad_()
+    dw, = torch.autograd.grad(bev.group_norm_act(x, 3, w, b, act="silu"), w, dy)
+    xg = x.clone().requires_grad_()
+    dx, dw2 = torch.autograd.grad(bev.group_norm_act(xg, 3, w, b, act="silu"), (xg, w), dy)
+    assert torch.equal(dw, dw2)
+    xg2 = x.clone().requires_grad_()
+    dx2, = torch.autograd.grad(bev.group_norm_act(xg2, 3, w.detach(), b, act="silu"), xg2, dy)
+    assert torch.equal(dx, dx2)
+
+
+def test_group_norm_empty_and_nonfinite(torch, bev):
+    for shape in ((0, 4, 4, 8), (2, 0, 8)):
+        x = torch.empty(shape, device="cuda", requires_grad=True)
+        w = torch.ones(8, device="cuda", requires_grad=True)
+        y = bev.group_norm_act(x, 2, w)
+        assert y.shape == x.shape
+        dx, dw = torch.autograd.grad(y, (x, w), torch.empty_like(y))
+        assert dx.shape == x.shape and torch.equal(dw, torch.zeros_like(dw))
+    x, w, b, _ = _norm_inputs(torch, (2, 12, 13, 24), 3, 0, "f32", "f32", "f32", 0.0)
+    clean = bev.group_norm_act(x, 3, w, b, act="silu")
+    x[1, 3, 4, 9] = math.inf          # frame 1, group 1
+    got = bev.group_norm_act(x, 3, w, b, act="silu")
+    assert got[1, :, :, 8:16].isnan().all()
+    got[1, :, :, 8:16] = clean[1, :, :, 8:16]
+    assert torch.equal(got, clean)
+
+
+def test_group_norm_of_a_constant_group(torch, bev):
+    """Zero variance: x - mean is 0 and y is act(bias)."""
+    x = torch.full((1, 20, 20, 8), 3.0, device="cuda")
+    b = torch.linspace(-1, 1, 8, device="cuda")
+    y = bev.group_norm_act(x, 2, None, b)
+    assert torch.equal(y, b.expand_as(y))
+
+
+def test_group_norm_offsets_past_32_bits(torch, bev):
+    """Rows of a channel slice of a map of 5.4 GB."""
+    rows, ld, C = 42000, 1 << 16, 16
+    x = torch.empty((1, rows, ld), dtype=torch.bfloat16, device="cuda")[..., ld - C:]
+    x.copy_(torch.randn((1, rows, C), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda"))
+    assert torch.equal(bev.group_norm_act(x, 4, act="silu"), bev.group_norm_act(x.contiguous(), 4, act="silu"))
+
+
+# ---------------------------------------------------------------- attention
+
+def _attend_reference(torch, q, k, v, scale, lengths, mask, dout, udt):
+    """Outputs, gradients and their bounds, over the states in use."""
+    B, N, H, D = q.shape
+    M, K = k.shape[1], k.shape[2]
+    use = torch.ones((B, M), dtype=torch.bool, device=q.device)
+    if lengths is not None:
+        use &= torch.arange(M, device=q.device)[None] < lengths[:, None]
+    if mask is not None:
+        use &= mask
+    up, tiny = (_u(udt), _tiny(udt)) if udt != "f32" else (0.0, 0.0)
+    names = ("out", "dq", "dk", "dv")
+    shapes = (q.shape, q.shape, k.shape, k.shape)
+    res = {n: [torch.zeros(s, dtype=torch.float64, device=q.device) for _ in range(2)] for n, s in zip(names, shapes)}
+    for i in range(B):
+        at = use[i].nonzero()[:, 0]
+        if not at.numel():
+            continue
+        for h in range(H):
+            j = h // (H // K)
+            Q, KK, V = q[i, :, h].double(), k[i, at, j].double(), v[i, at, j].double()
+            s = scale * Q @ KK.T
+            # of a score: its fp32 sum of dim products, the scale, the exponent's argument
+            ds_ = (D + 8) * U32 * abs(scale) * (Q.abs() @ KK.abs().T)
+            top = ds_.max(1, keepdim=True).values
+            p = torch.softmax(s, 1)
+            total = torch.exp(s - s.max(1, keepdim=True).values).sum(1, keepdim=True)
+            rel = 3 * top + 64 * U32
+            o, mag = p @ V, p @ V.abs()
+            o_tol = mag * (rel + up) + tiny * V.abs().sum(0) / total
+            res["out"][0][i, :, h] = o
+            res["out"][1][i, :, h] = o_tol
+            if dout is None:
+                continue
+            dO = dout[i, :, h].double()
+            dp, dp_tol = dO @ V.T, (D + 8) * U32 * (dO.abs() @ V.abs().T)
+            delta = (dO * o).sum(1, keepdim=True)
+            # the delta is formed from out as it was written, rounded probabilities and all
+            delta_tol = (dO.abs() * (o_tol + 2 * up * up * o.abs() + tiny * (1 if tiny else 0))).sum(1, keepdim=True) \
+                + (D + 8) * U32 * (dO * o).abs().sum(1, keepdim=True)
+            ds = p * (dp - delta)
+            ds_tol = ds.abs() * (rel + up) + p * (dp_tol + delta_tol + 4 * U32 * (dp.abs() + delta.abs())) + tiny
+            n_add = 64 * U32
+            res["dq"][0][i, :, h] = scale * ds @ KK
+            res["dq"][1][i, :, h] = abs(scale) * (ds_tol + n_add * ds.abs()) @ KK.abs()
+            res["dk"][0][i, at, j] += scale * ds.T @ Q
+            res["dk"][1][i, at, j] += abs(scale) * (ds_tol + n_add * ds.abs()).T @ Q.abs()
+            res["dv"][0][i, at, j] += p.T @ dO
+            res["dv"][1][i, at, j] += (p * (rel + up + n_add) + tiny).T @ dO.abs()
+    return res
+
+
+def _attend_inputs(torch, B, N, M, H, K, D, dt, layout, lengths, mask, sharp=2.0, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed + N * 7 + M)
+    dtype = _dtype(torch, dt)
+
+    def normal(*shape, scale=1.0):
+        return (scale * torch.randn(shape, generator=gen, device="cuda")).to(dtype)
+
+    if layout == "heads_first":       # [B][H][N][D] in memory
+        q = normal(B, H, N, D, scale=sharp).transpose(1, 2)
+        k, v = (normal(B, K, M, D).transpose(1, 2) for _ in range(2))
+    elif layout == "packed":          # one projection's output
+        q = normal(B, N, H, D, scale=sharp)
+        k, v = normal(B, M, 2, K, D).unbind(2)
+    elif layout == "odd":             # rows that start anywhere
+        q = normal(B, N, H, D + 3, scale=sharp)[..., 3:]
+        k, v = normal(B, M, K, 2 * D + 1)[..., 1:D + 1], normal(B, M, K, 2 * D + 1)[..., D + 1:]
+    else:
+        q = normal(B, N, H, D, scale=sharp)
+        k, v = normal(B, M, K, D), normal(B, M, K, D)
+    dout = normal(B, N, H, D)
+    use = torch.ones((B, M), dtype=torch.bool, device="cuda")
+    if lengths is not None:
+        lengths = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        use &= torch.arange(M, device="cuda")[None] < lengths[:, None]
+    if mask == "random":
+        mask = torch.rand((B, M), generator=gen, device="cuda") < 0.6
+    elif mask == "runs":
+        mask = (torch.rand((B, -(-M // 40)), generator=gen, device="cuda") < 0.5).repeat_interleave(40, 1)[:, :M]
+        mask = mask.contiguous()
+    elif mask == "last":
+        mask = torch.zeros((B, M), dtype=torch.bool, device="cuda")
+        mask[:, -1:] = True
+    elif mask == "none_left":
+        mask = torch.zeros((B, M), dtype=torch.bool, device="cuda")
+    if mask is not None:
+        use &= mask
+    fill = torch.where(torch.rand((B, M, 1, 1), generator=gen, device="cuda") < 0.5, math.nan, math.inf).to(dtype)
+    for t in (k, v):
+        t.copy_(torch.where(use[:, :, None, None], t, fill))
+    return q, k, v, dout, lengths, mask
+
+
+ATTEND_CASES = [
+    # B, N, M, H, K, D, dtype, layout, lengths, mask
+    (1, 1, 1, 1, 1, 1, "f32", "plain", None, None),
+    (1, 1, 1, 1, 1, 8, "bf16", "plain", None, None),
+    (3, 7, 77, 4, 4, 20, "f32", "plain", [77, 49, 0], None),
+    (2, 1, 4097, 8, 2, 64, "bf16", "plain", None, "random"),
+    (1, 1, 70000, 4, 1, 64, "f16", "packed", None, "runs"),
+    (1, 3, 20011, 4, 4, 32, "f32", "plain", None, "runs"),
+    (2, 33, 129, 2, 2, 32, "bf16", "packed", [129, 65], None),
+    (2, 130, 65, 4, 2, 64, "f16", "heads_first", None, "random"),
+    (1, 257, 511, 2, 1, 128, "bf16", "plain", [400], "random"),
+    (1, 100, 200, 4, 1, 128, "f32", "packed", None, None),
+    (2, 64, 64, 2, 2, 16, "f16", "odd", [64, 13], None),
+    (1, 95, 333, 3, 3, 53, "bf16", "odd", None, "random"),
+    (1, 45, 96, 3, 1, 100, "f32", "odd", None, None),
+    (1, 129, 300, 2, 2, 33, "f16", "plain", None, None),
+    (4, 40, 100, 2, 2, 32, "bf16", "plain", [0, 1, 1000, -5], None),
+    (2, 50, 90, 2, 2, 32, "f32", "plain", None, "none_left"),
+    (2, 50, 190, 2, 2, 48, "bf16", "plain", None, "last"),
+    (1, 2000, 31, 4, 2, 40, "f16", "plain", None, None),
+    (1, 700, 1500, 5, 5, 16, "f32", "packed", None, "random"),
+    (2, 513, 1025, 4, 4, 32, "bf16", "packed", [1025, 640], "runs"),
+    (1, 300, 700, 8, 2, 96, "f16", "plain", None, "runs"),
+    (1, 31, 2049, 16, 1, 80, "bf16", "heads_first", None, None),
+]
+
+
+@pytest.mark.parametrize("B,N,M,H,K,D,dt,layout,lengths,mask", ATTEND_CASES)
+def test_cross_attention(torch, bev, B, N, M, H, K, D, dt, layout, lengths, mask):
+    print(f"[attend] B={B} N={N} M={M} H={H}/{K} D={D} {dt} {layout} {lengths} {mask}", flush=True)
+    q, k, v, dout, lengths, mask = _attend_inputs(torch, B, N, M, H, K, D, dt, layout, lengths, mask)
+    scale = 1 / math.sqrt(D)
+    ref = _attend_reference(torch, q, k, v, scale, lengths, mask, dout, dt)
+    plain = bev.cross_attention(q, k, v, key_lengths=lengths, key_mask=mask)
+    q, k, v = (t.detach().requires_grad_() for t in (q, k, v))
+    out = bev.cross_attention(q, k, v, key_lengths=lengths, key_mask=mask)
+    assert out.is_contiguous() and out.dtype == q.dtype and torch.equal(out, plain)
+    grads = torch.autograd.grad(out, (q, k, v), dout)
+    with torch.no_grad():
+        for name, got in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+            r, tol = ref[name]
+            # results in fp32 carry the joining of parts, 16 roundings at most, on top
+            _check(name, got, r, tol * (1 + 16 * U32) + _u(dt) * (r.abs() + tol) + _tiny(dt) + 1e-30)
+    again = torch.autograd.grad(bev.cross_attention(q, k, v, key_lengths=lengths, key_mask=mask), (q, k, v), dout)
+    assert all(torch.equal(a, g) for a, g in zip(again, grads))
+
+
+def test_cross_attention_empty(torch, bev):
+    for B, N, M in ((0, 3, 4), (2, 0, 4), (2, 3, 0)):
+        q = torch.randn(B, N, 2, 8, device="cuda", requires_grad=True)
+        k, v = (torch.randn(B, M, 2, 8, device="cuda", requires_grad=True) for _ in range(2))
+        out = bev.cross_attention(q, k, v)
+        assert out.shape == q.shape and not out.any()
+        grads = torch.autograd.grad(out, (q, k, v), torch.ones_like(out))
+        assert all(g.shape == t.shape and not g.any() for g, t in zip(grads, (q, k, v)))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+def test_cross_attention_large_scores(torch, bev, dt):
+    """Scores of some hundreds, one state far above the rest, and all far below 0."""
+    q, k, v, dout, _, _ = _attend_inputs(torch, 1, 40, 200, 2, 2, 32, dt, "plain", None, None, sharp=30.0)
+    for shift in (0.0, -8.0):
+        q2 = q.detach().clone()
+        k2 = k.detach().clone()
+        if shift:
+            q2[..., 0], k2[..., 0] = 100.0, shift     # adds 100 * -8 / sqrt(32) to every score
+        ref = _attend_reference(torch, q2, k2, v, 32 ** -0.5, None, None, None, dt)["out"]
+        got = bev.cross_attention(q2, k2, v)
+        assert got.isfinite().all()
+        _check("out", got, ref[0], ref[1] * (1 + 16 * U32) + _u(dt) * (ref[0].abs() + ref[1]) + _tiny(dt))
+
+
+def test_cross_attention_broadcast_states(torch, bev):
+    """States shared over samples and heads by expanding: gradients sum over the copies."""
+    q, k, v, dout, _, _ = _attend_inputs(torch, 3, 20, 70, 4, 4, 16, "f32", "plain", None, None)
+    k1, v1 = (t[:1, :, :1].clone().requires_grad_() for t in (k, v))
+    out = bev.cross_attention(q, k1.expand(3, -1, 4, -1), v1.expand(3, -1, 4, -1))
+    dk, dv = torch.autograd.grad(out, (k1, v1), dout)
+    k2, v2 = (t.detach().expand(3, -1, 4, -1).contiguous().requires_grad_() for t in (k1, v1))
+    out2 = bev.cross_attention(q, k2, v2)
+    dk2, dv2 = torch.autograd.grad(out2, (k2, v2), dout)
+    assert torch.equal(out, out2)
+    assert torch.allclose(dk, dk2.sum((0, 2), keepdim=True), rtol=1e-5, atol=1e-5)
+    assert torch.allclose(dv, dv2.sum((0, 2), keepdim=True), rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("N", [1, 200])
+def test_cross_attention_offsets_past_32_bits(torch, bev, N):
+    """States whose rows are 128 KB apart: 5 GB from the first to the last."""
+    M, ld, D = 40000, 1 << 16, 64
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    store = torch.empty((1, M, 1, ld), dtype=torch.bfloat16, device="cuda")
+    k, v = store[..., ld - 2 * D:ld - D], store[..., ld - D:]
+    for t in (k, v):
+        t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+    q = torch.randn((1, N, 2, D), generator=gen, device="cuda").bfloat16()
+    dout = torch.randn((1, N, 2, D), generator=gen, device="cuda").bfloat16()
+
+    def step(k, v):
+        ts = [t.detach().requires_grad_() for t in (q, k, v)]
+        out = bev.cross_attention(*ts)
+        return (out, *torch.autograd.grad(out, ts, dout))
+
+    for a, b in zip(step(k, v), step(k.contiguous(), v.contiguous())):
+        assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- dropout
+
+def _philox(counter, key):
+    """philox4x32-10 in Python integers."""
+    c, k, low = list(counter), list(key), 0xFFFFFFFF
+    for _ in range(10):
+        p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(p1 >> 32) ^ c[1] ^ k[0], p1 & low, (p0 >> 32) ^ c[3] ^ k[1], p0 & low]
+        k = [(k[0] + 0x9E3779B9) & low, (k[1] + 0xBB67AE85) & low]
+    return c
+
+
+def _draws(first, n, seed, offset):
+    """16-bit draws of elements first .. first + n - 1."""
+    out, low = [], 0xFFFFFFFF
+    for block in range(first // 8, (first + n - 1) // 8 + 1):
+        words = _philox((block & low, block >> 32, offset & low, offset >> 32), (seed & low, seed >> 32))
+        out += [w >> s & 0xFFFF for w in words for s in (0, 16)]
+    return np.array(out[first % 8:first % 8 + n])
+
+
+def test_philox_known_answers():
+    """Vectors published with the generator."""
+    assert _philox((0,) * 4, (0,) * 2) == [0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]
+    assert _philox((0xffffffff,) * 4, (0xffffffff,) * 2) == [0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]
+
+
+@pytest.mark.parametrize("rows,columns,extra,p,dt,residual", [
+    (1, 1, 0, 0.5, "f32", True), (3, 5, 0, 0.3, "bf16", True), (7, 16, 8, 0.1, "f16", True),
+    (7, 16, 3, 0.1, "f16", False), (50, 33, 2, 0.7, "f32", True), (20, 80, 0, 0.0, "bf16", True),
+    (20, 80, 0, 1.0, "bf16", True), (9, 77, 0, 0.9999999, "f16", False), (60, 64, 0, 0.25, "bf16", False)])
+def test_dropout_add(torch, bev, rows, columns, extra, p, dt, residual):
+    seed, offset = 0x123456789ABCDEF0, 0xFEDCBA9876543210
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    dtype = _dtype(torch, dt)
+    x, res = (torch.randn((rows, columns + extra), generator=gen, device="cuda").to(dtype)[:, extra:]
+              .detach().requires_grad_() for _ in range(2))
+    dy = torch.randn((rows, columns), generator=gen, device="cuda").to(dtype)
+    y = bev.dropout_add(x, p, seed, offset, residual=res if residual else None)
+    threshold = math.floor(65536 * p + 0.5)
+    kept = torch.from_numpy(_draws(0, rows * columns, seed, offset) >= threshold).cuda().view(rows, columns)
+    scale = 65536 / (65536 - threshold) if threshold < 65536 else 0.0
+    assert y.dtype == dtype and y.is_contiguous()
+    with torch.no_grad():
+        drop = torch.where(kept, x.double() * scale, 0.0)
+        ref = drop + (res.double() if residual else 0.0)
+        # the scale, the product and the sum in fp32, then the type
+        tol = 3 * U32 * (drop.abs() + ref.abs())
+        _check("y", y, ref, tol + _u(dt) * (ref.abs() + tol) + _tiny(dt))
+        if not residual:
+            assert torch.equal(y == 0, ~kept | (x == 0))
+    grads = torch.autograd.grad(y, (x, res) if residual else (x,), dy)
+    ref = torch.where(kept, dy.double() * scale, 0.0)
+    tol = 3 * U32 * ref.abs()
+    _check("dx", grads[0], ref, tol + _u(dt) * (ref.abs() + tol) + _tiny(dt))
+    if residual:
+        assert torch.equal(grads[1], dy)
+
+
+def test_dropout_of_nonfinite_and_empty(torch, bev):
+    x = torch.full((64, 64), math.nan, device="cuda")
+    kept = torch.from_numpy(_draws(0, 4096, 9, 0) >= 32768).cuda().view(64, 64)
+    y = bev.dropout_add(x, 0.5, 9)
+    assert torch.equal(y.isnan(), kept) and not y[~kept].any()
+    assert not bev.dropout_add(x, 1.0, 9).any()
+    for shape in ((0, 8), (8, 0), (0,)):
+        assert bev.dropout_add(torch.empty(shape, device="cuda"), 0.5, 9).shape == shape
+    assert bev.dropout_add(torch.ones((), device="cuda"), 0.0, 9).item() == 1.0
+
+
+def test_dropout_shares_and_streams_of_numbers(torch, bev):
+    x = torch.ones((1 << 20,), device="cuda")
+    a, b, c = (bev.dropout_add(x, 0.1, s, o) for s, o in ((1, 0), (1, 1), (2, 0)))
+    n = x.numel()
+    for t in (a, b, c):      # five standard deviations of a binomial share
+        assert abs((t > 0).double().mean().item() - (1 - 6554 / 65536)) < 5 * math.sqrt(0.09 / n)
+    for s, t in ((a, b), (a, c)):
+        both = ((s == 0) & (t == 0)).double().mean().item()
+        assert abs(both - 0.01) < 5 * math.sqrt(0.01 / n) + 1e-5
+
+
+def test_dropout_indices_past_32_bits(torch, bev):
+    n = (1 << 32) + 24
+    x = torch.ones((n,), dtype=torch.bfloat16, device="cuda")
+    y = bev.dropout_add(x, 0.5, 77, 3)
+    for first in (0, (1 << 31) - 40, (1 << 32) - 32, n - 56):
+        kept = torch.from_numpy(_draws(first, 56, 77, 3) >= 32768).cuda()
+        assert torch.equal(y[first:first + 56] > 0, kept)
+
+
+# ---------------------------------------------------------------- all three
+
+def test_gradients_against_differences(torch, bev):
+    """Central differences along random directions, in fp32 with the sums in 64 bits.
+    Values are of order 1, so a step of 1/64 truncates at about 1e-4 of the
+    derivative's size and rounds at about 1e-5 of it."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda")
+
+    mask = torch.rand((2, 50), generator=gen, device="cuda") < 0.7
+    calls = [
+        (lambda x, w, b: bev.group_norm_act(x, 3, w, b, act="silu"), [normal(2, 7, 6, 12), normal(12), normal(12)]),
+        (lambda x, w, b: bev.group_norm_act(x, 2, w, b, act="gelu"), [normal(2, 30, 8), normal(8), normal(8)]),
+        (lambda q, k, v: bev.cross_attention(q, k, v, key_mask=mask),
+         [normal(2, 9, 4, 16), normal(2, 50, 2, 16), normal(2, 50, 2, 16)]),
+        (lambda x, r: bev.dropout_add(x, 0.3, 5, residual=r), [normal(40, 9), normal(40, 9)]),
+    ]
+    for call, inputs in calls:
+        weight = normal(*call(*inputs).shape).double()
+        leaves = [t.clone().requires_grad_() for t in inputs]
+        grads = torch.autograd.grad((call(*leaves).double() * weight).sum(), leaves)
+        for i, g in enumerate(grads):
+            along = normal(*inputs[i].shape)
+            along /= along.norm()
+            step = 2.0 ** -6
+
+            def at(s):
+                moved = [t + s * along if j == i else t for j, t in enumerate(inputs)]
+                return (call(*moved).double() * weight).sum().item()
+
+            # of fourth order, from two central differences
+            got = (8 * (at(step) - at(-step)) - (at(2 * step) - at(-2 * step))) / (12 * step)
+            want = (g.double() * along.double()).sum().item()
+            assert abs(got - want) <= 1e-3 * (abs(want) + g.double().norm().item() / math.sqrt(g.numel())) + 2e-3
+
+
+def _layer(torch, bev, x, w, b, wq, wkv, tokens, seen, seed, step):
+    B, C = x.shape[0], x.shape[-1]
+    states = bev.group_norm_act(x, 4, w, b, act="silu", out_dtype=torch.bfloat16).flatten(1, 2)
+    k, v = (states @ wkv).view(B, -1, 2, 4, C // 4).unbind(2)
+    q = (tokens @ wq).view(B, -1, 4, C // 4)
+    heard = bev.cross_attention(q, k, v, key_mask=seen).flatten(2)
+    return bev.dropout_add(heard, 0.2, seed, step, residual=tokens)
+
+
+def _layer_inputs(torch):
+    gen = torch.Generator(device="cuda").manual_seed(2)
+
+    def normal(*shape, s=1.0):
+        return s * torch.randn(shape, generator=gen, device="cuda")
+
+    return (normal(2, 20, 21, 64), 1 + normal(64, s=0.1), normal(64, s=0.1), normal(64, 64, s=0.1).bfloat16(),
+            normal(64, 128, s=0.1).bfloat16(), normal(2, 17, 64).bfloat16(),
+            torch.rand((2, 420), generator=gen, device="cuda") < 0.8)
+
+
+def test_on_another_stream(torch, bev):
+    """Inputs made on a side stream, used there at once, with nothing else to order them."""
+    args = _layer_inputs(torch)
+    ref = _layer(torch, bev, *args, 3, 1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        mine = [torch.empty_like(t) for t in args]
+        big = torch.randn(1 << 26, device="cuda")
+        for _ in range(8):
+            big = big * 1.5                     # keeps the stream busy
+        for t, a in zip(mine, args):
+            t.copy_(a)
+        got = _layer(torch, bev, *mine, 3, 1)
+    side.synchronize()
+    assert torch.equal(got, ref)
+
+
+def test_in_a_graph(torch, bev):
+    args = [t.clone() for t in _layer_inputs(torch)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        _layer(torch, bev, *args, 3, 1)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _layer(torch, bev, *args, 3, 1)
+    for i in range(4):
+        args[0].copy_(torch.randn(args[0].shape, generator=torch.Generator(device="cuda").manual_seed(50 + i),
+                                  device="cuda"))
+        graph.replay()
+        got = out.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, _layer(torch, bev, *args, 3, 1)), f"replay {i}"
+
+
+def test_refusals(torch, bev):
+    x = torch.zeros(2, 6, 5, 8, device="cuda")
+    q, k = torch.zeros(2, 3, 4, 8, device="cuda"), torch.zeros(2, 5, 2, 8, device="cuda")
+    lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+    mask = torch.ones(2, 5, dtype=torch.bool, device="cuda")
+    bad = [
+        lambda: bev.group_norm_act(x, 3),
+        lambda: bev.group_norm_act(x, 2, act="tanh"),
+        lambda: bev.group_norm_act(x, 2, torch.ones(7, device="cuda")),
+        lambda: bev.group_norm_act(x, 2, torch.ones(8)),
+        lambda: bev.group_norm_act(x.double(), 2),
+        lambda: bev.group_norm_act(x, 2, out_dtype=torch.int32),
+        lambda: bev.group_norm_act(x.transpose(1, 3), 2),
+        lambda: bev.group_norm_act(x[:, :, ::2], 2),
+        lambda: bev.group_norm_act(x[0, 0, 0], 2),
+        lambda: bev.cross_attention(q, k, k[:, :4]),
+        lambda: bev.cross_attention(q, k.half(), k.half()),
+        lambda: bev.cross_attention(q[:, :, :3], k, k),
+        lambda: bev.cross_attention(q[0], k[0], k[0]),
+        lambda: bev.cross_attention(q.transpose(2, 3), k, k),
+        lambda: bev.cross_attention(q, k, k, key_lengths=lengths[:1]),
+        lambda: bev.cross_attention(q, k, k, key_lengths=lengths.long()),
+        lambda: bev.cross_attention(q, k, k, key_mask=mask.float()),
+        lambda: bev.cross_attention(q, k, k, key_mask=mask[:, :4]),
+        lambda: bev.cross_attention(q, k, k, scale=math.inf),
+        lambda: bev.cross_attention(*(torch.zeros(1, 2, 2, 129, device="cuda") for _ in range(3))),
+        lambda: bev.dropout_add(x.double(), 0.5, 1),
+        lambda: bev.dropout_add(x, 0.5, 1, residual=x[:1]),
+        lambda: bev.dropout_add(x, 0.5, 1, residual=x.half()),
+        lambda: bev.dropout_add(x.transpose(1, 3), 0.5, 1),
+        lambda: bev.dropout_add(x.expand(2, 6, 5, 8)[..., :1].expand(2, 6, 5, 8), 0.5, 1),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(bev.BevpoolError):
+            call()
+            print(f"call {i} was not refused", flush=True)

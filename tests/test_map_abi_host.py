@@ -1,0 +1,131 @@
+"""Host-side checks of the map operators (no GPU needed): the library exports
+what include/bevmap.h declares, and refuses bad arguments before any device work."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2205_13542_amd import _binding, _map_binding, build
+    if not os.path.exists(_binding.LIB_PATH):
+        build.build()
+    return _map_binding.load()
+
+
+@pytest.fixture(scope="module")
+def mb(lib):
+    from paper_2205_13542_amd import _map_binding
+    return _map_binding
+
+
+def test_library_exports_every_declared_symbol(lib, mb):
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "bevmap.h")).read(), flags=re.S)
+    names = set(re.findall(r"BEVPOOL_API\s+[\w\s\*]+?\b(bevmap_\w+)\s*\(", text))
+    assert names == set(mb.EXPORTED)
+    for name in names:
+        assert hasattr(lib, name), name
+
+
+P = ctypes.c_void_p(16)     # a pointer that no refused call follows
+INVALID, DTYPE, OVERFLOW = -1, -3, -4
+
+
+def _norm(mb, **over):
+    vals = dict(batch=2, pixels=9, channels=12, groups=3, row_stride=12, eps=1e-5, act=0, x_dtype=0, y_dtype=0,
+                weight_dtype=0)
+    vals.update(over)
+    return mb.bevmap_norm(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(batch=-1), INVALID), (dict(pixels=-1), INVALID), (dict(channels=0), INVALID), (dict(groups=0), INVALID),
+    (dict(groups=5), INVALID), (dict(row_stride=11), INVALID), (dict(eps=-1.0), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(act=4), INVALID), (dict(act=-1), INVALID), (dict(x_dtype=3), DTYPE),
+    (dict(y_dtype=-1), DTYPE), (dict(weight_dtype=7), DTYPE), (dict(batch=65536), OVERFLOW),
+    (dict(batch=4096, pixels=1 << 20), OVERFLOW), (dict(channels=8193, groups=1, row_stride=8193), OVERFLOW),
+    (dict(row_stride=1 << 31), OVERFLOW)])
+def test_group_norm_refuses(lib, mb, over, code):
+    n = _norm(mb, **over)
+    assert lib.bevmap_group_norm_workspace(n, 0) == code
+    assert lib.bevmap_group_norm(n, P, P, P, P, P, P, P, 1 << 30, None) == code
+    assert lib.bevmap_group_norm_backward(n, P, P, P, P, P, P, P, P, P, P, 1 << 30, None) == code
+
+
+def test_group_norm_refuses_pointers_and_workspaces(lib, mb):
+    n = _norm(mb)
+    need = lib.bevmap_group_norm_workspace(n, 0)
+    assert need > 0 and lib.bevmap_group_norm_workspace(n, 1) > need
+    assert lib.bevmap_group_norm(n, None, P, P, P, P, P, P, need, None) == INVALID
+    assert lib.bevmap_group_norm(n, P, P, P, None, P, P, P, need, None) == INVALID
+    assert lib.bevmap_group_norm(n, P, P, P, P, P, P, P, need - 1, None) == INVALID
+    assert lib.bevmap_group_norm(n, P, P, P, P, P, P, None, need, None) == INVALID
+    assert lib.bevmap_group_norm(n, P, P, P, P, P, P, ctypes.c_void_p(8), need, None) == INVALID
+    assert lib.bevmap_group_norm(None, P, P, P, P, P, P, P, need, None) == INVALID
+    assert lib.bevmap_group_norm_backward(n, P, P, P, P, P, P, P, P, P, P, need, None) == INVALID
+    assert lib.bevmap_group_norm_backward(n, P, P, P, P, P, P, None, P, P, P, 1 << 30, None) == INVALID
+    empty = _norm(mb, pixels=0)
+    assert lib.bevmap_group_norm_workspace(empty, 0) == 0
+    assert lib.bevmap_group_norm(empty, None, None, None, None, None, None, None, 0, None) == 0
+
+
+def _attend(mb, **over):
+    vals = dict(batch=2, queries=5, keys=7, heads=4, key_heads=2, dim=8, dtype=0, scale=0.3, q_batch=160, q_row=32,
+                q_head=8, k_batch=112, k_row=16, k_head=8, v_batch=112, v_row=16, v_head=8, mask_batch=7)
+    vals.update(over)
+    return mb.bevmap_attend(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(batch=-1), INVALID), (dict(queries=-1), INVALID), (dict(keys=-1), INVALID), (dict(heads=0), INVALID),
+    (dict(key_heads=0), INVALID), (dict(heads=3), INVALID), (dict(dim=0), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(k_row=-1), INVALID), (dict(q_batch=-1), INVALID),
+    (dict(mask_batch=-1), INVALID), (dict(dtype=3), DTYPE), (dict(dim=129), OVERFLOW),
+    (dict(batch=40000), OVERFLOW), (dict(keys=1 << 30), OVERFLOW), (dict(queries=1 << 29), OVERFLOW),
+    (dict(v_row=1 << 22), OVERFLOW)])
+def test_attention_refuses(lib, mb, over, code):
+    a = _attend(mb, **over)
+    assert lib.bevmap_attention_workspace(a, 0) == code
+    assert lib.bevmap_attention(a, P, P, P, None, None, P, None, None, P, 1 << 40, None) == code
+    assert lib.bevmap_attention_backward(a, P, P, P, P, None, None, P, P, P, P, P, P, P, 1 << 40, None) == code
+
+
+def test_attention_refuses_pointers_and_workspaces(lib, mb):
+    a = _attend(mb)
+    need = lib.bevmap_attention_workspace(a, 1)
+    assert need > 0
+    assert lib.bevmap_attention(a, None, P, P, None, None, P, None, None, P, 1 << 40, None) == INVALID
+    assert lib.bevmap_attention(a, P, None, P, None, None, P, None, None, P, 1 << 40, None) == INVALID
+    assert lib.bevmap_attention(a, P, P, P, None, None, None, None, None, P, 1 << 40, None) == INVALID
+    assert lib.bevmap_attention_backward(a, P, P, P, P, None, None, P, P, P, P, P, P, P, need - 1, None) == INVALID
+    assert lib.bevmap_attention_backward(a, P, P, P, P, None, None, P, P, None, P, P, P, P, need, None) == INVALID
+
+
+@pytest.mark.parametrize("args,code", [
+    ((P, 8, P, 8, P, -1, 8, 0, 100, 1, 2), INVALID), ((P, 8, P, 8, P, 4, -8, 0, 100, 1, 2), INVALID),
+    ((P, 7, P, 8, P, 4, 8, 0, 100, 1, 2), INVALID), ((P, 8, P, 7, P, 4, 8, 0, 100, 1, 2), INVALID),
+    ((P, 8, P, 8, P, 4, 8, 0, -1, 1, 2), INVALID), ((P, 8, P, 8, P, 4, 8, 0, 65537, 1, 2), INVALID),
+    ((P, 8, P, 8, P, 4, 8, 3, 100, 1, 2), DTYPE), ((None, 8, P, 8, P, 4, 8, 0, 100, 1, 2), INVALID),
+    ((P, 8, P, 8, None, 4, 8, 0, 100, 1, 2), INVALID), ((P, 1 << 31, P, 8, P, 4, 8, 0, 100, 1, 2), OVERFLOW),
+    ((P, 1 << 30, None, 0, P, 1 << 12, 1 << 30, 0, 100, 1, 2), OVERFLOW),
+    ((None, 0, None, 0, None, 0, 8, 0, 100, 1, 2), 0)])
+def test_dropout_refuses(lib, args, code):
+    assert lib.bevmap_dropout(*args, None) == code
+
+
+def test_python_entries_refuse():
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    x = torch.zeros(2, 3, 8)
+    q = torch.zeros(1, 2, 2, 4)
+    for call in (lambda: bev.group_norm_act(x, 2), lambda: bev.cross_attention(q, q, q),
+                 lambda: bev.dropout_add(x, 0.1, 3)):
+        with pytest.raises(bev.BevpoolError, match="device tensors"):
+            call()
+    for p, seed, offset in ((-0.1, 0, 0), (1.5, 0, 0), (float("nan"), 0, 0), (0.1, -1, 0), (0.1, 0, 1 << 64)):
+        with pytest.raises(bev.BevpoolError, match="outside|must be in"):
+            bev.dropout_add(x, p, seed, offset)
