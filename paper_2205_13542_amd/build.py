@@ -18,7 +18,8 @@ LIB_PATH = os.path.join(HERE, "libbevpool.so")
 FLOOR_SOURCE = "floor.hip"
 FLOOR_LIB_PATH = os.path.join(HERE, "libbevpool_floor.so")
 SOURCES = ["bevpool.hip", "plan.hip", "forward.hip", "backward.hip", "layout.hip",
-           "mapops.hip", "norm.hip", "dropout.hip", "attention.hip"]
+           "mapops.hip", "norm.hip", "dropout.hip", "attention.hip",
+           "attention_backward.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,285 @@
+// Device pieces shared by the attention kernels (attention.hip, attention_backward.hip).
+//
+// The queries of the heads that share a key head are the rows of one problem:
+// row r = query * group + head of the group, against that key head's keys. All
+// products run on the matrix cores in 32x32 blocks, held so that no result has
+// to change lanes to become the next product's operand:
+//
+// - A block of scores is formed as keys x rows (or rows x keys): with x the tile
+//   in LDS and y in registers, mma gives lane l column l % 32 (one row of y) and
+//   the 16 tile rows 8 (i / 4) + 4 (l / 32) + i % 4, i = 0..15.
+// - The second product contracts over those tile rows. Its order of summation is
+//   free, so step s takes the rows that a lane already holds, and only the
+//   tile's operand has to follow that order: read transposed from LDS,
+//   four tile rows at a time.
+#pragma once
+
+#include "mapops.h"
+
+namespace bevmap {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kAttendBlock = 256;       // four waves
+
+struct AttendArgs {
+    bevmap_attend a;
+    const void *q, *k, *v, *dout, *out, *out_low;
+    const int32_t *lengths;
+    const uint8_t *mask;
+    void *o, *o_low, *dq, *dk, *dv;
+    float *lse, *delta;
+    float *part;                  // fp32 parts of a split axis
+    float2 *part_stats;           // forward: (maximum, sum) of a part's rows
+    int32_t group, rows;          // heads that share a key head, queries * group
+    bevpool::FastDiv by_group;
+    int32_t n_tiles, n_split;     // tiles of the axis that a workgroup owns, parts of the other
+    float scale, log2_scale;      // |scale|, |scale| log2(e); 1 and log2(e) where scale is 0
+    float sign;                   // of scale, 0 where it is 0: q is multiplied by it
+};
+
+namespace {
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+
+// A chunk is 16 bytes: 8 elements of a 16-bit type, one step of K = 16, or 4 of
+// fp32, four steps of K = 2. In a row's chunks 2 j and 2 j + 1 the two half waves
+// hold the contracted elements of step j.
+template <int DT>
+struct Mma {
+    using T = typename Num<DT>::T;
+    static constexpr int kElems = 8;
+    using Vec = T __attribute__((ext_vector_type(8)));
+    // a block's 16 values of a lane as the second product's operand
+    struct Rows {
+        u32x4 half[2];
+    };
+    static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
+        if constexpr (DT == BEVPOOL_BF16)
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec, a), __builtin_bit_cast(Vec, b), c,
+                                                           0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec, a), __builtin_bit_cast(Vec, b), c, 0,
+                                                          0, 0);
+    }
+    static __device__ __forceinline__ Rows rows(const f32x16 &p) {
+        Rows r;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            Vec v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = T(p[8 * s + e]);
+            r.half[s] = __builtin_bit_cast(u32x4, v);
+        }
+        return r;
+    }
+};
+template <>
+struct Mma<BEVPOOL_F32> {
+    using T = float;
+    static constexpr int kElems = 4;
+    struct Rows {
+        f32x16 p;
+    };
+    static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ Rows rows(const f32x16 &p) { return Rows{p}; }
+};
+
+// Layout of a tile in LDS: rows of CH chunks (a power of two), chunk c of row r at
+// chunk c ^ turn(r). Sixteen consecutive rows read at one chunk, and four
+// consecutive rows read along 64 bytes, then fall into distinct banks.
+template <int CH>
+__device__ __forceinline__ int turn(int row) {
+    if constexpr (CH <= 4) return (row >> 2) & 3;
+    if constexpr (CH == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+    return (row & 3) << 2 | ((row >> 2) & 3);
+}
+template <int CH>
+__device__ __forceinline__ int chunk_at(int row, int c) {
+    return (row * CH + (c ^ turn<CH>(row))) * 16;
+}
+
+constexpr int pow2_chunks(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : 32; }
+
+// DB blocks of 32 channels of type DT.
+template <int DT, int DB>
+struct Shape {
+    using M = Mma<DT>;
+    using T = typename M::T;
+    static constexpr int kUsed = DB * 32 / M::kElems;        // chunks of a row
+    static constexpr int kChunks = pow2_chunks(kUsed);       // of a row in LDS
+    static constexpr int kRowBytes = kChunks * 16;
+    static constexpr int kSteps = kUsed / 2;
+
+    // acc[32 tile rows from row0][32 columns] += tile x y^T over the channels.
+    static __device__ __forceinline__ f32x16 scores(const char *tile, int row0, const u32x4 *y, f32x16 acc) {
+        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + chunk_at<kChunks>(row, 2 * s + half));
+            acc = M::mul(x, y[s], acc);
+        }
+        return acc;
+    }
+
+    // acc[d][32 channels from 32 d][32 columns] += tile^T x p over the 32 tile rows from row0.
+    static __device__ __forceinline__ void sums(const char *tile, int row0, const typename M::Rows &p,
+                                                f32x16 *acc) {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        if constexpr (DT != BEVPOOL_F32) {
+            using s4 = short __attribute__((ext_vector_type(4)));
+            using lds4 = __attribute__((address_space(3))) s4;
+            // ds_read_b64_tr_b16: in 16 lanes, lane t names 4 elements of row t / 4 at columns 4 (t % 4) and
+            // gets column t of the four rows
+            const int t = lane & 15, sub = (lane >> 4) & 1;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    u32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = row0 + 16 * s + 8 * e + 4 * half + (t >> 2);
+                        const int col = 4 * d + 2 * sub + ((t & 3) >> 1);       // in chunks
+                        const char *at = tile + chunk_at<kChunks>(row, col) + (t & 1) * 8;
+                        const u32x2 r = __builtin_bit_cast(
+                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at)));
+                        x[2 * e] = r[0];
+                        x[2 * e + 1] = r[1];
+                    }
+                    acc[d] = M::mul(x, p.half[s], acc[d]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = row0 + 8 * (i >> 2) + 4 * half + (i & 3);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int c = 32 * d + (lane & 31);
+                    const float x =
+                        *reinterpret_cast<const float *>(tile + chunk_at<kChunks>(row, c >> 2) + (c & 3) * 4);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p.p[i], acc[d], 0, 0, 0);
+                }
+            }
+        }
+    }
+};
+
+// One chunk of a row: elements c * kElems.. of dim, zeros past dim. VEC: rows
+// start on 16-byte boundaries and dim is a multiple of the chunk.
+template <int DT, bool VEC>
+__device__ __forceinline__ u32x4 load_chunk(const typename Num<DT>::T *row, int c, int dim) {
+    using T = typename Num<DT>::T;
+    constexpr int E = Mma<DT>::kElems;
+    u32x4 out = {0, 0, 0, 0};
+    if constexpr (VEC) {
+        if (c * E < dim) out = *reinterpret_cast<const u32x4 *>(row + c * E);
+    } else {
+        T v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = c * E + e < dim ? row[c * E + e] : T(0.0f);
+        out = __builtin_bit_cast(u32x4, v);
+    }
+    return out;
+}
+
+// The largest of a lane and the lane 32 away, and their sum.
+__device__ __forceinline__ float both_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Sample, key head and its addresses.
+template <int DT>
+struct Problem {
+    using T = typename Num<DT>::T;
+    const AttendArgs &g;
+    int b, hk, len;
+    __device__ __forceinline__ Problem(const AttendArgs &g_, int bh) : g(g_) {
+        b = bh / g.a.key_heads;
+        hk = bh - b * g.a.key_heads;
+        len = g.lengths ? min(max(g.lengths[b], 0), g.a.keys) : g.a.keys;
+    }
+    __device__ __forceinline__ void split_row(int r, int &i, int &h) const {
+        i = int(bevpool::fdiv(uint32_t(r), g.by_group));
+        h = hk * g.group + r - i * g.group;
+    }
+    __device__ __forceinline__ const T *q(int r) const {
+        int i, h;
+        split_row(r, i, h);
+        return static_cast<const T *>(g.q) + b * g.a.q_batch + i * g.a.q_row + h * g.a.q_head;
+    }
+    __device__ __forceinline__ const T *k(int j) const {
+        return static_cast<const T *>(g.k) + b * g.a.k_batch + hk * g.a.k_head + j * g.a.k_row;
+    }
+    __device__ __forceinline__ const T *v(int j) const {
+        return static_cast<const T *>(g.v) + b * g.a.v_batch + hk * g.a.v_head + j * g.a.v_row;
+    }
+    __device__ __forceinline__ int64_t row(int r) const {      // of out and its like, in elements
+        int i, h;
+        split_row(r, i, h);
+        return ((int64_t(b) * g.a.queries + i) * g.a.heads + h) * g.a.dim;
+    }
+    __device__ __forceinline__ int64_t stat(int r) const {     // of lse, delta
+        int i, h;
+        split_row(r, i, h);
+        return (int64_t(b) * g.a.heads + h) * g.a.queries + i;
+    }
+    __device__ __forceinline__ int64_t key(int j) const {      // of the gradients of k and v
+        return ((int64_t(b) * g.a.keys + j) * g.a.key_heads + hk) * g.a.dim;
+    }
+    // Which of 64 keys are in use, bit by bit; every lane of a wave asks for its own key.
+    __device__ __forceinline__ int ask(int j) const {
+        return j < len ? (g.mask ? g.mask[b * g.a.mask_batch + j] : 1) : 0;
+    }
+};
+
+// Work of workgroup id of n in an order in which neighbours run on one XCD.
+__device__ __forceinline__ int near_order(int id, int n) {
+    const int q = n >> 3, r = n & 7, x = id & 7, k = id >> 3;
+    return x < r ? x * (q + 1) + k : r * (q + 1) + (x - r) * q + k;
+}
+
+inline int attend_ceil(int64_t a, int64_t b) { return int((a + b - 1) / b); }
+
+AttendArgs attend_fill(const bevmap_attend &a, const void *q, const void *k, const void *v, const int32_t *lengths,
+                       const uint8_t *mask) {
+    AttendArgs g{};
+    g.a = a;
+    g.q = q;
+    g.k = k;
+    g.v = v;
+    g.lengths = lengths;
+    g.mask = mask;
+    g.group = a.heads / a.key_heads;
+    g.rows = a.queries * g.group;
+    g.by_group = bevpool::make_fastdiv(uint32_t(g.group));
+    g.scale = a.scale == 0.0f ? 1.0f : a.scale < 0.0f ? -a.scale : a.scale;
+    g.log2_scale = g.scale * kLog2e;
+    g.sign = a.scale == 0.0f ? 0.0f : a.scale < 0.0f ? -1.0f : 1.0f;
+    return g;
+}
+
+// Rows that can be read 16 bytes at a time.
+bool attend_vec(const bevmap_attend &a, const void *q, const void *k, const void *v) {
+    const int e = a.dtype == BEVPOOL_F32 ? 4 : 8;
+    auto ok = [&](const void *p, int64_t batch, int64_t row, int64_t head) {
+        return aligned_for(p, batch, a.dtype, e) && aligned_for(p, row, a.dtype, e) && aligned_for(p, head, a.dtype, e);
+    };
+    return a.dim % e == 0 && ok(q, a.q_batch, a.q_row, a.q_head) && ok(k, a.k_batch, a.k_row, a.k_head) &&
+           ok(v, a.v_batch, a.v_row, a.v_head);
+}
+
+}  // namespace
+}  // namespace bevmap

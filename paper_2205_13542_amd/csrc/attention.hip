@@ -1,219 +1,386 @@
-// Attention of queries to an encoder's states of another length, and its
-// gradients (bevmap_attention, bevmap_attention_backward).
+// Attention of queries to an encoder's states of another length, forward
+// (bevmap_attention); the layout of the products is in attention.h.
 //
-// The queries of the heads that share a key head are the rows of one problem:
-// row r = query * group + head of the group, against that head's keys. This
-// form gives one wave to a row (forward, gradient of q) or to a key (gradients
-// of k and v): lanes are keys for the scores and channels for the sums.
-#include "mapops.h"
+// A workgroup takes a tile of rows and walks the keys tile by tile: keys and values
+// go through registers to LDS one tile ahead of the products, every lane holds the
+// scores of one row against 16 of 32 keys, and a softmax with a running maximum
+// and sum joins the tiles in one pass over the keys. Few rows leave the chip idle,
+// so the keys are then split over workgroups, and a second kernel joins the parts.
+#include "attention.h"
 
 namespace bevmap {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+// Where a row's maximum grows by no more than this (log2), its old one is kept:
+// the exponentials stay below 2^8, far from any type's largest value, and the sums
+// so far need no rescaling.
+constexpr float kKeepMax = 8.0f;
 
-struct AttendArgs {
-    bevmap_attend a;
-    const void *q, *k, *v, *dout, *out, *out_low;
-    const int32_t *lengths;
-    const uint8_t *mask;
-    void *o, *o_low, *dq, *dk, *dv;
-    float *lse, *delta;
-    int32_t group, rows;      // heads that share a key head, queries * group
+// WR waves side by side have rows of their own (4), or all share the tile's rows
+// and split each tile's keys (1).
+template <int DT, int WR>
+struct Tile {
+    static constexpr int kBlocks = WR == 1 || DT == BEVPOOL_F32 ? 1 : 2;    // 32-key blocks of a wave
+    static constexpr int kKeys = 32 * kBlocks * (4 / WR);
+    static constexpr int kRows = 32 * WR;
+    // tiles in LDS: two where four arrays fit beside each other, else one
+    static constexpr int buffers(int row_bytes) { return 4 * kKeys * row_bytes <= 128 * 1024 ? 2 : 1; }
 };
 
-template <int DT>
-struct At {
-    using T = typename Num<DT>::T;
-    const AttendArgs &g;
-    int b, hk, len;
-    __device__ At(const AttendArgs &g_, int bh) : g(g_) {
-        b = bh / g.a.key_heads;
-        hk = bh - b * g.a.key_heads;
-        len = g.lengths ? min(max(g.lengths[b], 0), g.a.keys) : g.a.keys;
-    }
-    __device__ bool in_use(int j) const {
-        return j < len && (!g.mask || g.mask[b * g.a.mask_batch + j]);
-    }
-    __device__ const T *q(int r) const {
-        const int i = r / g.group, h = hk * g.group + r - i * g.group;
-        return static_cast<const T *>(g.q) + b * g.a.q_batch + i * g.a.q_row + h * g.a.q_head;
-    }
-    __device__ const T *k(int j) const {
-        return static_cast<const T *>(g.k) + b * g.a.k_batch + j * g.a.k_row + hk * g.a.k_head;
-    }
-    __device__ const T *v(int j) const {
-        return static_cast<const T *>(g.v) + b * g.a.v_batch + j * g.a.v_row + hk * g.a.v_head;
-    }
-    __device__ int64_t row(int r) const {      // of out and its like, in elements
-        const int i = r / g.group, h = hk * g.group + r - i * g.group;
-        return ((int64_t(b) * g.a.queries + i) * g.a.heads + h) * g.a.dim;
-    }
-    __device__ int64_t stat(int r) const {     // of lse, delta
-        const int i = r / g.group, h = hk * g.group + r - i * g.group;
-        return (int64_t(b) * g.a.heads + h) * g.a.queries + i;
-    }
-    __device__ int64_t key(int j) const {      // of the gradients of k and v
-        return ((int64_t(b) * g.a.keys + j) * g.a.key_heads + hk) * g.a.dim;
-    }
-};
-
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-    return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-    for (int m = 1; m < 64; m <<= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
+// What a part of a row with this maximum and sum counts where the whole row's
+// maximum is `most`: nothing without keys; a sum that is NaN without a maximum
+// (every score was NaN) stays one.
+__device__ __forceinline__ float part_weight(float top, float sum, float most) {
+    if (sum == 0.0f) return 0.0f;
+    return top == -INFINITY ? 1.0f : exp2f(top - most);
 }
 
-template <class T>
-__device__ __forceinline__ float dot(const float *a, const T *b, int dim) {
-    float s = 0.0f;
-    for (int c = 0; c < dim; ++c) s = fmaf(a[c], float(b[c]), s);
-    return s;
-}
+template <int DT, int DB, bool VEC, int WR>
+__global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
+    using S = Shape<DT, DB>;
+    using T = typename S::T;
+    using M = typename S::M;
+    using W = Tile<DT, WR>;
+    constexpr int kTileBytes = W::kKeys * S::kRowBytes;
+    constexpr int kLoads = (W::kKeys * S::kUsed + kAttendBlock - 1) / kAttendBlock;   // chunks of a thread
+    constexpr int kBuffers = W::buffers(S::kRowBytes);
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // [kBuffers][k, v][tile]
 
-template <int DT>
-__global__ __launch_bounds__(64) void k_attend(AttendArgs g) {
-    using T = typename Num<DT>::T;
-    __shared__ float q[128];
-    const At<DT> at(g, blockIdx.y);
-    const int lane = threadIdx.x, dim = g.a.dim, r = blockIdx.x;
-    for (int c = lane; c < dim; c += 64) q[c] = float(at.q(r)[c]);
-    __syncthreads();
-    const float scale = g.a.scale * kLog2e;
-    float top = -INFINITY, sum = 0.0f, o[2] = {0.0f, 0.0f};
-    for (int j0 = 0; j0 < at.len; j0 += 64) {
-        const int j = j0 + lane;
-        const float s = at.in_use(j) ? dot(q, at.k(j), dim) * scale : -INFINITY;
-        const float now = fmaxf(top, wave_max(s));
-        if (now == -INFINITY) continue;
-        const float old = exp2f(top - now), p = exp2f(s - now);
-        sum = sum * old + wave_sum(p);
-        for (int k = 0; k < 2; ++k) o[k] *= old;
-        top = now;
-        for (int i = 0; i < 64; ++i) {
-            const float pi = __shfl(p, i);
-            if (pi == 0.0f) continue;
-            for (int k = 0; k < 2; ++k)
-                if (lane + 64 * k < dim) o[k] = fmaf(pi, float(at.v(j0 + i)[lane + 64 * k]), o[k]);
+    const int n_bh = g.a.batch * g.a.key_heads;
+    int id = near_order(blockIdx.x, n_bh * g.n_split * g.n_tiles);
+    const int tile = id % g.n_tiles;
+    id /= g.n_tiles;
+    const int split = id % g.n_split, bh = id / g.n_split;
+    const Problem<DT> at(g, bh);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int row = tile * W::kRows + (WR == 1 ? 0 : 32 * wave) + (lane & 31);
+    const int dim = g.a.dim;
+
+    u32x4 q[S::kSteps];
+#pragma unroll
+    for (int s = 0; s < S::kSteps; ++s) q[s] = u32x4{0, 0, 0, 0};
+    if (row < g.rows) {
+        const T *p = at.q(row);
+#pragma unroll
+        for (int s = 0; s < S::kSteps; ++s) q[s] = load_chunk<DT, VEC>(p, 2 * s + half, dim);
+    }
+    if (g.sign != 1.0f) {
+        const uint32_t flip = DT == BEVPOOL_F32 ? 0x80000000u : 0x80008000u;
+#pragma unroll
+        for (int s = 0; s < S::kSteps; ++s) q[s] = g.sign == 0.0f ? u32x4{0, 0, 0, 0} : q[s] ^ flip;
+    }
+
+    // this part's tiles of keys
+    const int tiles = (at.len + W::kKeys - 1) / W::kKeys;
+    const int per = (tiles + g.n_split - 1) / g.n_split;
+    const int t0 = split * per, t1 = min(t0 + per, tiles);
+
+    u32x4 next_k[kLoads], next_v[kLoads];
+    int used[W::kKeys < 64 ? 1 : W::kKeys / 64];       // whether key lane + 64 w of the tile is in use
+    constexpr int kWords = W::kKeys < 64 ? 1 : W::kKeys / 64;
+    auto fetch = [&](int t) {
+        const int j0 = t * W::kKeys;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+            used[w] = W::kKeys >= 64 || lane < W::kKeys ? at.ask(j0 + 64 * w + lane) : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
+            next_k[i] = next_v[i] = u32x4{0, 0, 0, 0};
+            if (r < W::kKeys && j0 + r < at.len) {
+                next_k[i] = load_chunk<DT, VEC>(at.k(j0 + r), c, dim);
+                next_v[i] = load_chunk<DT, VEC>(at.v(j0 + r), c, dim);
+            }
         }
-    }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    for (int k = 0; k < 2; ++k) {
-        const int c = lane + 64 * k;
-        if (c >= dim) continue;
-        const float full = o[k] * inv;
-        const T rounded = T(full);
-        static_cast<T *>(g.o)[at.row(r) + c] = rounded;
-        if (DT != BEVPOOL_F32 && g.o_low) static_cast<T *>(g.o_low)[at.row(r) + c] = T(full - float(rounded));
-    }
-    if (lane == 0 && g.lse) g.lse[at.stat(r)] = sum > 0.0f ? top + log2f(sum) : -INFINITY;
-}
-
-template <int DT>
-__global__ __launch_bounds__(64) void k_attend_dq(AttendArgs g) {
-    using T = typename Num<DT>::T;
-    __shared__ float q[128], d[128];
-    const At<DT> at(g, blockIdx.y);
-    const int lane = threadIdx.x, dim = g.a.dim, r = blockIdx.x;
-    float delta = 0.0f;
-    for (int c = lane; c < dim; c += 64) {
-        q[c] = float(at.q(r)[c]);
-        d[c] = float(static_cast<const T *>(g.dout)[at.row(r) + c]);
-        float o = float(static_cast<const T *>(g.out)[at.row(r) + c]);
-        if (DT != BEVPOOL_F32 && g.out_low) o += float(static_cast<const T *>(g.out_low)[at.row(r) + c]);
-        delta = fmaf(d[c], o, delta);
-    }
-    delta = wave_sum(delta);
-    if (lane == 0) g.delta[at.stat(r)] = delta;
-    __syncthreads();
-    const float scale = g.a.scale * kLog2e, lse = g.lse[at.stat(r)];
-    float acc[2] = {0.0f, 0.0f};
-    for (int j0 = 0; j0 < at.len; j0 += 64) {
-        const int j = j0 + lane;
-        float ds = 0.0f;
-        if (at.in_use(j)) {
-            const float p = exp2f(dot(q, at.k(j), dim) * scale - lse);
-            ds = p * (dot(d, at.v(j), dim) - delta) * g.a.scale;
+    };
+    // to LDS, keys out of use as zeros; returns the words of keys in use
+    struct Words {
+        uint64_t w[kWords];
+    };
+    auto put = [&](int buffer) {
+        Words m;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) m.w[w] = __ballot(used[w] != 0);
+        char *k = lds + buffer * 2 * kTileBytes, *v = k + kTileBytes;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
+            if (r >= W::kKeys) break;
+            uint64_t word = m.w[0];
+            if constexpr (kWords == 2) word = r >= 64 ? m.w[1] : word;
+            const bool in = (word >> (r & 63)) & 1;
+            *reinterpret_cast<u32x4 *>(k + chunk_at<S::kChunks>(r, c)) = in ? next_k[i] : u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(v + chunk_at<S::kChunks>(r, c)) = in ? next_v[i] : u32x4{0, 0, 0, 0};
         }
-        for (int i = 0; i < 64; ++i) {
-            const float di = __shfl(ds, i);
-            if (di == 0.0f) continue;
-            for (int k = 0; k < 2; ++k)
-                if (lane + 64 * k < dim) acc[k] = fmaf(di, float(at.k(j0 + i)[lane + 64 * k]), acc[k]);
-        }
-    }
-    for (int k = 0; k < 2; ++k)
-        if (lane + 64 * k < dim) static_cast<T *>(g.dq)[at.row(r) + lane + 64 * k] = T(acc[k]);
-}
+        return m;
+    };
 
-template <int DT>
-__global__ __launch_bounds__(64) void k_attend_dkv(AttendArgs g) {
-    using T = typename Num<DT>::T;
-    __shared__ float key[128], val[128];
-    const At<DT> at(g, blockIdx.y);
-    const int lane = threadIdx.x, dim = g.a.dim, j = blockIdx.x;
-    const bool used = at.in_use(j);
-    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    for (int c = lane; c < dim && used; c += 64) {
-        key[c] = float(at.k(j)[c]);
-        val[c] = float(at.v(j)[c]);
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;     // of log2 scores; sum over this lane's keys
+    const float c = g.log2_scale;
+
+    Words words = {};
+    if (t0 < t1) {
+        fetch(t0);
+        words = put(0);
+        if (t0 + 1 < t1) fetch(t0 + 1);
     }
     __syncthreads();
-    const float scale = g.a.scale * kLog2e;
-    for (int r0 = 0; r0 < g.rows && used; r0 += 64) {
-        const int r = r0 + lane;
-        float p = 0.0f, ds = 0.0f;
-        if (r < g.rows) {
-            p = exp2f(dot(key, at.q(r), dim) * scale - g.lse[at.stat(r)]);
-            ds = p * (dot(val, static_cast<const T *>(g.dout) + at.row(r), dim) - g.delta[at.stat(r)]) * g.a.scale;
-        }
-        for (int i = 0; i < min(64, g.rows - r0); ++i) {
-            const float pi = __shfl(p, i), di = __shfl(ds, i);
-            for (int k = 0; k < 2; ++k)
-                if (lane + 64 * k < dim) {
-                    dv[k] = fmaf(pi, float(static_cast<const T *>(g.dout)[at.row(r0 + i) + lane + 64 * k]), dv[k]);
-                    dk[k] = fmaf(di, float(at.q(r0 + i)[lane + 64 * k]), dk[k]);
+    for (int t = t0; t < t1; ++t) {
+        const char *k = lds + ((t - t0) & (kBuffers - 1)) * 2 * kTileBytes, *v = k + kTileBytes;
+        // the words of this wave's keys
+        const int row0 = WR == 1 ? 32 * wave : 0;
+        uint64_t mine = words.w[0];
+        if constexpr (kWords == 2) mine = row0 >= 64 ? words.w[1] : mine;
+        if constexpr (WR == 1) mine = (mine >> (row0 & 63)) & 0xFFFFFFFFull;
+        if (mine != 0) {
+            f32x16 s[W::kBlocks];
+#pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
+                s[n] = S::scores(k, row0 + 32 * n, q, s[n]);
+            }
+            constexpr uint64_t kAll = W::kBlocks == 2 ? ~0ull : 0xFFFFFFFFull;
+            if (mine != kAll) {
+#pragma unroll
+                for (int n = 0; n < W::kBlocks; ++n) {
+                    const uint32_t bits = uint32_t(mine >> (32 * n)) >> (4 * half);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[n][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[n][i] : -INFINITY;
                 }
+            }
+            float high = s[0][0];
+#pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) high = fmaxf(high, s[n][i]);
+            high = both_max(high) * c;
+            if (__any(high > top + kKeepMax || (top == -INFINITY && high > top))) {
+                const float now = fmaxf(top, high);
+                const float old = top == -INFINITY ? 0.0f : exp2f(top - now);
+                sum *= old;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= old;
+                top = now;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
+                    sum += s[n][i];
+                }
+                S::sums(v, row0 + 32 * n, M::rows(s[n]), o);
+            }
+        }
+        if constexpr (kBuffers == 1) __syncthreads();
+        if (t + 1 < t1) {
+            words = put((t + 1 - t0) & (kBuffers - 1));
+            if (t + 2 < t1) fetch(t + 2);
+        }
+        __syncthreads();
+    }
+    sum = both_sum(sum);
+
+    if constexpr (WR == 1) {
+        // join the four waves, which saw different keys, through LDS
+        float *parts = reinterpret_cast<float *>(lds);          // [4][32 rows][32 DB + 1]
+        constexpr int kPitch = 32 * DB + 1;
+        float2 *stats = reinterpret_cast<float2 *>(parts + 4 * 32 * kPitch + (4 * 32 * kPitch & 1));
+        if (half == 0) stats[wave * 32 + lane] = make_float2(top, sum);
+        __syncthreads();
+        float most = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, stats[w * 32 + (lane & 31)].x);
+        const float mul = part_weight(top, sum, most);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                parts[(wave * 32 + (lane & 31)) * kPitch + 32 * d + 8 * (i >> 2) + 4 * half + (i & 3)] = o[d][i] * mul;
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 st = stats[w * 32 + (lane & 31)];
+            all += st.y * part_weight(st.x, st.y, most);
+        }
+        __syncthreads();
+        top = most;
+        sum = all;
+        // wave w keeps channel block w of the joined sums (DB <= 4)
+        if (wave >= DB) return;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at_ch = 32 * wave + 8 * (i >> 2) + 4 * half + (i & 3);
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v += parts[(w * 32 + (lane & 31)) * kPitch + at_ch];
+            o[0][i] = v;
         }
     }
-    for (int k = 0; k < 2; ++k)
-        if (lane + 64 * k < dim) {
-            static_cast<T *>(g.dk)[at.key(j) + lane + 64 * k] = T(dk[k]);
-            static_cast<T *>(g.dv)[at.key(j) + lane + 64 * k] = T(dv[k]);
+
+    if (row >= g.rows) return;
+    const int first = WR == 1 ? wave : 0, blocks = WR == 1 ? 1 : DB;
+    if (g.n_split > 1) {
+        const int64_t slot = (int64_t(split) * n_bh + bh) * g.rows + row;
+        if (half == 0 && first == 0) g.part_stats[slot] = make_float2(top, sum);
+        if (sum == 0.0f) return;              // the joining kernel does not read it
+        float *p = g.part + slot * dim;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            if (d >= blocks) break;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = 32 * (first + d) + 8 * (i >> 2) + 4 * half + (i & 3);
+                if (ch < dim) p[ch] = o[d][i];
+            }
         }
+        return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t to = at.row(row);
+    T *out = static_cast<T *>(g.o) + to;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        if (d >= blocks) break;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int ch = 32 * (first + d) + 8 * (i >> 2) + 4 * half + (i & 3);
+            if (ch >= dim) continue;
+            const float full = o[d][i] * inv;
+            const T rounded = T(full);
+            out[ch] = rounded;
+            if (DT != BEVPOOL_F32 && g.o_low) static_cast<T *>(g.o_low)[to + ch] = T(full - float(rounded));
+        }
+    }
+    if (g.lse && half == 0 && first == 0) g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
-AttendArgs fill(const bevmap_attend &a, const void *q, const void *k, const void *v, const int32_t *lengths,
-                const uint8_t *mask) {
-    AttendArgs g{};
-    g.a = a;
-    g.q = q;
-    g.k = k;
-    g.v = v;
-    g.lengths = lengths;
-    g.mask = mask;
-    g.group = a.heads / a.key_heads;
-    g.rows = a.queries * g.group;
-    return g;
+// Joins the parts of a row: a workgroup to a row, its NW waves share the parts,
+// lanes are channels.
+template <int DT, int NW>
+__global__ __launch_bounds__(64 * NW) void k_attend_join(AttendArgs g) {
+    using T = typename Num<DT>::T;
+    __shared__ float red[2][NW], sums[NW][128];
+    const int64_t slot = blockIdx.x, total = gridDim.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = g.a.dim;
+    const int bh = int(slot / g.rows), row = int(slot - int64_t(bh) * g.rows);
+    const float2 *stats = g.part_stats + slot;
+    float top = -INFINITY;
+    for (int s = threadIdx.x; s < g.n_split; s += 64 * NW) top = fmaxf(top, stats[s * total].x);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if (lane == 0) red[0][wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, red[0][w]);
+    float sum = 0.0f, o[2] = {0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = wave; s < g.n_split; s += NW) {
+        const float2 st = stats[s * total];
+        const float mul = part_weight(st.x, st.y, top);
+        sum = fmaf(st.y, mul, sum);
+        const float *p = g.part + (s * total + slot) * dim;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float v = lane + 64 * k < dim ? p[lane + 64 * k] : 0.0f;
+            o[k] += st.y == 0.0f ? 0.0f : v * mul;        // a part without keys wrote no sums
+        }
+    }
+    sums[wave][lane] = o[0];
+    sums[wave][64 + lane] = o[1];
+    if (lane == 0) red[1][wave] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) sum += red[1][w];
+    const Problem<DT> at(g, bh);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t to = at.row(row);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int ch = lane + 64 * k;
+        if (ch >= dim) break;
+        float full = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) full += sums[w][ch];
+        full *= inv;
+        const T rounded = T(full);
+        static_cast<T *>(g.o)[to + ch] = rounded;
+        if (DT != BEVPOOL_F32 && g.o_low) static_cast<T *>(g.o_low)[to + ch] = T(full - float(rounded));
+    }
+    if (g.lse && lane == 0) g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
-template <int DT>
-int forward(const AttendArgs &g, hipStream_t stream) {
-    if (g.rows > 0)
-        hipLaunchKernelGGL((k_attend<DT>), dim3(g.rows, g.a.batch * g.a.key_heads), dim3(64), 0, stream, g);
+constexpr int kFill = 768;          // workgroups that fill the chip, three to a compute unit
+constexpr int kFewRows = 32;        // rows of a key head that one wave holds
+
+// Rows, row tiles and parts of the keys, a rule on the sizes alone. Workgroups
+// that do not fill the chip split the keys, down to two tiles of keys a part.
+void partition(const bevmap_attend &a, AttendArgs *g, bool *few) {
+    const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
+    *few = rows <= kFewRows;
+    const int tile_rows = *few ? 32 : 128;
+    const int tile_keys = *few ? 128 : a.dtype == BEVPOOL_F32 ? 32 : 64;
+    g->n_tiles = attend_ceil(rows, tile_rows);
+    const int64_t whole = int64_t(a.batch) * a.key_heads * g->n_tiles;
+    int64_t split = whole ? (kFill + whole - 1) / whole : 1;
+    const int64_t most = attend_ceil(a.keys, 2 * tile_keys);
+    if (split > most) split = most;
+    g->n_split = split < 1 ? 1 : int(split);
+}
+
+template <int DT, int DB, bool VEC, int WR>
+int launch(const AttendArgs &g, hipStream_t stream) {
+    using S = Shape<DT, DB>;
+    using W = Tile<DT, WR>;
+    size_t lds = 2 * W::buffers(S::kRowBytes) * size_t(W::kKeys) * S::kRowBytes;
+    if (WR == 1) {
+        const size_t join = (4 * 32 * (32 * DB + 1) + 2 * 128 + 1) * sizeof(float);
+        lds = lds > join ? lds : join;
+    }
+    if (lds > 64 * 1024)
+        BEVPOOL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_attend<DT, DB, VEC, WR>),
+                                        hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)));
+    const uint32_t grid = uint32_t(g.a.batch) * g.a.key_heads * g.n_split * g.n_tiles;
+    hipLaunchKernelGGL((k_attend<DT, DB, VEC, WR>), dim3(grid), dim3(kAttendBlock), lds, stream, g);
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
 
+template <int DT, int DB>
+int launch(const AttendArgs &g, bool vec, bool few, hipStream_t stream) {
+    if (few) return vec ? launch<DT, DB, true, 1>(g, stream) : launch<DT, DB, false, 1>(g, stream);
+    return vec ? launch<DT, DB, true, 4>(g, stream) : launch<DT, DB, false, 4>(g, stream);
+}
+
 template <int DT>
-int backward(const AttendArgs &g, hipStream_t stream) {
-    const uint32_t bh = g.a.batch * g.a.key_heads;
-    if (g.rows > 0) hipLaunchKernelGGL((k_attend_dq<DT>), dim3(g.rows, bh), dim3(64), 0, stream, g);
-    BEVPOOL_HIP(hipGetLastError());
-    if (g.a.keys > 0) hipLaunchKernelGGL((k_attend_dkv<DT>), dim3(g.a.keys, bh), dim3(64), 0, stream, g);
+int forward(const AttendArgs &g, bool vec, bool few, hipStream_t stream) {
+    int rc;
+    switch ((g.a.dim + 31) / 32) {
+        case 1: rc = launch<DT, 1>(g, vec, few, stream); break;
+        case 2: rc = launch<DT, 2>(g, vec, few, stream); break;
+        case 3: rc = launch<DT, 3>(g, vec, few, stream); break;
+        default: rc = launch<DT, 4>(g, vec, few, stream); break;
+    }
+    if (rc || g.n_split == 1) return rc;
+    const dim3 rows(uint32_t(g.a.batch) * g.a.key_heads * g.rows);
+    if (g.n_split >= 64)
+        hipLaunchKernelGGL((k_attend_join<DT, 16>), rows, dim3(1024), 0, stream, g);
+    else if (g.n_split >= 8)
+        hipLaunchKernelGGL((k_attend_join<DT, 4>), rows, dim3(256), 0, stream, g);
+    else
+        hipLaunchKernelGGL((k_attend_join<DT, 1>), rows, dim3(64), 0, stream, g);
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -224,41 +391,34 @@ int backward(const AttendArgs &g, hipStream_t stream) {
 using namespace bevmap;
 
 int64_t bevmap_attention_workspace_bytes(const bevmap_attend &a, bool backward) {
-    return backward ? int64_t(a.batch) * a.queries * a.heads * int64_t(sizeof(float)) : 0;
+    if (backward) return bevmap_attention_backward_bytes(a);
+    AttendArgs g{};
+    bool few;
+    partition(a, &g, &few);
+    if (g.n_split <= 1) return 0;
+    return int64_t(g.n_split) * a.batch * a.queries * a.heads *
+           (a.dim * int64_t(sizeof(float)) + int64_t(sizeof(float2)));
 }
 
 int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k, const void *v,
                             const int32_t *lengths, const uint8_t *mask, void *out, void *out_low, float *lse,
-                            void *, hipStream_t stream) {
-    AttendArgs g = fill(a, q, k, v, lengths, mask);
+                            void *workspace, hipStream_t stream) {
+    if (a.batch == 0 || a.queries == 0) return BEVPOOL_OK;
+    AttendArgs g = attend_fill(a, q, k, v, lengths, mask);
     g.o = out;
     g.o_low = out_low;
     g.lse = lse;
-    if (a.batch == 0) return BEVPOOL_OK;
+    bool few;
+    partition(a, &g, &few);
+    g.part_stats = static_cast<float2 *>(workspace);
+    g.part = reinterpret_cast<float *>(g.part_stats + int64_t(g.n_split) * a.batch * a.queries * a.heads);
+    if (int64_t(a.batch) * a.key_heads * g.n_split * g.n_tiles >= (int64_t(1) << 31) / kAttendBlock)
+        return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d heads=%d: too many tiles of rows", a.batch,
+                            a.queries, a.heads);
+    const bool vec = attend_vec(a, q, k, v);
     switch (a.dtype) {
-        case BEVPOOL_F32: return forward<BEVPOOL_F32>(g, stream);
-        case BEVPOOL_BF16: return forward<BEVPOOL_BF16>(g, stream);
-        default: return forward<BEVPOOL_F16>(g, stream);
-    }
-}
-
-int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_out, const void *q, const void *k,
-                                     const void *v, const int32_t *lengths, const uint8_t *mask, const void *out,
-                                     const void *out_low, const float *lse, void *grad_q, void *grad_k,
-                                     void *grad_v, void *workspace, hipStream_t stream) {
-    AttendArgs g = fill(a, q, k, v, lengths, mask);
-    g.dout = grad_out;
-    g.out = out;
-    g.out_low = out_low;
-    g.lse = const_cast<float *>(lse);
-    g.dq = grad_q;
-    g.dk = grad_k;
-    g.dv = grad_v;
-    g.delta = static_cast<float *>(workspace);
-    if (a.batch == 0) return BEVPOOL_OK;
-    switch (a.dtype) {
-        case BEVPOOL_F32: return backward<BEVPOOL_F32>(g, stream);
-        case BEVPOOL_BF16: return backward<BEVPOOL_BF16>(g, stream);
-        default: return backward<BEVPOOL_F16>(g, stream);
+        case BEVPOOL_F32: return forward<BEVPOOL_F32>(g, vec, few, stream);
+        case BEVPOOL_BF16: return forward<BEVPOOL_BF16>(g, vec, few, stream);
+        default: return forward<BEVPOOL_F16>(g, vec, few, stream);
     }
 }

@@ -20,6 +20,7 @@ int bevmap_launch_norm_backward(const bevmap_norm &n, const void *grad_y, const 
                                 const void *bias, const float *mean, const float *rstd, void *grad_x,
                                 void *grad_weight, void *grad_bias, void *workspace, hipStream_t stream);
 int64_t bevmap_attention_workspace_bytes(const bevmap_attend &a, bool backward);
+int64_t bevmap_attention_backward_bytes(const bevmap_attend &a);
 int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k, const void *v,
                             const int32_t *lengths, const uint8_t *mask, void *out, void *out_low, float *lse,
                             void *workspace, hipStream_t stream);
