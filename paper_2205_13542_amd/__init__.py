@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import _binding
+from . import _binding, _map_binding
 from ._binding import (BEVPOOL_BF16, BEVPOOL_F16, BEVPOOL_F32, BEVPOOL_MAX, BEVPOOL_MEAN,
                        BEVPOOL_SUM, BevpoolError,
                        bevpool_backward, bevpool_forward, bevpool_forward_ex,
@@ -23,7 +23,6 @@ from ._binding import (BEVPOOL_BF16, BEVPOOL_F16, BEVPOOL_F32, BEVPOOL_MAX, BEVP
                        bevpool_plan, bevpool_plan_destroy, bevpool_plan_export,
                        bevpool_plan_import, bevpool_associate_noalloc, bevpool_plan_slabs,
                        bevpool_plan_info_get, bevpool_version)
-from .map_ops import cross_attention, dropout_add, group_norm_act
 
 __all__ = [
     "Plan", "SlabPlan", "bev_pool", "BevpoolError", "bevpool_plan", "bevpool_forward", "bevpool_forward_ex",
@@ -35,6 +34,19 @@ __all__ = [
     "bevpool_associate_noalloc", "associate_noalloc", "bevpool_plan_slabs",
     "group_norm_act", "cross_attention", "dropout_add",
 ]
+
+_MAP_OPS = ("group_norm_act", "cross_attention", "dropout_add")
+
+
+def __getattr__(name):
+    """The map operators, whose module needs torch where the rest of the package
+    needs it only when called."""
+    if name in _MAP_OPS:
+        from . import map_ops
+        globals().update((n, getattr(map_ops, n)) for n in _MAP_OPS)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+
 
 _GEOM_FIELDS = [f for f, _ in bevpool_geometry._fields_]
 

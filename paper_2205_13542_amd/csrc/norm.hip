@@ -16,9 +16,11 @@
 namespace bevmap {
 namespace {
 
-constexpr int kNormBlock = 256;
-constexpr int kNormRows = 4;        // rows that a thread has in flight
-constexpr int kMergeLanes = 16;     // lanes that join one group's parts
+constexpr int kNormBlock = 256;     // apply passes
+constexpr int kSumBlock = 512;      // sum passes: few large workgroups, so that few parts are left to join
+constexpr int kSumRows = 8;         // rows that a thread has in flight, in k_norm_sum
+constexpr int kNormRows = 4;        // and elsewhere
+constexpr int kMergeLanes = 16;     // lanes that join one group's channels
 constexpr int kWgradChannels = 16;  // channels of a workgroup that sums weight gradients
 
 struct NormArgs {
@@ -74,10 +76,11 @@ struct Columns {
     int vectors, lanes;   // vectors of this block, row lanes that walk it
     int lane, vec;        // of this thread; lane >= lanes: idle
 };
+template <int BLOCK>
 __device__ __forceinline__ Columns columns(int first, int n_vec) {
     Columns c;
-    c.vectors = min(kNormBlock, n_vec - first);
-    c.lanes = kNormBlock / c.vectors;
+    c.vectors = min(BLOCK, n_vec - first);
+    c.lanes = BLOCK / c.vectors;
     c.lane = threadIdx.x / c.vectors;
     c.vec = first + threadIdx.x - c.lane * c.vectors;
     return c;
@@ -85,7 +88,7 @@ __device__ __forceinline__ Columns columns(int first, int n_vec) {
 
 // Statistics of a chunk of rows: parts[b][chunk][g] = (mean, M2).
 template <int DT, int V>
-__global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
+__global__ __launch_bounds__(kSumBlock) void k_norm_sum(NormArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float lds[];
     float *ch_mean = lds, *ch_m2 = lds + a.C;             // [C] each
@@ -93,8 +96,8 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
     const int b = blockIdx.y, r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
     const int n_vec = a.C / V;
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
-    for (int first = 0; first < n_vec; first += kNormBlock) {
-        const Columns c = columns(first, n_vec);
+    for (int first = 0; first < n_vec; first += kSumBlock) {
+        const Columns c = columns<kSumBlock>(first, n_vec);
         float mean[V], m2[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f;
@@ -102,25 +105,25 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
         if (c.lane < c.lanes) {
             const T *p = x + c.vec * V;
             int r = r0 + c.lane;
-            for (; r + (kNormRows - 1) * c.lanes < r1; r += kNormRows * c.lanes) {
-                float v[kNormRows][V];
+            for (; r + (kSumRows - 1) * c.lanes < r1; r += kSumRows * c.lanes) {
+                float v[kSumRows][V];
 #pragma unroll
-                for (int k = 0; k < kNormRows; ++k) load_n<T, V>(p + int64_t(r + k * c.lanes) * a.ldx, v[k]);
-                // join kNormRows values of each channel to the n before them
-                const float share = float(kNormRows) / float(n + kNormRows), both = float(n) * share;
+                for (int k = 0; k < kSumRows; ++k) load_n<T, V>(p + int64_t(r + k * c.lanes) * a.ldx, v[k]);
+                // join kSumRows values of each channel to the n before them
+                const float share = float(kSumRows) / float(n + kSumRows), both = float(n) * share;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float m = 0.0f, q = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < kNormRows; ++k) m += v[k][i];
-                    m *= 1.0f / kNormRows;
+                    for (int k = 0; k < kSumRows; ++k) m += v[k][i];
+                    m *= 1.0f / kSumRows;
 #pragma unroll
-                    for (int k = 0; k < kNormRows; ++k) q = fmaf(v[k][i] - m, v[k][i] - m, q);
+                    for (int k = 0; k < kSumRows; ++k) q = fmaf(v[k][i] - m, v[k][i] - m, q);
                     const float d = m - mean[i];
                     mean[i] = fmaf(d, share, mean[i]);
                     m2[i] += fmaf(d * d, both, q);
                 }
-                n += kNormRows;
+                n += kSumRows;
             }
             for (; r < r1; r += c.lanes) {
                 float v[V];
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
         __syncthreads();
         // join the row lanes; lane l walked ceil((rows - l) / lanes) rows
         const int rows = r1 - r0;
-        for (int i = threadIdx.x; i < width; i += kNormBlock) {
+        for (int i = threadIdx.x; i < width; i += kSumBlock) {
             float m = 0.0f, q = 0.0f;
             for (int l = 0; l < c.lanes; ++l) m += th[l * width + i] * float((rows - l + c.lanes - 1) / c.lanes);
             m /= float(rows);
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
     }
     // join a group's channels, all of equal counts
     const int lane = threadIdx.x % kMergeLanes;
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+    for (int g0 = 0; g0 < a.G; g0 += kSumBlock / kMergeLanes) {
         const int g = g0 + threadIdx.x / kMergeLanes;
         float m = 0.0f, q = 0.0f;
         if (g < a.G)
@@ -177,25 +180,56 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_sum(NormArgs a) {
     }
 }
 
-// Joins the chunks' statistics of frame b: group g's mean and rstd to LDS.
+// The lanes, a power of two, that join one group's parts in an apply pass: the
+// workgroup's threads divided among the groups.
+__device__ __forceinline__ int join_lanes(int G) {
+    int n = 64;
+    while (n > 1 && n * G > kNormBlock) n >>= 1;
+    return n;
+}
+__device__ __forceinline__ float sum_over(float v, int lanes) {
+    for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Joins the chunks' statistics of frame b: group g's mean and rstd to LDS. A
+// lane keeps its first kJoin parts in registers, where all of them are on the way at once.
+constexpr int kJoin = 8;
 __device__ __forceinline__ void join_chunks(const NormArgs &a, int b, float *mean, float *rstd, bool write) {
-    const int lane = threadIdx.x % kMergeLanes;
+    const int lanes = join_lanes(a.G), lane = threadIdx.x & (lanes - 1);
     const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
     const float total = float(a.rows);
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
-        const int g = g0 + threadIdx.x / kMergeLanes;
+    auto rows_of = [&](int k) { return float(min(a.chunk, a.rows - k * a.chunk)); };
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / lanes) {
+        const int g = g0 + threadIdx.x / lanes;
         float m = 0.0f, q = 0.0f;
-        if (g < a.G)
-            for (int k = lane; k < a.n_chunks; k += kMergeLanes)
-                m += parts[int64_t(k) * a.G + g].x * float(min(a.chunk, a.rows - k * a.chunk));
-        m = lane_sum(m) / total;
-        if (g < a.G)
-            for (int k = lane; k < a.n_chunks; k += kMergeLanes) {
-                const float2 p = parts[int64_t(k) * a.G + g];
-                const float d = p.x - m;
-                q += p.y + d * d * (float(min(a.chunk, a.rows - k * a.chunk)) * float(a.per));
+        float2 p[kJoin];
+        if (g < a.G) {
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i) {
+                const int k = lane + i * lanes;
+                p[i] = k < a.n_chunks ? parts[k * a.G + g] : make_float2(0.0f, 0.0f);
             }
-        q = lane_sum(q);
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i)
+                if (lane + i * lanes < a.n_chunks) m = fmaf(p[i].x, rows_of(lane + i * lanes), m);
+            for (int k = lane + kJoin * lanes; k < a.n_chunks; k += lanes) m = fmaf(parts[k * a.G + g].x, rows_of(k), m);
+        }
+        m = sum_over(m, lanes) / total;
+        if (g < a.G) {
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i)
+                if (lane + i * lanes < a.n_chunks) {
+                    const float d = p[i].x - m;
+                    q += fmaf(d * d, rows_of(lane + i * lanes) * float(a.per), p[i].y);
+                }
+            for (int k = lane + kJoin * lanes; k < a.n_chunks; k += lanes) {
+                const float2 r = parts[k * a.G + g];
+                const float d = r.x - m;
+                q += fmaf(d * d, rows_of(k) * float(a.per), r.y);
+            }
+        }
+        q = sum_over(q, lanes);
         if (g < a.G && lane == 0) {
             const float rs = 1.0f / sqrtf(q / (total * float(a.per)) + a.eps);
             mean[g] = m;
@@ -214,13 +248,15 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_apply(NormArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float lds[];
     float *mean = lds, *rstd = lds + a.G;
-    const int b = blockIdx.y, r0 = blockIdx.x * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
+    // back to front: what the sum pass read last is still in cache
+    const int b = a.batch - 1 - blockIdx.y;
+    const int r0 = (a.n_apply - 1 - blockIdx.x) * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
     join_chunks(a, b, mean, rstd, blockIdx.x == 0);
     const int n_vec = a.C / V;
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
     const int64_t out0 = int64_t(b) * a.rows * a.C;
     for (int first = 0; first < n_vec; first += kNormBlock) {
-        const Columns c = columns(first, n_vec);
+        const Columns c = columns<kNormBlock>(first, n_vec);
         if (c.lane >= c.lanes) continue;
         float mu[V], mul[V], add[V];
 #pragma unroll
@@ -249,7 +285,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_apply(NormArgs a) {
 // Per channel sums over a chunk of dz and dz * xh, with dz = dy act'(z); and per
 // group those sums with the channels' weights: parts = (sum e, sum e xh), e = dz w.
 template <int DT, int V>
-__global__ __launch_bounds__(kNormBlock) void k_norm_grad_sum(NormArgs a) {
+__global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float lds[];
     float *ch_sum = lds, *ch_dot = lds + a.C;
@@ -259,8 +295,8 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_sum(NormArgs a) {
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
     const int64_t dy0 = int64_t(b) * a.rows * a.C;
     float *sums = a.channel_sums + (int64_t(b) * a.n_chunks + blockIdx.x) * 2 * a.C;
-    for (int first = 0; first < n_vec; first += kNormBlock) {
-        const Columns c = columns(first, n_vec);
+    for (int first = 0; first < n_vec; first += kSumBlock) {
+        const Columns c = columns<kSumBlock>(first, n_vec);
         const int width = c.vectors * V;
         if (c.lane < c.lanes) {
             float mu[V], rs[V], w[V], add[V], sum[V], dot[V];
@@ -300,7 +336,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_sum(NormArgs a) {
             }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < width; i += kNormBlock) {
+        for (int i = threadIdx.x; i < width; i += kSumBlock) {
             float s = 0.0f, d = 0.0f;
             for (int l = 0; l < c.lanes; ++l) {
                 s += th[l * width + i];
@@ -316,7 +352,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_sum(NormArgs a) {
         __syncthreads();
     }
     const int lane = threadIdx.x % kMergeLanes;
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
+    for (int g0 = 0; g0 < a.G; g0 += kSumBlock / kMergeLanes) {
         const int g = g0 + threadIdx.x / kMergeLanes;
         float s = 0.0f, d = 0.0f;
         if (g < a.G)
@@ -361,26 +397,27 @@ template <int DT, int V>
 __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float lds[];
-    const int b = blockIdx.y;
+    const int b = a.batch - 1 - blockIdx.y;      // back to front, as k_norm_apply
     if (int(blockIdx.x) >= a.n_apply) {
         if (b == 0) weight_gradients(a, blockIdx.x - a.n_apply, lds);
         return;
     }
     float *m1 = lds, *m2 = lds + a.G;
-    const int r0 = blockIdx.x * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
-    const int lane = threadIdx.x % kMergeLanes;
+    const int r0 = (a.n_apply - 1 - blockIdx.x) * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
+    const int lanes = join_lanes(a.G), lane = threadIdx.x & (lanes - 1);
     const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / kMergeLanes) {
-        const int g = g0 + threadIdx.x / kMergeLanes;
+    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / lanes) {
+        const int g = g0 + threadIdx.x / lanes;
         float s = 0.0f, d = 0.0f;
         if (g < a.G)
-            for (int k = lane; k < a.n_chunks; k += kMergeLanes) {
-                const float2 p = parts[int64_t(k) * a.G + g];
+#pragma unroll 8
+            for (int k = lane; k < a.n_chunks; k += lanes) {
+                const float2 p = parts[k * a.G + g];
                 s += p.x;
                 d += p.y;
             }
-        s = lane_sum(s);
-        d = lane_sum(d);
+        s = sum_over(s, lanes);
+        d = sum_over(d, lanes);
         if (g < a.G && lane == 0) {
             const float inv = 1.0f / (float(a.rows) * float(a.per));
             m1[g] = s * inv;
@@ -393,7 +430,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
     T *dx = static_cast<T *>(a.dx) + int64_t(b) * a.rows * a.C;
     const int64_t dy0 = int64_t(b) * a.rows * a.C;
     for (int first = 0; first < n_vec; first += kNormBlock) {
-        const Columns c = columns(first, n_vec);
+        const Columns c = columns<kNormBlock>(first, n_vec);
         if (c.lane >= c.lanes) continue;
         float mu[V], rs[V], w[V], add[V], e1[V], e2[V];
 #pragma unroll
@@ -430,14 +467,18 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
 }
 
 constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
+constexpr int kMaxChunks = 256;     // chunks of a frame at most
 constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
 constexpr int kMinRows = 16;        // rows of a chunk at least
+constexpr int kMaxParts = 8192;     // parts of a frame (chunks x groups) at most, each apply workgroup joins them
 
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
 void split(const bevmap_norm &n, NormArgs *a) {
-    const int per_frame = kSumGrid / (n.batch < kSumGrid ? n.batch : kSumGrid);
-    a->chunk = ceil_div(n.pixels, per_frame);
+    int chunks = kSumGrid / (n.batch < kSumGrid ? n.batch : kSumGrid);
+    if (chunks > kMaxChunks) chunks = kMaxChunks;
+    if (chunks > kMaxParts / n.groups) chunks = kMaxParts / n.groups;
+    a->chunk = ceil_div(n.pixels, chunks);
     if (a->chunk < kMinRows) a->chunk = kMinRows;
     a->n_chunks = ceil_div(n.pixels, a->chunk);
     const int apply = kApplyGrid / (n.batch < kApplyGrid ? n.batch : kApplyGrid);
@@ -478,7 +519,7 @@ int vector_of(const bevmap_norm &n, const void *x, const void *y, const void *dx
 }
 
 // Bytes of LDS: two floats a channel, and two for each thread's V channels.
-size_t sum_lds(const NormArgs &a, int v) { return (2 * size_t(a.C) + 2 * size_t(kNormBlock) * v) * sizeof(float); }
+size_t sum_lds(const NormArgs &a, int v) { return (2 * size_t(a.C) + 2 * size_t(kSumBlock) * v) * sizeof(float); }
 
 // Raises a kernel's limit of dynamic LDS where it needs more than the default.
 template <class K>
@@ -493,7 +534,7 @@ template <int DT, int V>
 int forward(const NormArgs &a, hipStream_t stream) {
     const size_t lds = sum_lds(a, V);
     if (int rc = allow_lds(k_norm_sum<DT, V>, lds)) return rc;
-    hipLaunchKernelGGL((k_norm_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kNormBlock), lds, stream, a);
+    hipLaunchKernelGGL((k_norm_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kSumBlock), lds, stream, a);
     BEVPOOL_HIP(hipGetLastError());
     const size_t lds2 = 2 * size_t(a.G) * sizeof(float);
     if (int rc = allow_lds(k_norm_apply<DT, V>, lds2)) return rc;
@@ -506,7 +547,7 @@ template <int DT, int V>
 int backward(const NormArgs &a, hipStream_t stream) {
     const size_t lds = sum_lds(a, V);
     if (int rc = allow_lds(k_norm_grad_sum<DT, V>, lds)) return rc;
-    hipLaunchKernelGGL((k_norm_grad_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kNormBlock), lds, stream, a);
+    hipLaunchKernelGGL((k_norm_grad_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kSumBlock), lds, stream, a);
     BEVPOOL_HIP(hipGetLastError());
     const size_t lds2 = size_t(a.G > kNormBlock ? a.G : kNormBlock) * 2 * sizeof(float);
     if (int rc = allow_lds(k_norm_grad_apply<DT, V>, lds2)) return rc;

@@ -13,26 +13,22 @@ from __future__ import annotations
 
 import math
 
+import torch
+
 from . import _binding, _map_binding
 from ._binding import BevpoolError
 
 _ACTS = {"none": _map_binding.BEVMAP_ACT_NONE, "relu": _map_binding.BEVMAP_ACT_RELU,
          "silu": _map_binding.BEVMAP_ACT_SILU, "gelu": _map_binding.BEVMAP_ACT_GELU}
+_CODES = {torch.float32: _binding.BEVPOOL_F32, torch.bfloat16: _binding.BEVPOOL_BF16,
+          torch.float16: _binding.BEVPOOL_F16}
 
 
 def _refuse(message, code=_binding.BEVPOOL_ERR_INVALID_ARG):
     raise BevpoolError(code, message)
 
 
-_CODES = None
-
-
 def _code(dtype) -> int:
-    global _CODES
-    if _CODES is None:
-        import torch
-        _CODES = {torch.float32: _binding.BEVPOOL_F32, torch.bfloat16: _binding.BEVPOOL_BF16,
-                  torch.float16: _binding.BEVPOOL_F16}
     code = _CODES.get(dtype)
     if code is None:
         _refuse(f"dtype {dtype}", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
@@ -59,47 +55,48 @@ def _row_stride(t):
     return shape[-1] if step is None else step if step >= shape[-1] else None
 
 
-def _on(device, *tensors):
-    """Refuses tensors that are not all on one GPU."""
-    for t in tensors:
-        if t is not None and t.device != device:
-            _refuse("all tensors must be on one device")
-    if device.type != "cuda":
+def _device(first, *others) -> int:
+    """The index of the GPU that holds all tensors (None among them is skipped)."""
+    if not first.is_cuda:
         _refuse("inputs must be device tensors")
+    index = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            _refuse("all tensors must be on one device")
+    return index
 
 
-class _Current:
-    """Makes a device current and knows its current stream (an int)."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-        self.stream = torch.cuda.current_stream(device).cuda_stream
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(function, index, *args):
+    """function(*args, stream) with the device current and its current stream."""
+    # the C function behind torch.cuda.current_stream: calls here cost as little as their host time
+    if torch.cuda.current_device() == index:
+        return function(*args, torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return function(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
 def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+def _first_order_only():
+    """Backward passes run with gradients enabled only where a graph of them is asked for."""
+    if torch.is_grad_enabled():
+        raise RuntimeError("the map operators have no second derivatives")
+
+
 def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
-    import torch
+    """y, a buffer that starts with mean and rstd [2][B][groups], and the description."""
     if x.dim() < 2:
         _refuse("x must have a batch and a channel dimension")
-    _on(x.device, x, weight, bias)
-    if act not in _ACTS:
-        _refuse(f"act {act!r}")
-    C = x.shape[-1]
+    index = _device(x, weight, bias)
+    act = _ACTS.get(act)
+    if act is None:
+        _refuse(f"act must be one of {', '.join(_ACTS)}")
+    shape = x.shape
+    B, C = shape[0], shape[-1]
     for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is not None and (tuple(t.shape) != (C,) or not t.is_contiguous()):
+        if t is not None and (t.dim() != 1 or t.shape[0] != C or not t.is_contiguous()):
             _refuse(f"{name} must be a contiguous tensor of {C} elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         _refuse("weight and bias must share a dtype", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
@@ -107,53 +104,53 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
     if stride is None:
         _refuse("rows of x must be evenly spaced, their channels adjacent")
     w_like = weight if weight is not None else bias
-    norm = _map_binding.bevmap_norm(
-        x.shape[0], math.prod(x.shape[1:-1]), C, groups, stride, eps, _ACTS[act], _code(x.dtype),
-        _code(out_dtype or x.dtype), _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
+    out_dtype = out_dtype or x.dtype
+    norm = _map_binding.bevmap_norm(B, math.prod(shape[1:-1]), C, groups, stride, eps, act, _code(x.dtype),
+                                    _code(out_dtype),
+                                    _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
     size = _map_binding.bevmap_group_norm_workspace(norm, False)
-    y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-    stats = torch.empty((2, x.shape[0], groups), dtype=torch.float32, device=x.device)
-    space = torch.empty(size, dtype=torch.uint8, device=x.device)
-    mean = stats.data_ptr()
-    with _Current(x.device) as stream:
-        _map_binding.bevmap_group_norm(norm, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean,
-                                       mean + 4 * x.shape[0] * groups, space.data_ptr(), size, stream)
-    return y, stats, norm
+    y = torch.empty(shape, dtype=out_dtype, device=x.device)
+    stats = B * groups * 4
+    start = (2 * stats + 15) // 16 * 16       # of the workspace behind the statistics
+    space = torch.empty(start + size, dtype=torch.uint8, device=x.device)
+    mean = space.data_ptr()
+    _call(_map_binding.bevmap_group_norm, index, norm, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean,
+          mean + stats, mean + start, size)
+    return y, space, norm
 
 
-def _norm_backward(norm, stats, dy, x, weight, bias, want_weight, want_bias):
-    import torch
-    size = _map_binding.bevmap_group_norm_workspace(norm, True)
+def _norm_backward(norm, space, dy, x, weight, bias, want_weight, want_bias):
     dy = dy.contiguous()
+    size = _map_binding.bevmap_group_norm_workspace(norm, True)
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     dw = torch.empty_like(weight) if want_weight else None
     db = torch.empty_like(bias) if want_bias else None
-    space = torch.empty(size, dtype=torch.uint8, device=x.device)
-    mean = stats.data_ptr()
-    with _Current(x.device) as stream:
-        _map_binding.bevmap_group_norm_backward(norm, dy.data_ptr(), x.data_ptr(), _ptr(weight), _ptr(bias), mean,
-                                                mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw),
-                                                _ptr(db), space.data_ptr(), size, stream)
+    temp = torch.empty(size, dtype=torch.uint8, device=x.device)
+    mean = space.data_ptr()
+    _call(_map_binding.bevmap_group_norm_backward, x.get_device(), norm, dy.data_ptr(), x.data_ptr(), _ptr(weight),
+          _ptr(bias), mean, mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw), _ptr(db), temp.data_ptr(),
+          size)
     return dx, dw, db
 
 
 def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
-    import torch
-    _on(q.device, q, k, v, key_lengths, key_mask)
+    """out, what its rounding left over, lse (both for the backward) and the description."""
+    index = _device(q, k, v, key_lengths, key_mask)
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         _refuse("q, k and v must be 4-D", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
-    B, N, H, D = q.shape
-    M, K = k.shape[1], k.shape[2]
+    B, N, H, D = shape = q.shape
+    _, M, K, _ = k.shape
     if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
-        _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit",
+        _refuse(f"q {tuple(shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit",
                 _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
-    if q.dtype != k.dtype or q.dtype != v.dtype:
+    dtype = q.dtype
+    if k.dtype != dtype or v.dtype != dtype:
         _refuse("q, k and v must share a dtype", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     if D > 1 and (qs[3] != 1 or ks[3] != 1 or vs[3] != 1):
         _refuse("the channels of q, k and v must be adjacent")
     if key_lengths is not None:
-        if tuple(key_lengths.shape) != (B,) or not key_lengths.is_contiguous():
+        if key_lengths.dim() != 1 or key_lengths.shape[0] != B or not key_lengths.is_contiguous():
             _refuse(f"key_lengths must be a contiguous tensor of {B} elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
         if key_lengths.dtype != torch.int32:
             _refuse("key_lengths must be int32", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
@@ -161,119 +158,109 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
     if key_mask is not None:
         if tuple(key_mask.shape) != (B, M) or (M > 1 and key_mask.stride(1) != 1):
             _refuse(f"key_mask must be [{B}][{M}] with adjacent elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
-        if key_mask.dtype not in (torch.bool, torch.uint8):
+        if key_mask.dtype != torch.bool:
             _refuse("key_mask must be bool", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)
         mask_batch = key_mask.stride(0)
     if scale is None:
-        scale = 1.0 / math.sqrt(D) if D else 1.0
-    attend = _map_binding.bevmap_attend(B, N, M, H, K, D, _code(q.dtype), scale, *qs[:3], *ks[:3], *vs[:3],
-                                        mask_batch)
+        scale = D ** -0.5 if D else 1.0
+    attend = _map_binding.bevmap_attend(B, N, M, H, K, D, _code(dtype), scale, qs[0], qs[1], qs[2], ks[0], ks[1],
+                                        ks[2], vs[0], vs[1], vs[2], mask_batch)
     size = _map_binding.bevmap_attention_workspace(attend, False)
-    out = torch.empty((B, N, H, D), dtype=q.dtype, device=q.device)
-    low = torch.empty_like(out) if train and q.dtype != torch.float32 else None
+    out = torch.empty(shape, dtype=dtype, device=q.device)
+    low = torch.empty(shape, dtype=dtype, device=q.device) if train and dtype != torch.float32 else None
     lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device) if train else None
     space = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-    with _Current(q.device) as stream:
-        _map_binding.bevmap_attention(attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lengths),
-                                      _ptr(key_mask), out.data_ptr(), _ptr(low), _ptr(lse), _ptr(space), size,
-                                      stream)
+    _call(_map_binding.bevmap_attention, index, attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lengths),
+          _ptr(key_mask), out.data_ptr(), _ptr(low), _ptr(lse), _ptr(space), size)
     return out, low, lse, attend
 
 
 def _attend_backward(attend, dout, q, k, v, key_lengths, key_mask, out, low, lse):
-    import torch
-    size = _map_binding.bevmap_attention_workspace(attend, True)
     dout = dout.contiguous()
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-    space = torch.empty(size, dtype=torch.uint8, device=q.device)
-    with _Current(q.device) as stream:
-        _map_binding.bevmap_attention_backward(attend, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                               _ptr(key_lengths), _ptr(key_mask), out.data_ptr(), _ptr(low),
-                                               lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                               space.data_ptr(), size, stream)
+    size = _map_binding.bevmap_attention_workspace(attend, True)
+    dtype, device = q.dtype, q.device
+    dq = torch.empty(q.shape, dtype=dtype, device=device)
+    dk = torch.empty(k.shape, dtype=dtype, device=device)
+    dv = torch.empty(v.shape, dtype=dtype, device=device)
+    temp = torch.empty(size, dtype=torch.uint8, device=device)
+    _call(_map_binding.bevmap_attention_backward, q.get_device(), attend, dout.data_ptr(), q.data_ptr(),
+          k.data_ptr(), v.data_ptr(), _ptr(key_lengths), _ptr(key_mask), out.data_ptr(), _ptr(low), lse.data_ptr(),
+          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), temp.data_ptr(), size)
     return dq, dk, dv
 
 
 def _dropout(x, threshold, seed, offset, residual):
-    import torch
-    _on(x.device, x, residual)
+    index = _device(x, residual)
     stride = _row_stride(x)
-    residual_stride = 0 if residual is None else _row_stride(residual)
+    residual_stride = 0
+    if residual is not None:
+        residual_stride = _row_stride(residual)
+        if residual.shape != x.shape or residual.dtype != x.dtype:
+            _refuse("residual must have the shape and dtype of x", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
     if stride is None or residual_stride is None:
         _refuse("rows of x and residual must be evenly spaced, their elements adjacent")
-    if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
-        _refuse("residual must have the shape and dtype of x", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     columns = x.shape[-1] if x.dim() else 1
     rows = x.numel() // columns if columns else 0
-    with _Current(x.device) as stream:
-        _map_binding.bevmap_dropout(x.data_ptr(), stride, _ptr(residual), residual_stride, y.data_ptr(), rows,
-                                    columns, _code(x.dtype), threshold, seed, offset, stream)
+    _call(_map_binding.bevmap_dropout, index, x.data_ptr(), stride, _ptr(residual), residual_stride, y.data_ptr(),
+          rows, columns, _code(x.dtype), threshold, seed, offset)
     return y
 
 
-_FUNCTIONS = None
+class _GroupNormAct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
+        y, space, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
+        ctx.save_for_backward(x, weight, bias, space)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        _first_order_only()
+        x, weight, bias, space = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dw, db = _norm_backward(ctx.norm, space, dy, x, weight, bias, need[1], need[2])
+        return dx if need[0] else None, dw, db, None, None, None, None
 
 
-def _functions():
-    global _FUNCTIONS
-    if _FUNCTIONS is not None:
-        return _FUNCTIONS
-    import torch
-    from torch.autograd.function import once_differentiable
+class _CrossAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale, key_lengths, key_mask):
+        out, low, lse, ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
+        ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
+        return out
 
-    class _GroupNormAct(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
-            y, stats, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
-            ctx.save_for_backward(x, weight, bias, stats)
-            return y
+    @staticmethod
+    def backward(ctx, dout):
+        _first_order_only()
+        q, k, v, key_lengths, key_mask, out, low, lse = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dq, dk, dv = _attend_backward(ctx.attend, dout, q, k, v, key_lengths, key_mask, out, low, lse)
+        return dq if need[0] else None, dk if need[1] else None, dv if need[2] else None, None, None, None
 
-        @staticmethod
-        @once_differentiable
-        def backward(ctx, dy):
-            x, weight, bias, stats = ctx.saved_tensors
-            need = ctx.needs_input_grad
-            dx, dw, db = _norm_backward(ctx.norm, stats, dy, x, weight, bias, need[1], need[2])
-            return dx if need[0] else None, dw, db, None, None, None, None
 
-    class _CrossAttention(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, q, k, v, scale, key_lengths, key_mask):
-            out, low, lse, ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
-            ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
-            return out
+class _DropoutAdd(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, threshold, seed, offset):
+        ctx.draw = threshold, seed, offset
+        return _dropout(x, threshold, seed, offset, residual)
 
-        @staticmethod
-        @once_differentiable
-        def backward(ctx, dout):
-            q, k, v, key_lengths, key_mask, out, low, lse = ctx.saved_tensors
-            grads = _attend_backward(ctx.attend, dout, q, k, v, key_lengths, key_mask, out, low, lse)
-            return *(g if n else None for g, n in zip(grads, ctx.needs_input_grad)), None, None, None
-
-    class _DropoutAdd(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, x, residual, threshold, seed, offset):
-            ctx.draw = threshold, seed, offset
-            return _dropout(x, threshold, seed, offset, residual)
-
-        @staticmethod
-        @once_differentiable
-        def backward(ctx, dy):
-            dx = None
-            if ctx.needs_input_grad[0]:
-                dx = _dropout(dy if _row_stride(dy) is not None else dy.contiguous(), *ctx.draw, None)
-            return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
-
-    _FUNCTIONS = _GroupNormAct, _CrossAttention, _DropoutAdd
-    return _FUNCTIONS
+    @staticmethod
+    def backward(ctx, dy):
+        _first_order_only()
+        need = ctx.needs_input_grad
+        dx = None
+        if need[0]:
+            dx = _dropout(dy if _row_stride(dy) is not None else dy.contiguous(), *ctx.draw, None)
+        return dx, dy if need[1] else None, None, None, None
 
 
 def _learns(*tensors) -> bool:
-    import torch
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", out_dtype=None):
@@ -287,7 +274,7 @@ def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", out_
     erf). weight, bias: [C] of one dtype, or None. Statistics are fp32, y is
     rounded once. Differentiable in x, weight and bias."""
     if _learns(x, weight, bias):
-        return _functions()[0].apply(x, weight, bias, groups, eps, act, out_dtype)
+        return _GroupNormAct.apply(x, weight, bias, groups, eps, act, out_dtype)
     return _norm_forward(x, groups, weight, bias, eps, act, out_dtype)[0]
 
 
@@ -307,7 +294,7 @@ def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
     Few queries over many states (one token in serving) are split over the
     states. Differentiable in q, k and v, bitwise reproducible."""
     if _learns(q, k, v):
-        return _functions()[1].apply(q, k, v, scale, key_lengths, key_mask)
+        return _CrossAttention.apply(q, k, v, scale, key_lengths, key_mask)
     return _attend_forward(q, k, v, scale, key_lengths, key_mask, False)[0]
 
 
@@ -327,5 +314,5 @@ def dropout_add(x, p, seed, offset=0, residual=None):
         _refuse("seed and offset must be in [0, 2^64)")
     threshold = int(65536 * p + 0.5)
     if _learns(x, residual):
-        return _functions()[2].apply(x, residual, threshold, seed, offset)
+        return _DropoutAdd.apply(x, residual, threshold, seed, offset)
     return _dropout(x, threshold, seed, offset, residual)
