@@ -64,12 +64,25 @@ __device__ __forceinline__ void load_n(const T *p, float *out) {
     for (int i = 0; i < N; ++i) out[i] = float(q.v[i]);
 }
 
-template <class T, int N>
+// STREAM: past the caches, for results that are larger than they are. (A constant:
+// the compiler joins the two sides of a branch between such stores into a plain one.)
+template <class T, int N, bool STREAM = false>
 __device__ __forceinline__ void store_n(T *p, const float *in) {
+    using Chunk = uint32_t __attribute__((ext_vector_type(4)));
+    constexpr int kBytes = int(sizeof(T)) * N;
     Pack<T, N> q;
 #pragma unroll
     for (int i = 0; i < N; ++i) q.v[i] = T(in[i]);
-    *reinterpret_cast<Pack<T, N> *>(p) = q;
+    if constexpr (STREAM && kBytes % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i) {
+            Chunk c;
+            __builtin_memcpy(&c, reinterpret_cast<const char *>(&q) + 16 * i, 16);
+            __builtin_nontemporal_store(c, reinterpret_cast<Chunk *>(p) + i);
+        }
+    } else {
+        *reinterpret_cast<Pack<T, N> *>(p) = q;
+    }
 }
 
 // The same with the type chosen at run time (uniform over the launch).
@@ -83,14 +96,14 @@ __device__ __forceinline__ void load_any(const void *p, int64_t at, int dtype, f
         load_n<_Float16, N>(static_cast<const _Float16 *>(p) + at, out);
 }
 
-template <int N>
+template <int N, bool STREAM = false>
 __device__ __forceinline__ void store_any(void *p, int64_t at, int dtype, const float *in) {
     if (dtype == BEVPOOL_F32)
-        store_n<float, N>(static_cast<float *>(p) + at, in);
+        store_n<float, N, STREAM>(static_cast<float *>(p) + at, in);
     else if (dtype == BEVPOOL_BF16)
-        store_n<__bf16, N>(static_cast<__bf16 *>(p) + at, in);
+        store_n<__bf16, N, STREAM>(static_cast<__bf16 *>(p) + at, in);
     else
-        store_n<_Float16, N>(static_cast<_Float16 *>(p) + at, in);
+        store_n<_Float16, N, STREAM>(static_cast<_Float16 *>(p) + at, in);
 }
 
 inline int64_t dtype_bytes(int32_t dtype) { return dtype == BEVPOOL_F32 ? 4 : 2; }

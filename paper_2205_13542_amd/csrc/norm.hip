@@ -8,18 +8,20 @@
 // channels' statistics in registers. Statistics travel as (mean, sum of squared
 // deviations) and are joined by
 //   mean = sum n_i mean_i / n,  M2 = sum M2_i + sum n_i (mean_i - mean)^2,
-// so a large common offset costs no precision. In the apply pass every workgroup
-// joins the chunks' statistics of its frame (they are few, and in cache) and
-// then streams rows.
+// so a large common offset costs no precision. A small kernel between the passes
+// joins the chunks of each frame and group (and the weights' gradients): joined by
+// each workgroup of the apply pass instead, the parts' latency stood in front of
+// every one of them (360x360x80 fp32 to bf16: 33 us, now 29).
 #include "mapops.h"
 
 namespace bevmap {
 namespace {
 
 constexpr int kNormBlock = 256;     // apply passes
-constexpr int kSumBlock = 512;      // sum passes: few large workgroups, so that few parts are left to join
-constexpr int kSumRows = 8;         // rows that a thread has in flight, in k_norm_sum
-constexpr int kNormRows = 4;        // and elsewhere
+constexpr int kSumBlock = 256;      // sum passes
+constexpr int kJoinBlock = 256;
+constexpr int kSumRows = 4;         // rows that a thread has in flight, in k_norm_sum
+constexpr int kNormRows = 2;        // and elsewhere
 constexpr int kMergeLanes = 16;     // lanes that join one group's channels
 constexpr int kWgradChannels = 16;  // channels of a workgroup that sums weight gradients
 
@@ -28,34 +30,50 @@ struct NormArgs {
     void *y, *dx, *dweight, *dbias;
     float *mean, *rstd;             // [B][G]
     float2 *parts;                  // [B][chunks][G]
+    float2 *moments;                // backward: [B][G]
     float *channel_sums;            // backward: [B][chunks][2][C]
     int64_t ldx;
     int32_t batch, rows, C, G, per; // per: channels of a group
     int32_t chunk, n_chunks;        // rows of a chunk, chunks of a frame
     int32_t apply_rows, n_apply;    // the same for the apply pass
     int32_t y_dtype, w_dtype, act;
+    bool stream;                    // results past the caches
     float eps;
 };
 
-__device__ __forceinline__ float activate(float z, int act) {
-    switch (act) {
-        case BEVMAP_ACT_RELU: return z < 0.0f ? 0.0f : z;
-        case BEVMAP_ACT_SILU: return z / (1.0f + __expf(-z));
-        case BEVMAP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-        default: return z;
-    }
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if constexpr (ACT == BEVMAP_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == BEVMAP_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    if constexpr (ACT == BEVMAP_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    return z;
 }
 
-__device__ __forceinline__ float slope(float z, int act) {
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+    if constexpr (ACT == BEVMAP_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == BEVMAP_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+        return s * (1.0f + z * (1.0f - s));
+    }
+    if constexpr (ACT == BEVMAP_ACT_GELU)
+        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * __expf(-0.5f * z * z) * 0.39894228f;
+    return 1.0f;
+}
+
+// body(constant) with the activation as a constant: one uniform branch for a batch
+// of rows instead of one for an element.
+template <int V>
+struct Constant {
+    static constexpr int value = V;
+};
+template <class F>
+__device__ __forceinline__ void with_act(int act, F body) {
     switch (act) {
-        case BEVMAP_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-        case BEVMAP_ACT_SILU: {
-            const float s = 1.0f / (1.0f + __expf(-z));
-            return s * (1.0f + z * (1.0f - s));
-        }
-        case BEVMAP_ACT_GELU:
-            return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * __expf(-0.5f * z * z) * 0.39894228f;
-        default: return 1.0f;
+        case BEVMAP_ACT_RELU: body(Constant<BEVMAP_ACT_RELU>()); break;
+        case BEVMAP_ACT_SILU: body(Constant<BEVMAP_ACT_SILU>()); break;
+        case BEVMAP_ACT_GELU: body(Constant<BEVMAP_ACT_GELU>()); break;
+        default: body(Constant<BEVMAP_ACT_NONE>()); break;
     }
 }
 
@@ -104,38 +122,36 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_sum(NormArgs a) {
         int n = 0;
         if (c.lane < c.lanes) {
             const T *p = x + c.vec * V;
-            int r = r0 + c.lane;
-            for (; r + (kSumRows - 1) * c.lanes < r1; r += kSumRows * c.lanes) {
+            for (int r = r0 + c.lane; r < r1; r += kSumRows * c.lanes) {
                 float v[kSumRows][V];
+                int more = 0;                             // rows of this batch
 #pragma unroll
-                for (int k = 0; k < kSumRows; ++k) load_n<T, V>(p + int64_t(r + k * c.lanes) * a.ldx, v[k]);
-                // join kSumRows values of each channel to the n before them
-                const float share = float(kSumRows) / float(n + kSumRows), both = float(n) * share;
+                for (int k = 0; k < kSumRows; ++k) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[k][i] = 0.0f;
+                    if (r + k * c.lanes < r1) {
+                        load_n<T, V>(p + int64_t(r + k * c.lanes) * a.ldx, v[k]);
+                        ++more;
+                    }
+                }
+                // join them to the n rows before
+                const float inv = 1.0f / float(more), share = float(more) / float(n + more), both = float(n) * share;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float m = 0.0f, q = 0.0f;
 #pragma unroll
                     for (int k = 0; k < kSumRows; ++k) m += v[k][i];
-                    m *= 1.0f / kSumRows;
+                    m *= inv;
 #pragma unroll
-                    for (int k = 0; k < kSumRows; ++k) q = fmaf(v[k][i] - m, v[k][i] - m, q);
+                    for (int k = 0; k < kSumRows; ++k) {
+                        const float d = k < more ? v[k][i] - m : 0.0f;
+                        q = fmaf(d, d, q);
+                    }
                     const float d = m - mean[i];
                     mean[i] = fmaf(d, share, mean[i]);
                     m2[i] += fmaf(d * d, both, q);
                 }
-                n += kSumRows;
-            }
-            for (; r < r1; r += c.lanes) {
-                float v[V];
-                load_n<T, V>(p + int64_t(r) * a.ldx, v);
-                const float share = 1.0f / float(n + 1), both = float(n) * share;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = v[i] - mean[i];
-                    mean[i] = fmaf(d, share, mean[i]);
-                    m2[i] = fmaf(d * d, both, m2[i]);
-                }
-                ++n;
+                n += more;
             }
         }
         const int width = c.vectors * V;                  // channels of this block of columns
@@ -180,78 +196,51 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_sum(NormArgs a) {
     }
 }
 
-// The lanes, a power of two, that join one group's parts in an apply pass: the
-// workgroup's threads divided among the groups.
-__device__ __forceinline__ int join_lanes(int G) {
-    int n = 64;
-    while (n > 1 && n * G > kNormBlock) n >>= 1;
-    return n;
-}
-__device__ __forceinline__ float sum_over(float v, int lanes) {
-    for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor(v, m);
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
     return v;
 }
 
-// Joins the chunks' statistics of frame b: group g's mean and rstd to LDS. A
-// lane keeps its first kJoin parts in registers, where all of them are on the way at once.
-constexpr int kJoin = 8;
-__device__ __forceinline__ void join_chunks(const NormArgs &a, int b, float *mean, float *rstd, bool write) {
-    const int lanes = join_lanes(a.G), lane = threadIdx.x & (lanes - 1);
-    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
+// Joins the chunks of a frame's group, a wave to a group: mean and rstd. A lane
+// keeps its first kJoin parts in registers, all of them on the way at once.
+constexpr int kJoin = 16;
+__global__ __launch_bounds__(64) void k_norm_join(NormArgs a) {
+    const int g = blockIdx.x, b = blockIdx.y, lane = threadIdx.x;
+    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G + g;
     const float total = float(a.rows);
     auto rows_of = [&](int k) { return float(min(a.chunk, a.rows - k * a.chunk)); };
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / lanes) {
-        const int g = g0 + threadIdx.x / lanes;
-        float m = 0.0f, q = 0.0f;
-        float2 p[kJoin];
-        if (g < a.G) {
+    float2 p[kJoin];
 #pragma unroll
-            for (int i = 0; i < kJoin; ++i) {
-                const int k = lane + i * lanes;
-                p[i] = k < a.n_chunks ? parts[k * a.G + g] : make_float2(0.0f, 0.0f);
-            }
-#pragma unroll
-            for (int i = 0; i < kJoin; ++i)
-                if (lane + i * lanes < a.n_chunks) m = fmaf(p[i].x, rows_of(lane + i * lanes), m);
-            for (int k = lane + kJoin * lanes; k < a.n_chunks; k += lanes) m = fmaf(parts[k * a.G + g].x, rows_of(k), m);
-        }
-        m = sum_over(m, lanes) / total;
-        if (g < a.G) {
-#pragma unroll
-            for (int i = 0; i < kJoin; ++i)
-                if (lane + i * lanes < a.n_chunks) {
-                    const float d = p[i].x - m;
-                    q += fmaf(d * d, rows_of(lane + i * lanes) * float(a.per), p[i].y);
-                }
-            for (int k = lane + kJoin * lanes; k < a.n_chunks; k += lanes) {
-                const float2 r = parts[k * a.G + g];
-                const float d = r.x - m;
-                q += fmaf(d * d, rows_of(k) * float(a.per), r.y);
-            }
-        }
-        q = sum_over(q, lanes);
-        if (g < a.G && lane == 0) {
-            const float rs = 1.0f / sqrtf(q / (total * float(a.per)) + a.eps);
-            mean[g] = m;
-            rstd[g] = rs;
-            if (write) {
-                a.mean[int64_t(b) * a.G + g] = m;
-                a.rstd[int64_t(b) * a.G + g] = rs;
-            }
-        }
+    for (int i = 0; i < kJoin; ++i) {
+        const int k = lane + 64 * i;
+        p[i] = k < a.n_chunks ? parts[int64_t(k) * a.G] : make_float2(0.0f, 0.0f);
     }
-    __syncthreads();
+    float m = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+        if (lane + 64 * i < a.n_chunks) m = fmaf(p[i].x, rows_of(lane + 64 * i), m);
+    m = wave_sum(m) / total;
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+        if (lane + 64 * i < a.n_chunks) {
+            const float d = p[i].x - m;
+            q += fmaf(d * d, rows_of(lane + 64 * i) * float(a.per), p[i].y);
+        }
+    q = wave_sum(q);
+    if (lane == 0) {
+        a.mean[int64_t(b) * a.G + g] = m;
+        a.rstd[int64_t(b) * a.G + g] = 1.0f / sqrtf(q / (total * float(a.per)) + a.eps);
+    }
 }
 
-template <int DT, int V>
+template <int DT, int V, bool STREAM>
 __global__ __launch_bounds__(kNormBlock) void k_norm_apply(NormArgs a) {
     using T = typename Num<DT>::T;
-    extern __shared__ float lds[];
-    float *mean = lds, *rstd = lds + a.G;
     // back to front: what the sum pass read last is still in cache
-    const int b = a.batch - 1 - blockIdx.y;
+    const int b = gridDim.y - 1 - blockIdx.y;
     const int r0 = (a.n_apply - 1 - blockIdx.x) * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
-    join_chunks(a, b, mean, rstd, blockIdx.x == 0);
+    const float *mean = a.mean + int64_t(b) * a.G, *rstd = a.rstd + int64_t(b) * a.G;
     const int n_vec = a.C / V;
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
     const int64_t out0 = int64_t(b) * a.rows * a.C;
@@ -271,13 +260,16 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_apply(NormArgs a) {
 #pragma unroll
             for (int k = 0; k < kNormRows; ++k)
                 if (r + k * c.lanes < r1) load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
+            with_act(a.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < kNormRows; ++k) {
-                if (r + k * c.lanes >= r1) break;
+                for (int k = 0; k < kNormRows; ++k) {
+                    if (r + k * c.lanes >= r1) break;
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[k][i] = activate(fmaf(v[k][i] - mu[i], mul[i], add[i]), a.act);
-                store_any<V>(a.y, out0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, v[k]);
-            }
+                    for (int i = 0; i < V; ++i)
+                        v[k][i] = activate<act.value>(fmaf(v[k][i] - mu[i], mul[i], add[i]));
+                    store_any<V, STREAM>(a.y, out0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, v[k]);
+                }
+            });
         }
     }
 }
@@ -317,17 +309,19 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
                         load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
                         load_any<V>(a.dy, dy0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, d[k]);
                     }
+                with_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int k = 0; k < kNormRows; ++k) {
-                    if (r + k * c.lanes >= r1) break;
+                    for (int k = 0; k < kNormRows; ++k) {
+                        if (r + k * c.lanes >= r1) break;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float xh = (v[k][i] - mu[i]) * rs[i];
-                        const float dz = d[k][i] * slope(fmaf(xh, w[i], add[i]), a.act);
-                        sum[i] += dz;
-                        dot[i] = fmaf(dz, xh, dot[i]);
+                        for (int i = 0; i < V; ++i) {
+                            const float xh = (v[k][i] - mu[i]) * rs[i];
+                            const float dz = d[k][i] * slope<act.value>(fmaf(xh, w[i], add[i]));
+                            sum[i] += dz;
+                            dot[i] = fmaf(dz, xh, dot[i]);
+                        }
                     }
-                }
+                });
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -369,62 +363,60 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
 // Weight gradients of kWgradChannels channels: the chunks' sums of all frames.
 __device__ __forceinline__ void weight_gradients(const NormArgs &a, int block, float *lds) {
     const int ch = block * kWgradChannels + threadIdx.x % kWgradChannels;
-    const int lane = threadIdx.x / kWgradChannels, lanes = kNormBlock / kWgradChannels;
+    const int lane = threadIdx.x / kWgradChannels, lanes = kJoinBlock / kWgradChannels;
     const int64_t n = int64_t(a.batch) * a.n_chunks;
     float s = 0.0f, d = 0.0f;
     if (ch < a.C)
+#pragma unroll 8
         for (int64_t k = lane; k < n; k += lanes) {
             s += a.channel_sums[k * 2 * a.C + ch];
             d += a.channel_sums[k * 2 * a.C + a.C + ch];
         }
     lds[threadIdx.x] = s;
-    lds[kNormBlock + threadIdx.x] = d;
+    lds[kJoinBlock + threadIdx.x] = d;
     __syncthreads();
     if (lane == 0 && ch < a.C) {
         s = d = 0.0f;
         for (int l = 0; l < lanes; ++l) {
             s += lds[l * kWgradChannels + threadIdx.x];
-            d += lds[kNormBlock + l * kWgradChannels + threadIdx.x];
+            d += lds[kJoinBlock + l * kWgradChannels + threadIdx.x];
         }
         if (a.dbias) store_any<1>(a.dbias, ch, a.w_dtype, &s);
         if (a.dweight) store_any<1>(a.dweight, ch, a.w_dtype, &d);
     }
 }
 
-// dx = rstd (e - mean(e) - xh mean(e xh)). The grid's last workgroups of frame 0
-// sum the weight gradients.
-template <int DT, int V>
-__global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
-    using T = typename Num<DT>::T;
-    extern __shared__ float lds[];
-    const int b = a.batch - 1 - blockIdx.y;      // back to front, as k_norm_apply
-    if (int(blockIdx.x) >= a.n_apply) {
-        if (b == 0) weight_gradients(a, blockIdx.x - a.n_apply, lds);
+// Joins the chunks: per frame and group, a wave to a group, the means of e and e xh
+// (to moments [B][G]); and, in the grid's columns from n_join on, the weight
+// gradients.
+__global__ __launch_bounds__(kJoinBlock) void k_norm_grad_join(NormArgs a, int n_join) {
+    __shared__ float lds[2 * kJoinBlock];
+    if (int(blockIdx.x) >= n_join) {
+        if (blockIdx.y == 0) weight_gradients(a, blockIdx.x - n_join, lds);
         return;
     }
-    float *m1 = lds, *m2 = lds + a.G;
-    const int r0 = (a.n_apply - 1 - blockIdx.x) * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
-    const int lanes = join_lanes(a.G), lane = threadIdx.x & (lanes - 1);
-    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G;
-    for (int g0 = 0; g0 < a.G; g0 += kNormBlock / lanes) {
-        const int g = g0 + threadIdx.x / lanes;
-        float s = 0.0f, d = 0.0f;
-        if (g < a.G)
-#pragma unroll 8
-            for (int k = lane; k < a.n_chunks; k += lanes) {
-                const float2 p = parts[k * a.G + g];
-                s += p.x;
-                d += p.y;
-            }
-        s = sum_over(s, lanes);
-        d = sum_over(d, lanes);
-        if (g < a.G && lane == 0) {
-            const float inv = 1.0f / (float(a.rows) * float(a.per));
-            m1[g] = s * inv;
-            m2[g] = d * inv;
-        }
+    const int g = blockIdx.x * (kJoinBlock / 64) + threadIdx.x / 64, b = blockIdx.y, lane = threadIdx.x & 63;
+    if (g >= a.G) return;
+    const float2 *parts = a.parts + int64_t(b) * a.n_chunks * a.G + g;
+    float s = 0.0f, d = 0.0f;
+#pragma unroll 16
+    for (int k = lane; k < a.n_chunks; k += 64) {
+        const float2 p = parts[int64_t(k) * a.G];
+        s += p.x;
+        d += p.y;
     }
-    __syncthreads();
+    s = wave_sum(s);
+    d = wave_sum(d);
+    const float inv = 1.0f / (float(a.rows) * float(a.per));
+    if (lane == 0) a.moments[int64_t(b) * a.G + g] = make_float2(s * inv, d * inv);
+}
+
+// dx = rstd (e - mean(e) - xh mean(e xh)).
+template <int DT, int V, bool STREAM>
+__global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
+    using T = typename Num<DT>::T;
+    const int b = gridDim.y - 1 - blockIdx.y;      // back to front, as k_norm_apply
+    const int r0 = (a.n_apply - 1 - blockIdx.x) * a.apply_rows, r1 = min(r0 + a.apply_rows, a.rows);
     const int n_vec = a.C / V;
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
     T *dx = static_cast<T *>(a.dx) + int64_t(b) * a.rows * a.C;
@@ -440,8 +432,9 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
             rs[i] = a.rstd[int64_t(b) * a.G + g];
             w[i] = weight_at(a.weight, ch, a.w_dtype, 1.0f);
             add[i] = weight_at(a.bias, ch, a.w_dtype, 0.0f);
-            e1[i] = m1[g];
-            e2[i] = m2[g];
+            const float2 m = a.moments[int64_t(b) * a.G + g];
+            e1[i] = m.x;
+            e2[i] = m.y;
         }
         for (int r = r0 + c.lane; r < r1; r += kNormRows * c.lanes) {
             float v[kNormRows][V], d[kNormRows][V];
@@ -451,38 +444,40 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
                     load_n<T, V>(x + int64_t(r + k * c.lanes) * a.ldx + c.vec * V, v[k]);
                     load_any<V>(a.dy, dy0 + int64_t(r + k * c.lanes) * a.C + c.vec * V, a.y_dtype, d[k]);
                 }
+            with_act(a.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < kNormRows; ++k) {
-                if (r + k * c.lanes >= r1) break;
+                for (int k = 0; k < kNormRows; ++k) {
+                    if (r + k * c.lanes >= r1) break;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xh = (v[k][i] - mu[i]) * rs[i];
-                    const float e = d[k][i] * slope(fmaf(xh, w[i], add[i]), a.act) * w[i];
-                    v[k][i] = rs[i] * (e - e1[i] - xh * e2[i]);
+                    for (int i = 0; i < V; ++i) {
+                        const float xh = (v[k][i] - mu[i]) * rs[i];
+                        const float e = d[k][i] * slope<act.value>(fmaf(xh, w[i], add[i])) * w[i];
+                        v[k][i] = rs[i] * (e - e1[i] - xh * e2[i]);
+                    }
+                    store_n<T, V, STREAM>(dx + int64_t(r + k * c.lanes) * a.C + c.vec * V, v[k]);
                 }
-                store_n<T, V>(dx + int64_t(r + k * c.lanes) * a.C + c.vec * V, v[k]);
-            }
+            });
         }
     }
 }
 
 constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
-constexpr int kMaxChunks = 256;     // chunks of a frame at most
 constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
 constexpr int kMinRows = 16;        // rows of a chunk at least
-constexpr int kMaxParts = 8192;     // parts of a frame (chunks x groups) at most, each apply workgroup joins them
+// Maps that together exceed the 256 MB of cache behind the L2s: results are then
+// written past it, and more of x is still there for the second read.
+constexpr int64_t kCacheBytes = int64_t(256) << 20;
+static_assert(kSumGrid <= 64 * kJoin, "k_norm_join holds a group's parts in registers");
 
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
+int64_t elements(const bevmap_norm &n) { return int64_t(n.batch) * n.pixels * n.channels; }
+
 void split(const bevmap_norm &n, NormArgs *a) {
-    int chunks = kSumGrid / (n.batch < kSumGrid ? n.batch : kSumGrid);
-    if (chunks > kMaxChunks) chunks = kMaxChunks;
-    if (chunks > kMaxParts / n.groups) chunks = kMaxParts / n.groups;
-    a->chunk = ceil_div(n.pixels, chunks);
+    a->chunk = ceil_div(n.pixels, ceil_div(kSumGrid, n.batch));
     if (a->chunk < kMinRows) a->chunk = kMinRows;
     a->n_chunks = ceil_div(n.pixels, a->chunk);
-    const int apply = kApplyGrid / (n.batch < kApplyGrid ? n.batch : kApplyGrid);
-    a->apply_rows = ceil_div(n.pixels, apply);
+    a->apply_rows = ceil_div(n.pixels, ceil_div(kApplyGrid, n.batch));
     if (a->apply_rows < kMinRows) a->apply_rows = kMinRows;
     a->n_apply = ceil_div(n.pixels, a->apply_rows);
 }
@@ -504,7 +499,8 @@ NormArgs fill(const bevmap_norm &n, const void *x, const void *weight, const voi
     a.eps = n.eps;
     split(n, &a);
     a.parts = static_cast<float2 *>(workspace);
-    a.channel_sums = reinterpret_cast<float *>(a.parts + int64_t(n.batch) * a.n_chunks * n.groups);
+    a.moments = a.parts + int64_t(n.batch) * a.n_chunks * n.groups;
+    a.channel_sums = reinterpret_cast<float *>(a.moments + int64_t(n.batch) * n.groups);
     return a;
 }
 
@@ -536,9 +532,12 @@ int forward(const NormArgs &a, hipStream_t stream) {
     if (int rc = allow_lds(k_norm_sum<DT, V>, lds)) return rc;
     hipLaunchKernelGGL((k_norm_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kSumBlock), lds, stream, a);
     BEVPOOL_HIP(hipGetLastError());
-    const size_t lds2 = 2 * size_t(a.G) * sizeof(float);
-    if (int rc = allow_lds(k_norm_apply<DT, V>, lds2)) return rc;
-    hipLaunchKernelGGL((k_norm_apply<DT, V>), dim3(a.n_apply, a.batch), dim3(kNormBlock), lds2, stream, a);
+    hipLaunchKernelGGL(k_norm_join, dim3(a.G, a.batch), dim3(64), 0, stream, a);
+    BEVPOOL_HIP(hipGetLastError());
+    if (V >= 4 && a.stream)
+        hipLaunchKernelGGL((k_norm_apply<DT, V, (V >= 4)>), dim3(a.n_apply, a.batch), dim3(kNormBlock), 0, stream, a);
+    else
+        hipLaunchKernelGGL((k_norm_apply<DT, V, false>), dim3(a.n_apply, a.batch), dim3(kNormBlock), 0, stream, a);
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -549,11 +548,13 @@ int backward(const NormArgs &a, hipStream_t stream) {
     if (int rc = allow_lds(k_norm_grad_sum<DT, V>, lds)) return rc;
     hipLaunchKernelGGL((k_norm_grad_sum<DT, V>), dim3(a.n_chunks, a.batch), dim3(kSumBlock), lds, stream, a);
     BEVPOOL_HIP(hipGetLastError());
-    const size_t lds2 = size_t(a.G > kNormBlock ? a.G : kNormBlock) * 2 * sizeof(float);
-    if (int rc = allow_lds(k_norm_grad_apply<DT, V>, lds2)) return rc;
-    const int extra = a.dweight || a.dbias ? ceil_div(a.C, kWgradChannels) : 0;
-    hipLaunchKernelGGL((k_norm_grad_apply<DT, V>), dim3(a.n_apply + extra, a.batch), dim3(kNormBlock), lds2, stream,
-                       a);
+    const int n_join = ceil_div(a.G, kJoinBlock / 64), extra = a.dweight || a.dbias ? ceil_div(a.C, kWgradChannels) : 0;
+    hipLaunchKernelGGL(k_norm_grad_join, dim3(n_join + extra, a.batch), dim3(kJoinBlock), 0, stream, a, n_join);
+    BEVPOOL_HIP(hipGetLastError());
+    if (V >= 4 && a.stream)
+        hipLaunchKernelGGL((k_norm_grad_apply<DT, V, (V >= 4)>), dim3(a.n_apply, a.batch), dim3(kNormBlock), 0, stream, a);
+    else
+        hipLaunchKernelGGL((k_norm_grad_apply<DT, V, false>), dim3(a.n_apply, a.batch), dim3(kNormBlock), 0, stream, a);
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -594,8 +595,10 @@ int64_t bevmap_norm_workspace_bytes(const bevmap_norm &n, bool backward) {
     NormArgs a{};
     split(n, &a);
     const int64_t chunks = int64_t(n.batch) * a.n_chunks;
-    return chunks * n.groups * int64_t(sizeof(float2)) +
-           (backward ? chunks * 2 * n.channels * int64_t(sizeof(float)) : 0);
+    const int64_t parts = chunks * n.groups * int64_t(sizeof(float2));
+    if (!backward) return parts;
+    return parts + int64_t(n.batch) * n.groups * int64_t(sizeof(float2)) +
+           chunks * 2 * n.channels * int64_t(sizeof(float));
 }
 
 int bevmap_launch_norm(const bevmap_norm &n, const void *x, const void *weight, const void *bias, void *y,
@@ -603,6 +606,7 @@ int bevmap_launch_norm(const bevmap_norm &n, const void *x, const void *weight, 
     if (n.batch == 0 || n.pixels == 0) return BEVPOOL_OK;
     NormArgs a = fill(n, x, weight, bias, workspace);
     a.y = y;
+    a.stream = elements(n) * (dtype_bytes(n.x_dtype) + dtype_bytes(n.y_dtype)) > kCacheBytes;
     a.mean = mean;
     a.rstd = rstd;
     return dispatch(n.x_dtype, a, vector_of(n, x, y, nullptr), false, stream);
@@ -621,6 +625,7 @@ int bevmap_launch_norm_backward(const bevmap_norm &n, const void *grad_y, const 
     }
     NormArgs a = fill(n, x, weight, bias, workspace);
     a.dy = grad_y;
+    a.stream = elements(n) * (2 * dtype_bytes(n.x_dtype) + dtype_bytes(n.y_dtype)) > kCacheBytes;
     a.dx = grad_x;
     a.dweight = grad_weight;
     a.dbias = grad_bias;
