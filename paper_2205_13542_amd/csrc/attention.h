@@ -30,6 +30,7 @@ struct AttendArgs {
     float *lse, *delta;
     float *part;                  // fp32 parts of a split axis
     float2 *part_stats;           // forward: (maximum, sum) of a part's rows
+    int32_t part_pitch;           // floats from row to row of a part
     int32_t group, rows;          // heads that share a key head, queries * group
     bevpool::FastDiv by_group;
     int32_t n_tiles, n_split;     // tiles of the axis that a workgroup owns, parts of the other
@@ -51,10 +52,28 @@ struct Mma {
     using T = typename Num<DT>::T;
     static constexpr int kElems = 8;
     using Vec = T __attribute__((ext_vector_type(8)));
-    // a block's 16 values of a lane as the second product's operand
+    // a block's 16 values of a lane as the second product's operand, rounded to T
     struct Rows {
         u32x4 half[2];
+        // their sum, as rounded
+        __device__ __forceinline__ float sum() const {
+            float a = 0.0f, b = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a = pair_sum(half[0][i], a);
+                b = pair_sum(half[1][i], b);
+            }
+            return a + b;
+        }
     };
+    static __device__ __forceinline__ float pair_sum(uint32_t v, float c) {
+        using Two = T __attribute__((ext_vector_type(2)));
+        const Two ones = {T(1.0f), T(1.0f)};
+        if constexpr (DT == BEVPOOL_BF16)
+            return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Two, v), ones, c, false);
+        else
+            return __builtin_amdgcn_fdot2(__builtin_bit_cast(Two, v), ones, c, false);
+    }
     static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
         if constexpr (DT == BEVPOOL_BF16)
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec, a), __builtin_bit_cast(Vec, b), c,
@@ -81,6 +100,12 @@ struct Mma<BEVPOOL_F32> {
     static constexpr int kElems = 4;
     struct Rows {
         f32x16 p;
+        __device__ __forceinline__ float sum() const {
+            float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 16; ++i) a[i & 3] += p[i];
+            return (a[0] + a[1]) + (a[2] + a[3]);
+        }
     };
     static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
 #pragma unroll
@@ -190,6 +215,19 @@ __device__ __forceinline__ u32x4 load_chunk(const typename Num<DT>::T *row, int 
     return out;
 }
 
+// Four consecutive channels of a row from channel ch, of dim; VEC: they are
+// aligned and dim is a multiple of four.
+template <bool VEC, class T>
+__device__ __forceinline__ void write4(T *row, int ch, int dim, const float *v) {
+    if constexpr (VEC) {
+        if (ch < dim) store_n<T, 4>(row + ch, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < dim) row[ch + e] = T(v[e]);
+    }
+}
+
 // The largest of a lane and the lane 32 away, and their sum.
 __device__ __forceinline__ float both_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -245,11 +283,110 @@ struct Problem {
     }
 };
 
-// Work of workgroup id of n in an order in which neighbours run on one XCD.
-__device__ __forceinline__ int near_order(int id, int n) {
-    const int q = n >> 3, r = n & 7, x = id & 7, k = id >> 3;
-    return x < r ? x * (q + 1) + k : r * (q + 1) + (x - r) * q + k;
+// Work of a workgroup: item n of `per` of problem bh (sample, key head). Workgroups are
+// dealt to the 8 XCDs round-robin, and a problem's workgroups share its keys and
+// values, so problem bh's all go to XCD bh % 8, which also spreads samples of
+// unequal length; what is left of the last 8 problems is cut into eighths.
+__device__ __forceinline__ void work_of(int n_bh, int per, int &bh, int &n) {
+    int id = blockIdx.x;
+    const int whole = (n_bh & ~7) * per;
+    if (id < whole) {
+        const int k = id >> 3, round = k / per;
+        bh = 8 * round + (id & 7);
+        n = k - round * per;
+        return;
+    }
+    id -= whole;
+    const int left = (n_bh & 7) * per, q = left >> 3, r = left & 7, x = id & 7, k = id >> 3;
+    id = x < r ? x * (q + 1) + k : r * (q + 1) + (x - r) * q + k;
+    const int p = id / per;
+    bh = (n_bh & ~7) + p;
+    n = id - p * per;
 }
+
+// Rows of a tile on their way from memory to LDS, a few chunks to a thread; rows are
+// `stride` bytes apart. Chunks past the last channel are copies of the last one:
+// they meet zeros in the other operand, or their results are not written.
+template <int DT, int DB, bool VEC, int ROWS>
+struct Stage {
+    using S = Shape<DT, DB>;
+    using T = typename S::T;
+    static constexpr int kLoads = (ROWS * S::kUsed + kAttendBlock - 1) / kAttendBlock;
+    static constexpr bool kEven = ROWS * S::kUsed % kAttendBlock == 0;      // no thread is left over
+    u32x4 reg[kLoads];
+
+    static __device__ __forceinline__ int row(int i) { return (threadIdx.x + i * kAttendBlock) / S::kUsed; }
+    static __device__ __forceinline__ int chunk(int i) { return (threadIdx.x + i * kAttendBlock) % S::kUsed; }
+
+    // base: the tile's first row (uniform). rows: how many of its rows there are.
+    __device__ __forceinline__ void load(const char *base, uint32_t stride, int rows, int dim) {
+        const int last = (dim - 1) / S::M::kElems;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = row(i), c = min(chunk(i), last);
+            const bool there = kEven || r < ROWS;
+            if constexpr (VEC) {
+                const uint32_t at = uint32_t(r) * stride + uint32_t(c) * 16;
+                if (rows >= ROWS) {
+                    if (there) reg[i] = *reinterpret_cast<const u32x4 *>(base + at);
+                } else {
+                    reg[i] = u32x4{0, 0, 0, 0};
+                    if (there && r < rows) reg[i] = *reinterpret_cast<const u32x4 *>(base + at);
+                }
+            } else {
+                reg[i] = u32x4{0, 0, 0, 0};
+                if (there && r < rows)
+                    reg[i] = load_chunk<DT, false>(reinterpret_cast<const T *>(base + uint32_t(r) * stride), chunk(i), dim);
+            }
+        }
+    }
+    // Words of rows in use; the others go to LDS as zeros.
+    template <int WORDS>
+    __device__ __forceinline__ void store(char *tile, const uint64_t (&words)[WORDS], bool all) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = row(i);
+            if (!kEven && r >= ROWS) break;
+            char *to = tile + chunk_at<S::kChunks>(r, chunk(i));
+            if (all) {
+                *reinterpret_cast<u32x4 *>(to) = reg[i];
+            } else {
+                uint64_t word = words[0];
+                if constexpr (WORDS == 2) word = r >= 64 ? words[1] : word;
+                *reinterpret_cast<u32x4 *>(to) = (word >> (r & 63)) & 1 ? reg[i] : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+};
+
+// Words of the keys in use of a tile of KEYS keys from j0; every lane of a wave has
+// asked for its own (used), where there is a mask.
+template <int KEYS>
+struct InUse {
+    static constexpr int kWords = KEYS <= 64 ? 1 : KEYS / 64;
+    int used[kWords];
+    uint64_t words[kWords];
+    bool all;
+    template <class P>
+    __device__ __forceinline__ void ask(const P &at, int j0) {
+        const int lane = threadIdx.x & 63;
+        if (at.g.mask)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) used[w] = KEYS >= 64 || lane < KEYS ? at.ask(j0 + 64 * w + lane) : 0;
+    }
+    template <class P>
+    __device__ __forceinline__ void count(const P &at, int j0) {
+        constexpr uint64_t kFull = KEYS >= 64 ? ~0ull : (1ull << (KEYS & 63)) - 1;
+        all = true;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            const int there = at.len - j0 - 64 * w;
+            words[w] = at.g.mask ? __ballot(used[w] != 0)
+                                 : there >= 64 ? kFull : there <= 0 ? 0ull : kFull & ((1ull << there) - 1);
+            all = all && words[w] == kFull;
+        }
+    }
+};
 
 inline int attend_ceil(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 

@@ -11,10 +11,12 @@
 namespace bevmap {
 namespace {
 
-// Where a row's maximum grows by no more than this (log2), its old one is kept:
-// the exponentials stay below 2^8, far from any type's largest value, and the sums
-// so far need no rescaling.
-constexpr float kKeepMax = 8.0f;
+// Exponentials are taken relative to a maximum that is not kept up to date: a
+// tile whose sum for some row passes this (log2: 12) forms the rows' maxima, rescales
+// what is summed and takes its exponentials again. The first tile always does. In
+// between, a tile costs no maximum, and what is lost is nothing: the exponentials
+// keep their relative precision, in fp16 too, whose largest value is 2^16.
+constexpr float kMaxTileSum = 4096.0f;
 
 // WR waves side by side have rows of their own (4), or all share the tile's rows
 // and split each tile's keys (1).
@@ -36,21 +38,20 @@ __device__ __forceinline__ float part_weight(float top, float sum, float most) {
 }
 
 template <int DT, int DB, bool VEC, int WR>
-__global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
     using W = Tile<DT, WR>;
     constexpr int kTileBytes = W::kKeys * S::kRowBytes;
-    constexpr int kLoads = (W::kKeys * S::kUsed + kAttendBlock - 1) / kAttendBlock;   // chunks of a thread
     constexpr int kBuffers = W::buffers(S::kRowBytes);
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [kBuffers][k, v][tile]
 
     const int n_bh = g.a.batch * g.a.key_heads;
-    int id = near_order(blockIdx.x, n_bh * g.n_split * g.n_tiles);
-    const int tile = id % g.n_tiles;
-    id /= g.n_tiles;
-    const int split = id % g.n_split, bh = id / g.n_split;
+    int bh, tile;
+    work_of(n_bh, g.n_split * g.n_tiles, bh, tile);
+    const int split = tile / g.n_tiles;
+    tile -= split * g.n_tiles;
     const Problem<DT> at(g, bh);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int row = tile * W::kRows + (WR == 1 ? 0 : 32 * wave) + (lane & 31);
@@ -75,44 +76,20 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
     const int per = (tiles + g.n_split - 1) / g.n_split;
     const int t0 = split * per, t1 = min(t0 + per, tiles);
 
-    u32x4 next_k[kLoads], next_v[kLoads];
-    int used[W::kKeys < 64 ? 1 : W::kKeys / 64];       // whether key lane + 64 w of the tile is in use
-    constexpr int kWords = W::kKeys < 64 ? 1 : W::kKeys / 64;
+    const uint32_t k_step = uint32_t(g.a.k_row * int(sizeof(T))), v_step = uint32_t(g.a.v_row * int(sizeof(T)));
+    Stage<DT, DB, VEC, W::kKeys> next_k, next_v;
+    InUse<W::kKeys> use;
     auto fetch = [&](int t) {
         const int j0 = t * W::kKeys;
-#pragma unroll
-        for (int w = 0; w < kWords; ++w)
-            used[w] = W::kKeys >= 64 || lane < W::kKeys ? at.ask(j0 + 64 * w + lane) : 0;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
-            next_k[i] = next_v[i] = u32x4{0, 0, 0, 0};
-            if (r < W::kKeys && j0 + r < at.len) {
-                next_k[i] = load_chunk<DT, VEC>(at.k(j0 + r), c, dim);
-                next_v[i] = load_chunk<DT, VEC>(at.v(j0 + r), c, dim);
-            }
-        }
+        use.ask(at, j0);
+        next_k.load(reinterpret_cast<const char *>(at.k(j0)), k_step, at.len - j0, dim);
+        next_v.load(reinterpret_cast<const char *>(at.v(j0)), v_step, at.len - j0, dim);
     };
-    // to LDS, keys out of use as zeros; returns the words of keys in use
-    struct Words {
-        uint64_t w[kWords];
-    };
-    auto put = [&](int buffer) {
-        Words m;
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) m.w[w] = __ballot(used[w] != 0);
-        char *k = lds + buffer * 2 * kTileBytes, *v = k + kTileBytes;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
-            if (r >= W::kKeys) break;
-            uint64_t word = m.w[0];
-            if constexpr (kWords == 2) word = r >= 64 ? m.w[1] : word;
-            const bool in = (word >> (r & 63)) & 1;
-            *reinterpret_cast<u32x4 *>(k + chunk_at<S::kChunks>(r, c)) = in ? next_k[i] : u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(v + chunk_at<S::kChunks>(r, c)) = in ? next_v[i] : u32x4{0, 0, 0, 0};
-        }
-        return m;
+    auto put = [&](int t) {
+        use.count(at, t * W::kKeys);
+        char *k = lds + ((t - t0) & (kBuffers - 1)) * 2 * kTileBytes;
+        next_k.store(k, use.words, use.all);
+        next_v.store(k + kTileBytes, use.words, use.all);
     };
 
     f32x16 o[DB];
@@ -122,28 +99,27 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;     // of log2 scores; sum over this lane's keys
     const float c = g.log2_scale;
+    const int row0 = WR == 1 ? 32 * wave : 0;       // of this wave's keys in a tile
 
-    Words words = {};
     if (t0 < t1) {
         fetch(t0);
-        words = put(0);
-        if (t0 + 1 < t1) fetch(t0 + 1);
+        put(t0);
     }
-    __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const char *k = lds + ((t - t0) & (kBuffers - 1)) * 2 * kTileBytes, *v = k + kTileBytes;
-        // the words of this wave's keys
-        const int row0 = WR == 1 ? 32 * wave : 0;
-        uint64_t mine = words.w[0];
-        if constexpr (kWords == 2) mine = row0 >= 64 ? words.w[1] : mine;
+        uint64_t mine = use.words[0];
+        if constexpr (use.kWords == 2) mine = row0 >= 64 ? use.words[1] : mine;
         if constexpr (WR == 1) mine = (mine >> (row0 & 63)) & 0xFFFFFFFFull;
+        if (t + 1 < t1) fetch(t + 1);
+        __syncthreads();
         if (mine != 0) {
             f32x16 s[W::kBlocks];
 #pragma unroll
             for (int n = 0; n < W::kBlocks; ++n) {
+                f32x16 zero;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
-                s[n] = S::scores(k, row0 + 32 * n, q, s[n]);
+                for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
+                s[n] = S::scores(k, row0 + 32 * n, q, zero);
             }
             constexpr uint64_t kAll = W::kBlocks == 2 ? ~0ull : 0xFFFFFFFFull;
             if (mine != kAll) {
@@ -155,14 +131,27 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
                         s[n][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[n][i] : -INFINITY;
                 }
             }
-            float high = s[0][0];
+            typename M::Rows p[W::kBlocks];
+            auto exponentials = [&](float base) {
+                float part = 0.0f;
 #pragma unroll
-            for (int n = 0; n < W::kBlocks; ++n)
+                for (int n = 0; n < W::kBlocks; ++n) {
+                    f32x16 e;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) high = fmaxf(high, s[n][i]);
-            high = both_max(high) * c;
-            if (__any(high > top + kKeepMax || (top == -INFINITY && high > top))) {
-                const float now = fmaxf(top, high);
+                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
+                    p[n] = M::rows(e);
+                    part += p[n].sum();
+                }
+                return part;
+            };
+            float part = exponentials(top);
+            if (__any(!(part <= kMaxTileSum))) {
+                float high = s[0][0];
+#pragma unroll
+                for (int n = 0; n < W::kBlocks; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) high = fmaxf(high, s[n][i]);
+                const float now = fmaxf(top, both_max(high) * c);
                 const float old = top == -INFINITY ? 0.0f : exp2f(top - now);
                 sum *= old;
 #pragma unroll
@@ -170,25 +159,16 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[d][i] *= old;
                 top = now;
+                part = exponentials(top == -INFINITY ? 0.0f : top);
             }
-            const float base = top == -INFINITY ? 0.0f : top;
+            sum += part;
 #pragma unroll
-            for (int n = 0; n < W::kBlocks; ++n) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
-                    sum += s[n][i];
-                }
-                S::sums(v, row0 + 32 * n, M::rows(s[n]), o);
-            }
+            for (int n = 0; n < W::kBlocks; ++n) S::sums(v, row0 + 32 * n, p[n], o);
         }
         if constexpr (kBuffers == 1) __syncthreads();
-        if (t + 1 < t1) {
-            words = put((t + 1 - t0) & (kBuffers - 1));
-            if (t + 2 < t1) fetch(t + 2);
-        }
-        __syncthreads();
+        if (t + 1 < t1) put(t + 1);
     }
+    __syncthreads();
     sum = both_sum(sum);
 
     if constexpr (WR == 1) {
@@ -230,39 +210,39 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend(AttendArgs g) {
 
     if (row >= g.rows) return;
     const int first = WR == 1 ? wave : 0, blocks = WR == 1 ? 1 : DB;
-    if (g.n_split > 1) {
-        const int64_t slot = (int64_t(split) * n_bh + bh) * g.rows + row;
-        if (half == 0 && first == 0) g.part_stats[slot] = make_float2(top, sum);
-        if (sum == 0.0f) return;              // the joining kernel does not read it
-        float *p = g.part + slot * dim;
+    // fn(channel, four values) of this lane
+    auto each4 = [&](float mul, auto fn) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
             if (d >= blocks) break;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = 32 * (first + d) + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (ch < dim) p[ch] = o[d][i];
+            for (int i = 0; i < 16; i += 4) {
+                const float x[4] = {o[d][i] * mul, o[d][i + 1] * mul, o[d][i + 2] * mul, o[d][i + 3] * mul};
+                fn(32 * (first + d) + 2 * i + 4 * half, x);
             }
         }
+    };
+    if (g.n_split > 1) {
+        const int64_t slot = (int64_t(split) * n_bh + bh) * g.rows + row;
+        if (half == 0 && first == 0) g.part_stats[slot] = make_float2(top, sum);
+        if (sum == 0.0f) return;              // the joining kernel does not read it
+        float *p = g.part + slot * g.part_pitch;
+        each4(1.0f, [&](int ch, const float *x) { write4<true>(p, ch, g.part_pitch, x); });
         return;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t to = at.row(row);
     T *out = static_cast<T *>(g.o) + to;
+    each4(sum == 0.0f ? 0.0f : 1.0f / sum, [&](int ch, const float *x) {
+        write4<VEC>(out, ch, dim, x);
+        if (DT != BEVPOOL_F32 && g.o_low) {
+            float low[4];
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-        if (d >= blocks) break;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int ch = 32 * (first + d) + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (ch >= dim) continue;
-            const float full = o[d][i] * inv;
-            const T rounded = T(full);
-            out[ch] = rounded;
-            if (DT != BEVPOOL_F32 && g.o_low) static_cast<T *>(g.o_low)[to + ch] = T(full - float(rounded));
+            for (int e = 0; e < 4; ++e) low[e] = x[e] - float(T(x[e]));
+            write4<VEC>(static_cast<T *>(g.o_low) + to, ch, dim, low);
         }
-    }
-    if (g.lse && half == 0 && first == 0) g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    });
+    if (g.lse && half == 0 && first == 0)
+        g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
 // Joins the parts of a row: a workgroup to a row, its NW waves share the parts,
@@ -289,7 +269,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_join(AttendArgs g) {
         const float2 st = stats[s * total];
         const float mul = part_weight(st.x, st.y, top);
         sum = fmaf(st.y, mul, sum);
-        const float *p = g.part + (s * total + slot) * dim;
+        const float *p = g.part + (s * total + slot) * g.part_pitch;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const float v = lane + 64 * k < dim ? p[lane + 64 * k] : 0.0f;
@@ -324,6 +304,8 @@ __global__ __launch_bounds__(64 * NW) void k_attend_join(AttendArgs g) {
 
 constexpr int kFill = 768;          // workgroups that fill the chip, three to a compute unit
 constexpr int kFewRows = 32;        // rows of a key head that one wave holds
+
+int part_pitch(const bevmap_attend &a) { return (a.dim + 3) / 4 * 4; }
 
 // Rows, row tiles and parts of the keys, a rule on the sizes alone. Workgroups
 // that do not fill the chip split the keys, down to two tiles of keys a part.
@@ -397,7 +379,7 @@ int64_t bevmap_attention_workspace_bytes(const bevmap_attend &a, bool backward) 
     partition(a, &g, &few);
     if (g.n_split <= 1) return 0;
     return int64_t(g.n_split) * a.batch * a.queries * a.heads *
-           (a.dim * int64_t(sizeof(float)) + int64_t(sizeof(float2)));
+           (part_pitch(a) * int64_t(sizeof(float)) + int64_t(sizeof(float2)));
 }
 
 int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k, const void *v,
@@ -410,12 +392,15 @@ int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k
     g.lse = lse;
     bool few;
     partition(a, &g, &few);
-    g.part_stats = static_cast<float2 *>(workspace);
-    g.part = reinterpret_cast<float *>(g.part_stats + int64_t(g.n_split) * a.batch * a.queries * a.heads);
+    // 16-byte aligned parts first, then their rows' statistics
+    g.part_pitch = part_pitch(a);
+    g.part = static_cast<float *>(workspace);
+    g.part_stats = reinterpret_cast<float2 *>(g.part + int64_t(g.n_split) * a.batch * a.queries * a.heads * g.part_pitch);
     if (int64_t(a.batch) * a.key_heads * g.n_split * g.n_tiles >= (int64_t(1) << 31) / kAttendBlock)
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d heads=%d: too many tiles of rows", a.batch,
                             a.queries, a.heads);
-    const bool vec = attend_vec(a, q, k, v);
+    const bool vec = attend_vec(a, q, k, v) && aligned_for(out, 0, a.dtype, 4) &&
+                     (!out_low || aligned_for(out_low, 0, a.dtype, 4));
     switch (a.dtype) {
         case BEVPOOL_F32: return forward<BEVPOOL_F32>(g, vec, few, stream);
         case BEVPOOL_BF16: return forward<BEVPOOL_BF16>(g, vec, few, stream);

@@ -64,17 +64,17 @@ __device__ __forceinline__ void write_row(const f32x16 *acc, bool on, float mul,
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock) void k_attend_dq(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dq(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
     using W = Walk<DT, DB>;
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][k, v][tile]
     const int n_bh = g.a.batch * g.a.key_heads;
-    int id = near_order(blockIdx.x, n_bh * g.n_split * g.n_tiles);
-    const int tile = id % g.n_tiles;
-    id /= g.n_tiles;
-    const int split = id % g.n_split, bh = id / g.n_split;
+    int bh, tile;
+    work_of(n_bh, g.n_split * g.n_tiles, bh, tile);
+    const int split = tile / g.n_tiles;
+    tile -= split * g.n_tiles;
     const Problem<DT> at(g, bh);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, dim = g.a.dim;
     const int row = tile * kOwn + 32 * wave + (lane & 31);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_dq(AttendArgs g) {
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock) void k_attend_dkv(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dkv(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -178,10 +178,10 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_dkv(AttendArgs g) {
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][q, dout][tile], then [2][lse, delta][kWalk]
     float *stats = reinterpret_cast<float *>(lds + 4 * W::kTileBytes);
     const int n_bh = g.a.batch * g.a.key_heads;
-    int id = near_order(blockIdx.x, n_bh * g.n_split * g.n_tiles);
-    const int tile = id % g.n_tiles;
-    id /= g.n_tiles;
-    const int split = id % g.n_split, bh = id / g.n_split;
+    int bh, tile;
+    work_of(n_bh, g.n_split * g.n_tiles, bh, tile);
+    const int split = tile / g.n_tiles;
+    tile -= split * g.n_tiles;
     const Problem<DT> at(g, bh);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, dim = g.a.dim;
     const int key = tile * kOwn + 32 * wave + (lane & 31);
