@@ -31,6 +31,7 @@ struct AttendArgs {
     float *part;                  // fp32 parts of a split axis
     float2 *part_stats;           // forward: (maximum, sum) of a part's rows
     int32_t part_pitch;           // floats from row to row of a part
+    bool out_aligned;             // four elements of out and out_low can be written at a time
     int32_t group, rows;          // heads that share a key head, queries * group
     bevpool::FastDiv by_group;
     int32_t n_tiles, n_split;     // tiles of the axis that a workgroup owns, parts of the other

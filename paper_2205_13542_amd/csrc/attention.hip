@@ -245,64 +245,97 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
         g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
-// Joins the parts of a row: a workgroup to a row, its NW waves share the parts,
-// lanes are channels.
-template <int DT, int NW>
-__global__ __launch_bounds__(64 * NW) void k_attend_join(AttendArgs g) {
+// Joins the parts of rows. A thread holds four channels of a row and every SL-th
+// part, kJoinAhead of them on the way at once; the SL threads of a row's four
+// channels meet in LDS.
+constexpr int kJoinAhead = 8;
+template <int SL>
+struct Join {
+    static constexpr int kBlock = SL == 16 ? 1024 : 256;
+    static constexpr int kColumns = kBlock / SL;        // (row, four channels) of a workgroup
+};
+template <int DT, int SL>
+__global__ __launch_bounds__(Join<SL>::kBlock) void k_attend_join(AttendArgs g) {
     using T = typename Num<DT>::T;
-    __shared__ float red[2][NW], sums[NW][128];
-    const int64_t slot = blockIdx.x, total = gridDim.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = g.a.dim;
-    const int bh = int(slot / g.rows), row = int(slot - int64_t(bh) * g.rows);
-    const float2 *stats = g.part_stats + slot;
-    float top = -INFINITY;
-    for (int s = threadIdx.x; s < g.n_split; s += 64 * NW) top = fmaxf(top, stats[s * total].x);
+    constexpr int kColumns = Join<SL>::kColumns;
+    __shared__ float meet[6][SL == 1 ? 1 : SL * kColumns];
+    const int per_row = g.part_pitch / 4, rows_here = kColumns / per_row;
+    const int lane = threadIdx.x / kColumns, column = threadIdx.x % kColumns;
+    const int64_t total = int64_t(g.a.batch) * g.a.key_heads * g.rows;
+    const int64_t slot = int64_t(blockIdx.x) * rows_here + column / per_row;
+    const int ch = column % per_row * 4;
+    const bool here = column < rows_here * per_row && slot < total;
+    float top = -INFINITY, sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // adds a part, or a joined set of parts, with maximum x and sum w
+    auto add = [&](float x, float w, const float *v) {
+        if (w == 0.0f) return;
+        const float now = fmaxf(top, x), a = part_weight(top, sum, now), b = part_weight(x, w, now);
+        sum = sum * a + w * b;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if (lane == 0) red[0][wave] = top;
-    __syncthreads();
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * a + v[e] * b;
+        top = now;
+    };
+    if (here)
+        for (int s0 = lane; s0 < g.n_split; s0 += SL * kJoinAhead) {
+            float2 st[kJoinAhead];
+            float4 v[kJoinAhead];
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, red[0][w]);
-    float sum = 0.0f, o[2] = {0.0f, 0.0f};
-#pragma unroll 4
-    for (int s = wave; s < g.n_split; s += NW) {
-        const float2 st = stats[s * total];
-        const float mul = part_weight(st.x, st.y, top);
-        sum = fmaf(st.y, mul, sum);
-        const float *p = g.part + (s * total + slot) * g.part_pitch;
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int s = s0 + i * SL;
+                st[i] = make_float2(-INFINITY, 0.0f);
+                v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (s < g.n_split) {
+                    st[i] = g.part_stats[s * total + slot];
+                    v[i] = *reinterpret_cast<const float4 *>(g.part + (s * total + slot) * g.part_pitch + ch);
+                }
+            }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float v = lane + 64 * k < dim ? p[lane + 64 * k] : 0.0f;
-            o[k] += st.y == 0.0f ? 0.0f : v * mul;        // a part without keys wrote no sums
+            for (int i = 0; i < kJoinAhead; ++i) add(st[i].x, st[i].y, reinterpret_cast<const float *>(&v[i]));
+        }
+    if constexpr (SL > 1) {
+        meet[0][threadIdx.x] = top;
+        meet[1][threadIdx.x] = sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) meet[2 + e][threadIdx.x] = o[e];
+        __syncthreads();
+        if (lane != 0) return;
+        for (int l = 1; l < SL; ++l) {
+            const int from = l * kColumns + column;
+            const float v[4] = {meet[2][from], meet[3][from], meet[4][from], meet[5][from]};
+            add(meet[0][from], meet[1][from], v);
         }
     }
-    sums[wave][lane] = o[0];
-    sums[wave][64 + lane] = o[1];
-    if (lane == 0) red[1][wave] = sum;
-    __syncthreads();
-    if (wave != 0) return;
-    sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) sum += red[1][w];
+    if (!here) return;
+    const int bh = int(slot / g.rows), row = int(slot - int64_t(bh) * g.rows);
     const Problem<DT> at(g, bh);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t to = at.row(row);
+    float low[4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int ch = lane + 64 * k;
-        if (ch >= dim) break;
-        float full = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) full += sums[w][ch];
-        full *= inv;
-        const T rounded = T(full);
-        static_cast<T *>(g.o)[to + ch] = rounded;
-        if (DT != BEVPOOL_F32 && g.o_low) static_cast<T *>(g.o_low)[to + ch] = T(full - float(rounded));
+    for (int e = 0; e < 4; ++e) {
+        o[e] *= inv;
+        low[e] = o[e] - float(T(o[e]));
     }
-    if (g.lse && lane == 0) g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    // rows of out start on four elements only if dim is a multiple of four
+    if (g.a.dim % 4 == 0 && g.out_aligned) {
+        write4<true>(static_cast<T *>(g.o) + to, ch, g.a.dim, o);
+        if (DT != BEVPOOL_F32 && g.o_low) write4<true>(static_cast<T *>(g.o_low) + to, ch, g.a.dim, low);
+    } else {
+        write4<false>(static_cast<T *>(g.o) + to, ch, g.a.dim, o);
+        if (DT != BEVPOOL_F32 && g.o_low) write4<false>(static_cast<T *>(g.o_low) + to, ch, g.a.dim, low);
+    }
+    if (g.lse && ch == 0) g.lse[at.stat(row)] = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+}
+
+template <int DT, int SL>
+void launch_join(const AttendArgs &g, hipStream_t stream) {
+    const int64_t rows_here = Join<SL>::kColumns / (g.part_pitch / 4), rows = int64_t(g.a.batch) * g.a.key_heads * g.rows;
+    hipLaunchKernelGGL((k_attend_join<DT, SL>), dim3(uint32_t((rows + rows_here - 1) / rows_here)),
+                       dim3(Join<SL>::kBlock), 0, stream, g);
 }
 
 constexpr int kFill = 768;          // workgroups that fill the chip, three to a compute unit
+constexpr int kFillFew = 256;       // the same for few rows, where a workgroup's loads fill its unit's share
 constexpr int kFewRows = 32;        // rows of a key head that one wave holds
 
 int part_pitch(const bevmap_attend &a) { return (a.dim + 3) / 4 * 4; }
@@ -316,7 +349,8 @@ void partition(const bevmap_attend &a, AttendArgs *g, bool *few) {
     const int tile_keys = *few ? 128 : a.dtype == BEVPOOL_F32 ? 32 : 64;
     g->n_tiles = attend_ceil(rows, tile_rows);
     const int64_t whole = int64_t(a.batch) * a.key_heads * g->n_tiles;
-    int64_t split = whole ? (kFill + whole - 1) / whole : 1;
+    const int fill = *few ? kFillFew : kFill;
+    int64_t split = whole ? (fill + whole - 1) / whole : 1;
     const int64_t most = attend_ceil(a.keys, 2 * tile_keys);
     if (split > most) split = most;
     g->n_split = split < 1 ? 1 : int(split);
@@ -356,13 +390,13 @@ int forward(const AttendArgs &g, bool vec, bool few, hipStream_t stream) {
         default: rc = launch<DT, 4>(g, vec, few, stream); break;
     }
     if (rc || g.n_split == 1) return rc;
-    const dim3 rows(uint32_t(g.a.batch) * g.a.key_heads * g.rows);
-    if (g.n_split >= 64)
-        hipLaunchKernelGGL((k_attend_join<DT, 16>), rows, dim3(1024), 0, stream, g);
-    else if (g.n_split >= 8)
-        hipLaunchKernelGGL((k_attend_join<DT, 4>), rows, dim3(256), 0, stream, g);
+    // a thread reads its parts in one go, or in two
+    if (g.n_split > 4 * kJoinAhead)
+        launch_join<DT, 16>(g, stream);
+    else if (g.n_split > kJoinAhead)
+        launch_join<DT, 4>(g, stream);
     else
-        hipLaunchKernelGGL((k_attend_join<DT, 1>), rows, dim3(64), 0, stream, g);
+        launch_join<DT, 1>(g, stream);
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -399,8 +433,8 @@ int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k
     if (int64_t(a.batch) * a.key_heads * g.n_split * g.n_tiles >= (int64_t(1) << 31) / kAttendBlock)
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d heads=%d: too many tiles of rows", a.batch,
                             a.queries, a.heads);
-    const bool vec = attend_vec(a, q, k, v) && aligned_for(out, 0, a.dtype, 4) &&
-                     (!out_low || aligned_for(out_low, 0, a.dtype, 4));
+    g.out_aligned = aligned_for(out, 0, a.dtype, 4) && (!out_low || aligned_for(out_low, 0, a.dtype, 4));
+    const bool vec = attend_vec(a, q, k, v) && g.out_aligned;
     switch (a.dtype) {
         case BEVPOOL_F32: return forward<BEVPOOL_F32>(g, vec, few, stream);
         case BEVPOOL_BF16: return forward<BEVPOOL_BF16>(g, vec, few, stream);
