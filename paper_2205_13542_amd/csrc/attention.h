@@ -45,6 +45,13 @@ using f32x16 = float __attribute__((ext_vector_type(16)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 
+__device__ __forceinline__ f32x16 zeros() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
 // A chunk is 16 bytes: 8 elements of a 16-bit type, one step of K = 16, or 4 of
 // fp32, four steps of K = 2. In a row's chunks 2 j and 2 j + 1 the two half waves
 // hold the contracted elements of step j.
@@ -315,77 +322,83 @@ struct Stage {
     static constexpr int kLoads = (ROWS * S::kUsed + kAttendBlock - 1) / kAttendBlock;
     static constexpr bool kEven = ROWS * S::kUsed % kAttendBlock == 0;      // no thread is left over
     u32x4 reg[kLoads];
+    uint32_t at[kLoads];        // bytes from the tile's first row
 
     static __device__ __forceinline__ int row(int i) { return (threadIdx.x + i * kAttendBlock) / S::kUsed; }
     static __device__ __forceinline__ int chunk(int i) { return (threadIdx.x + i * kAttendBlock) % S::kUsed; }
 
-    // base: the tile's first row (uniform). rows: how many of its rows there are.
-    __device__ __forceinline__ void load(const char *base, uint32_t stride, int rows, int dim) {
+    __device__ __forceinline__ Stage(uint32_t stride, int dim) {
         const int last = (dim - 1) / S::M::kElems;
 #pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            at[i] = uint32_t(row(i)) * stride + (VEC ? uint32_t(min(chunk(i), last)) * 16 : 0);
+    }
+    // base: the tile's first row (uniform). words: its rows in use, the others are
+    // not read and count as zeros; all: whether every row is.
+    template <int WORDS>
+    __device__ __forceinline__ void load(const char *base, const uint64_t (&words)[WORDS], bool all, int dim) {
+#pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int r = row(i), c = min(chunk(i), last);
+            const int r = row(i);
             const bool there = kEven || r < ROWS;
+            uint64_t word = words[0];
+            if constexpr (WORDS == 2) word = r >= 64 ? words[1] : word;
             if constexpr (VEC) {
-                const uint32_t at = uint32_t(r) * stride + uint32_t(c) * 16;
-                if (rows >= ROWS) {
-                    if (there) reg[i] = *reinterpret_cast<const u32x4 *>(base + at);
+                if (all) {
+                    if (there) reg[i] = *reinterpret_cast<const u32x4 *>(base + at[i]);
                 } else {
                     reg[i] = u32x4{0, 0, 0, 0};
-                    if (there && r < rows) reg[i] = *reinterpret_cast<const u32x4 *>(base + at);
+                    if (there && (word >> (r & 63)) & 1) reg[i] = *reinterpret_cast<const u32x4 *>(base + at[i]);
                 }
             } else {
                 reg[i] = u32x4{0, 0, 0, 0};
-                if (there && r < rows)
-                    reg[i] = load_chunk<DT, false>(reinterpret_cast<const T *>(base + uint32_t(r) * stride), chunk(i), dim);
+                if (there && (word >> (r & 63)) & 1)
+                    reg[i] = load_chunk<DT, false>(reinterpret_cast<const T *>(base + at[i]), chunk(i), dim);
             }
         }
     }
-    // Words of rows in use; the others go to LDS as zeros.
-    template <int WORDS>
-    __device__ __forceinline__ void store(char *tile, const uint64_t (&words)[WORDS], bool all) const {
+    __device__ __forceinline__ void store(char *tile) const {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = row(i);
             if (!kEven && r >= ROWS) break;
-            char *to = tile + chunk_at<S::kChunks>(r, chunk(i));
-            if (all) {
-                *reinterpret_cast<u32x4 *>(to) = reg[i];
-            } else {
-                uint64_t word = words[0];
-                if constexpr (WORDS == 2) word = r >= 64 ? words[1] : word;
-                *reinterpret_cast<u32x4 *>(to) = (word >> (r & 63)) & 1 ? reg[i] : u32x4{0, 0, 0, 0};
-            }
+            *reinterpret_cast<u32x4 *>(tile + chunk_at<S::kChunks>(r, chunk(i))) = reg[i];
         }
     }
 };
 
-// Words of the keys in use of a tile of KEYS keys from j0; every lane of a wave has
-// asked for its own (used), where there is a mask.
+// The keys in use of a tile of KEYS keys, a bit to a key.
 template <int KEYS>
 struct InUse {
     static constexpr int kWords = KEYS <= 64 ? 1 : KEYS / 64;
-    int used[kWords];
+    static constexpr uint64_t kFull = KEYS >= 64 ? ~0ull : (1ull << (KEYS & 63)) - 1;
     uint64_t words[kWords];
     bool all;
+};
+// ask() sends for the mask of the tile at key j0, count() makes the tile's words of it.
+template <int KEYS>
+struct Mask {
+    using Tile = InUse<KEYS>;
+    int used[Tile::kWords];
     template <class P>
     __device__ __forceinline__ void ask(const P &at, int j0) {
         const int lane = threadIdx.x & 63;
         if (at.g.mask)
 #pragma unroll
-            for (int w = 0; w < kWords; ++w) used[w] = KEYS >= 64 || lane < KEYS ? at.ask(j0 + 64 * w + lane) : 0;
+            for (int w = 0; w < Tile::kWords; ++w) used[w] = KEYS >= 64 || lane < KEYS ? at.ask(j0 + 64 * w + lane) : 0;
     }
     template <class P>
-    __device__ __forceinline__ void count(const P &at, int j0) {
-        constexpr uint64_t kFull = KEYS >= 64 ? ~0ull : (1ull << (KEYS & 63)) - 1;
-        all = true;
+    __device__ __forceinline__ Tile count(const P &at, int j0) const {
+        Tile t;
+        t.all = true;
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
+        for (int w = 0; w < Tile::kWords; ++w) {
             const int there = at.len - j0 - 64 * w;
-            words[w] = at.g.mask ? __ballot(used[w] != 0)
-                                 : there >= 64 ? kFull : there <= 0 ? 0ull : kFull & ((1ull << there) - 1);
-            all = all && words[w] == kFull;
+            t.words[w] = at.g.mask ? __ballot(used[w] != 0)
+                                   : there >= 64 ? Tile::kFull : there <= 0 ? 0ull : Tile::kFull & ((1ull << there) - 1);
+            t.all = t.all && t.words[w] == Tile::kFull;
         }
+        return t;
     }
 };
 

@@ -20,13 +20,15 @@ constexpr float kMaxTileSum = 4096.0f;
 
 // WR waves side by side have rows of their own (4), or all share the tile's rows
 // and split each tile's keys (1).
-template <int DT, int WR>
+template <int DT, int DB, int WR>
 struct Tile {
     static constexpr int kBlocks = WR == 1 || DT == BEVPOOL_F32 ? 1 : 2;    // 32-key blocks of a wave
-    static constexpr int kKeys = 32 * kBlocks * (4 / WR);
+    static constexpr int kKeys = 32 * kBlocks * (4 / WR);       // of a tile
     static constexpr int kRows = 32 * WR;
-    // tiles in LDS: two where four arrays fit beside each other, else one
-    static constexpr int buffers(int row_bytes) { return 4 * kKeys * row_bytes <= 128 * 1024 ? 2 : 1; }
+    static constexpr int kBytes = kKeys * Shape<DT, DB>::kRowBytes;
+    // pairs of tiles, keys and values, in LDS: two where they fit
+    static constexpr int kPairs = 4 * kBytes <= 128 * 1024 ? 2 : 1;
+    static constexpr int kLds = 2 * kPairs * kBytes;
 };
 
 // What a part of a row with this maximum and sum counts where the whole row's
@@ -42,10 +44,8 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
-    using W = Tile<DT, WR>;
-    constexpr int kTileBytes = W::kKeys * S::kRowBytes;
-    constexpr int kBuffers = W::buffers(S::kRowBytes);
-    extern __shared__ __attribute__((aligned(16))) char lds[];       // [kBuffers][k, v][tile]
+    using W = Tile<DT, DB, WR>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
 
     const int n_bh = g.a.batch * g.a.key_heads;
     int bh, tile;
@@ -77,96 +77,98 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
     const int t0 = split * per, t1 = min(t0 + per, tiles);
 
     const uint32_t k_step = uint32_t(g.a.k_row * int(sizeof(T))), v_step = uint32_t(g.a.v_row * int(sizeof(T)));
-    Stage<DT, DB, VEC, W::kKeys> next_k, next_v;
-    InUse<W::kKeys> use;
-    auto fetch = [&](int t) {
-        const int j0 = t * W::kKeys;
-        use.ask(at, j0);
-        next_k.load(reinterpret_cast<const char *>(at.k(j0)), k_step, at.len - j0, dim);
-        next_v.load(reinterpret_cast<const char *>(at.v(j0)), v_step, at.len - j0, dim);
-    };
-    auto put = [&](int t) {
-        use.count(at, t * W::kKeys);
-        char *k = lds + ((t - t0) & (kBuffers - 1)) * 2 * kTileBytes;
-        next_k.store(k, use.words, use.all);
-        next_v.store(k + kTileBytes, use.words, use.all);
-    };
+    using Used = InUse<W::kKeys>;
+    Stage<DT, DB, VEC, W::kKeys> next_k(k_step, dim), next_v(v_step, dim);
+    Mask<W::kKeys> mask;
+    auto key_rows = [&](int t) { return reinterpret_cast<const char *>(at.k(t * W::kKeys)); };
+    auto value_rows = [&](int t) { return reinterpret_cast<const char *>(at.v(t * W::kKeys)); };
 
     f32x16 o[DB];
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    for (int d = 0; d < DB; ++d) o[d] = zeros();
     float top = -INFINITY, sum = 0.0f;     // of log2 scores; sum over this lane's keys
     const float c = g.log2_scale;
-    const int row0 = WR == 1 ? 32 * wave : 0;       // of this wave's keys in a tile
+    typename M::Rows p;
+    // p and this lane's sum of the exponentials of a block's scores relative to base
+    auto exponentials = [&](const f32x16 &s, float base) {
+        f32x16 e;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -base));
+        p = M::rows(e);
+        return p.sum();
+    };
+    // keys out of use: bit k of word is key k of the block
+    auto leave_out = [&](f32x16 &s, uint32_t word) {
+        const uint32_t bits = word >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[i] : -INFINITY;
+    };
+    // new maxima; what is summed and p again, relative to them
+    auto raise = [&](const f32x16 &s) {
+        float high = s[0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) high = fmaxf(high, s[i]);
+        const float now = fmaxf(top, both_max(high) * c);
+        const float old = top == -INFINITY ? 0.0f : exp2f(top - now);
+        sum *= old;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= old;
+        top = now;
+        return exponentials(s, top == -INFINITY ? 0.0f : top);
+    };
 
+    // While a tile is used the next one is read, and the mask of the one after it, so that rows out of use are
+    // not read. The buffer is a constant, which leaves no address to compute: the loop takes two tiles a turn.
+    const int row0 = WR == 1 ? 32 * wave : 0;          // of this wave's keys in a tile
+    Used use = {}, next = {};
     if (t0 < t1) {
-        fetch(t0);
-        put(t0);
+        mask.ask(at, t0 * W::kKeys);
+        use = mask.count(at, t0 * W::kKeys);
+        next_k.load(key_rows(t0), use.words, use.all, dim);
+        next_v.load(value_rows(t0), use.words, use.all, dim);
+        mask.ask(at, (t0 + 1) * W::kKeys);
+        next_k.store(lds);
+        next_v.store(lds + W::kBytes);
     }
-    for (int t = t0; t < t1; ++t) {
-        const char *k = lds + ((t - t0) & (kBuffers - 1)) * 2 * kTileBytes, *v = k + kTileBytes;
-        uint64_t mine = use.words[0];
-        if constexpr (use.kWords == 2) mine = row0 >= 64 ? use.words[1] : mine;
-        if constexpr (WR == 1) mine = (mine >> (row0 & 63)) & 0xFFFFFFFFull;
-        if (t + 1 < t1) fetch(t + 1);
-        __syncthreads();
-        if (mine != 0) {
+    for (int t2 = t0; t2 < t1; t2 += 2) {
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {
+            const int t = t2 + turn, buffer = turn & (W::kPairs - 1);
+            if (t >= t1) break;
+            const char *k = lds + buffer * 2 * W::kBytes, *v = k + W::kBytes;
+            if (t + 1 < t1) {
+                next = mask.count(at, (t + 1) * W::kKeys);
+                next_k.load(key_rows(t + 1), next.words, next.all, dim);
+                next_v.load(value_rows(t + 1), next.words, next.all, dim);
+                mask.ask(at, (t + 2) * W::kKeys);
+            }
+            __syncthreads();
+            const uint64_t mine = use.words[W::kKeys == 128 ? row0 >> 6 : 0] >> (row0 & 63);
             f32x16 s[W::kBlocks];
 #pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n) s[n] = S::scores(k, row0 + 32 * n, q, zeros());
+#pragma unroll
             for (int n = 0; n < W::kBlocks; ++n) {
-                f32x16 zero;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
-                s[n] = S::scores(k, row0 + 32 * n, q, zero);
-            }
-            constexpr uint64_t kAll = W::kBlocks == 2 ? ~0ull : 0xFFFFFFFFull;
-            if (mine != kAll) {
-#pragma unroll
-                for (int n = 0; n < W::kBlocks; ++n) {
-                    const uint32_t bits = uint32_t(mine >> (32 * n)) >> (4 * half);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[n][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[n][i] : -INFINITY;
+                const uint32_t word = uint32_t(mine >> (32 * n));
+                if (__builtin_expect(word != 0xFFFFFFFFu, 0)) {
+                    if (word == 0) continue;
+                    leave_out(s[n], word);
                 }
+                float part = exponentials(s[n], top);
+                if (__builtin_expect(__any(!(part <= kMaxTileSum)), 0)) part = raise(s[n]);
+                sum += part;
+                S::sums(v, row0 + 32 * n, p, o);
             }
-            typename M::Rows p[W::kBlocks];
-            auto exponentials = [&](float base) {
-                float part = 0.0f;
-#pragma unroll
-                for (int n = 0; n < W::kBlocks; ++n) {
-                    f32x16 e;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
-                    p[n] = M::rows(e);
-                    part += p[n].sum();
-                }
-                return part;
-            };
-            float part = exponentials(top);
-            if (__any(!(part <= kMaxTileSum))) {
-                float high = s[0][0];
-#pragma unroll
-                for (int n = 0; n < W::kBlocks; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) high = fmaxf(high, s[n][i]);
-                const float now = fmaxf(top, both_max(high) * c);
-                const float old = top == -INFINITY ? 0.0f : exp2f(top - now);
-                sum *= old;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= old;
-                top = now;
-                part = exponentials(top == -INFINITY ? 0.0f : top);
+            if constexpr (W::kPairs == 1) __syncthreads();
+            if (t + 1 < t1) {
+                char *to = lds + (W::kPairs == 1 ? 0 : 1 - buffer) * 2 * W::kBytes;
+                next_k.store(to);
+                next_v.store(to + W::kBytes);
+                use = next;
             }
-            sum += part;
-#pragma unroll
-            for (int n = 0; n < W::kBlocks; ++n) S::sums(v, row0 + 32 * n, p[n], o);
         }
-        if constexpr (kBuffers == 1) __syncthreads();
-        if (t + 1 < t1) put(t + 1);
     }
     __syncthreads();
     sum = both_sum(sum);
@@ -346,7 +348,7 @@ void partition(const bevmap_attend &a, AttendArgs *g, bool *few) {
     const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
     *few = rows <= kFewRows;
     const int tile_rows = *few ? 32 : 128;
-    const int tile_keys = *few ? 128 : a.dtype == BEVPOOL_F32 ? 32 : 64;
+    const int tile_keys = *few ? 128 : 64;
     g->n_tiles = attend_ceil(rows, tile_rows);
     const int64_t whole = int64_t(a.batch) * a.key_heads * g->n_tiles;
     const int fill = *few ? kFillFew : kFill;
@@ -358,9 +360,7 @@ void partition(const bevmap_attend &a, AttendArgs *g, bool *few) {
 
 template <int DT, int DB, bool VEC, int WR>
 int launch(const AttendArgs &g, hipStream_t stream) {
-    using S = Shape<DT, DB>;
-    using W = Tile<DT, WR>;
-    size_t lds = 2 * W::buffers(S::kRowBytes) * size_t(W::kKeys) * S::kRowBytes;
+    size_t lds = Tile<DT, DB, WR>::kLds;
     if (WR == 1) {
         const size_t join = (4 * 32 * (32 * DB + 1) + 2 * 128 + 1) * sizeof(float);
         lds = lds > join ? lds : join;

@@ -25,13 +25,6 @@ struct Walk {
     static constexpr int kLoads = (kWalk * S::kUsed + kAttendBlock - 1) / kAttendBlock;
 };
 
-__device__ __forceinline__ f32x16 zeros() {
-    f32x16 z;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-    return z;
-}
-
 template <int DT>
 __device__ __forceinline__ float pair_dot(u32x4 a, u32x4 b, u32x4 low) {
     using T = typename Num<DT>::T;
