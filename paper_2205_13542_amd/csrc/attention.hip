@@ -40,7 +40,7 @@ __device__ __forceinline__ float part_weight(float top, float sum, float most) {
 }
 
 template <int DT, int DB, bool VEC, int WR>
-__global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, (DT == BEVPOOL_F32 && DB == 4 ? 1 : 2)) void k_attend(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -145,7 +145,9 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend(AttendArgs g) {
                 mask.ask(at, (t + 2) * W::kKeys);
             }
             __syncthreads();
-            const uint64_t mine = use.words[W::kKeys == 128 ? row0 >> 6 : 0] >> (row0 & 63);
+            uint64_t mine = use.words[0];
+            if constexpr (Used::kWords == 2) mine = row0 >= 64 ? use.words[1] : mine;
+            mine >>= row0 & 63;
             f32x16 s[W::kBlocks];
 #pragma unroll
             for (int n = 0; n < W::kBlocks; ++n) s[n] = S::scores(k, row0 + 32 * n, q, zeros());

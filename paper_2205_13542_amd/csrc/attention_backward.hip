@@ -16,13 +16,17 @@ namespace bevmap {
 namespace {
 
 constexpr int kOwn = 128;           // rows or keys that a workgroup owns, 32 a wave
-constexpr int kWalk = 32;           // keys or rows of a tile that it walks
 
+// Rows or keys of a tile that is walked, and what a thread moves of it.
 template <int DT, int DB>
 struct Walk {
     using S = Shape<DT, DB>;
-    static constexpr int kTileBytes = kWalk * S::kRowBytes;
-    static constexpr int kLoads = (kWalk * S::kUsed + kAttendBlock - 1) / kAttendBlock;
+    static constexpr int kBlocks = DT != BEVPOOL_F32 && DB <= 2 ? 2 : 1;        // of 32
+    static constexpr int kSize = 32 * kBlocks;
+    static constexpr int kBytes = kSize * S::kRowBytes;
+    static constexpr int kLds = 4 * kBytes + 4 * kSize * int(sizeof(float));
+    // Waves of a SIMD: the sums of 128 channels (fp32: 96) do not leave room for two
+    static constexpr int kWaves = DB == 4 || (DT == BEVPOOL_F32 && DB == 3) ? 1 : 2;
 };
 
 template <int DT>
@@ -38,26 +42,26 @@ __device__ __forceinline__ float pair_dot(u32x4 a, u32x4 b, u32x4 low) {
 }
 
 // A lane's row or key of a gradient: 16 channels of each block, whole or to a part.
-template <int DT, int DB>
+template <int DT, int DB, bool VEC>
 __device__ __forceinline__ void write_row(const f32x16 *acc, bool on, float mul, typename Num<DT>::T *to,
                                           float *part, int dim, int half) {
-    using T = typename Num<DT>::T;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int ch = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (ch >= dim) continue;
-            const float v = on ? acc[d][i] * mul : 0.0f;
+        for (int i = 0; i < 16; i += 4) {
+            const int ch = 32 * d + 2 * i + 4 * half;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = on ? acc[d][i + e] * mul : 0.0f;
             if (part)
-                part[ch] = v;
+                write4<VEC>(part, ch, dim, v);
             else
-                to[ch] = T(v);
+                write4<VEC>(to, ch, dim, v);
         }
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dq(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, (Walk<DT, DB>::kWaves)) void k_attend_dq(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -96,80 +100,78 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dq(AttendArgs g) {
     if (in && half == 0 && split == 0) g.delta[at.stat(row)] = delta;
     if (lse == -INFINITY) lse = INFINITY;        // a row without keys: every p is 0
 
-    const int tiles = (at.len + kWalk - 1) / kWalk, per = (tiles + g.n_split - 1) / g.n_split;
+    const int tiles = (at.len + W::kSize - 1) / W::kSize, per = (tiles + g.n_split - 1) / g.n_split;
     const int t0 = split * per, t1 = min(t0 + per, tiles);
-    u32x4 next_k[W::kLoads], next_v[W::kLoads];
-    int used;
-    auto fetch = [&](int t) {
-        const int j0 = t * kWalk;
-        used = lane < kWalk ? at.ask(j0 + lane) : 0;
-#pragma unroll
-        for (int i = 0; i < W::kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
-            next_k[i] = next_v[i] = u32x4{0, 0, 0, 0};
-            if (r < kWalk && j0 + r < at.len) {
-                next_k[i] = load_chunk<DT, VEC>(at.k(j0 + r), c, dim);
-                next_v[i] = load_chunk<DT, VEC>(at.v(j0 + r), c, dim);
-            }
-        }
-    };
-    auto put = [&](int buffer) {
-        const uint32_t word = uint32_t(__ballot(used != 0));
-        char *k = lds + buffer * 2 * W::kTileBytes, *v = k + W::kTileBytes;
-#pragma unroll
-        for (int i = 0; i < W::kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
-            if (r >= kWalk) break;
-            const bool use = (word >> r) & 1;
-            *reinterpret_cast<u32x4 *>(k + chunk_at<S::kChunks>(r, c)) = use ? next_k[i] : u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(v + chunk_at<S::kChunks>(r, c)) = use ? next_v[i] : u32x4{0, 0, 0, 0};
-        }
-        return word;
-    };
+    using Used = InUse<W::kSize>;
+    Stage<DT, DB, VEC, W::kSize> next_k(uint32_t(g.a.k_row * int(sizeof(T))), dim), next_v(uint32_t(g.a.v_row * int(sizeof(T))), dim);
+    Mask<W::kSize> mask;
+    auto key_rows = [&](int t) { return reinterpret_cast<const char *>(at.k(t * W::kSize)); };
+    auto value_rows = [&](int t) { return reinterpret_cast<const char *>(at.v(t * W::kSize)); };
     f32x16 dq[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) dq[i] = zeros();
     const float c = g.sign * g.log2_scale;
-    uint32_t word = 0;
+    Used use = {}, next = {};
     if (t0 < t1) {
-        fetch(t0);
-        word = put(0);
-        if (t0 + 1 < t1) fetch(t0 + 1);
+        mask.ask(at, t0 * W::kSize);
+        use = mask.count(at, t0 * W::kSize);
+        next_k.load(key_rows(t0), use.words, use.all, dim);
+        next_v.load(value_rows(t0), use.words, use.all, dim);
+        mask.ask(at, (t0 + 1) * W::kSize);
+        next_k.store(lds);
+        next_v.store(lds + W::kBytes);
     }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const char *k = lds + ((t - t0) & 1) * 2 * W::kTileBytes, *v = k + W::kTileBytes;
-        if (word != 0) {
-            f32x16 s = S::scores(k, 0, q, zeros());
-            const f32x16 dp = S::scores(v, 0, d, zeros());
-            const uint32_t bits = word >> (4 * half);
+    for (int t2 = t0; t2 < t1; t2 += 2) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse));
-                s[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? p * (dp[i] - delta) : 0.0f;
+        for (int buffer = 0; buffer < 2; ++buffer) {
+            const int t = t2 + buffer;
+            if (t >= t1) break;
+            const char *k = lds + buffer * 2 * W::kBytes, *v = k + W::kBytes;
+            if (t + 1 < t1) {
+                next = mask.count(at, (t + 1) * W::kSize);
+                next_k.load(key_rows(t + 1), next.words, next.all, dim);
+                next_v.load(value_rows(t + 1), next.words, next.all, dim);
+                mask.ask(at, (t + 2) * W::kSize);
             }
-            S::sums(k, 0, M::rows(s), dq);
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n) {
+                const uint32_t word = uint32_t(use.words[0] >> (32 * n));
+                if (__builtin_expect(word == 0, 0)) continue;
+                f32x16 s = S::scores(k, 32 * n, q, zeros());
+                const f32x16 dp = S::scores(v, 32 * n, d, zeros());
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
+                if (__builtin_expect(word != 0xFFFFFFFFu, 0)) {
+                    const uint32_t bits = word >> (4 * half);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[i] : 0.0f;
+                }
+                S::sums(k, 32 * n, M::rows(s), dq);
+            }
+            if (t + 1 < t1) {
+                char *to = lds + (1 - buffer) * 2 * W::kBytes;
+                next_k.store(to);
+                next_v.store(to + W::kBytes);
+                use = next;
+            }
         }
-        if (t + 1 < t1) {
-            word = put((t + 1 - t0) & 1);
-            if (t + 2 < t1) fetch(t + 2);
-        }
-        __syncthreads();
     }
     if (!in) return;
     float *part = nullptr;
     if (g.n_split > 1) part = g.part + ((int64_t(split) * n_bh + bh) * g.rows + row) * dim;
-    write_row<DT, DB>(dq, true, g.a.scale, static_cast<T *>(g.dq) + at.row(row), part, dim, half);
+    write_row<DT, DB, VEC>(dq, true, g.a.scale, static_cast<T *>(g.dq) + at.row(row), part, dim, half);
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dkv(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, (Walk<DT, DB>::kWaves)) void k_attend_dkv(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
     using W = Walk<DT, DB>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][q, dout][tile], then [2][lse, delta][kWalk]
-    float *stats = reinterpret_cast<float *>(lds + 4 * W::kTileBytes);
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][q, dout][tile], then [2][lse, delta][row]
+    float *stats = reinterpret_cast<float *>(lds + 4 * W::kBytes);
     const int n_bh = g.a.batch * g.a.key_heads;
     int bh, tile;
     work_of(n_bh, g.n_split * g.n_tiles, bh, tile);
@@ -190,39 +192,41 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dkv(AttendArgs g) {
             v[s] = load_chunk<DT, VEC>(at.v(key), 2 * s + half, dim);
         }
     }
-    const int tiles = (g.rows + kWalk - 1) / kWalk, per = (tiles + g.n_split - 1) / g.n_split;
+    const int tiles = (g.rows + W::kSize - 1) / W::kSize, per = (tiles + g.n_split - 1) / g.n_split;
     // a tile of keys past the sample's length has nothing to walk
     const int t0 = split * per, t1 = tile * kOwn < at.len ? min(t0 + per, tiles) : t0;
-    u32x4 next_q[W::kLoads], next_d[W::kLoads];
+    using Rows = Stage<DT, DB, VEC, W::kSize>;
+    u32x4 next_q[Rows::kLoads], next_d[Rows::kLoads];
     float next_stat = 0.0f;
     auto fetch = [&](int t) {
-        const int r0 = t * kWalk;
+        const int r0 = t * W::kSize;
 #pragma unroll
-        for (int i = 0; i < W::kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
+        for (int i = 0; i < Rows::kLoads; ++i) {
+            const int r = Rows::row(i), c = Rows::chunk(i);
             next_q[i] = next_d[i] = u32x4{0, 0, 0, 0};
-            if (r < kWalk && r0 + r < g.rows) {
-                next_q[i] = load_chunk<DT, VEC>(at.q(r0 + r), c, dim);
-                next_d[i] = load_chunk<DT, VEC>(static_cast<const T *>(g.dout) + at.row(r0 + r), c, dim);
+            if ((Rows::kEven || r < W::kSize) && r0 + r < g.rows) {
+                int query, head;
+                at.split_row(r0 + r, query, head);
+                next_q[i] = load_chunk<DT, VEC>(at.q(query, head), c, dim);
+                next_d[i] = load_chunk<DT, VEC>(static_cast<const T *>(g.dout) + at.row(query, head), c, dim);
             }
         }
-        if (threadIdx.x < 2 * kWalk) {
-            const int r = r0 + (threadIdx.x & (kWalk - 1));
-            const float none = threadIdx.x < kWalk ? INFINITY : 0.0f;       // lse, delta of rows past the last
-            next_stat = r < g.rows ? (threadIdx.x < kWalk ? g.lse : g.delta)[at.stat(r)] : none;
+        if (threadIdx.x < 2 * W::kSize) {
+            const int r = r0 + (threadIdx.x & (W::kSize - 1));
+            const float none = threadIdx.x < W::kSize ? INFINITY : 0.0f;     // lse, delta of rows past the last
+            next_stat = r < g.rows ? (threadIdx.x < W::kSize ? g.lse : g.delta)[at.stat(r)] : none;
             if (next_stat == -INFINITY) next_stat = INFINITY;
         }
     };
-    auto put = [&](int buffer) {
-        char *q = lds + buffer * 2 * W::kTileBytes, *d = q + W::kTileBytes;
+    auto put = [&](char *q, float *stat) {
 #pragma unroll
-        for (int i = 0; i < W::kLoads; ++i) {
-            const int n = threadIdx.x + i * kAttendBlock, r = n / S::kUsed, c = n - r * S::kUsed;
-            if (r >= kWalk) break;
-            *reinterpret_cast<u32x4 *>(q + chunk_at<S::kChunks>(r, c)) = next_q[i];
-            *reinterpret_cast<u32x4 *>(d + chunk_at<S::kChunks>(r, c)) = next_d[i];
+        for (int i = 0; i < Rows::kLoads; ++i) {
+            const int r = Rows::row(i);
+            if (!Rows::kEven && r >= W::kSize) break;
+            *reinterpret_cast<u32x4 *>(q + S::chunk_at(r, Rows::chunk(i))) = next_q[i];
+            *reinterpret_cast<u32x4 *>(q + W::kBytes + S::chunk_at(r, Rows::chunk(i))) = next_d[i];
         }
-        if (threadIdx.x < 2 * kWalk) stats[buffer * 2 * kWalk + threadIdx.x] = next_stat;
+        if (threadIdx.x < 2 * W::kSize) stat[threadIdx.x] = next_stat;
     };
     f32x16 dk[DB], dv[DB];
 #pragma unroll
@@ -230,29 +234,37 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dkv(AttendArgs g) {
     const float c = g.sign * g.log2_scale;
     if (t0 < t1) {
         fetch(t0);
-        put(0);
-        if (t0 + 1 < t1) fetch(t0 + 1);
+        put(lds, stats);
     }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const int buffer = (t - t0) & 1;
-        const char *q = lds + buffer * 2 * W::kTileBytes, *d = q + W::kTileBytes;
-        const float *lse = stats + buffer * 2 * kWalk, *delta = lse + kWalk;
-        f32x16 p = S::scores(q, 0, k, zeros());
-        f32x16 ds = S::scores(d, 0, v, zeros());
+    for (int t2 = t0; t2 < t1; t2 += 2) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = 8 * (i >> 2) + 4 * half + (i & 3);
-            p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse[r]));
-            ds[i] = p[i] * (ds[i] - delta[r]);
+        for (int buffer = 0; buffer < 2; ++buffer) {
+            const int t = t2 + buffer;
+            if (t >= t1) break;
+            const char *q = lds + buffer * 2 * W::kBytes, *d = q + W::kBytes;
+            const float *lse = stats + buffer * 2 * W::kSize + 4 * half, *delta = lse + W::kSize;
+            if (t + 1 < t1) fetch(t + 1);
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < W::kBlocks; ++n) {
+                f32x16 p = S::scores(q, 32 * n, k, zeros());
+                f32x16 ds = S::scores(d, 32 * n, v, zeros());
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 l = *reinterpret_cast<const float4 *>(lse + 32 * n + 2 * i);
+                    const float4 m = *reinterpret_cast<const float4 *>(delta + 32 * n + 2 * i);
+                    const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[i + e] = __builtin_amdgcn_exp2f(fmaf(p[i + e], c, -ls[e]));
+                        ds[i + e] = p[i + e] * (ds[i + e] - de[e]);
+                    }
+                }
+                S::sums(d, 32 * n, M::rows(p), dv);
+                S::sums(q, 32 * n, M::rows(ds), dk);
+            }
+            if (t + 1 < t1) put(lds + (1 - buffer) * 2 * W::kBytes, stats + (1 - buffer) * 2 * W::kSize);
         }
-        S::sums(d, 0, M::rows(p), dv);
-        S::sums(q, 0, M::rows(ds), dk);
-        if (t + 1 < t1) {
-            put((t + 1 - t0) & 1);
-            if (t + 2 < t1) fetch(t + 2);
-        }
-        __syncthreads();
     }
     if (!in) return;
     float *part_k = nullptr, *part_v = nullptr;
@@ -262,8 +274,8 @@ __global__ __launch_bounds__(kAttendBlock, 2) void k_attend_dkv(AttendArgs g) {
         part_v = part_k + all;
     }
     // a key out of use is a zero key here, whose sums are not its gradients
-    write_row<DT, DB>(dk, use, g.a.scale, static_cast<T *>(g.dk) + at.key(key), part_k, dim, half);
-    write_row<DT, DB>(dv, use, 1.0f, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
+    write_row<DT, DB, VEC>(dk, use, g.a.scale, static_cast<T *>(g.dk) + at.key(key), part_k, dim, half);
+    write_row<DT, DB, VEC>(dv, use, 1.0f, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
 }
 
 // Joins parts, one thread to an element. KEYS: of the gradients of k (grid z 0)
@@ -289,14 +301,14 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_add(AttendArgs g) {
 
 constexpr int kFill = 512;          // workgroups that fill the chip, two to a compute unit
 
-// Workgroups that own `own` rows or keys, and parts of the `walk` others; a part
-// has at least kPartTiles tiles.
-constexpr int kPartTiles = 4;
+// Workgroups that own `own` rows or keys, and parts of the `walk` others, of at least
+// kPartSize each.
+constexpr int kPartSize = 128;
 void partition(const bevmap_attend &a, int64_t own, int64_t walk, int32_t *n_tiles, int32_t *n_split) {
     *n_tiles = attend_ceil(own, kOwn);
     const int64_t whole = int64_t(a.batch) * a.key_heads * *n_tiles;
     int64_t split = whole ? (kFill + whole - 1) / whole : 1;
-    const int64_t most = attend_ceil(walk, kWalk * kPartTiles);
+    const int64_t most = attend_ceil(walk, kPartSize);
     if (split > most) split = most;
     *n_split = split < 1 ? 1 : int32_t(split);
 }
@@ -306,7 +318,7 @@ int64_t rows_of(const bevmap_attend &a) { return int64_t(a.queries) * (a.heads /
 template <int DT, int DB, bool VEC>
 int launch(AttendArgs g, hipStream_t stream) {
     using W = Walk<DT, DB>;
-    const size_t lds = 4 * size_t(W::kTileBytes) + 4 * kWalk * sizeof(float);
+    const size_t lds = W::kLds;
     if (lds > 64 * 1024) {
         BEVPOOL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_attend_dq<DT, DB, VEC>),
                                         hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)));
@@ -353,6 +365,9 @@ int backward(const AttendArgs &g, bool vec, hipStream_t stream) {
     }
 }
 
+// Of the workspace, ahead of the parts, which start on 16 bytes.
+int64_t delta_floats(const bevmap_attend &a) { return (int64_t(a.batch) * a.queries * a.heads + 3) / 4 * 4; }
+
 }  // namespace
 }  // namespace bevmap
 
@@ -366,7 +381,7 @@ int64_t bevmap_attention_backward_bytes(const bevmap_attend &a) {
     const int64_t parts_q = split_q > 1 ? split_q * rows * a.dim : 0;
     const int64_t parts_k = split_k > 1 ? 2 * split_k * keys * a.dim : 0;
     // delta, then the parts of one gradient at a time
-    return (rows + (parts_q > parts_k ? parts_q : parts_k)) * int64_t(sizeof(float));
+    return (delta_floats(a) + (parts_q > parts_k ? parts_q : parts_k)) * int64_t(sizeof(float));
 }
 
 int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_out, const void *q, const void *k,
@@ -391,10 +406,11 @@ int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_ou
     g.dk = grad_k;
     g.dv = grad_v;
     g.delta = static_cast<float *>(workspace);
-    g.part = g.delta + int64_t(a.batch) * a.queries * a.heads;
+    g.part = g.delta + delta_floats(a);
     const int e = a.dtype == BEVPOOL_F32 ? 4 : 8;
-    const bool vec = attend_vec(a, q, k, v) && aligned_for(grad_out, 0, a.dtype, e) && aligned_for(out, 0, a.dtype, e) &&
-                     (!out_low || aligned_for(out_low, 0, a.dtype, e));
+    const auto ok = [&](const void *p) { return !p || aligned_for(p, 0, a.dtype, e); };
+    const bool vec = attend_vec(a, q, k, v) && ok(grad_out) && ok(out) && ok(out_low) && ok(grad_q) && ok(grad_k) &&
+                     ok(grad_v);
     switch (a.dtype) {
         case BEVPOOL_F32: return backward<BEVPOOL_F32>(g, vec, stream);
         case BEVPOOL_BF16: return backward<BEVPOOL_BF16>(g, vec, stream);
