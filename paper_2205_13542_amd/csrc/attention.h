@@ -414,6 +414,37 @@ struct Mask {
 
 inline int attend_ceil(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
+// Parts that `walk` keys or rows are split into for `whole` workgroups that own the
+// others, where `slots` run at once: the fewest rounds of workgroups by parts of the
+// work, against the writing and joining of parts. A part's are `join` / walk of all the
+// work: it moves 8 bytes of a row and channel (at 3 TB/s), where the forward takes
+// about 150 ns of a SIMD for 32 rows, 32 keys and 32 channels, which makes join 600.
+inline int pick_split(int64_t whole, int slots, int64_t walk, int64_t most, double join) {
+    if (whole <= 0 || walk <= 0) return 1;
+    const int64_t limit = 2 * int64_t(slots) / whole + 1;
+    const int end = int(most < limit ? most : limit);
+    const double part = join / double(walk) * double(whole) / slots;
+    int best = 1;
+    double least = double((whole + slots - 1) / slots);
+    for (int s = 2; s <= end; ++s) {
+        const double cost = double((whole * s + slots - 1) / slots) / s + s * part;
+        if (cost < least * 0.98) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+constexpr int kUnits = 256;     // compute units
+
+// Waves of a SIMD, which is workgroups of a compute unit, that the registers allow by
+// blocks of 32 channels; the kernels' launch bounds hold them to it.
+constexpr int waves_forward(int dt, int db) { return db == 1 ? 4 : db == 2 ? 3 : db == 3 || dt != BEVPOOL_F32 ? 2 : 1; }
+constexpr int waves_dq(int dt, int db) {
+    return dt == BEVPOOL_F32 ? (db == 1 ? 4 : db == 2 ? 2 : 1) : (db == 1 ? 4 : db == 2 ? 3 : 2);
+}
+constexpr int waves_dkv(int dt, int db) { return db == 1 ? 3 : db == 2 || (db == 3 && dt != BEVPOOL_F32) ? 2 : 1; }
+
 AttendArgs attend_fill(const bevmap_attend &a, const void *q, const void *k, const void *v, const int32_t *lengths,
                        const uint8_t *mask) {
     AttendArgs g{};

@@ -40,7 +40,7 @@ __device__ __forceinline__ float part_weight(float top, float sum, float most) {
 }
 
 template <int DT, int DB, bool VEC, int WR>
-__global__ __launch_bounds__(kAttendBlock, (DT == BEVPOOL_F32 && DB == 4 ? 1 : 2)) void k_attend(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT == BEVPOOL_F32) ? 1 : 2) : waves_forward(DT, DB))) void k_attend(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -301,13 +301,20 @@ __global__ __launch_bounds__(Join<SL>::kBlock) void k_attend_join(AttendArgs g) 
         meet[1][threadIdx.x] = sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) meet[2 + e][threadIdx.x] = o[e];
-        __syncthreads();
-        if (lane != 0) return;
-        for (int l = 1; l < SL; ++l) {
-            const int from = l * kColumns + column;
+        // halves meet halves
+#pragma unroll
+        for (int m = SL / 2; m > 0; m >>= 1) {
+            __syncthreads();
+            if (lane >= m) continue;
+            const int from = (lane + m) * kColumns + column;
             const float v[4] = {meet[2][from], meet[3][from], meet[4][from], meet[5][from]};
             add(meet[0][from], meet[1][from], v);
+            meet[0][threadIdx.x] = top;
+            meet[1][threadIdx.x] = sum;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) meet[2 + e][threadIdx.x] = o[e];
         }
+        if (lane != 0) return;
     }
     if (!here) return;
     const int bh = int(slot / g.rows), row = int(slot - int64_t(bh) * g.rows);
@@ -338,26 +345,21 @@ void launch_join(const AttendArgs &g, hipStream_t stream) {
                        dim3(Join<SL>::kBlock), 0, stream, g);
 }
 
-constexpr int kFill = 768;          // workgroups that fill the chip, three to a compute unit
-constexpr int kFillFew = 256;       // the same for few rows, where a workgroup's loads fill its unit's share
 constexpr int kFewRows = 32;        // rows of a key head that one wave holds
 
 int part_pitch(const bevmap_attend &a) { return (a.dim + 3) / 4 * 4; }
 
-// Rows, row tiles and parts of the keys, a rule on the sizes alone. Workgroups
-// that do not fill the chip split the keys, down to two tiles of keys a part.
-void partition(const bevmap_attend &a, AttendArgs *g, bool *few) {
+// Rows, row tiles and parts of the keys, a rule on the sizes alone, and on whether
+// samples have lengths: unequal ones need more workgroups to even out, and do less
+// work by the row. Few rows are bound by reading, two workgroups a compute unit.
+void partition(const bevmap_attend &a, bool lengths, AttendArgs *g, bool *few) {
     const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
     *few = rows <= kFewRows;
-    const int tile_rows = *few ? 32 : 128;
-    const int tile_keys = *few ? 128 : 64;
-    g->n_tiles = attend_ceil(rows, tile_rows);
-    const int64_t whole = int64_t(a.batch) * a.key_heads * g->n_tiles;
-    const int fill = *few ? kFillFew : kFill;
-    int64_t split = whole ? (fill + whole - 1) / whole : 1;
-    const int64_t most = attend_ceil(a.keys, 2 * tile_keys);
-    if (split > most) split = most;
-    g->n_split = split < 1 ? 1 : int(split);
+    g->n_tiles = attend_ceil(rows, *few ? 32 : 128);
+    int slots = kUnits * (*few ? 2 : waves_forward(a.dtype, (a.dim + 31) / 32));
+    if (lengths) slots += slots / 2;
+    g->n_split = pick_split(int64_t(a.batch) * a.key_heads * g->n_tiles, slots, a.keys,
+                            attend_ceil(a.keys, *few ? 256 : 128), lengths ? 1200.0 : 600.0);
 }
 
 template <int DT, int DB, bool VEC, int WR>
@@ -412,9 +414,12 @@ int64_t bevmap_attention_workspace_bytes(const bevmap_attend &a, bool backward) 
     if (backward) return bevmap_attention_backward_bytes(a);
     AttendArgs g{};
     bool few;
-    partition(a, &g, &few);
-    if (g.n_split <= 1) return 0;
-    return int64_t(g.n_split) * a.batch * a.queries * a.heads *
+    partition(a, false, &g, &few);
+    const int without = g.n_split;
+    partition(a, true, &g, &few);
+    const int parts = without > g.n_split ? without : g.n_split;
+    if (parts <= 1) return 0;
+    return int64_t(parts) * a.batch * a.queries * a.heads *
            (part_pitch(a) * int64_t(sizeof(float)) + int64_t(sizeof(float2)));
 }
 
@@ -427,7 +432,7 @@ int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k
     g.o_low = out_low;
     g.lse = lse;
     bool few;
-    partition(a, &g, &few);
+    partition(a, lengths != nullptr, &g, &few);
     // 16-byte aligned parts first, then their rows' statistics
     g.part_pitch = part_pitch(a);
     g.part = static_cast<float *>(workspace);

@@ -25,8 +25,6 @@ struct Walk {
     static constexpr int kSize = 32 * kBlocks;
     static constexpr int kBytes = kSize * S::kRowBytes;
     static constexpr int kLds = 4 * kBytes + 4 * kSize * int(sizeof(float));
-    // Waves of a SIMD: the sums of 128 channels (fp32: 96) do not leave room for two
-    static constexpr int kWaves = DB == 4 || (DT == BEVPOOL_F32 && DB == 3) ? 1 : 2;
 };
 
 template <int DT>
@@ -61,7 +59,7 @@ __device__ __forceinline__ void write_row(const f32x16 *acc, bool on, float mul,
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock, (Walk<DT, DB>::kWaves)) void k_attend_dq(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -165,7 +163,7 @@ __global__ __launch_bounds__(kAttendBlock, (Walk<DT, DB>::kWaves)) void k_attend
 }
 
 template <int DT, int DB, bool VEC>
-__global__ __launch_bounds__(kAttendBlock, (Walk<DT, DB>::kWaves)) void k_attend_dkv(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -299,21 +297,24 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_add(AttendArgs g) {
     to[(KEYS ? at.key(i) : at.row(i)) + ch] = T(sum);
 }
 
-constexpr int kFill = 512;          // workgroups that fill the chip, two to a compute unit
-
-// Workgroups that own `own` rows or keys, and parts of the `walk` others, of at least
-// kPartSize each.
-constexpr int kPartSize = 128;
-void partition(const bevmap_attend &a, int64_t own, int64_t walk, int32_t *n_tiles, int32_t *n_split) {
-    *n_tiles = attend_ceil(own, kOwn);
-    const int64_t whole = int64_t(a.batch) * a.key_heads * *n_tiles;
-    int64_t split = whole ? (kFill + whole - 1) / whole : 1;
-    const int64_t most = attend_ceil(walk, kPartSize);
-    if (split > most) split = most;
-    *n_split = split < 1 ? 1 : int32_t(split);
-}
-
 int64_t rows_of(const bevmap_attend &a) { return int64_t(a.queries) * (a.heads / a.key_heads); }
+
+// Workgroups that own kOwn rows (of q) or keys, and parts of the others, of at least
+// kPartSize each. More workgroups even out samples of unequal length where rows walk
+// the keys; where keys walk the rows, parts are as large as all keys, and not for that.
+constexpr int kPartSize = 128;
+void partition_q(const bevmap_attend &a, bool lengths, int32_t *n_tiles, int32_t *n_split) {
+    *n_tiles = attend_ceil(rows_of(a), kOwn);
+    int slots = kUnits * waves_dq(a.dtype, (a.dim + 31) / 32);
+    if (lengths) slots += slots / 2;
+    *n_split = pick_split(int64_t(a.batch) * a.key_heads * *n_tiles, slots, a.keys, attend_ceil(a.keys, kPartSize),
+                          lengths ? 600.0 : 300.0);         // twice the forward's work for the same parts
+}
+void partition_k(const bevmap_attend &a, int32_t *n_tiles, int32_t *n_split) {
+    *n_tiles = attend_ceil(a.keys, kOwn);
+    *n_split = pick_split(int64_t(a.batch) * a.key_heads * *n_tiles, kUnits * waves_dkv(a.dtype, (a.dim + 31) / 32),
+                          rows_of(a), attend_ceil(rows_of(a), kPartSize), 480.0);     // two parts, 2.5 times the work
+}
 
 template <int DT, int DB, bool VEC>
 int launch(AttendArgs g, hipStream_t stream) {
@@ -328,7 +329,7 @@ int launch(AttendArgs g, hipStream_t stream) {
     const int64_t bh = int64_t(g.a.batch) * g.a.key_heads;
     const auto blocks = [](int64_t n) { return uint32_t((n + kAttendBlock - 1) / kAttendBlock); };
     if (g.rows > 0) {
-        partition(g.a, g.rows, g.a.keys, &g.n_tiles, &g.n_split);
+        partition_q(g.a, g.lengths != nullptr, &g.n_tiles, &g.n_split);
         hipLaunchKernelGGL((k_attend_dq<DT, DB, VEC>), dim3(uint32_t(bh * g.n_split * g.n_tiles)),
                            dim3(kAttendBlock), lds, stream, g);
         BEVPOOL_HIP(hipGetLastError());
@@ -338,7 +339,7 @@ int launch(AttendArgs g, hipStream_t stream) {
         BEVPOOL_HIP(hipGetLastError());
     }
     if (g.a.keys > 0) {
-        partition(g.a, g.a.keys, g.rows, &g.n_tiles, &g.n_split);
+        partition_k(g.a, &g.n_tiles, &g.n_split);
         hipLaunchKernelGGL((k_attend_dkv<DT, DB, VEC>), dim3(uint32_t(bh * g.n_split * g.n_tiles)),
                            dim3(kAttendBlock), lds, stream, g);
         BEVPOOL_HIP(hipGetLastError());
@@ -374,9 +375,11 @@ int64_t delta_floats(const bevmap_attend &a) { return (int64_t(a.batch) * a.quer
 using namespace bevmap;
 
 int64_t bevmap_attention_backward_bytes(const bevmap_attend &a) {
-    int32_t tiles, split_q, split_k;
-    partition(a, rows_of(a), a.keys, &tiles, &split_q);
-    partition(a, a.keys, rows_of(a), &tiles, &split_k);
+    int32_t tiles, split_q, split_lengths, split_k;
+    partition_q(a, false, &tiles, &split_q);
+    partition_q(a, true, &tiles, &split_lengths);
+    if (split_lengths > split_q) split_q = split_lengths;
+    partition_k(a, &tiles, &split_k);
     const int64_t rows = int64_t(a.batch) * a.queries * a.heads, keys = int64_t(a.batch) * a.keys * a.key_heads;
     const int64_t parts_q = split_q > 1 ? split_q * rows * a.dim : 0;
     const int64_t parts_k = split_k > 1 ? 2 * split_k * keys * a.dim : 0;
@@ -391,9 +394,9 @@ int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_ou
     if (a.batch == 0) return BEVPOOL_OK;
     const int64_t bh = int64_t(a.batch) * a.key_heads, most = int64_t(1) << 23;
     int32_t tiles, split;
-    partition(a, rows_of(a), a.keys, &tiles, &split);
+    partition_q(a, lengths != nullptr, &tiles, &split);
     const bool wide = bh * tiles * split >= most;
-    partition(a, a.keys, rows_of(a), &tiles, &split);
+    partition_k(a, &tiles, &split);
     if (wide || bh * tiles * split >= most)
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d keys=%d heads=%d: too many tiles", a.batch,
                             a.queries, a.keys, a.heads);
