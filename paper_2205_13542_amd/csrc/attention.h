@@ -74,6 +74,30 @@ struct Mma {
             return a + b;
         }
     };
+    // What rows(p) left over: p - rows(p) to another 8 or 11 bits. rows of such a pair cut p off instead of rounding it.
+    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &low) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            Vec l;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float x = p[8 * s + e], y = p[8 * s + e + 1];
+                uint32_t both;
+                if constexpr (DT == BEVPOOL_BF16) {
+                    both = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
+                    l[e] = T(x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u));
+                    l[e + 1] = T(y - __uint_as_float(__float_as_uint(y) & 0xFFFF0000u));
+                } else {
+                    const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
+                    both = __builtin_bit_cast(uint32_t, cut);
+                    l[e] = T(x - float(cut[0]));
+                    l[e + 1] = T(y - float(cut[1]));
+                }
+                high.half[s][e / 2] = both;
+            }
+            low.half[s] = __builtin_bit_cast(u32x4, l);
+        }
+    }
     static __device__ __forceinline__ float pair_sum(uint32_t v, float c) {
         using Two = T __attribute__((ext_vector_type(2)));
         const Two ones = {T(1.0f), T(1.0f)};
@@ -122,6 +146,7 @@ struct Mma<BEVPOOL_F32> {
         return c;
     }
     static __device__ __forceinline__ Rows rows(const f32x16 &p) { return Rows{p}; }
+    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &) { high = Rows{p}; }
 };
 
 // Layout of a tile in LDS. 16-bit types: rows of CH chunks (a power of two), chunk c
@@ -165,9 +190,9 @@ struct Shape {
         return acc;
     }
 
-    // acc[d][32 channels from 32 d][32 columns] += tile^T x p over the 32 tile rows from row0.
-    static __device__ __forceinline__ void sums(const char *tile, int row0, const typename M::Rows &p,
-                                                f32x16 *acc) {
+    // acc[d][32 channels from 32 d][32 columns] += tile^T x p over the 32 tile rows from row0; with low, += tile^T x low.
+    static __device__ __forceinline__ void sums(const char *tile, int row0, const typename M::Rows &p, f32x16 *acc,
+                                                const typename M::Rows *low = nullptr) {
         const int lane = threadIdx.x & 63, half = lane >> 5;
         if constexpr (DT != BEVPOOL_F32) {
             using s4 = short __attribute__((ext_vector_type(4)));
@@ -191,6 +216,7 @@ struct Shape {
                         x[2 * e + 1] = r[1];
                     }
                     acc[d] = M::mul(x, p.half[s], acc[d]);
+                    if (low) acc[d] = M::mul(x, low->half[s], acc[d]);
                 }
             }
         } else {

@@ -146,7 +146,11 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[i] : 0.0f;
                 }
-                S::sums(k, 32 * n, M::rows(s), dq);
+                // in two pieces of the type: a row's ds sum to 0, so that their rounding weighs more in dq than that of
+                // dq itself, and together they were 1.55 times as far off as dq in fp32 rounded once
+                typename M::Rows high, low;
+                M::rows_of_two(s, high, low);
+                S::sums(k, 32 * n, high, dq, DT == BEVPOOL_F32 ? nullptr : &low);
             }
             if (t + 1 < t1) {
                 char *to = lds + (1 - buffer) * 2 * W::kBytes;
@@ -259,7 +263,9 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
                     }
                 }
                 S::sums(d, 32 * n, M::rows(p), dv);
-                S::sums(q, 32 * n, M::rows(ds), dk);
+                typename M::Rows high, low;         // as in k_attend_dq
+                M::rows_of_two(ds, high, low);
+                S::sums(q, 32 * n, high, dk, DT == BEVPOOL_F32 ? nullptr : &low);
             }
             if (t + 1 < t1) put(lds + (1 - buffer) * 2 * W::kBytes, stats + (1 - buffer) * 2 * W::kSize);
         }
