@@ -461,6 +461,132 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
     }
 }
 
+// Small maps: a launch costs the host about 3.3 us, more than the work, so a group
+// that one workgroup holds in registers takes one kernel in each direction instead of three.
+constexpr int kSmallBlock = 1024;
+constexpr int kSmallRows = 8;       // values of a thread (16 spill in the backward)
+constexpr int kSmallFrames = 4;     // of the backward, whose workgroup takes a group of all frames in turn
+
+// Sum over the workgroup; red: kSmallBlock / 64 floats, free on entry and exit.
+__device__ __forceinline__ float block_sum(float v, float *red) {
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = (threadIdx.x & 63) < kSmallBlock / 64 ? red[threadIdx.x & 63] : 0.0f;
+    v = wave_sum(v);
+    __syncthreads();
+    return v;
+}
+
+// Thread -> (row lane, channel of the group); row lanes past the last are idle.
+struct SmallPlace {
+    int lanes, lane, ch;
+};
+__device__ __forceinline__ SmallPlace small_place(int per) {
+    SmallPlace p;
+    p.lanes = kSmallBlock / per;
+    p.lane = threadIdx.x / per;
+    p.ch = threadIdx.x - p.lane * per;
+    return p;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kSmallBlock) void k_norm_small(NormArgs a) {
+    using T = typename Num<DT>::T;
+    __shared__ float red[kSmallBlock / 64];
+    const int g = blockIdx.x, b = blockIdx.y, n = a.rows * a.per;
+    const SmallPlace p = small_place(a.per);
+    const int ch = g * a.per + p.ch;
+    const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx + ch;
+    auto in = [&](int k) { return p.lane < p.lanes && p.lane + k * p.lanes < a.rows; };
+    float v[kSmallRows], sum = 0.0f, m2 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSmallRows; ++k) v[k] = in(k) ? float(x[int64_t(p.lane + k * p.lanes) * a.ldx]) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSmallRows; ++k) sum += v[k];
+    const float mean = block_sum(sum, red) / float(n);
+#pragma unroll
+    for (int k = 0; k < kSmallRows; ++k) {
+        const float d = in(k) ? v[k] - mean : 0.0f;
+        m2 = fmaf(d, d, m2);
+    }
+    const float rstd = 1.0f / sqrtf(block_sum(m2, red) / float(n) + a.eps);
+    if (threadIdx.x == 0) {
+        a.mean[int64_t(b) * a.G + g] = mean;
+        a.rstd[int64_t(b) * a.G + g] = rstd;
+    }
+    if (p.lane >= p.lanes) return;
+    const float mul = rstd * weight_at(a.weight, ch, a.w_dtype, 1.0f), add = weight_at(a.bias, ch, a.w_dtype, 0.0f);
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < kSmallRows; ++k) {
+            if (!in(k)) continue;
+            const float y = activate<act.value>(fmaf(v[k] - mean, mul, add));
+            store_any<1>(a.y, (int64_t(b) * a.rows + p.lane + k * p.lanes) * a.C + ch, a.y_dtype, &y);
+        }
+    });
+}
+
+template <int DT>
+__global__ __launch_bounds__(kSmallBlock) void k_norm_small_grad(NormArgs a) {
+    using T = typename Num<DT>::T;
+    __shared__ float red[kSmallBlock / 64], meet[2][kSmallBlock];
+    const int g = blockIdx.x;
+    const SmallPlace p = small_place(a.per);
+    const int ch = min(g * a.per + p.ch, a.C - 1);
+    const float w = weight_at(a.weight, ch, a.w_dtype, 1.0f), add = weight_at(a.bias, ch, a.w_dtype, 0.0f);
+    const float inv = 1.0f / (float(a.rows) * float(a.per));
+    float all = 0.0f, all_dot = 0.0f;              // of this thread's channel, over the frames
+    for (int b = 0; b < a.batch; ++b) {
+        const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx + ch;
+        const int64_t to = int64_t(b) * a.rows * a.C + ch;
+        const float mean = a.mean[int64_t(b) * a.G + g], rstd = a.rstd[int64_t(b) * a.G + g];
+        auto in = [&](int k) { return p.lane < p.lanes && p.lane + k * p.lanes < a.rows; };
+        float xh[kSmallRows], dz[kSmallRows], sum = 0.0f, dot = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSmallRows; ++k) {
+            const int r = p.lane + k * p.lanes;
+            xh[k] = mean;
+            dz[k] = 0.0f;
+            if (in(k)) {
+                xh[k] = float(x[int64_t(r) * a.ldx]);
+                load_any<1>(a.dy, to + int64_t(r) * a.C, a.y_dtype, &dz[k]);
+            }
+        }
+        with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int k = 0; k < kSmallRows; ++k) {
+                if (!in(k)) continue;
+                xh[k] = (xh[k] - mean) * rstd;
+                dz[k] *= slope<act.value>(fmaf(xh[k], w, add));
+                sum += dz[k];
+                dot = fmaf(dz[k], xh[k], dot);
+            }
+        });
+        all += sum;
+        all_dot += dot;
+        const float m1 = block_sum(sum * w, red) * inv, m2 = block_sum(dot * w, red) * inv;
+        T *dx = static_cast<T *>(a.dx) + to;
+#pragma unroll
+        for (int k = 0; k < kSmallRows; ++k)
+            if (in(k)) dx[int64_t(p.lane + k * p.lanes) * a.C] = T(rstd * (dz[k] * w - m1 - xh[k] * m2));
+    }
+    // the row lanes' upper halves go to the lower ones
+    meet[0][threadIdx.x] = all;
+    meet[1][threadIdx.x] = all_dot;
+    for (int n = p.lanes; n > 1; n = (n + 1) / 2) {
+        const int half = (n + 1) / 2, from = threadIdx.x + half * a.per;
+        __syncthreads();
+        if (p.lane < n - half) {
+            meet[0][threadIdx.x] = all += meet[0][from];
+            meet[1][threadIdx.x] = all_dot += meet[1][from];
+        }
+    }
+    if (p.lane != 0) return;
+    if (a.dbias) store_any<1>(a.dbias, ch, a.w_dtype, &all);
+    if (a.dweight) store_any<1>(a.dweight, ch, a.w_dtype, &all_dot);
+}
+
 constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
 constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
 constexpr int kMinRows = 16;        // rows of a chunk at least
@@ -472,6 +598,12 @@ static_assert(kSumGrid <= 64 * kJoin, "k_norm_join holds a group's parts in regi
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
 int64_t elements(const bevmap_norm &n) { return int64_t(n.batch) * n.pixels * n.channels; }
+
+bool small(const bevmap_norm &n, bool backward) {
+    const int per = n.channels / n.groups;
+    return per <= kSmallBlock && ceil_div(n.pixels, kSmallBlock / per) <= kSmallRows &&
+           (!backward || n.batch <= kSmallFrames);
+}
 
 void split(const bevmap_norm &n, NormArgs *a) {
     a->chunk = ceil_div(n.pixels, ceil_div(kSumGrid, n.batch));
@@ -562,6 +694,13 @@ int backward(const NormArgs &a, hipStream_t stream) {
 template <int DT>
 int dispatch(const NormArgs &a, int v, bool back, hipStream_t stream) {
     switch (v) {
+        case 0:
+            if (back)
+                hipLaunchKernelGGL((k_norm_small_grad<DT>), dim3(a.G), dim3(kSmallBlock), 0, stream, a);
+            else
+                hipLaunchKernelGGL((k_norm_small<DT>), dim3(a.G, a.batch), dim3(kSmallBlock), 0, stream, a);
+            BEVPOOL_HIP(hipGetLastError());
+            return BEVPOOL_OK;
         case 8:
             if constexpr (DT != BEVPOOL_F32) return back ? backward<DT, 8>(a, stream) : forward<DT, 8>(a, stream);
         case 4: return back ? backward<DT, 4>(a, stream) : forward<DT, 4>(a, stream);
@@ -570,6 +709,7 @@ int dispatch(const NormArgs &a, int v, bool back, hipStream_t stream) {
     }
 }
 
+// v: elements of an access; 0 for the kernels of small maps.
 int dispatch(int dtype, const NormArgs &a, int v, bool back, hipStream_t stream) {
     switch (dtype) {
         case BEVPOOL_F32: return dispatch<BEVPOOL_F32>(a, v, back, stream);
@@ -591,7 +731,7 @@ __global__ void k_zero_weights(void *a, void *b, int n, int dtype) {
 using namespace bevmap;
 
 int64_t bevmap_norm_workspace_bytes(const bevmap_norm &n, bool backward) {
-    if (n.batch == 0 || n.pixels == 0) return 0;
+    if (n.batch == 0 || n.pixels == 0 || small(n, backward)) return 0;
     NormArgs a{};
     split(n, &a);
     const int64_t chunks = int64_t(n.batch) * a.n_chunks;
@@ -609,7 +749,7 @@ int bevmap_launch_norm(const bevmap_norm &n, const void *x, const void *weight, 
     a.stream = elements(n) * (dtype_bytes(n.x_dtype) + dtype_bytes(n.y_dtype)) > kCacheBytes;
     a.mean = mean;
     a.rstd = rstd;
-    return dispatch(n.x_dtype, a, vector_of(n, x, y, nullptr), false, stream);
+    return dispatch(n.x_dtype, a, small(n, false) ? 0 : vector_of(n, x, y, nullptr), false, stream);
 }
 
 int bevmap_launch_norm_backward(const bevmap_norm &n, const void *grad_y, const void *x, const void *weight,
@@ -631,5 +771,5 @@ int bevmap_launch_norm_backward(const bevmap_norm &n, const void *grad_y, const 
     a.dbias = grad_bias;
     a.mean = const_cast<float *>(mean);
     a.rstd = const_cast<float *>(rstd);
-    return dispatch(n.x_dtype, a, vector_of(n, x, grad_y, grad_x), true, stream);
+    return dispatch(n.x_dtype, a, small(n, true) ? 0 : vector_of(n, x, grad_y, grad_x), true, stream);
 }

@@ -75,6 +75,10 @@ def _call(function, index, *args):
         return function(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
+def _empty_like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -109,10 +113,10 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
                                     _code(out_dtype),
                                     _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
     size = _map_binding.bevmap_group_norm_workspace(norm, False)
-    y = torch.empty(shape, dtype=out_dtype, device=x.device)
+    y = x.new_empty(shape, dtype=out_dtype)
     stats = B * groups * 4
     start = (2 * stats + 15) // 16 * 16       # of the workspace behind the statistics
-    space = torch.empty(start + size, dtype=torch.uint8, device=x.device)
+    space = x.new_empty(start + size, dtype=torch.uint8)
     mean = space.data_ptr()
     _call(_map_binding.bevmap_group_norm, index, norm, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean,
           mean + stats, mean + start, size)
@@ -122,14 +126,13 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
 def _norm_backward(norm, space, dy, x, weight, bias, want_weight, want_bias):
     dy = dy.contiguous()
     size = _map_binding.bevmap_group_norm_workspace(norm, True)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = _empty_like(x)
     dw = torch.empty_like(weight) if want_weight else None
     db = torch.empty_like(bias) if want_bias else None
-    temp = torch.empty(size, dtype=torch.uint8, device=x.device)
+    temp = space.new_empty(size) if size else None
     mean = space.data_ptr()
     _call(_map_binding.bevmap_group_norm_backward, x.get_device(), norm, dy.data_ptr(), x.data_ptr(), _ptr(weight),
-          _ptr(bias), mean, mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw), _ptr(db), temp.data_ptr(),
-          size)
+          _ptr(bias), mean, mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw), _ptr(db), _ptr(temp), size)
     return dx, dw, db
 
 
@@ -166,10 +169,10 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
     attend = _map_binding.bevmap_attend(B, N, M, H, K, D, _code(dtype), scale, qs[0], qs[1], qs[2], ks[0], ks[1],
                                         ks[2], vs[0], vs[1], vs[2], mask_batch)
     size = _map_binding.bevmap_attention_workspace(attend, False)
-    out = torch.empty(shape, dtype=dtype, device=q.device)
-    low = torch.empty(shape, dtype=dtype, device=q.device) if train and dtype != torch.float32 else None
-    lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device) if train else None
-    space = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+    out = _empty_like(q)
+    low = _empty_like(q) if train and dtype != torch.float32 else None
+    lse = q.new_empty((B, H, N), dtype=torch.float32) if train else None
+    space = q.new_empty(size, dtype=torch.uint8) if size else None
     _call(_map_binding.bevmap_attention, index, attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lengths),
           _ptr(key_mask), out.data_ptr(), _ptr(low), _ptr(lse), _ptr(space), size)
     return out, low, lse, attend
@@ -178,11 +181,8 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
 def _attend_backward(attend, dout, q, k, v, key_lengths, key_mask, out, low, lse):
     dout = dout.contiguous()
     size = _map_binding.bevmap_attention_workspace(attend, True)
-    dtype, device = q.dtype, q.device
-    dq = torch.empty(q.shape, dtype=dtype, device=device)
-    dk = torch.empty(k.shape, dtype=dtype, device=device)
-    dv = torch.empty(v.shape, dtype=dtype, device=device)
-    temp = torch.empty(size, dtype=torch.uint8, device=device)
+    dq, dk, dv = _empty_like(q), _empty_like(k), _empty_like(v)
+    temp = q.new_empty(size, dtype=torch.uint8)
     _call(_map_binding.bevmap_attention_backward, q.get_device(), attend, dout.data_ptr(), q.data_ptr(),
           k.data_ptr(), v.data_ptr(), _ptr(key_lengths), _ptr(key_mask), out.data_ptr(), _ptr(low), lse.data_ptr(),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), temp.data_ptr(), size)
@@ -199,7 +199,7 @@ def _dropout(x, threshold, seed, offset, residual):
             _refuse("residual must have the shape and dtype of x", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
     if stride is None or residual_stride is None:
         _refuse("rows of x and residual must be evenly spaced, their elements adjacent")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _empty_like(x)
     columns = x.shape[-1] if x.dim() else 1
     rows = x.numel() // columns if columns else 0
     _call(_map_binding.bevmap_dropout, index, x.data_ptr(), stride, _ptr(residual), residual_stride, y.data_ptr(),

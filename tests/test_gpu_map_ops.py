@@ -118,6 +118,14 @@ NORM_CASES = [
     ((1, 40, 40, 16), 16, 0, "f32", "f32", "f32", "gelu", 1000.0),    # mean far above the deviation
     ((17, 11, 3, 32), 4, 0, "bf16", "f32", "f32", "gelu", -3.0),
     ((1, 50000, 4), 2, 1, "f32", "f32", "f32", "silu", 0.0),
+    # both sides of the one-workgroup form: rows of a lane, channels of a group, frames of the backward
+    ((2, 2728, 9), 3, 0, "f32", "f32", "f32", "gelu", 0.0),
+    ((2, 2729, 9), 3, 0, "bf16", "bf16", "f32", "silu", 0.0),
+    ((4, 8, 1024), 1, 0, "f16", "f16", "f32", "silu", 0.0),
+    ((4, 9, 1024), 1, 0, "f32", "f32", "f32", "relu", 0.0),
+    ((5, 20, 48), 6, 0, "f32", "f32", "f32", "silu", 0.0),
+    ((1, 3, 2050), 2, 0, "f32", "bf16", "bf16", "gelu", 0.0),
+    ((3, 300, 80), 8, 8, "f32", "bf16", "f32", "silu", 0.2),
 ]
 
 
