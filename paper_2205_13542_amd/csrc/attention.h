@@ -52,9 +52,19 @@ __device__ __forceinline__ f32x16 zeros() {
     return z;
 }
 
-// A chunk is 16 bytes: 8 elements of a 16-bit type, one step of K = 16, or 4 of
-// fp32, four steps of K = 2. In a row's chunks 2 j and 2 j + 1 the two half waves
-// hold the contracted elements of step j.
+// fp32 goes through the bf16 matrix cores: x is the sum of three bf16 pieces, exactly
+// (8 + 8 + 8 of its 24 bits), and six of the nine products of pieces, all but those
+// below 2^-23 of the whole, make a product of fp32 accuracy in 6 / 16 of the time that
+// the fp32 matrix instructions take (32x32x16 in 32 cycles, 32x32x2 in 64).
+//
+// A chunk is 16 bytes of a row in memory: 8 elements of a 16-bit type, 4 of fp32. In
+// step s of a product, K = 16, the two half waves hold elements 16 s + 8 half ..
+// Two fp32 numbers cut off to bf16, and what is left of one.
+__device__ __forceinline__ uint32_t cut_pair(float x, float y) {
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
+}
+__device__ __forceinline__ float left_of(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+
 template <int DT>
 struct Mma {
     using T = typename Num<DT>::T;
@@ -84,9 +94,9 @@ struct Mma {
                 const float x = p[8 * s + e], y = p[8 * s + e + 1];
                 uint32_t both;
                 if constexpr (DT == BEVPOOL_BF16) {
-                    both = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
-                    l[e] = T(x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u));
-                    l[e + 1] = T(y - __uint_as_float(__float_as_uint(y) & 0xFFFF0000u));
+                    both = cut_pair(x, y);
+                    l[e] = T(left_of(x));
+                    l[e + 1] = T(left_of(y));
                 } else {
                     const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
                     both = __builtin_bit_cast(uint32_t, cut);
@@ -126,35 +136,68 @@ struct Mma {
         return r;
     }
 };
+// The three pieces of a pair of fp32 numbers.
+__device__ __forceinline__ void three_pieces(float x, float y, uint32_t *piece) {
+    using Two = __bf16 __attribute__((ext_vector_type(2)));
+    piece[0] = cut_pair(x, y);
+    x = left_of(x);
+    y = left_of(y);
+    piece[1] = cut_pair(x, y);
+    const Two last = {__bf16(left_of(x)), __bf16(left_of(y))};
+    piece[2] = __builtin_bit_cast(uint32_t, last);
+}
+// The same for numbers that may be infinite: an infinity is its own first piece.
+__device__ __forceinline__ float left_of_any(float x) { return __builtin_isinf(x) ? 0.0f : left_of(x); }
+__device__ __forceinline__ void three_pieces_any(float x, float y, uint32_t *piece) {
+    const uint32_t first = cut_pair(x, y);
+    // a NaN may be cut off to an infinity; what is left of it is a NaN
+    three_pieces(left_of_any(x), left_of_any(y), piece);
+    piece[2] = piece[1];
+    piece[1] = piece[0];
+    piece[0] = first;
+}
+
 template <>
 struct Mma<BEVPOOL_F32> {
     using T = float;
     static constexpr int kElems = 4;
     struct Rows {
-        f32x16 p;
-        __device__ __forceinline__ float sum() const {
-            float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 16; ++i) a[i & 3] += p[i];
-            return (a[0] + a[1]) + (a[2] + a[3]);
-        }
+        u32x4 piece[3][2];
+        float total;
+        __device__ __forceinline__ float sum() const { return total; }
     };
-    static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-        return c;
+    using Piece = Mma<BEVPOOL_BF16>;
+    // c += a b, the least products first; a[i], b[i]: the pieces of a step's operands
+    static __device__ __forceinline__ f32x16 mul(const u32x4 *a, u32x4 b0, u32x4 b1, u32x4 b2, f32x16 c) {
+        c = Piece::mul(a[2], b0, c);
+        c = Piece::mul(a[0], b2, c);
+        c = Piece::mul(a[1], b1, c);
+        c = Piece::mul(a[1], b0, c);
+        c = Piece::mul(a[0], b1, c);
+        return Piece::mul(a[0], b0, c);
     }
-    static __device__ __forceinline__ Rows rows(const f32x16 &p) { return Rows{p}; }
-    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &) { high = Rows{p}; }
+    static __device__ __forceinline__ Rows rows(const f32x16 &p) {
+        Rows r;
+        float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[i & 3] += p[i];
+        r.total = (a[0] + a[1]) + (a[2] + a[3]);
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            uint32_t piece[3];
+            three_pieces(p[i], p[i + 1], piece);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) r.piece[k][i >> 3][(i & 7) >> 1] = piece[k];
+        }
+        return r;
+    }
+    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &) { high = rows(p); }
 };
 
-// Layout of a tile in LDS. 16-bit types: rows of CH chunks (a power of two), chunk c
-// of row r at chunk c ^ turn(r); sixteen consecutive rows read at one chunk, and four
-// consecutive rows read along 64 bytes, then fall into distinct banks. fp32, whose
-// second operand is read by the element: rows 16 bytes further apart than they are
-// long, so that one address and constants reach a whole tile (turned chunks took an
-// address each and spilled; 128 channels forward: 6.6 ms, now 2.4 for 537 GFLOP).
+// Layout of a tile in LDS: rows of CH chunks (a power of two; of fp32 one such row
+// for each piece, side by side), chunk c of row r at chunk c ^ turn(r). Sixteen
+// consecutive rows read at one chunk, and four consecutive rows read along 64 bytes,
+// then fall into distinct banks.
 template <int CH>
 __device__ __forceinline__ int turn(int row) {
     if constexpr (CH <= 4) return (row >> 2) & 3;
@@ -163,77 +206,6 @@ __device__ __forceinline__ int turn(int row) {
 }
 
 constexpr int pow2_chunks(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : 16; }
-
-// DB blocks of 32 channels of type DT.
-template <int DT, int DB>
-struct Shape {
-    using M = Mma<DT>;
-    using T = typename M::T;
-    static constexpr int kUsed = DB * 32 / M::kElems;        // chunks of a row
-    static constexpr int kRowBytes = DT == BEVPOOL_F32 ? kUsed * 16 + 16 : pow2_chunks(kUsed) * 16;     // in LDS
-    static constexpr int kSteps = kUsed / 2;
-
-    // Bytes of chunk c of a row in LDS.
-    static __device__ __forceinline__ int chunk_at(int row, int c) {
-        if constexpr (DT == BEVPOOL_F32) return row * kRowBytes + c * 16;
-        return row * kRowBytes + (c ^ turn<kRowBytes / 16>(row)) * 16;
-    }
-
-    // acc[32 tile rows from row0][32 columns] += tile x y^T over the channels.
-    static __device__ __forceinline__ f32x16 scores(const char *tile, int row0, const u32x4 *y, f32x16 acc) {
-        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + chunk_at(row, 2 * s + half));
-            acc = M::mul(x, y[s], acc);
-        }
-        return acc;
-    }
-
-    // acc[d][32 channels from 32 d][32 columns] += tile^T x p over the 32 tile rows from row0; with low, += tile^T x low.
-    static __device__ __forceinline__ void sums(const char *tile, int row0, const typename M::Rows &p, f32x16 *acc,
-                                                const typename M::Rows *low = nullptr) {
-        const int lane = threadIdx.x & 63, half = lane >> 5;
-        if constexpr (DT != BEVPOOL_F32) {
-            using s4 = short __attribute__((ext_vector_type(4)));
-            using lds4 = __attribute__((address_space(3))) s4;
-            // ds_read_b64_tr_b16: in 16 lanes, lane t names 4 elements of row t / 4 at columns 4 (t % 4) and
-            // gets column t of the four rows
-            const int t = lane & 15, sub = (lane >> 4) & 1;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    u32x4 x;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int row = row0 + 16 * s + 8 * e + 4 * half + (t >> 2);
-                        const int col = 4 * d + 2 * sub + ((t & 3) >> 1);       // in chunks
-                        const char *at = tile + chunk_at(row, col) + (t & 1) * 8;
-                        const u32x2 r = __builtin_bit_cast(
-                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at)));
-                        x[2 * e] = r[0];
-                        x[2 * e + 1] = r[1];
-                    }
-                    acc[d] = M::mul(x, p.half[s], acc[d]);
-                    if (low) acc[d] = M::mul(x, low->half[s], acc[d]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int row = row0 + 8 * (i >> 2) + 4 * half + (i & 3);
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int c = 32 * d + (lane & 31);
-                    const float x =
-                        *reinterpret_cast<const float *>(tile + chunk_at(row, c >> 2) + (c & 3) * 4);
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p.p[i], acc[d], 0, 0, 0);
-                }
-            }
-        }
-    }
-};
 
 // One chunk of a row: elements c * kElems.. of dim, zeros past dim. VEC: rows
 // start on 16-byte boundaries and dim is a multiple of the chunk.
@@ -252,6 +224,115 @@ __device__ __forceinline__ u32x4 load_chunk(const typename Num<DT>::T *row, int 
     }
     return out;
 }
+
+// DB blocks of 32 channels of type DT.
+template <int DT, int DB>
+struct Shape {
+    using M = Mma<DT>;
+    using T = typename M::T;
+    static constexpr int kPieces = DT == BEVPOOL_F32 ? 3 : 1;
+    static constexpr int kUsed = DB * 32 / M::kElems;        // chunks of a row in memory
+    static constexpr int kChunks = pow2_chunks(DB * 4);      // of a row's piece in LDS
+    static constexpr int kPieceBytes = kChunks * 16;
+    static constexpr int kRowBytes = kPieces * kPieceBytes;
+    static constexpr int kSteps = 2 * DB;
+    static constexpr int kOperand = kPieces * kSteps;        // registers of a row as an operand: [piece][step]
+
+    // Bytes of 8 elements from 8 c of a row's first piece in LDS.
+    static __device__ __forceinline__ int chunk_at(int row, int c) {
+        return row * kRowBytes + (c ^ turn<kChunks>(row)) * 16;
+    }
+    // Chunk c of a row, as it was in memory, to LDS.
+    static __device__ __forceinline__ void put(char *tile, int row, int c, u32x4 v) {
+        if constexpr (DT != BEVPOOL_F32) {
+            *reinterpret_cast<u32x4 *>(tile + chunk_at(row, c)) = v;
+        } else {
+            uint32_t piece[2][3];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                three_pieces_any(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), piece[i]);
+            char *to = tile + chunk_at(row, c >> 1) + (c & 1) * 8;
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<u32x2 *>(to + k * kPieceBytes) = u32x2{piece[0][k], piece[1][k]};
+        }
+    }
+    // A row in memory as an operand of scores().
+    template <bool VEC>
+    static __device__ __forceinline__ void operand(const T *row, int half, int dim, u32x4 *y) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if constexpr (DT != BEVPOOL_F32) {
+                y[s] = load_chunk<DT, VEC>(row, 2 * s + half, dim);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 v = load_chunk<DT, VEC>(row, 4 * s + 2 * half + i, dim);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t piece[3];
+                        three_pieces_any(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), piece);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) y[k * kSteps + s][2 * i + j] = piece[k];
+                    }
+                }
+            }
+        }
+    }
+
+    // acc[32 tile rows from row0][32 columns] += tile x y^T over the channels.
+    static __device__ __forceinline__ f32x16 scores(const char *tile, int row0, const u32x4 *y, f32x16 acc) {
+        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const char *at = tile + chunk_at(row, 2 * s + half);
+            u32x4 x[kPieces];
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) x[k] = *reinterpret_cast<const u32x4 *>(at + k * kPieceBytes);
+            if constexpr (DT != BEVPOOL_F32)
+                acc = M::mul(x[0], y[s], acc);
+            else
+                acc = M::mul(x, y[s], y[kSteps + s], y[2 * kSteps + s], acc);
+        }
+        return acc;
+    }
+
+    // acc[d][32 channels from 32 d][32 columns] += tile^T x p over the 32 tile rows from row0; with low, += tile^T x low.
+    static __device__ __forceinline__ void sums(const char *tile, int row0, const typename M::Rows &p, f32x16 *acc,
+                                                const typename M::Rows *low = nullptr) {
+        using s4 = short __attribute__((ext_vector_type(4)));
+        using lds4 = __attribute__((address_space(3))) s4;
+        // ds_read_b64_tr_b16: in 16 lanes, lane t names 4 elements of row t / 4 at columns 4 (t % 4) and
+        // gets column t of the four rows
+        const int lane = threadIdx.x & 63, half = lane >> 5, t = lane & 15, sub = (lane >> 4) & 1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                u32x4 x[kPieces];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = row0 + 16 * s + 8 * e + 4 * half + (t >> 2);
+                    const int col = 4 * d + 2 * sub + ((t & 3) >> 1);       // in chunks
+                    const char *at = tile + chunk_at(row, col) + (t & 1) * 8;
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) {
+                        const u32x2 r = __builtin_bit_cast(
+                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + k * kPieceBytes)));
+                        x[k][2 * e] = r[0];
+                        x[k][2 * e + 1] = r[1];
+                    }
+                }
+                if constexpr (DT != BEVPOOL_F32) {
+                    acc[d] = M::mul(x[0], p.half[s], acc[d]);
+                    if (low) acc[d] = M::mul(x[0], low->half[s], acc[d]);
+                } else {
+                    acc[d] = M::mul(x, p.piece[0][s], p.piece[1][s], p.piece[2][s], acc[d]);
+                }
+            }
+        }
+    }
+};
 
 // Four consecutive channels of a row from channel ch, of dim; VEC: they are
 // aligned and dim is a multiple of four.
@@ -398,7 +479,7 @@ struct Stage {
         for (int i = 0; i < kLoads; ++i) {
             const int r = row(i);
             if (!kEven && r >= ROWS) break;
-            *reinterpret_cast<u32x4 *>(tile + S::chunk_at(r, chunk(i))) = reg[i];
+            S::put(tile, r, chunk(i), reg[i]);
         }
     }
 };
@@ -444,9 +525,11 @@ inline int attend_ceil(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 // others, where `slots` run at once: the fewest rounds of workgroups by parts of the
 // work, against the writing and joining of parts. A part's are `join` / walk of all the
 // work: it moves 8 bytes of a row and channel (at 3 TB/s), where the forward takes
-// about 150 ns of a SIMD for 32 rows, 32 keys and 32 channels, which makes join 600.
-inline int pick_split(int64_t whole, int slots, int64_t walk, int64_t most, double join) {
+// about 150 ns of a SIMD for 32 rows, 32 keys and 32 channels, which makes join 600;
+// fp32 takes four times as long.
+inline int pick_split(int64_t whole, int slots, int64_t walk, int64_t most, double join, int dtype) {
     if (whole <= 0 || walk <= 0) return 1;
+    if (dtype == BEVPOOL_F32) join *= 0.25;
     const int64_t limit = 2 * int64_t(slots) / whole + 1;
     const int end = int(most < limit ? most : limit);
     const double part = join / double(walk) * double(whole) / slots;
@@ -467,9 +550,9 @@ constexpr int kUnits = 256;     // compute units
 // blocks of 32 channels; the kernels' launch bounds hold them to it.
 constexpr int waves_forward(int dt, int db) { return db == 1 ? 4 : db == 2 ? 3 : db == 3 || dt != BEVPOOL_F32 ? 2 : 1; }
 constexpr int waves_dq(int dt, int db) {
-    return dt == BEVPOOL_F32 ? (db == 1 ? 4 : db == 2 ? 2 : 1) : (db == 1 ? 4 : db == 2 ? 3 : 2);
+    return dt == BEVPOOL_F32 ? (db == 1 ? 3 : db == 2 ? 2 : 1) : (db == 1 ? 4 : db == 2 ? 3 : 2);
 }
-constexpr int waves_dkv(int dt, int db) { return db == 1 ? 3 : db == 2 || (db == 3 && dt != BEVPOOL_F32) ? 2 : 1; }
+constexpr int waves_dkv(int dt, int db) { return dt == BEVPOOL_F32 ? (db == 1 ? 2 : 1) : db == 1 ? 3 : db <= 3 ? 2 : 1; }
 
 AttendArgs attend_fill(const bevmap_attend &a, const void *q, const void *k, const void *v, const int32_t *lengths,
                        const uint8_t *mask) {

@@ -57,18 +57,13 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
     const int row = tile * W::kRows + (WR == 1 ? 0 : 32 * wave) + (lane & 31);
     const int dim = g.a.dim;
 
-    u32x4 q[S::kSteps];
+    u32x4 q[S::kOperand];
 #pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) q[s] = u32x4{0, 0, 0, 0};
-    if (row < g.rows) {
-        const T *p = at.q(row);
-#pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) q[s] = load_chunk<DT, VEC>(p, 2 * s + half, dim);
-    }
+    for (int s = 0; s < S::kOperand; ++s) q[s] = u32x4{0, 0, 0, 0};
+    if (row < g.rows) S::template operand<VEC>(at.q(row), half, dim, q);
     if (g.sign != 1.0f) {
-        const uint32_t flip = DT == BEVPOOL_F32 ? 0x80000000u : 0x80008000u;
 #pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) q[s] = g.sign == 0.0f ? u32x4{0, 0, 0, 0} : q[s] ^ flip;
+        for (int s = 0; s < S::kOperand; ++s) q[s] = g.sign == 0.0f ? u32x4{0, 0, 0, 0} : q[s] ^ 0x80008000u;
     }
 
     // this part's tiles of keys
@@ -354,12 +349,13 @@ int part_pitch(const bevmap_attend &a) { return (a.dim + 3) / 4 * 4; }
 // work by the row. Few rows are bound by reading, two workgroups a compute unit.
 void partition(const bevmap_attend &a, bool lengths, AttendArgs *g, bool *few) {
     const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
-    *few = rows <= kFewRows;
+    // (fp32 tiles of 128 keys and more than 64 channels do not fit LDS)
+    *few = rows <= kFewRows && (a.dtype != BEVPOOL_F32 || a.dim <= 64);
     g->n_tiles = attend_ceil(rows, *few ? 32 : 128);
     int slots = kUnits * (*few ? 2 : waves_forward(a.dtype, (a.dim + 31) / 32));
     if (lengths) slots += slots / 2;
     g->n_split = pick_split(int64_t(a.batch) * a.key_heads * g->n_tiles, slots, a.keys,
-                            attend_ceil(a.keys, *few ? 256 : 128), lengths ? 1200.0 : 600.0);
+                            attend_ceil(a.keys, *few ? 256 : 128), lengths ? 1200.0 : 600.0, a.dtype);
 }
 
 template <int DT, int DB, bool VEC, int WR>
@@ -380,7 +376,8 @@ int launch(const AttendArgs &g, hipStream_t stream) {
 
 template <int DT, int DB>
 int launch(const AttendArgs &g, bool vec, bool few, hipStream_t stream) {
-    if (few) return vec ? launch<DT, DB, true, 1>(g, stream) : launch<DT, DB, false, 1>(g, stream);
+    if constexpr (DT != BEVPOOL_F32 || DB <= 2)
+        if (few) return vec ? launch<DT, DB, true, 1>(g, stream) : launch<DT, DB, false, 1>(g, stream);
     return vec ? launch<DT, DB, true, 4>(g, stream) : launch<DT, DB, false, 4>(g, stream);
 }
 

@@ -75,22 +75,22 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     const int row = tile * kOwn + 32 * wave + (lane & 31);
     const bool in = row < g.rows;
 
-    u32x4 q[S::kSteps], d[S::kSteps];
+    u32x4 q[S::kOperand], d[S::kOperand];
     float delta = 0.0f, lse = INFINITY;
 #pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) q[s] = d[s] = u32x4{0, 0, 0, 0};
+    for (int s = 0; s < S::kOperand; ++s) q[s] = d[s] = u32x4{0, 0, 0, 0};
     if (in) {
-        const T *p = at.q(row);
         const int64_t to = at.row(row);
+        const T *dout = static_cast<const T *>(g.dout) + to, *out = static_cast<const T *>(g.out) + to;
+        S::template operand<VEC>(at.q(row), half, dim, q);
+        S::template operand<VEC>(dout, half, dim, d);
 #pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) {
-            q[s] = load_chunk<DT, VEC>(p, 2 * s + half, dim);
-            d[s] = load_chunk<DT, VEC>(static_cast<const T *>(g.dout) + to, 2 * s + half, dim);
-            const u32x4 o = load_chunk<DT, VEC>(static_cast<const T *>(g.out) + to, 2 * s + half, dim);
+        for (int c = 0; c < S::kUsed / 2; ++c) {
             u32x4 low = {0, 0, 0, 0};
             if (DT != BEVPOOL_F32 && g.out_low)
-                low = load_chunk<DT, VEC>(static_cast<const T *>(g.out_low) + to, 2 * s + half, dim);
-            delta += pair_dot<DT>(d[s], o, low);
+                low = load_chunk<DT, VEC>(static_cast<const T *>(g.out_low) + to, 2 * c + half, dim);
+            delta += pair_dot<DT>(load_chunk<DT, VEC>(dout, 2 * c + half, dim), load_chunk<DT, VEC>(out, 2 * c + half, dim),
+                                  low);
         }
         lse = g.lse[at.stat(row)];
     }
@@ -184,15 +184,12 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
     const int key = tile * kOwn + 32 * wave + (lane & 31);
     const bool in = key < g.a.keys, use = in && at.ask(key) != 0;
 
-    u32x4 k[S::kSteps], v[S::kSteps];
+    u32x4 k[S::kOperand], v[S::kOperand];
 #pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) k[s] = v[s] = u32x4{0, 0, 0, 0};
+    for (int s = 0; s < S::kOperand; ++s) k[s] = v[s] = u32x4{0, 0, 0, 0};
     if (use) {
-#pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) {
-            k[s] = load_chunk<DT, VEC>(at.k(key), 2 * s + half, dim);
-            v[s] = load_chunk<DT, VEC>(at.v(key), 2 * s + half, dim);
-        }
+        S::template operand<VEC>(at.k(key), half, dim, k);
+        S::template operand<VEC>(at.v(key), half, dim, v);
     }
     const int tiles = (g.rows + W::kSize - 1) / W::kSize, per = (tiles + g.n_split - 1) / g.n_split;
     // a tile of keys past the sample's length has nothing to walk
@@ -225,8 +222,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
         for (int i = 0; i < Rows::kLoads; ++i) {
             const int r = Rows::row(i);
             if (!Rows::kEven && r >= W::kSize) break;
-            *reinterpret_cast<u32x4 *>(q + S::chunk_at(r, Rows::chunk(i))) = next_q[i];
-            *reinterpret_cast<u32x4 *>(q + W::kBytes + S::chunk_at(r, Rows::chunk(i))) = next_d[i];
+            S::put(q, r, Rows::chunk(i), next_q[i]);
+            S::put(q + W::kBytes, r, Rows::chunk(i), next_d[i]);
         }
         if (threadIdx.x < 2 * W::kSize) stat[threadIdx.x] = next_stat;
     };
@@ -314,12 +311,12 @@ void partition_q(const bevmap_attend &a, bool lengths, int32_t *n_tiles, int32_t
     int slots = kUnits * waves_dq(a.dtype, (a.dim + 31) / 32);
     if (lengths) slots += slots / 2;
     *n_split = pick_split(int64_t(a.batch) * a.key_heads * *n_tiles, slots, a.keys, attend_ceil(a.keys, kPartSize),
-                          lengths ? 600.0 : 300.0);         // twice the forward's work for the same parts
+                          lengths ? 600.0 : 300.0, a.dtype);       // twice the forward's work for the same parts
 }
 void partition_k(const bevmap_attend &a, int32_t *n_tiles, int32_t *n_split) {
     *n_tiles = attend_ceil(a.keys, kOwn);
     *n_split = pick_split(int64_t(a.batch) * a.key_heads * *n_tiles, kUnits * waves_dkv(a.dtype, (a.dim + 31) / 32),
-                          rows_of(a), attend_ceil(rows_of(a), kPartSize), 480.0);     // two parts, 2.5 times the work
+                          rows_of(a), attend_ceil(rows_of(a), kPartSize), 480.0, a.dtype);     // two parts, 2.5 times the work
 }
 
 template <int DT, int DB, bool VEC>
