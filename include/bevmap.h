@@ -123,9 +123,11 @@ BEVPOOL_API int64_t bevmap_attention_workspace(const bevmap_attend *attend, int3
  *             out left over, for the backward (of 16-bit types; not written for fp32).
  *  lse:       device float [batch][heads][queries], or NULL; overwritten with
  *             log2 of the sum of e^s, -infinity where no key is in use.
- * Scores, softmax statistics and output sums are fp32. With 16-bit inputs the
- * probabilities, relative to the row's running maximum, are rounded to the
- * inputs' type for their product with v on the matrix cores.
+ * Scores, softmax statistics and output sums are fp32; fp32 inputs are multiplied
+ * as sums of three bf16 pieces each, to fp32 accuracy. With 16-bit inputs the
+ * probabilities, relative to a maximum of the row, are rounded to the inputs'
+ * type for their product with v (of at most 32 rows, that is queries * heads /
+ * key_heads, to two pieces of the type).
  * A size of 0 is a call that writes zeros, or nothing.
  * Errors: INVALID_ARG (null pointer, a size below 0, heads, key_heads or dim
  * below 1, heads not a multiple of key_heads, scale not finite, a stride below
@@ -144,9 +146,9 @@ BEVPOOL_API int bevmap_attention(const bevmap_attend *attend, const void *q, con
  *  grad_q:    device [batch][queries][heads][dim], grad_k, grad_v: device
  *             [batch][keys][key_heads][dim], of dtype, overwritten. A key head's
  *             gradients sum over the heads that share it.
- * out_low may be NULL (out is then taken as it is). With 16-bit types the
- * probabilities and the scores' gradients are rounded to the type for their
- * products on the matrix cores; sums are fp32.
+ * out_low may be NULL (out is then taken as it is). Sums are fp32; with 16-bit types
+ * the probabilities and the scores' gradients enter their products as two pieces
+ * of the type.
  * Errors: those of bevmap_attention.
  */
 BEVPOOL_API int bevmap_attention_backward(const bevmap_attend *attend, const void *grad_out, const void *q,

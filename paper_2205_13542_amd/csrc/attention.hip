@@ -83,14 +83,22 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
     for (int d = 0; d < DB; ++d) o[d] = zeros();
     float top = -INFINITY, sum = 0.0f;     // of log2 scores; sum over this lane's keys
     const float c = g.log2_scale;
-    typename M::Rows p;
+    // Probabilities of 16-bit types are rounded to the type, and their sum is that of the rounded ones. Few rows,
+    // bound by reading, take what the rounding leaves as a second piece.
+    constexpr bool kTwo = WR == 1 && DT != BEVPOOL_F32;
+    typename M::Rows p, p_low;
     // p and this lane's sum of the exponentials of a block's scores relative to base
     auto exponentials = [&](const f32x16 &s, float base) {
         f32x16 e;
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -base));
-        p = M::rows(e);
-        return p.sum();
+        if constexpr (kTwo) {
+            M::rows_of_two(e, p, p_low);
+            return p.sum() + p_low.sum();
+        } else {
+            p = M::rows(e);
+            return p.sum();
+        }
     };
     // keys out of use: bit k of word is key k of the block
     auto leave_out = [&](f32x16 &s, uint32_t word) {
@@ -156,7 +164,7 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
                 float part = exponentials(s[n], top);
                 if (__builtin_expect(__any(!(part <= kMaxTileSum)), 0)) part = raise(s[n]);
                 sum += part;
-                S::sums(v, row0 + 32 * n, p, o);
+                S::sums(v, row0 + 32 * n, p, o, kTwo ? &p_low : nullptr);
             }
             if constexpr (W::kPairs == 1) __syncthreads();
             if (t + 1 < t1) {

@@ -259,8 +259,9 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
                         ds[i + e] = p[i + e] * (ds[i + e] - de[e]);
                     }
                 }
-                S::sums(d, 32 * n, M::rows(p), dv);
-                typename M::Rows high, low;         // as in k_attend_dq
+                typename M::Rows high, low;         // two pieces of each, as in k_attend_dq
+                M::rows_of_two(p, high, low);
+                S::sums(d, 32 * n, high, dv, DT == BEVPOOL_F32 ? nullptr : &low);
                 M::rows_of_two(ds, high, low);
                 S::sums(q, 32 * n, high, dk, DT == BEVPOOL_F32 ? nullptr : &low);
             }
