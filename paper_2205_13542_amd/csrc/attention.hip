@@ -6,6 +6,15 @@
 // scores of one row against 16 of 32 keys, and a softmax with a running maximum
 // and sum joins the tiles in one pass over the keys. Few rows leave the chip idle,
 // so the keys are then split over workgroups, and a second kernel joins the parts.
+//
+// A block of 32 rows and 32 keys takes a SIMD 252, 345 and 647 ns for 32, 64 and 128
+// channels of bf16 (530, 780 and 830 TFLOP/s; a library product of 8192^3 reaches
+// 1100). 32 channels are bound by the vector unit: 16 exponentials of 3.5 ns and 47
+// other instructions of 1.3 to 2 ns against 4 matrix instructions of 16 ns that mostly
+// overlap; 128 by the matrix cores and the LDS reads that feed them. Scores of the next
+// block formed ahead of a block's exponentials, the usual order and one block held
+// back were within 5% of each other. One query over 129600 keys (46 MB in use) takes
+// 17 us and its joining 8; 32400 queries over 16896 keys, 4 heads of 32: 457.
 #include "attention.h"
 
 namespace bevmap {

@@ -10,6 +10,13 @@
 // that share them. Scores are formed in both, seven products in place of
 // five. An axis that is too short to fill the chip has the walk of the other
 // split, and k_attend_add joins the parts.
+//
+// p and ds enter their products as two pieces of a 16-bit type: rounded once they
+// left dq, dk and dv of bf16 up to 1.55 times as far off as gradients in fp32 rounded
+// at the end; the pieces cost 11% of a step. 4 x 600 queries of 8 heads over 8100
+// masked keys, ragged, 64 channels: dq 61 us and its joining 9, dk and dv 77, two waves
+// a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
+// reaches 390, 490 and 390 TFLOP/s at 32, 64 and 128 channels, five products counted.
 #include "attention.h"
 
 namespace bevmap {
@@ -146,8 +153,6 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[i] : 0.0f;
                 }
-                // in two pieces of the type: a row's ds sum to 0, so that their rounding weighs more in dq than that of
-                // dq itself, and together they were 1.55 times as far off as dq in fp32 rounded once
                 typename M::Rows high, low;
                 M::rows_of_two(s, high, low);
                 S::sums(k, 32 * n, high, dq, DT == BEVPOOL_F32 ? nullptr : &low);
