@@ -67,8 +67,8 @@ BEVPOOL_API int64_t bevmap_group_norm_workspace(const bevmap_norm *norm, int32_t
  * Errors: INVALID_ARG (null pointer, a size below 0, channels or groups below 1,
  * channels not a multiple of groups, row_stride < channels, eps negative or not
  * finite, unknown act, workspace too small or not 16-byte aligned),
- * UNSUPPORTED_DTYPE, OVERFLOW (batch above 65535, batch * pixels or row_stride reaching 2^31, channels above
- * 8192), HIP (launch failure).
+ * UNSUPPORTED_DTYPE, OVERFLOW (batch above 65535, batch * pixels reaching 2^30, row_stride reaching 2^31,
+ * channels above 8192), HIP (launch failure).
  */
 BEVPOOL_API int bevmap_group_norm(const bevmap_norm *norm, const void *x, const void *weight, const void *bias,
                                   void *y, float *mean, float *rstd, void *workspace,
@@ -95,7 +95,8 @@ BEVPOOL_API int bevmap_group_norm_backward(const bevmap_norm *norm, const void *
  *   out_i = sum_j p_j v_j;  0 where no key is in use.
  * Key j of sample b is in use if j < key_lengths[b] and key_mask[b][j] is not 0.
  * Keys and values not in use are not read into any sum: they may hold anything,
- * NaN included, and their gradients are 0.
+ * NaN included, and their gradients are 0. Queries, and keys and values in use, must
+ * be finite: where they are not, their sample's results are unspecified.
  * Element (b, i, h, c) of q is at q + b * q_batch + i * q_row + h * q_head + c,
  * strides in elements; k and v alike. out and the gradients are contiguous.
  */

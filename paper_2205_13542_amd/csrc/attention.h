@@ -14,6 +14,8 @@
 //   four tile rows at a time.
 #pragma once
 
+#include <math.h>
+
 #include "mapops.h"
 
 namespace bevmap {
@@ -147,17 +149,6 @@ __device__ __forceinline__ void three_pieces(float x, float y, uint32_t *piece) 
     const Two last = {__bf16(left_of(x)), __bf16(left_of(y))};
     piece[2] = __builtin_bit_cast(uint32_t, last);
 }
-// The same for numbers that may be infinite: an infinity is its own first piece.
-__device__ __forceinline__ float left_of_any(float x) { return __builtin_isinf(x) ? 0.0f : left_of(x); }
-__device__ __forceinline__ void three_pieces_any(float x, float y, uint32_t *piece) {
-    const uint32_t first = cut_pair(x, y);
-    // a NaN may be cut off to an infinity; what is left of it is a NaN
-    three_pieces(left_of_any(x), left_of_any(y), piece);
-    piece[2] = piece[1];
-    piece[1] = piece[0];
-    piece[0] = first;
-}
-
 template <>
 struct Mma<BEVPOOL_F32> {
     using T = float;
@@ -251,7 +242,7 @@ struct Shape {
             uint32_t piece[2][3];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                three_pieces_any(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), piece[i]);
+                three_pieces(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), piece[i]);
             char *to = tile + chunk_at(row, c >> 1) + (c & 1) * 8;
 #pragma unroll
             for (int k = 0; k < 3; ++k)
@@ -272,7 +263,7 @@ struct Shape {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t piece[3];
-                        three_pieces_any(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), piece);
+                        three_pieces(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), piece);
 #pragma unroll
                         for (int k = 0; k < 3; ++k) y[k * kSteps + s][2 * i + j] = piece[k];
                     }
@@ -531,19 +522,22 @@ inline int attend_ceil(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 inline int pick_split(int64_t whole, int slots, int64_t walk, int64_t most, double join, int dtype) {
     if (whole <= 0 || walk <= 0) return 1;
     if (dtype == BEVPOOL_F32) join *= 0.25;
-    const int64_t limit = 2 * int64_t(slots) / whole + 1;
-    const int end = int(most < limit ? most : limit);
     const double part = join / double(walk) * double(whole) / slots;
-    int best = 1;
+    int64_t best = 1;
     double least = double((whole + slots - 1) / slots);
-    for (int s = 2; s <= end; ++s) {
-        const double cost = double((whole * s + slots - 1) / slots) / s + s * part;
+    for (int rounds = 1; rounds <= 3; ++rounds) {
+        // the most parts of so many rounds, or fewer where rounds / s + s * part is least
+        int64_t s = rounds * int64_t(slots) / whole, fewer = int64_t(sqrt(rounds / part) + 0.5);
+        if (s > fewer) s = fewer;
+        if (s > most) s = most;
+        if (s < 2) continue;
+        const double cost = double((whole * s + slots - 1) / slots) / double(s) + double(s) * part;
         if (cost < least * 0.98) {
             least = cost;
             best = s;
         }
     }
-    return best;
+    return int(best);
 }
 constexpr int kUnits = 256;     // compute units
 
@@ -576,11 +570,13 @@ AttendArgs attend_fill(const bevmap_attend &a, const void *q, const void *k, con
 // Rows that can be read 16 bytes at a time.
 bool attend_vec(const bevmap_attend &a, const void *q, const void *k, const void *v) {
     const int e = a.dtype == BEVPOOL_F32 ? 4 : 8;
-    auto ok = [&](const void *p, int64_t batch, int64_t row, int64_t head) {
-        return aligned_for(p, batch, a.dtype, e) && aligned_for(p, row, a.dtype, e) && aligned_for(p, head, a.dtype, e);
+    auto ok = [&](const void *p, int64_t batch, int64_t row, int64_t head, int rows, int heads) {
+        return aligned_for(p, a.batch > 1 ? batch : 0, a.dtype, e) && aligned_for(p, rows > 1 ? row : 0, a.dtype, e) &&
+               aligned_for(p, heads > 1 ? head : 0, a.dtype, e);
     };
-    return a.dim % e == 0 && ok(q, a.q_batch, a.q_row, a.q_head) && ok(k, a.k_batch, a.k_row, a.k_head) &&
-           ok(v, a.v_batch, a.v_row, a.v_head);
+    return a.dim % e == 0 && ok(q, a.q_batch, a.q_row, a.q_head, a.queries, a.heads) &&
+           ok(k, a.k_batch, a.k_row, a.k_head, a.keys, a.key_heads) &&
+           ok(v, a.v_batch, a.v_row, a.v_head, a.keys, a.key_heads);
 }
 
 }  // namespace

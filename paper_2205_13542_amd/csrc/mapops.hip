@@ -26,7 +26,7 @@ int check(const bevmap_norm *n) {
     if (!known_dtype(n->x_dtype) || !known_dtype(n->y_dtype) || !known_dtype(n->weight_dtype))
         return bevpool_fail(BEVPOOL_ERR_UNSUPPORTED_DTYPE, "dtypes %d, %d, %d", n->x_dtype, n->y_dtype,
                             n->weight_dtype);
-    if (int64_t(n->batch) * n->pixels >= (int64_t(1) << 31) || n->channels > kNormMaxChannels || n->batch > 65535 ||
+    if (int64_t(n->batch) * n->pixels >= (int64_t(1) << 30) || n->channels > kNormMaxChannels || n->batch > 65535 ||
         n->row_stride >= (int64_t(1) << 31))
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d pixels=%d channels=%d row stride %lld: too large",
                             n->batch, n->pixels, n->channels, (long long)n->row_stride);

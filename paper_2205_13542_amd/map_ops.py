@@ -291,6 +291,7 @@ def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
     are clamped to [0, M]). key_mask: bool [B][M], states with False are not in
     use. States not in use may hold anything, NaN too; they do not reach the
     output, and their gradients are 0. A query without a state in use gets 0.
+    Queries and states in use must be finite.
     Few queries over many states (one token in serving) are split over the
     states. Differentiable in q, k and v, bitwise reproducible."""
     if _learns(q, k, v):

@@ -535,6 +535,14 @@ def test_gradients_against_differences(torch, bev):
             assert abs(got - want) <= 1e-3 * (abs(want) + g.double().norm().item() / math.sqrt(g.numel())) + 2e-3
 
 
+def test_second_derivatives_are_refused(torch, bev):
+    x = torch.randn(2, 8, 8, device="cuda", requires_grad=True)
+    q = torch.randn(1, 3, 2, 8, device="cuda", requires_grad=True)
+    for y, t in ((bev.group_norm_act(x, 2), x), (bev.cross_attention(q, q, q), q), (bev.dropout_add(x, 0.5, 1), x)):
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(y.sum(), t, create_graph=True)
+
+
 def _layer(torch, bev, x, w, b, wq, wkv, tokens, seen, seed, step):
     B, C = x.shape[0], x.shape[-1]
     states = bev.group_norm_act(x, 4, w, b, act="silu", out_dtype=torch.bfloat16).flatten(1, 2)

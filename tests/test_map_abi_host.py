@@ -47,7 +47,7 @@ def _norm(mb, **over):
     (dict(groups=5), INVALID), (dict(row_stride=11), INVALID), (dict(eps=-1.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(act=4), INVALID), (dict(act=-1), INVALID), (dict(x_dtype=3), DTYPE),
     (dict(y_dtype=-1), DTYPE), (dict(weight_dtype=7), DTYPE), (dict(batch=65536), OVERFLOW),
-    (dict(batch=4096, pixels=1 << 20), OVERFLOW), (dict(channels=8193, groups=1, row_stride=8193), OVERFLOW),
+    (dict(batch=4096, pixels=1 << 20), OVERFLOW), (dict(batch=1, pixels=1 << 30), OVERFLOW), (dict(channels=8193, groups=1, row_stride=8193), OVERFLOW),
     (dict(row_stride=1 << 31), OVERFLOW)])
 def test_group_norm_refuses(lib, mb, over, code):
     n = _norm(mb, **over)
