@@ -13,10 +13,10 @@
 //
 // p and ds enter their products as two pieces of a 16-bit type: rounded once they
 // left dq, dk and dv of bf16 up to 1.55 times as far off as gradients in fp32 rounded
-// at the end; the pieces cost 11% of a step. 4 x 600 queries of 8 heads over 8100
+// at the end; the pieces cost a quarter of the pair of kernels at large sizes. 4 x 600 queries of 8 heads over 8100
 // masked keys, ragged, 64 channels: dq 61 us and its joining 9, dk and dv 77, two waves
 // a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
-// reaches 390, 490 and 390 TFLOP/s at 32, 64 and 128 channels, five products counted.
+// reaches 360, 450 and 380 TFLOP/s at 32, 64 and 128 channels, five products counted.
 #include "attention.h"
 
 namespace bevmap {
@@ -285,25 +285,29 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
     write_row<DT, DB, VEC>(dv, use, 1.0f, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
 }
 
-// Joins parts, one thread to an element. KEYS: of the gradients of k (grid z 0)
-// and v (1), else of q.
-template <int DT, bool KEYS>
-__global__ __launch_bounds__(kAttendBlock) void k_attend_add(AttendArgs g) {
+// Joins parts, one thread to an element: of the gradient of q (grid z 0), k (1) and v (2).
+struct Parts {
+    const float *q, *k;       // of k, then of v, for each part
+    int32_t split_q, split_k; // 1: written whole, nothing to join
+};
+template <int DT>
+__global__ __launch_bounds__(kAttendBlock) void k_attend_add(AttendArgs g, Parts parts) {
     using T = typename Num<DT>::T;
-    const int per_bh = KEYS ? g.a.keys : g.rows, dim = g.a.dim;
+    const bool keys = blockIdx.z != 0;
+    const int split = keys ? parts.split_k : parts.split_q, per_bh = keys ? g.a.keys : g.rows, dim = g.a.dim;
     const int64_t total = int64_t(g.a.batch) * g.a.key_heads * per_bh * dim;
     const int64_t n = int64_t(blockIdx.x) * kAttendBlock + threadIdx.x;
-    if (n >= total) return;
+    if (split <= 1 || n >= total) return;
     const int64_t slot = n / dim;
     const int ch = int(n - slot * dim), bh = int(slot / per_bh), i = int(slot - int64_t(bh) * per_bh);
     const Problem<DT> at(g, bh);
-    const float *part = g.part + (KEYS ? int64_t(blockIdx.z) * total : 0) + n;
-    const int64_t step = KEYS ? 2 * total : total;
+    const float *part = (keys ? parts.k + int64_t(blockIdx.z - 1) * total : parts.q) + n;
+    const int64_t step = keys ? 2 * total : total;
     float sum = 0.0f;
 #pragma unroll 4
-    for (int s = 0; s < g.n_split; ++s) sum += part[s * step];
-    T *to = static_cast<T *>(!KEYS ? g.dq : blockIdx.z ? g.dv : g.dk);
-    to[(KEYS ? at.key(i) : at.row(i)) + ch] = T(sum);
+    for (int s = 0; s < split; ++s) sum += part[s * step];
+    T *to = static_cast<T *>(!keys ? g.dq : blockIdx.z == 1 ? g.dk : g.dv);
+    to[(keys ? at.key(i) : at.row(i)) + ch] = T(sum);
 }
 
 int64_t rows_of(const bevmap_attend &a) { return int64_t(a.queries) * (a.heads / a.key_heads); }
@@ -325,6 +329,10 @@ void partition_k(const bevmap_attend &a, int32_t *n_tiles, int32_t *n_split) {
                           rows_of(a), attend_ceil(rows_of(a), kPartSize), 480.0, a.dtype);     // two parts, 2.5 times the work
 }
 
+// Floats of the workspace: delta, ahead of the parts, and parts, which start on 16 bytes.
+int64_t delta_floats(const bevmap_attend &a) { return (int64_t(a.batch) * a.queries * a.heads + 3) / 4 * 4; }
+int64_t part_floats(int64_t parts, int64_t floats) { return (parts * floats + 3) / 4 * 4; }
+
 template <int DT, int DB, bool VEC>
 int launch(AttendArgs g, hipStream_t stream) {
     using W = Walk<DT, DB>;
@@ -336,25 +344,29 @@ int launch(AttendArgs g, hipStream_t stream) {
                                         hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)));
     }
     const int64_t bh = int64_t(g.a.batch) * g.a.key_heads;
-    const auto blocks = [](int64_t n) { return uint32_t((n + kAttendBlock - 1) / kAttendBlock); };
+    Parts parts{g.part, nullptr, 1, 1};
     if (g.rows > 0) {
         partition_q(g.a, g.lengths != nullptr, &g.n_tiles, &g.n_split);
+        parts.split_q = g.n_split;
         hipLaunchKernelGGL((k_attend_dq<DT, DB, VEC>), dim3(uint32_t(bh * g.n_split * g.n_tiles)),
                            dim3(kAttendBlock), lds, stream, g);
         BEVPOOL_HIP(hipGetLastError());
-        if (g.n_split > 1)
-            hipLaunchKernelGGL((k_attend_add<DT, false>), dim3(blocks(bh * g.rows * g.a.dim)), dim3(kAttendBlock), 0,
-                               stream, g);
-        BEVPOOL_HIP(hipGetLastError());
     }
     if (g.a.keys > 0) {
+        if (parts.split_q > 1) g.part += part_floats(parts.split_q, bh * g.rows * g.a.dim);
         partition_k(g.a, &g.n_tiles, &g.n_split);
+        parts.k = g.part;
+        parts.split_k = g.n_split;
         hipLaunchKernelGGL((k_attend_dkv<DT, DB, VEC>), dim3(uint32_t(bh * g.n_split * g.n_tiles)),
                            dim3(kAttendBlock), lds, stream, g);
         BEVPOOL_HIP(hipGetLastError());
-        if (g.n_split > 1)
-            hipLaunchKernelGGL((k_attend_add<DT, true>), dim3(blocks(bh * g.a.keys * g.a.dim), 1, 2),
-                               dim3(kAttendBlock), 0, stream, g);
+    }
+    const int64_t of_q = parts.split_q > 1 ? bh * g.rows * g.a.dim : 0;
+    const int64_t of_k = parts.split_k > 1 ? bh * g.a.keys * g.a.dim : 0;
+    if (of_q || of_k) {
+        const int64_t most = of_q > of_k ? of_q : of_k;
+        hipLaunchKernelGGL((k_attend_add<DT>), dim3(uint32_t((most + kAttendBlock - 1) / kAttendBlock), 1, of_k ? 3 : 1),
+                           dim3(kAttendBlock), 0, stream, g, parts);
         BEVPOOL_HIP(hipGetLastError());
     }
     return BEVPOOL_OK;
@@ -375,9 +387,6 @@ int backward(const AttendArgs &g, bool vec, hipStream_t stream) {
     }
 }
 
-// Of the workspace, ahead of the parts, which start on 16 bytes.
-int64_t delta_floats(const bevmap_attend &a) { return (int64_t(a.batch) * a.queries * a.heads + 3) / 4 * 4; }
-
 }  // namespace
 }  // namespace bevmap
 
@@ -390,10 +399,9 @@ int64_t bevmap_attention_backward_bytes(const bevmap_attend &a) {
     if (split_lengths > split_q) split_q = split_lengths;
     partition_k(a, &tiles, &split_k);
     const int64_t rows = int64_t(a.batch) * a.queries * a.heads, keys = int64_t(a.batch) * a.keys * a.key_heads;
-    const int64_t parts_q = split_q > 1 ? split_q * rows * a.dim : 0;
-    const int64_t parts_k = split_k > 1 ? 2 * split_k * keys * a.dim : 0;
-    // delta, then the parts of one gradient at a time
-    return (delta_floats(a) + (parts_q > parts_k ? parts_q : parts_k)) * int64_t(sizeof(float));
+    const int64_t parts_q = split_q > 1 ? part_floats(split_q, rows * a.dim) : 0;
+    const int64_t parts_k = split_k > 1 ? part_floats(2 * int64_t(split_k), keys * a.dim) : 0;
+    return (delta_floats(a) + parts_q + parts_k) * int64_t(sizeof(float));
 }
 
 int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_out, const void *q, const void *k,
