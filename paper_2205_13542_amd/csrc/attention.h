@@ -33,6 +33,7 @@ struct AttendArgs {
     float *part;                  // fp32 parts of a split axis
     float2 *part_stats;           // forward: (maximum, sum) of a part's rows
     int32_t part_pitch;           // floats from row to row of a part
+    bool pairs;                   // rows can be read two elements at a time
     bool out_aligned;             // four elements of out and out_low can be written at a time
     int32_t group, rows;          // heads that share a key head, queries * group
     bevpool::FastDiv by_group;
@@ -200,14 +201,20 @@ __device__ __forceinline__ int turn(int row) {
 constexpr int pow2_chunks(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : 16; }
 
 // One chunk of a row: elements c * kElems.. of dim, zeros past dim. VEC: rows
-// start on 16-byte boundaries and dim is a multiple of the chunk.
+// start on 16-byte boundaries and dim is a multiple of the chunk. Else elements are
+// read one by one, or, with 16-bit types, by twos where rows start on 4 bytes and dim
+// is even (pairs, uniform).
 template <int DT, bool VEC>
-__device__ __forceinline__ u32x4 load_chunk(const typename Num<DT>::T *row, int c, int dim) {
+__device__ __forceinline__ u32x4 load_chunk(const typename Num<DT>::T *row, int c, int dim, bool pairs) {
     using T = typename Num<DT>::T;
     constexpr int E = Mma<DT>::kElems;
     u32x4 out = {0, 0, 0, 0};
     if constexpr (VEC) {
         if (c * E < dim) out = *reinterpret_cast<const u32x4 *>(row + c * E);
+    } else if (DT != BEVPOOL_F32 && pairs) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c * E + 2 * e < dim) out[e] = *reinterpret_cast<const uint32_t *>(row + c * E + 2 * e);
     } else {
         T v[E];
 #pragma unroll
@@ -251,15 +258,15 @@ struct Shape {
     }
     // A row in memory as an operand of scores().
     template <bool VEC>
-    static __device__ __forceinline__ void operand(const T *row, int half, int dim, u32x4 *y) {
+    static __device__ __forceinline__ void operand(const T *row, int half, int dim, bool pairs, u32x4 *y) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             if constexpr (DT != BEVPOOL_F32) {
-                y[s] = load_chunk<DT, VEC>(row, 2 * s + half, dim);
+                y[s] = load_chunk<DT, VEC>(row, 2 * s + half, dim, pairs);
             } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const u32x4 v = load_chunk<DT, VEC>(row, 4 * s + 2 * half + i, dim);
+                    const u32x4 v = load_chunk<DT, VEC>(row, 4 * s + 2 * half + i, dim, pairs);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t piece[3];
@@ -445,7 +452,8 @@ struct Stage {
     // base: the tile's first row (uniform). words: its rows in use, the others are
     // not read and count as zeros; all: whether every row is.
     template <int WORDS>
-    __device__ __forceinline__ void load(const char *base, const uint64_t (&words)[WORDS], bool all, int dim) {
+    __device__ __forceinline__ void load(const char *base, const uint64_t (&words)[WORDS], bool all, int dim,
+                                         bool pairs) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = row(i);
@@ -462,7 +470,7 @@ struct Stage {
             } else {
                 reg[i] = u32x4{0, 0, 0, 0};
                 if (there && (word >> (r & 63)) & 1)
-                    reg[i] = load_chunk<DT, false>(reinterpret_cast<const T *>(base + at[i]), chunk(i), dim);
+                    reg[i] = load_chunk<DT, false>(reinterpret_cast<const T *>(base + at[i]), chunk(i), dim, pairs);
             }
         }
     }
@@ -567,9 +575,8 @@ AttendArgs attend_fill(const bevmap_attend &a, const void *q, const void *k, con
     return g;
 }
 
-// Rows that can be read 16 bytes at a time.
-bool attend_vec(const bevmap_attend &a, const void *q, const void *k, const void *v) {
-    const int e = a.dtype == BEVPOOL_F32 ? 4 : 8;
+// Whether rows can be read n elements at a time.
+bool attend_by(const bevmap_attend &a, const void *q, const void *k, const void *v, int e) {
     auto ok = [&](const void *p, int64_t batch, int64_t row, int64_t head, int rows, int heads) {
         return aligned_for(p, a.batch > 1 ? batch : 0, a.dtype, e) && aligned_for(p, rows > 1 ? row : 0, a.dtype, e) &&
                aligned_for(p, heads > 1 ? head : 0, a.dtype, e);

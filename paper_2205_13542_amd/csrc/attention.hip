@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
     u32x4 q[S::kOperand];
 #pragma unroll
     for (int s = 0; s < S::kOperand; ++s) q[s] = u32x4{0, 0, 0, 0};
-    if (row < g.rows) S::template operand<VEC>(at.q(row), half, dim, q);
+    if (row < g.rows) S::template operand<VEC>(at.q(row), half, dim, g.pairs, q);
     if (g.sign != 1.0f) {
 #pragma unroll
         for (int s = 0; s < S::kOperand; ++s) q[s] = g.sign == 0.0f ? u32x4{0, 0, 0, 0} : q[s] ^ 0x80008000u;
@@ -138,8 +138,8 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
     if (t0 < t1) {
         mask.ask(at, t0 * W::kKeys);
         use = mask.count(at, t0 * W::kKeys);
-        next_k.load(key_rows(t0), use.words, use.all, dim);
-        next_v.load(value_rows(t0), use.words, use.all, dim);
+        next_k.load(key_rows(t0), use.words, use.all, dim, g.pairs);
+        next_v.load(value_rows(t0), use.words, use.all, dim, g.pairs);
         mask.ask(at, (t0 + 1) * W::kKeys);
         next_k.store(lds);
         next_v.store(lds + W::kBytes);
@@ -152,8 +152,8 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
             const char *k = lds + buffer * 2 * W::kBytes, *v = k + W::kBytes;
             if (t + 1 < t1) {
                 next = mask.count(at, (t + 1) * W::kKeys);
-                next_k.load(key_rows(t + 1), next.words, next.all, dim);
-                next_v.load(value_rows(t + 1), next.words, next.all, dim);
+                next_k.load(key_rows(t + 1), next.words, next.all, dim, g.pairs);
+                next_v.load(value_rows(t + 1), next.words, next.all, dim, g.pairs);
                 mask.ask(at, (t + 2) * W::kKeys);
             }
             __syncthreads();
@@ -455,7 +455,8 @@ int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d heads=%d: too many tiles of rows", a.batch,
                             a.queries, a.heads);
     g.out_aligned = aligned_for(out, 0, a.dtype, 4) && (!out_low || aligned_for(out_low, 0, a.dtype, 4));
-    const bool vec = attend_vec(a, q, k, v) && g.out_aligned;
+    const bool vec = attend_by(a, q, k, v, a.dtype == BEVPOOL_F32 ? 4 : 8) && g.out_aligned;
+    g.pairs = attend_by(a, q, k, v, 2);
     switch (a.dtype) {
         case BEVPOOL_F32: return forward<BEVPOOL_F32>(g, vec, few, stream);
         case BEVPOOL_BF16: return forward<BEVPOOL_BF16>(g, vec, few, stream);

@@ -89,14 +89,14 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     if (in) {
         const int64_t to = at.row(row);
         const T *dout = static_cast<const T *>(g.dout) + to, *out = static_cast<const T *>(g.out) + to;
-        S::template operand<VEC>(at.q(row), half, dim, q);
-        S::template operand<VEC>(dout, half, dim, d);
+        S::template operand<VEC>(at.q(row), half, dim, g.pairs, q);
+        S::template operand<VEC>(dout, half, dim, g.pairs, d);
 #pragma unroll
         for (int c = 0; c < S::kUsed / 2; ++c) {
             u32x4 low = {0, 0, 0, 0};
             if (DT != BEVPOOL_F32 && g.out_low)
-                low = load_chunk<DT, VEC>(static_cast<const T *>(g.out_low) + to, 2 * c + half, dim);
-            delta += pair_dot<DT>(load_chunk<DT, VEC>(dout, 2 * c + half, dim), load_chunk<DT, VEC>(out, 2 * c + half, dim),
+                low = load_chunk<DT, VEC>(static_cast<const T *>(g.out_low) + to, 2 * c + half, dim, g.pairs);
+            delta += pair_dot<DT>(load_chunk<DT, VEC>(dout, 2 * c + half, dim, g.pairs), load_chunk<DT, VEC>(out, 2 * c + half, dim, g.pairs),
                                   low);
         }
         lse = g.lse[at.stat(row)];
@@ -120,8 +120,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     if (t0 < t1) {
         mask.ask(at, t0 * W::kSize);
         use = mask.count(at, t0 * W::kSize);
-        next_k.load(key_rows(t0), use.words, use.all, dim);
-        next_v.load(value_rows(t0), use.words, use.all, dim);
+        next_k.load(key_rows(t0), use.words, use.all, dim, g.pairs);
+        next_v.load(value_rows(t0), use.words, use.all, dim, g.pairs);
         mask.ask(at, (t0 + 1) * W::kSize);
         next_k.store(lds);
         next_v.store(lds + W::kBytes);
@@ -134,8 +134,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
             const char *k = lds + buffer * 2 * W::kBytes, *v = k + W::kBytes;
             if (t + 1 < t1) {
                 next = mask.count(at, (t + 1) * W::kSize);
-                next_k.load(key_rows(t + 1), next.words, next.all, dim);
-                next_v.load(value_rows(t + 1), next.words, next.all, dim);
+                next_k.load(key_rows(t + 1), next.words, next.all, dim, g.pairs);
+                next_v.load(value_rows(t + 1), next.words, next.all, dim, g.pairs);
                 mask.ask(at, (t + 2) * W::kSize);
             }
             __syncthreads();
@@ -193,8 +193,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
 #pragma unroll
     for (int s = 0; s < S::kOperand; ++s) k[s] = v[s] = u32x4{0, 0, 0, 0};
     if (use) {
-        S::template operand<VEC>(at.k(key), half, dim, k);
-        S::template operand<VEC>(at.v(key), half, dim, v);
+        S::template operand<VEC>(at.k(key), half, dim, g.pairs, k);
+        S::template operand<VEC>(at.v(key), half, dim, g.pairs, v);
     }
     const int tiles = (g.rows + W::kSize - 1) / W::kSize, per = (tiles + g.n_split - 1) / g.n_split;
     // a tile of keys past the sample's length has nothing to walk
@@ -211,8 +211,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
             if ((Rows::kEven || r < W::kSize) && r0 + r < g.rows) {
                 int query, head;
                 at.split_row(r0 + r, query, head);
-                next_q[i] = load_chunk<DT, VEC>(at.q(query, head), c, dim);
-                next_d[i] = load_chunk<DT, VEC>(static_cast<const T *>(g.dout) + at.row(query, head), c, dim);
+                next_q[i] = load_chunk<DT, VEC>(at.q(query, head), c, dim, g.pairs);
+                next_d[i] = load_chunk<DT, VEC>(static_cast<const T *>(g.dout) + at.row(query, head), c, dim, g.pairs);
             }
         }
         if (threadIdx.x < 2 * W::kSize) {
@@ -428,9 +428,13 @@ int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_ou
     g.delta = static_cast<float *>(workspace);
     g.part = g.delta + delta_floats(a);
     const int e = a.dtype == BEVPOOL_F32 ? 4 : 8;
-    const auto ok = [&](const void *p) { return !p || aligned_for(p, 0, a.dtype, e); };
-    const bool vec = attend_vec(a, q, k, v) && ok(grad_out) && ok(out) && ok(out_low) && ok(grad_q) && ok(grad_k) &&
-                     ok(grad_v);
+    const auto by = [&](int n) {
+        const auto ok = [&](const void *p) { return !p || aligned_for(p, 0, a.dtype, n); };
+        return attend_by(a, q, k, v, n) && ok(grad_out) && ok(out) && ok(out_low) && ok(grad_q) && ok(grad_k) &&
+               ok(grad_v);
+    };
+    const bool vec = by(e);
+    g.pairs = by(2);
     switch (a.dtype) {
         case BEVPOOL_F32: return backward<BEVPOOL_F32>(g, vec, stream);
         case BEVPOOL_BF16: return backward<BEVPOOL_BF16>(g, vec, stream);

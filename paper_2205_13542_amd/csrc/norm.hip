@@ -22,7 +22,7 @@ namespace bevmap {
 namespace {
 
 constexpr int kNormBlock = 256;     // apply passes
-constexpr int kSumBlock = 256;      // sum passes
+constexpr int kSumBlock = kNormBlock;   // sum passes
 constexpr int kJoinBlock = 256;
 constexpr int kSumRows = 4;         // rows that a thread has in flight, in k_norm_sum
 constexpr int kNormRows = 2;        // and elsewhere
@@ -108,13 +108,35 @@ __device__ __forceinline__ Columns columns(int first, int n_vec) {
     return c;
 }
 
+// Sums v over the row lanes, in halves; every lane gets the sums. th: a float for each
+// thread's channels, free on entry and exit.
+template <int V>
+__device__ __forceinline__ void add_lanes(const Columns &c, int first, int width, float *v, float *th) {
+    float *mine = th + c.lane * width + (c.vec - first) * V;
+    if (c.lane < c.lanes)
+#pragma unroll
+        for (int i = 0; i < V; ++i) mine[i] = v[i];
+    for (int n = c.lanes; n > 1; n = (n + 1) / 2) {
+        const int half = (n + 1) / 2;
+        __syncthreads();
+        if (c.lane < n - half)
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine[i] += mine[half * width + i];
+    }
+    __syncthreads();
+    if (c.lane < c.lanes)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = th[(c.vec - first) * V + i];
+    __syncthreads();
+}
+
 // Statistics of a chunk of rows: parts[b][chunk][g] = (mean, M2).
 template <int DT, int V>
 __global__ __launch_bounds__(kSumBlock) void k_norm_sum(NormArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float lds[];
     float *ch_mean = lds, *ch_m2 = lds + a.C;             // [C] each
-    float *th = lds + 2 * a.C;                            // [2][lanes][V * vectors]
+    float *th = lds + 2 * a.C;                            // [lanes][V * vectors]
     const int b = blockIdx.y, r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
     const int n_vec = a.C / V;
     const T *x = static_cast<const T *>(a.x) + int64_t(b) * a.rows * a.ldx;
@@ -159,27 +181,25 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_sum(NormArgs a) {
             }
         }
         const int width = c.vectors * V;                  // channels of this block of columns
-        if (c.lane < c.lanes) {
+        // join the row lanes: lane l walked ceil((rows - l) / lanes) rows
+        const float rows = float(r1 - r0), mine = c.lane < c.lanes ? float(n) : 0.0f;
+        float total[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                th[c.lane * width + (c.vec - first) * V + i] = mean[i];
-                th[(c.lanes + c.lane) * width + (c.vec - first) * V + i] = m2[i];
-            }
+        for (int i = 0; i < V; ++i) total[i] = mean[i] * mine;
+        add_lanes<V>(c, first, width, total, th);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            total[i] /= rows;
+            const float d = mean[i] - total[i];
+            m2[i] = mine > 0.0f ? fmaf(d * d, mine, m2[i]) : 0.0f;
         }
-        __syncthreads();
-        // join the row lanes; lane l walked ceil((rows - l) / lanes) rows
-        const int rows = r1 - r0;
-        for (int i = threadIdx.x; i < width; i += kSumBlock) {
-            float m = 0.0f, q = 0.0f;
-            for (int l = 0; l < c.lanes; ++l) m += th[l * width + i] * float((rows - l + c.lanes - 1) / c.lanes);
-            m /= float(rows);
-            for (int l = 0; l < c.lanes; ++l) {
-                const float d = th[l * width + i] - m;
-                q += th[(c.lanes + l) * width + i] + d * d * float((rows - l + c.lanes - 1) / c.lanes);
-            }
-            ch_mean[first * V + i] = m;
-            ch_m2[first * V + i] = q;
-        }
+        if (c.lane == 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i) ch_mean[c.vec * V + i] = total[i];
+        add_lanes<V>(c, first, width, m2, th);
+        if (c.lane == 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i) ch_m2[c.vec * V + i] = m2[i];
         __syncthreads();
     }
     // join a group's channels, all of equal counts
@@ -294,8 +314,11 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
     for (int first = 0; first < n_vec; first += kSumBlock) {
         const Columns c = columns<kSumBlock>(first, n_vec);
         const int width = c.vectors * V;
+        float w[V], sum[V], dot[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = sum[i] = dot[i] = 0.0f;
         if (c.lane < c.lanes) {
-            float mu[V], rs[V], w[V], add[V], sum[V], dot[V];
+            float mu[V], rs[V], add[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int ch = c.vec * V + i, g = ch / a.per;
@@ -303,7 +326,6 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
                 rs[i] = a.rstd[int64_t(b) * a.G + g];
                 w[i] = weight_at(a.weight, ch, a.w_dtype, 1.0f);
                 add[i] = weight_at(a.bias, ch, a.w_dtype, 0.0f);
-                sum[i] = dot[i] = 0.0f;
             }
             for (int r = r0 + c.lane; r < r1; r += kNormRows * c.lanes) {
                 float v[kNormRows][V], d[kNormRows][V];
@@ -327,26 +349,18 @@ __global__ __launch_bounds__(kSumBlock) void k_norm_grad_sum(NormArgs a) {
                     }
                 });
             }
+        }
+        add_lanes<V>(c, first, width, sum, th);
+        add_lanes<V>(c, first, width, dot, th);
+        if (c.lane == 0)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                th[c.lane * width + (c.vec - first) * V + i] = sum[i];
-                th[(c.lanes + c.lane) * width + (c.vec - first) * V + i] = dot[i];
+                const int ch = c.vec * V + i;
+                sums[ch] = sum[i];
+                sums[a.C + ch] = dot[i];
+                ch_sum[ch] = sum[i] * w[i];
+                ch_dot[ch] = dot[i] * w[i];
             }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < width; i += kSumBlock) {
-            float s = 0.0f, d = 0.0f;
-            for (int l = 0; l < c.lanes; ++l) {
-                s += th[l * width + i];
-                d += th[(c.lanes + l) * width + i];
-            }
-            const int ch = first * V + i;
-            sums[ch] = s;
-            sums[a.C + ch] = d;
-            const float w = weight_at(a.weight, ch, a.w_dtype, 1.0f);
-            ch_sum[ch] = s * w;
-            ch_dot[ch] = d * w;
-        }
         __syncthreads();
     }
     const int lane = threadIdx.x % kMergeLanes;
@@ -593,7 +607,7 @@ __global__ __launch_bounds__(kSmallBlock) void k_norm_small_grad(NormArgs a) {
 
 constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
 constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
-constexpr int kMinRows = 16;        // rows of a chunk at least
+constexpr int kThreadRows = 8;      // rows of a thread, about, at least
 // Maps that together exceed the 256 MB of cache behind the L2s: results are then
 // written past it, and more of x is still there for the second read.
 constexpr int64_t kCacheBytes = int64_t(256) << 20;
@@ -610,11 +624,16 @@ bool small(const bevmap_norm &n, bool backward) {
 }
 
 void split(const bevmap_norm &n, NormArgs *a) {
+    // row lanes of a workgroup with the widest accesses (by the sizes alone: the workspace goes by this)
+    int vec = n.x_dtype == BEVPOOL_F32 ? 4 : 8;
+    while (n.channels % vec) vec >>= 1;
+    const int vectors = n.channels / vec, lanes = vectors < kNormBlock ? kNormBlock / vectors : 1;
+    const int least = kThreadRows * lanes;
     a->chunk = ceil_div(n.pixels, ceil_div(kSumGrid, n.batch));
-    if (a->chunk < kMinRows) a->chunk = kMinRows;
+    if (a->chunk < least) a->chunk = least;
     a->n_chunks = ceil_div(n.pixels, a->chunk);
     a->apply_rows = ceil_div(n.pixels, ceil_div(kApplyGrid, n.batch));
-    if (a->apply_rows < kMinRows) a->apply_rows = kMinRows;
+    if (a->apply_rows < least) a->apply_rows = least;
     a->n_apply = ceil_div(n.pixels, a->apply_rows);
 }
 
@@ -650,8 +669,8 @@ int vector_of(const bevmap_norm &n, const void *x, const void *y, const void *dx
     return 1;
 }
 
-// Bytes of LDS: two floats a channel, and two for each thread's V channels.
-size_t sum_lds(const NormArgs &a, int v) { return (2 * size_t(a.C) + 2 * size_t(kSumBlock) * v) * sizeof(float); }
+// Bytes of LDS: two floats a channel, and one for each thread's V channels.
+size_t sum_lds(const NormArgs &a, int v) { return (2 * size_t(a.C) + size_t(kSumBlock) * v) * sizeof(float); }
 
 // Raises a kernel's limit of dynamic LDS where it needs more than the default.
 template <class K>
