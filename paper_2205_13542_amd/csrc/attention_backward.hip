@@ -32,6 +32,7 @@ struct Walk {
     static constexpr int kSize = 32 * kBlocks;
     static constexpr int kBytes = kSize * S::kRowBytes;
     static constexpr int kLds = 4 * kBytes + 4 * kSize * int(sizeof(float));
+    static_assert(kLds >= 4 * 32 * 32 * DB * int(sizeof(typename S::T)), "write_rows() of four waves");
 };
 
 template <int DT>
@@ -171,6 +172,40 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     write_row<DT, DB, VEC>(dq, true, g.a.scale, static_cast<T *>(g.dq) + at.row(row), part, dim, half);
 }
 
+// LDS written by a wave's lanes may be read by its others, and the other way round.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The same for a wave's 32 rows from `first` on, through LDS (32 rows of 32 DB elements,
+// the wave's own): a lane holds pieces of its row, and rows are written 16 bytes a lane
+// one after the other. With few queries the gradients of k and v are mostly this.
+template <int DT, int DB, class Row>
+__device__ __forceinline__ void write_rows(const f32x16 *acc, bool on, float mul, char *lds, int dim, int rows, Row to) {
+    using T = typename Num<DT>::T;
+    constexpr int kChunks = DB * 32 * int(sizeof(T)) / 16;
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    const auto at = [&](int r, int c) { return lds + (r * kChunks + (c ^ (r & 3))) * 16; };
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int byte = (32 * d + 2 * i + 4 * half) * int(sizeof(T));
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = on ? acc[d][i + e] * mul : 0.0f;
+            store_n<T, 4>(reinterpret_cast<T *>(at(row, byte / 16) + byte % 16), v);
+        }
+    wave_sync();
+    const int used = dim * int(sizeof(T)) / 16;
+    for (int n = lane; n < rows * used; n += 64) {
+        const int r = n / used, c = n - r * used;
+        *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to(r)) + c * 16) = *reinterpret_cast<const u32x4 *>(at(r, c));
+    }
+    wave_sync();
+}
+
 template <int DT, int DB, bool VEC>
 __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(AttendArgs g) {
     using S = Shape<DT, DB>;
@@ -251,6 +286,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < W::kBlocks; ++n) {
+                if (n > 0 && t * W::kSize + 32 * n >= g.rows) break;       // a block past the last row
                 f32x16 p = S::scores(q, 32 * n, k, zeros());
                 f32x16 ds = S::scores(d, 32 * n, v, zeros());
 #pragma unroll
@@ -273,6 +309,16 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
             if (t + 1 < t1) put(lds + (1 - buffer) * 2 * W::kBytes, stats + (1 - buffer) * 2 * W::kSize);
         }
     }
+    // a key out of use is a zero key here, whose sums are not its gradients
+    if (VEC && sizeof(T) == 2 && g.n_split == 1) {
+        const int first = tile * kOwn + 32 * wave, rows = min(32, g.a.keys - first);
+        char *mine = lds + wave * (32 * 32 * DB * int(sizeof(T)));
+        __syncthreads();                       // the last tile may still be read
+        if (rows <= 0) return;
+        write_rows<DT, DB>(dk, use, g.a.scale, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dk) + at.key(first + r); });
+        write_rows<DT, DB>(dv, use, 1.0f, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dv) + at.key(first + r); });
+        return;
+    }
     if (!in) return;
     float *part_k = nullptr, *part_v = nullptr;
     if (g.n_split > 1) {
@@ -280,7 +326,6 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
         part_k = g.part + split * 2 * all + (int64_t(bh) * g.a.keys + key) * dim;
         part_v = part_k + all;
     }
-    // a key out of use is a zero key here, whose sums are not its gradients
     write_row<DT, DB, VEC>(dk, use, g.a.scale, static_cast<T *>(g.dk) + at.key(key), part_k, dim, half);
     write_row<DT, DB, VEC>(dv, use, 1.0f, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
 }

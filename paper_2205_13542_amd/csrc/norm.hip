@@ -607,7 +607,8 @@ __global__ __launch_bounds__(kSmallBlock) void k_norm_small_grad(NormArgs a) {
 
 constexpr int kSumGrid = 1024;      // workgroups of a sum pass, about
 constexpr int kApplyGrid = 2048;    // workgroups of an apply pass, about
-constexpr int kThreadRows = 8;      // rows of a thread, about, at least
+constexpr int kThreadRows = 8;      // rows of a thread, about, at least,
+constexpr int kLeastGrid = 512;     // unless fewer workgroups than this were left: two to a compute unit
 // Maps that together exceed the 256 MB of cache behind the L2s: results are then
 // written past it, and more of x is still there for the second read.
 constexpr int64_t kCacheBytes = int64_t(256) << 20;
@@ -628,7 +629,8 @@ void split(const bevmap_norm &n, NormArgs *a) {
     int vec = n.x_dtype == BEVPOOL_F32 ? 4 : 8;
     while (n.channels % vec) vec >>= 1;
     const int vectors = n.channels / vec, lanes = vectors < kNormBlock ? kNormBlock / vectors : 1;
-    const int least = kThreadRows * lanes;
+    const int spread = ceil_div(int64_t(n.batch) * n.pixels, kLeastGrid);
+    const int least = kThreadRows * lanes < spread ? kThreadRows * lanes : spread;
     a->chunk = ceil_div(n.pixels, ceil_div(kSumGrid, n.batch));
     if (a->chunk < least) a->chunk = least;
     a->n_chunks = ceil_div(n.pixels, a->chunk);
