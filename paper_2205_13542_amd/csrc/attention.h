@@ -59,7 +59,7 @@ __device__ __forceinline__ f32x16 zeros() {
 // (8 + 8 + 8 of its 24 bits), and six of the nine products of pieces, all but those
 // below 2^-23 of the whole, make a product of fp32 accuracy in 6 / 16 of the time that
 // the fp32 matrix instructions take (32x32x16 in 32 cycles, 32x32x2 in 64): 175, 201 and
-// 154 TFLOP/s forward at 32, 64 and 128 channels, where those reached 118, 127 and 112.
+// 157 TFLOP/s forward at 32, 64 and 128 channels, where those reached 118, 127 and 112.
 //
 // A chunk is 16 bytes of a row in memory: 8 elements of a 16-bit type, 4 of fp32. In
 // step s of a product, K = 16, the two half waves hold elements 16 s + 8 half ..

@@ -8,7 +8,7 @@
 // so the keys are then split over workgroups, and a second kernel joins the parts.
 //
 // A block of 32 rows and 32 keys takes a SIMD 252, 345 and 647 ns for 32, 64 and 128
-// channels of bf16 (530, 780 and 830 TFLOP/s; a library product of 8192^3 reaches
+// channels of bf16 (530, 770 and 850 TFLOP/s; a library product of 8192^3 reaches
 // 1100). 32 channels are bound by the vector unit: 16 exponentials of 3.5 ns and 47
 // other instructions of 1.3 to 2 ns against 4 matrix instructions of 16 ns that mostly
 // overlap; 128 by the matrix cores and the LDS reads that feed them. Scores of the next

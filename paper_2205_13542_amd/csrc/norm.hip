@@ -14,7 +14,7 @@
 // every one of them (360x360x80 fp32 to bf16: 33 us, now 28). The apply pass runs
 // back to front, and the results of maps beyond the cache go past it, so that part of
 // what it reads is still there.
-// Eight frames of 360x360x80 in bf16 take 33 + 56 us forward and 80 + 94 backward: the
+// Eight frames of 360x360x80 in bf16 take 33 + 56 us forward and 80-84 + 94 backward: the
 // 1.33 GB that two passes move, at 4.8 TB/s, what a large copy reaches.
 #include "mapops.h"
 
