@@ -87,6 +87,11 @@ struct Mma {
             }
             return a + b;
         }
+        // whether some value of fp16 is 2 or more: the exponent's highest bit
+        __device__ __forceinline__ bool reaches_two() const {
+            const u32x4 any = half[0] | half[1];
+            return ((any[0] | any[1] | any[2] | any[3]) & 0x40004000u) != 0;
+        }
     };
     // What rows(p) left over: p - rows(p) to another 8 or 11 bits. rows of such a pair cut p off instead of rounding it.
     static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &low) {
@@ -333,6 +338,40 @@ struct Shape {
     }
 };
 
+// The largest of a lane and the lane 32 away, and their sum.
+__device__ __forceinline__ float both_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// fp16 ends at 2^-24, so its probabilities and their gradients are held multiplied by
+// powers of two: probabilities by 2^kRaised, and a row's or key's gradients by one of its
+// own, 2^lift, that starts too large and is lowered when a value reaches 2.
+template <int DT>
+constexpr float kRaised = DT == BEVPOOL_F16 ? 12.0f : 0.0f;
+constexpr float kFirstLift = 60.0f;
+__device__ __forceinline__ float power_of_two(float n) { return ldexpf(1.0f, int(n)); }
+
+// Lowers the lifts of the lanes' columns where x, of them and in both half waves, reaches 2;
+// returns what to multiply the column's sums by, x being multiplied here. To 1/8: what
+// comes is seldom 16 times the largest so far.
+__device__ __forceinline__ float lower(f32x16 &x, float &lift) {
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]));
+    most = both_max(most);
+    const int by = most >= 2.0f ? -3 - __builtin_amdgcn_frexp_expf(most) : 0;
+    lift += float(by);
+    const float mul = ldexpf(1.0f, by);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= mul;
+    return mul;
+}
+
 // Four consecutive channels of a row from channel ch, of dim; VEC: they are
 // aligned and dim is a multiple of four.
 template <bool VEC, class T>
@@ -344,16 +383,6 @@ __device__ __forceinline__ void write4(T *row, int ch, int dim, const float *v) 
         for (int e = 0; e < 4; ++e)
             if (ch + e < dim) row[ch + e] = T(v[e]);
     }
-}
-
-// The largest of a lane and the lane 32 away, and their sum.
-__device__ __forceinline__ float both_max(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float both_sum(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // Sample, key head and its addresses.

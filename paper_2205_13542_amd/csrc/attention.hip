@@ -24,8 +24,12 @@ namespace {
 // tile whose sum for some row passes this (log2: 12) forms the rows' maxima, rescales
 // what is summed and takes its exponentials again. The first tile always does. In
 // between, a tile costs no maximum, and what is lost is nothing: the exponentials
-// keep their relative precision, in fp16 too, whose largest value is 2^16.
-constexpr float kMaxTileSum = 4096.0f;
+// keep their relative precision. Those of fp16, from 2^-24 to 2^16, are taken relative to
+// 2^-7 of the maximum, so that many small ones beside a large one are not lost.
+template <int DT>
+constexpr float kMaxTileSum = DT == BEVPOOL_F16 ? 32768.0f : 4096.0f;
+template <int DT>
+constexpr float kBelowTop = DT == BEVPOOL_F16 ? 7.0f : 0.0f;
 
 // WR waves side by side have rows of their own (4), or all share the tile's rows
 // and split each tile's keys (1).
@@ -120,7 +124,7 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
         float high = s[0];
 #pragma unroll
         for (int i = 0; i < 16; ++i) high = fmaxf(high, s[i]);
-        const float now = fmaxf(top, both_max(high) * c);
+        const float now = fmaxf(top, both_max(high) * c - kBelowTop<DT>);
         const float old = top == -INFINITY ? 0.0f : exp2f(top - now);
         sum *= old;
 #pragma unroll
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT
                     leave_out(s[n], word);
                 }
                 float part = exponentials(s[n], top);
-                if (__builtin_expect(__any(!(part <= kMaxTileSum)), 0)) part = raise(s[n]);
+                if (__builtin_expect(__any(!(part <= kMaxTileSum<DT>)), 0)) part = raise(s[n]);
                 sum += part;
                 S::sums(v, row0 + 32 * n, p, o, kTwo ? &p_low : nullptr);
             }

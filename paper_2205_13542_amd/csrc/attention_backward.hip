@@ -11,10 +11,15 @@
 // five. An axis that is too short to fill the chip has the walk of the other
 // split, and k_attend_add joins the parts.
 //
+// fp16's p and ds are held scaled by powers of two (attention.h): unscaled they end at
+// 2^-24, which probabilities of 10^5 keys are near (dv 5 times as far off as its own
+// rounding; dq of small gradients 37 times). It costs 7 to 10% of the pair's time.
+//
 // p and ds enter their products as two pieces of a 16-bit type: rounded once they
 // left dq, dk and dv of bf16 up to 1.55 times as far off as gradients in fp32 rounded
-// at the end; the pieces cost a quarter of the pair of kernels at large sizes. 4 x 600 queries of 8 heads over 8100
-// masked keys, ragged, 64 channels: dq 61 us and its joining 9, dk and dv 76, two waves
+// at the end; the pieces cost a quarter of the pair of kernels at large sizes.
+//
+// 4 x 600 queries of 8 heads over 8100 masked keys, ragged, 64 channels: dq 61 us and its joining 9, dk and dv 76, two waves
 // a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
 // reaches 360, 450 and 380 TFLOP/s at 32, 64 and 128 channels, five products counted.
 #include "attention.h"
@@ -117,6 +122,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
 #pragma unroll
     for (int i = 0; i < DB; ++i) dq[i] = zeros();
     const float c = g.sign * g.log2_scale;
+    float lift = DT == BEVPOOL_F16 ? kFirstLift : 0.0f;
     Used use = {}, next = {};
     if (t0 < t1) {
         mask.ask(at, t0 * W::kSize);
@@ -148,7 +154,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
                 const f32x16 dp = S::scores(v, 32 * n, d, zeros());
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
+                    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, lift - lse)) * (dp[i] - delta);
                 if (__builtin_expect(word != 0xFFFFFFFFu, 0)) {
                     const uint32_t bits = word >> (4 * half);
 #pragma unroll
@@ -156,6 +162,15 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
                 }
                 typename M::Rows high, low;
                 M::rows_of_two(s, high, low);
+                if constexpr (DT == BEVPOOL_F16)
+                    if (__builtin_expect(__any(high.reaches_two()), 0)) {
+                        const float mul = lower(s, lift);
+#pragma unroll
+                        for (int b = 0; b < DB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) dq[b][i] *= mul;
+                        M::rows_of_two(s, high, low);
+                    }
                 S::sums(k, 32 * n, high, dq, DT == BEVPOOL_F32 ? nullptr : &low);
             }
             if (t + 1 < t1) {
@@ -169,10 +184,10 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     if (!in) return;
     float *part = nullptr;
     if (g.n_split > 1) part = g.part + ((int64_t(split) * n_bh + bh) * g.rows + row) * dim;
-    write_row<DT, DB, VEC>(dq, true, g.a.scale, static_cast<T *>(g.dq) + at.row(row), part, dim, half);
+    write_row<DT, DB, VEC>(dq, true, g.a.scale * power_of_two(-lift), static_cast<T *>(g.dq) + at.row(row), part, dim, half);
 }
 
-// LDS written by a wave's lanes may be read by its others, and the other way round.
+// What a wave's lanes wrote to LDS, its others may now read, and the other way round.
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -255,6 +270,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
             const float none = threadIdx.x < W::kSize ? INFINITY : 0.0f;     // lse, delta of rows past the last
             next_stat = r < g.rows ? (threadIdx.x < W::kSize ? g.lse : g.delta)[at.stat(r)] : none;
             if (next_stat == -INFINITY) next_stat = INFINITY;
+            if (threadIdx.x < W::kSize) next_stat -= kRaised<DT>;
         }
     };
     auto put = [&](char *q, float *stat) {
@@ -271,6 +287,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
 #pragma unroll
     for (int i = 0; i < DB; ++i) dk[i] = dv[i] = zeros();
     const float c = g.sign * g.log2_scale;
+    float lift = DT == BEVPOOL_F16 ? kFirstLift - kRaised<DT> : 0.0f;       // beyond kRaised
     if (t0 < t1) {
         fetch(t0);
         put(lds, stats);
@@ -289,6 +306,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
                 if (n > 0 && t * W::kSize + 32 * n >= g.rows) break;       // a block past the last row
                 f32x16 p = S::scores(q, 32 * n, k, zeros());
                 f32x16 ds = S::scores(d, 32 * n, v, zeros());
+                const float up = power_of_two(lift);
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const float4 l = *reinterpret_cast<const float4 *>(lse + 32 * n + 2 * i);
@@ -298,25 +316,36 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
                     for (int e = 0; e < 4; ++e) {
                         p[i + e] = __builtin_amdgcn_exp2f(fmaf(p[i + e], c, -ls[e]));
                         ds[i + e] = p[i + e] * (ds[i + e] - de[e]);
+                        if constexpr (DT == BEVPOOL_F16) ds[i + e] *= up;
                     }
                 }
                 typename M::Rows high, low;         // two pieces of each, as in k_attend_dq
                 M::rows_of_two(p, high, low);
                 S::sums(d, 32 * n, high, dv, DT == BEVPOOL_F32 ? nullptr : &low);
                 M::rows_of_two(ds, high, low);
+                if constexpr (DT == BEVPOOL_F16)
+                    if (__builtin_expect(__any(high.reaches_two()), 0)) {
+                        const float mul = lower(ds, lift);
+#pragma unroll
+                        for (int b = 0; b < DB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) dk[b][i] *= mul;
+                        M::rows_of_two(ds, high, low);
+                    }
                 S::sums(q, 32 * n, high, dk, DT == BEVPOOL_F32 ? nullptr : &low);
             }
             if (t + 1 < t1) put(lds + (1 - buffer) * 2 * W::kBytes, stats + (1 - buffer) * 2 * W::kSize);
         }
     }
     // a key out of use is a zero key here, whose sums are not its gradients
+    const float of_k = g.a.scale * power_of_two(-lift - kRaised<DT>), of_v = power_of_two(-kRaised<DT>);
     if (VEC && sizeof(T) == 2 && g.n_split == 1) {
         const int first = tile * kOwn + 32 * wave, rows = min(32, g.a.keys - first);
         char *mine = lds + wave * (32 * 32 * DB * int(sizeof(T)));
         __syncthreads();                       // the last tile may still be read
         if (rows <= 0) return;
-        write_rows<DT, DB>(dk, use, g.a.scale, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dk) + at.key(first + r); });
-        write_rows<DT, DB>(dv, use, 1.0f, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dv) + at.key(first + r); });
+        write_rows<DT, DB>(dk, use, of_k, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dk) + at.key(first + r); });
+        write_rows<DT, DB>(dv, use, of_v, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dv) + at.key(first + r); });
         return;
     }
     if (!in) return;
@@ -326,8 +355,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
         part_k = g.part + split * 2 * all + (int64_t(bh) * g.a.keys + key) * dim;
         part_v = part_k + all;
     }
-    write_row<DT, DB, VEC>(dk, use, g.a.scale, static_cast<T *>(g.dk) + at.key(key), part_k, dim, half);
-    write_row<DT, DB, VEC>(dv, use, 1.0f, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
+    write_row<DT, DB, VEC>(dk, use, of_k, static_cast<T *>(g.dk) + at.key(key), part_k, dim, half);
+    write_row<DT, DB, VEC>(dv, use, of_v, static_cast<T *>(g.dv) + at.key(key), part_v, dim, half);
 }
 
 // Joins parts, one thread to an element: of the gradient of q (grid z 0), k (1) and v (2).

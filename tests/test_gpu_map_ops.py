@@ -372,6 +372,47 @@ def test_cross_attention_large_scores(torch, bev, dt):
         _check("out", got, ref[0], ref[1] * (1 + 16 * U32) + _u(dt) * (ref[0].abs() + ref[1]) + _tiny(dt))
 
 
+@pytest.mark.parametrize("N,B,M", [(1, 1, 2 ** 20), (64, 1, 2 ** 20), (1, 2048, 2 ** 17), (64, 2048, 2 ** 17)])
+def test_cross_attention_many_small_probabilities(torch, bev, N, B, M):
+    """fp16: one key of nearly all the weight, and many whose little adds up; many samples so that one
+    workgroup walks all keys. Each small probability may be off by 2^-32 of the largest, half of fp16's
+    last place 2^-24 where that one is held as 2^7."""
+    D = 32
+    q = torch.zeros((1, N, 1, D), device="cuda", dtype=torch.float16)
+    q[..., 0] = 4.0
+    k = torch.zeros((1, M, 1, D), device="cuda", dtype=torch.float16)
+    k[0, 5, 0, 0] = 4.35
+    v = torch.ones((1, M, 1, D), device="cuda", dtype=torch.float16)
+    v[0, 5] = 0.0
+    q, k, v = (t.expand(B, -1, -1, -1) for t in (q, k, v))
+    got = bev.cross_attention(q, k, v, scale=1.0).double()
+    gap = 4.0 * float(k[0, 5, 0, 0])
+    ref = (M - 1) / (M - 1 + math.exp(gap))
+    assert (got - ref).abs().max() <= M * 2.0 ** -32 + 2.0 ** -11 * ref
+
+
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -10])
+@pytest.mark.parametrize("N,D", [(4, 64), (320, 64), (160, 128), (70, 84)])
+def test_cross_attention_gradients_of_many_keys(torch, bev, N, D, size):
+    """fp16: gradients are as good as the type's own rounding lets them be where probabilities, or
+    the gradient of out, are near its least values. Beside that rounding: 2^-21 of a row's or key's
+    largest term in each (two pieces, the largest being held at 2^-4 or more), with the spread
+    of the terms, their sums in fp32, delta's part of the rounding of out: 2^-12 of each norm."""
+    M = 100_003
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    q, k, v, dout = (torch.randn((1, n, 1, D), generator=gen, device="cuda").half().requires_grad_() for n in (N, M, M, N))
+    dout = (dout.detach() * size)
+    scale = D ** -0.5
+    got = torch.autograd.grad(bev.cross_attention(q, k, v, scale=scale), (q, k, v), dout)
+    Q, K, V, dO = (t.detach()[0, :, 0].double() for t in (q, k, v, dout))
+    p = torch.softmax(scale * Q @ K.T, 1)
+    ds = p * (dO @ V.T - (dO * (p @ V)).sum(1, keepdim=True))
+    for name, g, ref in zip(("dq", "dk", "dv"), got, (scale * ds @ K, scale * ds.T @ Q, p.T @ dO)):
+        off, rounding = (g[0, :, 0].double() - ref).norm(), (ref.half().double() - ref).norm()
+        print(f"{name}: {off / ref.norm():.2e}, rounding {rounding / ref.norm():.2e}")
+        assert off <= 1.1 * rounding + 2.0 ** -12 * ref.norm(), name
+
+
 def test_cross_attention_broadcast_states(torch, bev):
     """States shared over samples and heads by expanding: gradients sum over the copies."""
     q, k, v, dout, _, _ = _attend_inputs(torch, 3, 20, 70, 4, 4, 16, "f32", "plain", None, None)
