@@ -23,6 +23,8 @@ _ACTS = {"none": _map_binding.BEVMAP_ACT_NONE, "relu": _map_binding.BEVMAP_ACT_R
 _CODES = {torch.float32: _binding.BEVPOOL_F32, torch.bfloat16: _binding.BEVPOOL_BF16,
           torch.float16: _binding.BEVPOOL_F16}
 
+_MOST = (1 << 31) - 1       # of a size in the C descriptions, where ctypes would wrap it round
+
 
 def _refuse(message, code=_binding.BEVPOOL_ERR_INVALID_ARG):
     raise BevpoolError(code, message)
@@ -99,6 +101,9 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
         _refuse(f"act must be one of {', '.join(_ACTS)}")
     shape = x.shape
     B, C = shape[0], shape[-1]
+    pixels = math.prod(shape[1:-1])
+    if B > _MOST or pixels > _MOST or C > _MOST or not -_MOST <= groups <= _MOST:
+        _refuse(f"x {tuple(shape)}, groups={groups}: too large", _binding.BEVPOOL_ERR_OVERFLOW)
     for t, name in ((weight, "weight"), (bias, "bias")):
         if t is not None and (t.dim() != 1 or t.shape[0] != C or not t.is_contiguous()):
             _refuse(f"{name} must be a contiguous tensor of {C} elements", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
@@ -109,7 +114,7 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
         _refuse("rows of x must be evenly spaced, their channels adjacent")
     w_like = weight if weight is not None else bias
     out_dtype = out_dtype or x.dtype
-    norm = _map_binding.bevmap_norm(B, math.prod(shape[1:-1]), C, groups, stride, eps, act, _code(x.dtype),
+    norm = _map_binding.bevmap_norm(B, pixels, C, groups, stride, eps, act, _code(x.dtype),
                                     _code(out_dtype),
                                     _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
     size = _map_binding.bevmap_group_norm_workspace(norm, False)
@@ -146,6 +151,8 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
     if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
         _refuse(f"q {tuple(shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit",
                 _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+    if B > _MOST or N > _MOST or M > _MOST or H > _MOST or K > _MOST or D > _MOST:
+        _refuse(f"q {tuple(shape)}, k {tuple(k.shape)}: too large", _binding.BEVPOOL_ERR_OVERFLOW)
     dtype = q.dtype
     if k.dtype != dtype or v.dtype != dtype:
         _refuse("q, k and v must share a dtype", _binding.BEVPOOL_ERR_UNSUPPORTED_DTYPE)

@@ -676,3 +676,21 @@ def test_refusals(torch, bev):
         with pytest.raises(bev.BevpoolError):
             call()
             print(f"call {i} was not refused", flush=True)
+
+
+def test_refusals_of_sizes_past_32_bits(torch, bev):
+    """Sizes that would be small again if their upper bits were lost."""
+    n = 2 ** 32 + 8
+    q, k = torch.zeros((1, 1, 1, 8), device="cuda"), torch.zeros((1, 1, 1, 8), device="cuda")
+    cells = torch.empty((1, n, 1), dtype=torch.float16, device="cuda")
+    bad = [
+        lambda: bev.group_norm_act(cells, 1),
+        lambda: bev.group_norm_act(torch.zeros(1, 4, 8, device="cuda"), n),
+        lambda: bev.cross_attention(q, k.expand(-1, n, -1, -1), k.expand(-1, n, -1, -1)),
+        lambda: bev.cross_attention(q.expand(-1, n, -1, -1), k, k),
+        lambda: bev.cross_attention(q.expand(-1, -1, n, -1), k, k),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(bev.BevpoolError):
+            call()
+            print(f"call {i} was not refused", flush=True)
