@@ -14,7 +14,7 @@
 // overlap; 128 by the matrix cores and the LDS reads that feed them. Scores of the next
 // block formed ahead of a block's exponentials, the usual order and one block held
 // back were within 5% of each other. One query over 129600 keys (46 MB in use) takes
-// 17 us and its joining 8; 32400 queries over 16896 keys, 4 heads of 32: 457.
+// 17 us and its joining 5; 32400 queries over 16896 keys, 4 heads of 32: 457.
 #include "attention.h"
 
 namespace bevmap {

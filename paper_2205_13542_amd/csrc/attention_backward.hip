@@ -19,8 +19,8 @@
 // left dq, dk and dv of bf16 up to 1.55 times as far off as gradients in fp32 rounded
 // at the end; the pieces cost a quarter of the pair of kernels at large sizes.
 //
-// 4 x 600 queries of 8 heads over 8100 masked keys, ragged, 64 channels: dq 61 us and its joining 9, dk and dv 76, two waves
-// a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
+// 4 x 600 queries of 8 heads over 8100 masked keys, ragged, 64 channels: dq 61 us and
+// its joining 9, dk and dv 74, two waves a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
 // reaches 360, 450 and 380 TFLOP/s at 32, 64 and 128 channels, five products counted.
 #include "attention.h"
 
