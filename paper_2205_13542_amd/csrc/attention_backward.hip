@@ -193,15 +193,20 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// Chunk c of row r of a wave's 32 rows in LDS.
+template <int DT, int DB>
+__device__ __forceinline__ int wave_chunk(int r, int c) {
+    return (r * (DB * 32 * int(sizeof(typename Num<DT>::T)) / 16) + (c ^ (r & 3))) * 16;
+}
+
 // The same for a wave's 32 rows from `first` on, through LDS (32 rows of 32 DB elements,
 // the wave's own): a lane holds pieces of its row, and rows are written 16 bytes a lane
 // one after the other. With few queries the gradients of k and v are mostly this.
-template <int DT, int DB, class Row>
+template <int DT, int DB, class Unit, class Row>
 __device__ __forceinline__ void write_rows(const f32x16 *acc, bool on, float mul, char *lds, int dim, int rows, Row to) {
     using T = typename Num<DT>::T;
-    constexpr int kChunks = DB * 32 * int(sizeof(T)) / 16;
     const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
-    const auto at = [&](int r, int c) { return lds + (r * kChunks + (c ^ (r & 3))) * 16; };
+    const auto at = [&](int r, int c) { return lds + wave_chunk<DT, DB>(r, c); };
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -213,10 +218,35 @@ __device__ __forceinline__ void write_rows(const f32x16 *acc, bool on, float mul
             store_n<T, 4>(reinterpret_cast<T *>(at(row, byte / 16) + byte % 16), v);
         }
     wave_sync();
-    const int used = dim * int(sizeof(T)) / 16;
+    constexpr int kUnit = int(sizeof(Unit));
+    const int used = dim * int(sizeof(T)) / kUnit;
     for (int n = lane; n < rows * used; n += 64) {
-        const int r = n / used, c = n - r * used;
-        *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to(r)) + c * 16) = *reinterpret_cast<const u32x4 *>(at(r, c));
+        const int r = n / used, byte = (n - r * used) * kUnit;
+        Unit x;
+        __builtin_memcpy(&x, at(r, byte / 16) + byte % 16, kUnit);
+        *reinterpret_cast<Unit *>(reinterpret_cast<char *>(to(r)) + byte) = x;
+    }
+    wave_sync();
+}
+// And the other way: a lane's row as an operand of scores(), read by the wave a unit a lane.
+template <int DT, int DB, class Unit, class Row>
+__device__ __forceinline__ void read_rows(u32x4 *y, bool use, char *lds, int dim, int rows, Row from) {
+    using S = Shape<DT, DB>;
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    constexpr int kUnit = int(sizeof(Unit)), kUnits = S::kUsed * 16 / kUnit;
+    const int used = dim * int(sizeof(typename S::T)) / kUnit;
+    for (int n = lane; n < 32 * kUnits; n += 64) {
+        const int r = n / kUnits, c = n - r * kUnits, byte = c * kUnit;
+        Unit x = 0;
+        if (r < rows && c < used) x = *reinterpret_cast<const Unit *>(reinterpret_cast<const char *>(from(r)) + byte);
+        __builtin_memcpy(lds + wave_chunk<DT, DB>(r, byte / 16) + byte % 16, &x, kUnit);
+    }
+    wave_sync();
+#pragma unroll
+    for (int s = 0; s < S::kSteps; ++s) {
+        u32x4 x = {0, 0, 0, 0};
+        if (use) x = *reinterpret_cast<const u32x4 *>(lds + wave_chunk<DT, DB>(row, 2 * s + half));
+        y[s] = x;
     }
     wave_sync();
 }
@@ -344,8 +374,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
         char *mine = lds + wave * (32 * 32 * DB * int(sizeof(T)));
         __syncthreads();                       // the last tile may still be read
         if (rows <= 0) return;
-        write_rows<DT, DB>(dk, use, of_k, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dk) + at.key(first + r); });
-        write_rows<DT, DB>(dv, use, of_v, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dv) + at.key(first + r); });
+        write_rows<DT, DB, u32x4>(dk, use, of_k, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dk) + at.key(first + r); });
+        write_rows<DT, DB, u32x4>(dv, use, of_v, mine, dim, rows, [&](int r) { return static_cast<T *>(g.dv) + at.key(first + r); });
         return;
     }
     if (!in) return;
@@ -364,6 +394,8 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
 // three waves to a SIMD where k_attend_dkv has one, the memory, which bounds it, is kept
 // busy: 2 x 40000 keys of 8 heads, bf16, 64 channels 72 us, now 62, 128 channels 220, now
 // 136 (656 MB read and written, 4.8 TB/s); fp32 220, now 152, and 552, now 368.
+// 16-bit rows that do not start on 16 bytes go through LDS both ways (84 channels: 400,
+// now 258).
 constexpr int kFewRows = 32;
 template <int DT, int DB>
 struct Few {
@@ -394,9 +426,23 @@ __global__ __launch_bounds__(kAttendBlock, (Few<DT, DB>::kWaves)) void k_attend_
     u32x4 k[S::kOperand], v[S::kOperand];
 #pragma unroll
     for (int s = 0; s < S::kOperand; ++s) k[s] = v[s] = u32x4{0, 0, 0, 0};
-    if (use) {
-        S::template operand<VEC>(at.k(key), half, dim, g.pairs, k);
-        S::template operand<VEC>(at.v(key), half, dim, g.pairs, v);
+    const int first = tile * kOwn + 32 * wave, rows = min(32, g.a.keys - first);
+    char *mine = lds + F::kRead + wave * (F::kWrite / 4);
+    if constexpr (VEC || DT == BEVPOOL_F32) {
+        if (use) {
+            S::template operand<VEC>(at.k(key), half, dim, g.pairs, k);
+            S::template operand<VEC>(at.v(key), half, dim, g.pairs, v);
+        }
+    } else {
+        const auto key_row = [&](int r) { return at.k(first + r); };
+        const auto value_row = [&](int r) { return at.v(first + r); };
+        if (g.pairs) {
+            read_rows<DT, DB, uint32_t>(k, use, mine, dim, rows, key_row);
+            read_rows<DT, DB, uint32_t>(v, use, mine, dim, rows, value_row);
+        } else {
+            read_rows<DT, DB, uint16_t>(k, use, mine, dim, rows, key_row);
+            read_rows<DT, DB, uint16_t>(v, use, mine, dim, rows, value_row);
+        }
     }
     for (int n = threadIdx.x; n < kFewRows * S::kUsed; n += kAttendBlock) {
         const int r = n / S::kUsed, c = n % S::kUsed;
@@ -433,14 +479,17 @@ __global__ __launch_bounds__(kAttendBlock, (Few<DT, DB>::kWaves)) void k_attend_
             ds[i + e] = p[i + e] * (ds[i + e] - delta[4 * half + 2 * i + e]);
             if constexpr (DT == BEVPOOL_F16) ds[i + e] *= up;
         }
-    const int first = tile * kOwn + 32 * wave, rows = min(32, g.a.keys - first);
-    char *mine = lds + F::kRead + wave * (F::kWrite / 4);
     f32x16 sum[DB];
     auto write = [&](void *to, float mul) {
         T *rows_of = static_cast<T *>(to);
         if constexpr (VEC && DT != BEVPOOL_F32)
-            write_rows<DT, DB>(sum, use, mul, mine, dim, rows, [&](int r) { return rows_of + at.key(first + r); });
-        else if (in)
+            write_rows<DT, DB, u32x4>(sum, use, mul, mine, dim, rows, [&](int r) { return rows_of + at.key(first + r); });
+        else if constexpr (DT != BEVPOOL_F32) {
+            if (g.pairs)
+                write_rows<DT, DB, uint32_t>(sum, use, mul, mine, dim, rows, [&](int r) { return rows_of + at.key(first + r); });
+            else
+                write_rows<DT, DB, uint16_t>(sum, use, mul, mine, dim, rows, [&](int r) { return rows_of + at.key(first + r); });
+        } else if (in)
             write_row<DT, DB, VEC>(sum, use, mul, rows_of + at.key(key), nullptr, dim, half);
     };
     typename M::Rows high, low;

@@ -347,6 +347,22 @@ def test_cross_attention(torch, bev, B, N, M, H, K, D, dt, layout, lengths, mask
     assert all(torch.equal(a, g) for a, g in zip(again, grads))
 
 
+@pytest.mark.parametrize("B,N,M,H,K,D,dt,layout,lengths,mask", [
+    (2, 5, 300, 4, 2, 53, "bf16", "odd", [300, 131], "random"),
+    (2, 1, 701, 4, 1, 84, "f16", "plain", [700, 3], "runs"),
+    (1, 3, 129, 6, 3, 84, "bf16", "packed", None, None),
+    (3, 8, 257, 4, 1, 128, "bf16", "packed", [257, 0, 90], "random"),
+    (1, 16, 1000, 4, 2, 128, "f16", "heads_first", None, "random"),
+    (2, 2, 333, 4, 4, 128, "f32", "plain", None, "runs"),
+    (1, 4, 95, 2, 1, 101, "f32", "odd", [64], None),
+    (1, 32, 130, 2, 2, 96, "f16", "plain", None, None),
+    (1, 7, 64, 3, 3, 1, "f16", "odd", None, "random"),
+])
+def test_cross_attention_of_few_rows(torch, bev, B, N, M, H, K, D, dt, layout, lengths, mask):
+    """At most 32 rows to a key head, whose gradients have a kernel of their own."""
+    test_cross_attention(torch, bev, B, N, M, H, K, D, dt, layout, lengths, mask)
+
+
 def test_cross_attention_empty(torch, bev):
     for B, N, M in ((0, 3, 4), (2, 0, 4), (2, 3, 0)):
         q = torch.randn(B, N, 2, 8, device="cuda", requires_grad=True)
