@@ -9,7 +9,7 @@
 // walks the keys, k_attend_dkv owns a tile of keys and walks the rows of all heads
 // that share them. Scores are formed in both, seven products in place of
 // five. An axis that is too short to fill the chip has the walk of the other
-// split, and k_attend_add joins the parts.
+// split, and k_attend_add joins the parts. Few rows take k_attend_dkv_few.
 //
 // fp16's p and ds are held scaled by powers of two (attention.h): unscaled they end at
 // 2^-24, which probabilities of 10^5 keys are near (dv 5 times as far off as its own
