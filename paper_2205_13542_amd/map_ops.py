@@ -5,7 +5,8 @@
     tokens = dropout_add(heard, 0.1, seed, step, residual=tokens)
 
 Each runs in libbevpool.so (include/bevmap.h) on the current stream of its
-inputs' device, and is differentiable. Temporaries come from torch's allocator.
+inputs' device, and is differentiable (backwards; inputs with a tangent of
+torch.autograd.forward_ad are refused). Temporaries come from torch's allocator.
 There is no CPU form: tensors elsewhere are refused with a BevpoolError, as
 are types and layouts that a call does not take (nothing is copied silently).
 """
@@ -14,6 +15,7 @@ from __future__ import annotations
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _binding, _map_binding
 from ._binding import BevpoolError
@@ -263,6 +265,11 @@ class _DropoutAdd(torch.autograd.Function):
 
 
 def _learns(*tensors) -> bool:
+    """Whether a call has to go through its autograd function: where a gradient is asked for,
+    and while a level of forward-mode differentiation is open, so that a tangent among the
+    inputs is refused there (the operators have no forward-mode form) and not dropped."""
+    if forward_ad._current_level >= 0:
+        return True
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:

@@ -129,3 +129,28 @@ def test_python_entries_refuse():
     for p, seed, offset in ((-0.1, 0, 0), (1.5, 0, 0), (float("nan"), 0, 0), (0.1, -1, 0), (0.1, 0, 1 << 64)):
         with pytest.raises(bev.BevpoolError, match="outside|must be in"):
             bev.dropout_add(x, p, seed, offset)
+
+
+def test_forward_mode_is_refused(monkeypatch):
+    """An input with a tangent is refused, with gradients enabled or not; the launches are stubs."""
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import map_ops
+    from torch.autograd import forward_ad
+    monkeypatch.setattr(map_ops, "_norm_forward", lambda x, *a: (x.clone(), x.clone(), None))
+    monkeypatch.setattr(map_ops, "_attend_forward", lambda q, *a: (q.clone(), None, q.clone(), None))
+    monkeypatch.setattr(map_ops, "_dropout", lambda x, *a: x.clone())
+    x, q = torch.ones(2, 3, 8), torch.ones(1, 2, 2, 4)
+    with forward_ad.dual_level():
+        xd, qd = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, q))
+        w = forward_ad.make_dual(torch.ones(8), torch.ones(8))
+        for call in (lambda: bev.group_norm_act(xd, 2), lambda: bev.group_norm_act(x, 2, w),
+                     lambda: bev.cross_attention(qd, q, q), lambda: bev.cross_attention(q, q, qd),
+                     lambda: bev.dropout_add(xd, 0.1, 3), lambda: bev.dropout_add(x, 0.1, 3, residual=xd)):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+        # inputs without a tangent work
+        assert torch.equal(bev.group_norm_act(x, 2), x) and not bev.dropout_add(x, 0.1, 3).requires_grad
+    assert torch.equal(bev.cross_attention(q, q, q), q)
