@@ -8,7 +8,9 @@ the points of each cell are summed. The work runs in libbevpool.so
 package is the thin binding: ``_binding`` mirrors the C calls one to one, and
 ``Plan`` adds torch tensor plumbing (device memory and the current stream
 only). ``group_norm_act``, ``cross_attention`` and ``dropout_add`` are the
-operators of a model that reads the pooled map (include/bevmap.h). There is no CPU fallback. A missing library raises ImportError.
+operators of a model that reads the pooled map (``map_ops``, include/bevmap.h).
+There is no CPU fallback. A missing library raises ImportError. torch is
+imported where a call needs it, not before.
 """
 from __future__ import annotations
 
@@ -34,19 +36,6 @@ __all__ = [
     "bevpool_associate_noalloc", "associate_noalloc", "bevpool_plan_slabs",
     "group_norm_act", "cross_attention", "dropout_add",
 ]
-
-_MAP_OPS = ("group_norm_act", "cross_attention", "dropout_add")
-
-
-def __getattr__(name):
-    """The map operators, whose module needs torch where the rest of the package
-    needs it only when called."""
-    if name in _MAP_OPS:
-        from . import map_ops
-        globals().update((n, getattr(map_ops, n)) for n in _MAP_OPS)
-        return globals()[name]
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-
 
 _GEOM_FIELDS = [f for f, _ in bevpool_geometry._fields_]
 
@@ -347,3 +336,29 @@ def bev_pool(depth_prob, cam_feat, plan):
     if _BEVPOOL_FN is None:
         _BEVPOOL_FN = _autograd_function()
     return _BEVPOOL_FN.apply(depth_prob, cam_feat, plan)
+
+
+_MAP_OPS = None
+
+
+def _map_ops():
+    global _MAP_OPS
+    if _MAP_OPS is None:
+        from . import map_ops
+        _MAP_OPS = map_ops
+    return _MAP_OPS
+
+
+def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", out_dtype=None):
+    """Group norm over a map with an activation, channels last: ``map_ops.group_norm_act``."""
+    return _map_ops().group_norm_act(x, groups, weight, bias, eps, act, out_dtype)
+
+
+def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
+    """Attention of queries to a map's cells or other states: ``map_ops.cross_attention``."""
+    return _map_ops().cross_attention(q, k, v, scale, key_lengths, key_mask)
+
+
+def dropout_add(x, p, seed, offset=0, residual=None):
+    """residual + dropout(x), the mask drawn where it is used: ``map_ops.dropout_add``."""
+    return _map_ops().dropout_add(x, p, seed, offset, residual)

@@ -1,8 +1,11 @@
 """Host-side checks of the map operators (no GPU needed): the library exports
 what include/bevmap.h declares, and refuses bad arguments before any device work."""
 import ctypes
+import inspect
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 
@@ -154,3 +157,31 @@ def test_forward_mode_is_refused(monkeypatch):
         # inputs without a tangent work
         assert torch.equal(bev.group_norm_act(x, 2), x) and not bev.dropout_add(x, 0.1, 3).requires_grad
     assert torch.equal(bev.cross_attention(q, q, q), q)
+
+
+def test_star_import_needs_no_torch():
+    """Nor does it import torch where there is one; the map operators ask for it when called."""
+    code = """
+import sys
+sys.modules["torch"] = None            # an import of torch raises ImportError
+from paper_2205_13542_amd import *
+assert bevpool_version() and callable(Plan)
+for call in (lambda: group_norm_act(None, 1), lambda: cross_attention(None, None, None),
+             lambda: dropout_add(None, 0.1, 3)):
+    try:
+        call()
+    except ImportError:
+        continue
+    raise SystemExit("a map operator ran without torch")
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
+
+
+def test_package_names_are_the_map_operators():
+    pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import map_ops
+    for name in ("group_norm_act", "cross_attention", "dropout_add"):
+        assert name in bev.__all__
+        assert inspect.signature(getattr(bev, name)) == inspect.signature(getattr(map_ops, name))
