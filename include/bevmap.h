@@ -125,7 +125,7 @@ BEVPOOL_API int64_t bevmap_attention_workspace(const bevmap_attend *attend, int3
  *  lse:       device float [batch][heads][queries], or NULL; overwritten with
  *             log2 of the sum of e^s, -infinity where no key is in use.
  * Scores, softmax statistics and output sums are fp32; fp32 inputs are multiplied
- * as sums of three bf16 pieces each, to fp32 accuracy. With 16-bit inputs the
+ * as sums of three bf16 pieces each, which leaves out at most 2^-24 of a product. With 16-bit inputs the
  * probabilities, relative to a maximum of the row, are rounded to the inputs'
  * type for their product with v (of at most 32 rows, that is queries * heads /
  * key_heads, to two pieces of the type).

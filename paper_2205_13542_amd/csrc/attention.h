@@ -56,10 +56,14 @@ __device__ __forceinline__ f32x16 zeros() {
 }
 
 // fp32 goes through the bf16 matrix cores: x is the sum of three bf16 pieces, exactly
-// (8 + 8 + 8 of its 24 bits), and six of the nine products of pieces, all but those
-// below 2^-23 of the whole, make a product of fp32 accuracy in 6 / 16 of the time that
-// the fp32 matrix instructions take (32x32x16 in 32 cycles, 32x32x2 in 64): 175, 201 and
-// 157 TFLOP/s forward at 32, 64 and 128 channels, where those reached 118, 127 and 112.
+// (8 + 8 + 8 of its 24 bits), each what the ones before leave rounded to nearest, so that
+// a second piece is at most 2^-8 of its number and a third 2^-17. Six of the nine products
+// of pieces are formed; the others together are at most 2^-24 of the product, of either
+// sign. (Pieces cut off towards zero take 3 to 7% less time, but leave out up to 2^-21,
+// all with the product's own sign.) That takes 6 / 16 of the time of the fp32 matrix
+// instructions (32x32x16 in 32 cycles, 32x32x2 in 64): 143, 181 and 150 TFLOP/s forward
+// at 32, 64 and 128 channels (4096 rows, 8192 keys, 8 heads), where those reached 118,
+// 127 and 112.
 //
 // A chunk is 16 bytes of a row in memory: 8 elements of a 16-bit type, 4 of fp32. In
 // step s of a product, K = 16, the two half waves hold elements 16 s + 8 half ..
@@ -145,15 +149,22 @@ struct Mma {
         return r;
     }
 };
-// The three pieces of a pair of fp32 numbers.
+// The three pieces of a pair of fp32 numbers. ANY: the numbers may be so large that
+// bf16 would round them to infinity, and are held to its largest there.
+template <bool ANY>
 __device__ __forceinline__ void three_pieces(float x, float y, uint32_t *piece) {
     using Two = __bf16 __attribute__((ext_vector_type(2)));
-    piece[0] = cut_pair(x, y);
-    x = left_of(x);
-    y = left_of(y);
-    piece[1] = cut_pair(x, y);
-    const Two last = {__bf16(left_of(x)), __bf16(left_of(y))};
-    piece[2] = __builtin_bit_cast(uint32_t, last);
+    constexpr float kMost = 0x1.FEp127f;
+    Two p = {__bf16(ANY ? __builtin_amdgcn_fmed3f(x, -kMost, kMost) : x),
+             __bf16(ANY ? __builtin_amdgcn_fmed3f(y, -kMost, kMost) : y)};
+    piece[0] = __builtin_bit_cast(uint32_t, p);
+#pragma unroll
+    for (int k = 1; k < 3; ++k) {
+        x -= __uint_as_float(piece[k - 1] << 16);
+        y -= __uint_as_float(piece[k - 1] & 0xFFFF0000u);
+        p = Two{__bf16(x), __bf16(y)};
+        piece[k] = __builtin_bit_cast(uint32_t, p);
+    }
 }
 template <>
 struct Mma<BEVPOOL_F32> {
@@ -174,6 +185,8 @@ struct Mma<BEVPOOL_F32> {
         c = Piece::mul(a[0], b1, c);
         return Piece::mul(a[0], b0, c);
     }
+    // ANY: p may be of any size (three_pieces)
+    template <bool ANY = false>
     static __device__ __forceinline__ Rows rows(const f32x16 &p) {
         Rows r;
         float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -183,13 +196,13 @@ struct Mma<BEVPOOL_F32> {
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
             uint32_t piece[3];
-            three_pieces(p[i], p[i + 1], piece);
+            three_pieces<ANY>(p[i], p[i + 1], piece);
 #pragma unroll
             for (int k = 0; k < 3; ++k) r.piece[k][i >> 3][(i & 7) >> 1] = piece[k];
         }
         return r;
     }
-    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &) { high = rows(p); }
+    static __device__ __forceinline__ void rows_of_two(const f32x16 &p, Rows &high, Rows &) { high = rows<true>(p); }
 };
 
 // Layout of a tile in LDS: rows of CH chunks (a power of two; of fp32 one such row
@@ -254,7 +267,7 @@ struct Shape {
             uint32_t piece[2][3];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                three_pieces(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), piece[i]);
+                three_pieces<true>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), piece[i]);
             char *to = tile + chunk_at(row, c >> 1) + (c & 1) * 8;
 #pragma unroll
             for (int k = 0; k < 3; ++k)
@@ -275,7 +288,7 @@ struct Shape {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t piece[3];
-                        three_pieces(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), piece);
+                        three_pieces<true>(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), piece);
 #pragma unroll
                         for (int k = 0; k < 3; ++k) y[k * kSteps + s][2 * i + j] = piece[k];
                     }

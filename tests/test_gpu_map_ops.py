@@ -388,6 +388,37 @@ def test_cross_attention_large_scores(torch, bev, dt):
         _check("out", got, ref[0], ref[1] * (1 + 16 * U32) + _u(dt) * (ref[0].abs() + ref[1]) + _tiny(dt))
 
 
+@pytest.mark.parametrize("copies", [1, 40])
+def test_cross_attention_products_of_fp32(torch, bev, copies):
+    """Scores 2^20 (x y - c), c = x y rounded to fp32, so that errors of the products show in the softmax of
+    two keys, the second of score 0. Of x y a product may leave out 2^-24 (a little over); c goes in whole; and of the
+    two products' sum each of two additions may round, or cut off, magnitudes of up to 2 x y: 4 times 2^-24 of
+    x y, and 2^-7 of that for the pieces' sums before. In all less than 5.5 times 2^-24."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    B = 4096
+    x, y = (1 + torch.rand(B, generator=gen, device="cuda") * s for s in (2.0 ** -7, 2.0 ** -7))
+    x[: B // 2] = 1 + torch.rand(B // 2, generator=gen, device="cuda")
+    x[0] = y[0] = 1 + 2.0 ** -7 - 2.0 ** -23
+    c = x * y
+    q = torch.stack((x, -torch.ones_like(x)), 1).view(B, 1, 1, 2).repeat(1, copies, 1, 1)
+    k = torch.stack((torch.stack((y, c), 1), torch.zeros(B, 2, device="cuda")), 1).view(B, 2, 1, 2)
+    v = torch.tensor([1.0, 0.0], device="cuda").view(1, 2, 1, 1).repeat(B, 1, 1, 2)
+    p = bev.cross_attention(q, k, v, scale=2.0 ** 20)[:, -1, 0, 0].double()
+    xy = x.double() * y.double()
+    # p is off by some 2^-23 of itself, which is nothing beside the bound
+    off = (torch.log(p / (1 - p)) / 2.0 ** 20 - (xy - c.double())).abs() / xy
+    assert off.max() <= 5.5 * U32, f"{float(off.max() / U32):.3g}"
+
+
+def test_cross_attention_of_the_largest_fp32(torch, bev):
+    """Values that the nearest bf16 would turn into infinity come out as they are."""
+    most = torch.finfo(torch.float32).max
+    v = torch.tensor([most, -most, 0.998 * most, 1.0], device="cuda").view(1, 1, 1, 4)
+    q, k = torch.ones(1, 1, 1, 4, device="cuda"), torch.ones(1, 1, 1, 4, device="cuda")
+    assert torch.equal(bev.cross_attention(q, k, v), v)
+    assert torch.equal(bev.cross_attention(q.expand(1, 50, 1, 4), k, v), v.expand(1, 50, 1, 4))
+
+
 @pytest.mark.parametrize("N,B,M", [(1, 1, 2 ** 20), (64, 1, 2 ** 20), (1, 2048, 2 ** 17), (64, 2048, 2 ** 17)])
 def test_cross_attention_many_small_probabilities(torch, bev, N, B, M):
     """fp16: one key of nearly all the weight, and many whose little adds up; many samples so that one
