@@ -134,7 +134,8 @@ BEVPOOL_API int64_t bevmap_attention_workspace(const bevmap_attend *attend, int3
  * below 1, heads not a multiple of key_heads, scale not finite, a stride below
  * 0, workspace too small or not 16-byte aligned), UNSUPPORTED_DTYPE, OVERFLOW (dim above 128, batch * key_heads above
  * 65535, queries * heads / key_heads or keys reaching 2^30, k_row or v_row
- * reaching 2^22), HIP (launch failure).
+ * reaching 2^22, batch * key_heads * the tiles of 128 that queries * heads /
+ * key_heads make reaching 2^23), HIP (launch failure).
  */
 BEVPOOL_API int bevmap_attention(const bevmap_attend *attend, const void *q, const void *k, const void *v,
                                  const int32_t *key_lengths, const uint8_t *key_mask, void *out,
@@ -150,7 +151,8 @@ BEVPOOL_API int bevmap_attention(const bevmap_attend *attend, const void *q, con
  * out_low may be NULL (out is then taken as it is). Sums are fp32; with 16-bit types
  * the probabilities and the scores' gradients enter their products as two pieces
  * of the type.
- * Errors: those of bevmap_attention.
+ * Errors: those of bevmap_attention, and OVERFLOW where batch * key_heads * the tiles
+ * of 128 that the keys make reach 2^23 (bevmap_attention_workspace says so as well).
  */
 BEVPOOL_API int bevmap_attention_backward(const bevmap_attend *attend, const void *grad_out, const void *q,
                                           const void *k, const void *v, const int32_t *key_lengths,

@@ -370,7 +370,7 @@ void partition(const bevmap_attend &a, bool lengths, AttendArgs *g, bool *few) {
     const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
     // (fp32 tiles of 128 keys and more than 64 channels do not fit LDS)
     *few = rows <= kFewRows && (a.dtype != BEVPOOL_F32 || a.dim <= 64);
-    g->n_tiles = attend_ceil(rows, *few ? 32 : 128);
+    g->n_tiles = attend_ceil(rows, *few ? kFewRows : kAttendTile);
     int slots = kUnits * (*few ? 2 : waves_forward(a.dtype, (a.dim + 31) / 32));
     if (lengths) slots += slots / 2;
     g->n_split = pick_split(int64_t(a.batch) * a.key_heads * g->n_tiles, slots, a.keys,
@@ -457,9 +457,6 @@ int bevmap_launch_attention(const bevmap_attend &a, const void *q, const void *k
     g.part_pitch = part_pitch(a);
     g.part = static_cast<float *>(workspace);
     g.part_stats = reinterpret_cast<float2 *>(g.part + int64_t(g.n_split) * a.batch * a.queries * a.heads * g.part_pitch);
-    if (int64_t(a.batch) * a.key_heads * g.n_split * g.n_tiles >= (int64_t(1) << 31) / kAttendBlock)
-        return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d heads=%d: too many tiles of rows", a.batch,
-                            a.queries, a.heads);
     g.out_aligned = aligned_for(out, 0, a.dtype, 4) && (!out_low || aligned_for(out_low, 0, a.dtype, 4));
     const bool vec = attend_by(a, q, k, v, a.dtype == BEVPOOL_F32 ? 4 : 8) && g.out_aligned;
     g.pairs = attend_by(a, q, k, v, 2);

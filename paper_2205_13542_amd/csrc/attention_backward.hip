@@ -27,7 +27,7 @@
 namespace bevmap {
 namespace {
 
-constexpr int kOwn = 128;           // rows or keys that a workgroup owns, 32 a wave
+constexpr int kOwn = kAttendTile;   // rows or keys that a workgroup owns, 32 a wave
 
 // Rows or keys of a tile that is walked, and what a thread moves of it.
 template <int DT, int DB>
@@ -638,14 +638,6 @@ int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_ou
                                      const void *out_low, const float *lse, void *grad_q, void *grad_k,
                                      void *grad_v, void *workspace, hipStream_t stream) {
     if (a.batch == 0) return BEVPOOL_OK;
-    const int64_t bh = int64_t(a.batch) * a.key_heads, most = int64_t(1) << 23;
-    int32_t tiles, split;
-    partition_q(a, lengths != nullptr, &tiles, &split);
-    const bool wide = bh * tiles * split >= most;
-    partition_k(a, &tiles, &split);
-    if (wide || bh * tiles * split >= most)
-        return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d keys=%d heads=%d: too many tiles", a.batch,
-                            a.queries, a.keys, a.heads);
     AttendArgs g = attend_fill(a, q, k, v, lengths, mask);
     g.dout = grad_out;
     g.out = out;

@@ -11,6 +11,8 @@
 // Limits that the kernels assume.
 constexpr int kNormMaxChannels = 8192;  // two floats a channel in LDS
 constexpr int kAttendMaxDim = 128;
+constexpr int kAttendTile = 128;        // rows or keys that a workgroup owns
+constexpr int64_t kAttendMaxTiles = int64_t(1) << 23;   // workgroups of a launch; more are never needed to split an axis
 
 // Launches; arguments are checked by the caller (mapops.hip).
 int64_t bevmap_norm_workspace_bytes(const bevmap_norm &n, bool backward);

@@ -33,7 +33,8 @@ int check(const bevmap_norm *n) {
     return BEVPOOL_OK;
 }
 
-int check(const bevmap_attend *a) {
+// backward: the tiles of keys are limited too.
+int check(const bevmap_attend *a, bool backward) {
     if (!a) return bevpool_fail(BEVPOOL_ERR_INVALID_ARG, "null description");
     if (a->batch < 0 || a->queries < 0 || a->keys < 0 || a->heads < 1 || a->key_heads < 1 || a->dim < 1)
         return bevpool_fail(BEVPOOL_ERR_INVALID_ARG, "batch=%d queries=%d keys=%d heads=%d key_heads=%d dim=%d",
@@ -52,6 +53,11 @@ int check(const bevmap_attend *a) {
         return bevpool_fail(BEVPOOL_ERR_OVERFLOW,
                             "dim=%d batch=%d queries=%d keys=%d heads=%d key_heads=%d, or a key's or value's row "
                             "stride, is outside the limits", a->dim, a->batch, a->queries, a->keys, a->heads, a->key_heads);
+    const int64_t rows = int64_t(a->queries) * (a->heads / a->key_heads);
+    const int64_t owned = backward && a->keys > rows ? a->keys : rows;
+    if (int64_t(a->batch) * a->key_heads * ((owned + kAttendTile - 1) / kAttendTile) >= kAttendMaxTiles)
+        return bevpool_fail(BEVPOOL_ERR_OVERFLOW, "batch=%d queries=%d keys=%d heads=%d key_heads=%d: too many tiles of "
+                            "%s", a->batch, a->queries, a->keys, a->heads, a->key_heads, owned > rows ? "keys" : "rows");
     return BEVPOOL_OK;
 }
 
@@ -98,14 +104,14 @@ int bevmap_group_norm_backward(const bevmap_norm *norm, const void *grad_y, cons
 }
 
 int64_t bevmap_attention_workspace(const bevmap_attend *attend, int32_t backward) {
-    if (int rc = check(attend)) return rc;
+    if (int rc = check(attend, backward != 0)) return rc;
     return bevmap_attention_workspace_bytes(*attend, backward != 0);
 }
 
 int bevmap_attention(const bevmap_attend *attend, const void *q, const void *k, const void *v,
                      const int32_t *key_lengths, const uint8_t *key_mask, void *out, void *out_low, float *lse,
                      void *workspace, int64_t workspace_bytes, void *hip_stream) {
-    if (int rc = check(attend)) return rc;
+    if (int rc = check(attend, false)) return rc;
     const bool asked = attend->batch > 0 && attend->queries > 0;
     if (asked && (!q || !out || (attend->keys > 0 && (!k || !v))))
         return bevpool_fail(BEVPOOL_ERR_INVALID_ARG, "null pointer argument");
@@ -119,7 +125,7 @@ int bevmap_attention_backward(const bevmap_attend *attend, const void *grad_out,
                               const void *v, const int32_t *key_lengths, const uint8_t *key_mask, const void *out,
                               const void *out_low, const float *lse, void *grad_q, void *grad_k, void *grad_v,
                               void *workspace, int64_t workspace_bytes, void *hip_stream) {
-    if (int rc = check(attend)) return rc;
+    if (int rc = check(attend, true)) return rc;
     const bool asked = attend->batch > 0 && attend->queries > 0, stored = attend->batch > 0 && attend->keys > 0;
     if ((asked && (!grad_out || !q || !out || !lse || !grad_q)) || (stored && (!k || !v || !grad_k || !grad_v)))
         return bevpool_fail(BEVPOOL_ERR_INVALID_ARG, "null pointer argument");

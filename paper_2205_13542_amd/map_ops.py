@@ -144,7 +144,8 @@ def _norm_backward(norm, space, dy, x, weight, bias, want_weight, want_bias):
 
 
 def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
-    """out, what its rounding left over, lse (both for the backward) and the description."""
+    """out, what its rounding left over, lse (both for the backward), the description and the
+    backward's bytes of workspace: what the backward would refuse is refused here."""
     index = _device(q, k, v, key_lengths, key_mask)
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         _refuse("q, k and v must be 4-D", _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
@@ -178,18 +179,18 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
     attend = _map_binding.bevmap_attend(B, N, M, H, K, D, _code(dtype), scale, qs[0], qs[1], qs[2], ks[0], ks[1],
                                         ks[2], vs[0], vs[1], vs[2], mask_batch)
     size = _map_binding.bevmap_attention_workspace(attend, False)
+    back_size = _map_binding.bevmap_attention_workspace(attend, True) if train else 0
     out = _empty_like(q)
     low = _empty_like(q) if train and dtype != torch.float32 else None
     lse = q.new_empty((B, H, N), dtype=torch.float32) if train else None
     space = q.new_empty(size, dtype=torch.uint8) if size else None
     _call(_map_binding.bevmap_attention, index, attend, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lengths),
           _ptr(key_mask), out.data_ptr(), _ptr(low), _ptr(lse), _ptr(space), size)
-    return out, low, lse, attend
+    return out, low, lse, attend, back_size
 
 
-def _attend_backward(attend, dout, q, k, v, key_lengths, key_mask, out, low, lse):
+def _attend_backward(attend, size, dout, q, k, v, key_lengths, key_mask, out, low, lse):
     dout = dout.contiguous()
-    size = _map_binding.bevmap_attention_workspace(attend, True)
     dq, dk, dv = _empty_like(q), _empty_like(k), _empty_like(v)
     temp = q.new_empty(size, dtype=torch.uint8)
     _call(_map_binding.bevmap_attention_backward, q.get_device(), attend, dout.data_ptr(), q.data_ptr(),
@@ -235,7 +236,7 @@ class _GroupNormAct(torch.autograd.Function):
 class _CrossAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, key_lengths, key_mask):
-        out, low, lse, ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
+        out, low, lse, *ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
         ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
         return out
 
@@ -244,7 +245,7 @@ class _CrossAttention(torch.autograd.Function):
         _first_order_only()
         q, k, v, key_lengths, key_mask, out, low, lse = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dq, dk, dv = _attend_backward(ctx.attend, dout, q, k, v, key_lengths, key_mask, out, low, lse)
+        dq, dk, dv = _attend_backward(*ctx.attend, dout, q, k, v, key_lengths, key_mask, out, low, lse)
         return dq if need[0] else None, dk if need[1] else None, dv if need[2] else None, None, None, None
 
 

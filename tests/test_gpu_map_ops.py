@@ -725,6 +725,14 @@ def test_refusals(torch, bev):
             print(f"call {i} was not refused", flush=True)
 
 
+def test_a_step_is_refused_in_its_forward(torch, bev):
+    """Where the backward has more tiles of keys than a launch takes."""
+    q = torch.zeros((1, 1, 1, 4), device="cuda")
+    k = torch.zeros((1, 1, 1, 4), device="cuda").expand(2048, 70000, 8, 4)
+    with pytest.raises(bev.BevpoolError, match="tiles of keys"):
+        bev.cross_attention(q.clone().requires_grad_().expand(2048, 1, 8, 4), k, k)
+
+
 def test_refusals_of_sizes_past_32_bits(torch, bev):
     """Sizes that would be small again if their upper bits were lost."""
     n = 2 ** 32 + 8

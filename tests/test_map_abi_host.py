@@ -97,6 +97,19 @@ def test_attention_refuses(lib, mb, over, code):
     assert lib.bevmap_attention_backward(a, P, P, P, P, None, None, P, P, P, P, P, P, P, 1 << 40, None) == code
 
 
+def test_attention_refuses_more_tiles_than_a_launch_has(lib, mb):
+    """By the call that asks for the workspace already: 2048 x 8 problems of 547 tiles each."""
+    size = dict(batch=2048, heads=8, key_heads=8, dim=4)
+    queries = _attend(mb, **size, queries=70000)
+    for backward in (0, 1):
+        assert lib.bevmap_attention_workspace(queries, backward) == OVERFLOW
+    assert lib.bevmap_attention(queries, P, P, P, None, None, P, None, None, P, 1 << 60, None) == OVERFLOW
+    keys = _attend(mb, **size, keys=70000)      # only the backward owns tiles of keys
+    assert lib.bevmap_attention_workspace(keys, 0) >= 0
+    assert lib.bevmap_attention_workspace(keys, 1) == OVERFLOW
+    assert lib.bevmap_attention_backward(keys, P, P, P, P, None, None, P, P, P, P, P, P, P, 1 << 60, None) == OVERFLOW
+
+
 def test_attention_refuses_pointers_and_workspaces(lib, mb):
     a = _attend(mb)
     need = lib.bevmap_attention_workspace(a, 1)
@@ -141,7 +154,7 @@ def test_forward_mode_is_refused(monkeypatch):
     from paper_2205_13542_amd import map_ops
     from torch.autograd import forward_ad
     monkeypatch.setattr(map_ops, "_norm_forward", lambda x, *a: (x.clone(), x.clone(), None))
-    monkeypatch.setattr(map_ops, "_attend_forward", lambda q, *a: (q.clone(), None, q.clone(), None))
+    monkeypatch.setattr(map_ops, "_attend_forward", lambda q, *a: (q.clone(), None, q.clone(), None, 0))
     monkeypatch.setattr(map_ops, "_dropout", lambda x, *a: x.clone())
     x, q = torch.ones(2, 3, 8), torch.ones(1, 2, 2, 4)
     with forward_ad.dual_level():
