@@ -480,7 +480,8 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_grad_apply(NormArgs a) {
 }
 
 // Small maps: a launch costs the host about 3.3 us, more than the work, so a group
-// that one workgroup holds in registers takes one kernel in each direction instead of three.
+// that one workgroup holds in registers takes one kernel in each direction instead of three,
+// where small() does not expect that to take longer.
 constexpr int kSmallBlock = 1024;
 constexpr int kSmallRows = 8;       // values of a thread (16 spill in the backward)
 constexpr int kSmallFrames = 4;     // of the backward, whose workgroup takes a group of all frames in turn
@@ -618,10 +619,24 @@ int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
 int64_t elements(const bevmap_norm &n) { return int64_t(n.batch) * n.pixels * n.channels; }
 
+// A workgroup to a group reads a piece of every row, and a cache line for it, so many groups
+// ask for the same lines again and again; and workgroups of 16 waves start at 7 ns each (11
+// of the backward, one frame after the other). So one kernel is taken where that costs less
+// than the three, which depend little on the sizes as long as a launch is most of their time,
+// but join every group. Microseconds, fitted to both forms of 654 shapes (fp32 and bf16, 1 to 80
+// channels of a group, 32 to 1024 channels, 16 to 8100 rows, 1 to 64 frames). Of the faster
+// form's time the rule costs 0.5% forward and 1.2% backward on average; one kernel for all
+// would cost 34% and 15%: 64 frames of 8100 rows and 80 groups of one channel in fp32, 714 us
+// and 88; four frames of 8100 rows and 32 such groups, backward, 99 and 18.
 bool small(const bevmap_norm &n, bool backward) {
     const int per = n.channels / n.groups;
-    return per <= kSmallBlock && ceil_div(n.pixels, kSmallBlock / per) <= kSmallRows &&
-           (!backward || n.batch <= kSmallFrames);
+    if (per > kSmallBlock || ceil_div(n.pixels, kSmallBlock / per) > kSmallRows ||
+        (backward && n.batch > kSmallFrames))
+        return false;
+    const double rows = double(n.batch) * n.pixels, groups = double(n.batch) * n.groups;
+    const double lines = rows * n.groups;
+    const double one = backward ? 15e-6 * lines + 11e-3 * groups + 2e-3 * rows : 12.5e-6 * lines + 6.7e-3 * groups;
+    return one <= 12.0 + 0.03 * n.groups;
 }
 
 void split(const bevmap_norm &n, NormArgs *a) {

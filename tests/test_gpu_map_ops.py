@@ -129,6 +129,16 @@ NORM_CASES = [
 ]
 
 
+MANY_GROUPS = [
+    # a channel or two to a group: both sides of the rule for one kernel, each direction
+    ((4, 2100, 64), 64, 0, "bf16", "bf16", "f32", "silu", 0.0),
+    ((1, 90, 90, 80), 80, 0, "f32", "f32", "f32", "gelu", 0.0),
+    ((1, 90, 91, 80), 80, 0, "f32", "f32", "f32", "gelu", 0.0),
+    ((64, 16, 130), 65, 6, "f16", "f16", "f32", "relu", 0.0),
+    ((3, 500, 1000), 1000, 0, "bf16", "f32", "bf16", "none", 0.0),
+]
+
+
 def _norm_inputs(torch, shape, groups, extra, xdt, ydt, wdt, offset, seed=0):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     wide = torch.randn((*shape[:-1], shape[-1] + extra), generator=gen, device="cuda")
@@ -155,6 +165,11 @@ def test_group_norm(torch, bev, shape, groups, extra, xdt, ydt, wdt, act, offset
             _check(name, got, r, tol + _u(dt) * (r.abs() + tol) + _tiny(dt) + 1e-35)
         again = bev.group_norm_act(x, groups, w, b, act=act, out_dtype=_dtype(torch, ydt))
         assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("shape,groups,extra,xdt,ydt,wdt,act,offset", MANY_GROUPS)
+def test_group_norm_of_many_groups(torch, bev, shape, groups, extra, xdt, ydt, wdt, act, offset):
+    test_group_norm(torch, bev, shape, groups, extra, xdt, ydt, wdt, act, offset)
 
 
 def test_group_norm_without_weights_and_partial_gradients(torch, bev):

@@ -76,6 +76,20 @@ def test_group_norm_refuses_pointers_and_workspaces(lib, mb):
     assert lib.bevmap_group_norm(empty, None, None, None, None, None, None, None, 0, None) == 0
 
 
+def test_group_norm_of_many_groups_takes_three_kernels(lib, mb):
+    """One workgroup to a group reads every cache line of the map once for each group in it: such maps
+    need the workspace of the three kernels, small ones with as many groups do not."""
+    def workspaces(batch, pixels, channels, groups):
+        n = _norm(mb, batch=batch, pixels=pixels, channels=channels, groups=groups, row_stride=channels, x_dtype=1)
+        return [lib.bevmap_group_norm_workspace(n, backward) for backward in (0, 1)]
+
+    assert all(size > 0 for size in workspaces(8, 8100, 256, 256))
+    assert all(size > 0 for size in workspaces(4, 8100, 32, 32))
+    assert all(size > 0 for size in workspaces(64, 16, 1024, 1024))
+    assert all(size == 0 for size in workspaces(1, 512, 256, 256))
+    assert all(size == 0 for size in workspaces(2, 1073, 66, 11))
+
+
 def _attend(mb, **over):
     vals = dict(batch=2, queries=5, keys=7, heads=4, key_heads=2, dim=8, dtype=0, scale=0.3, q_batch=160, q_row=32,
                 q_head=8, k_batch=112, k_row=16, k_head=8, v_batch=112, v_row=16, v_head=8, mask_batch=7)
