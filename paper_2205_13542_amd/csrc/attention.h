@@ -592,8 +592,11 @@ inline int pick_split(int64_t whole, int slots, int64_t walk, int64_t most, doub
 constexpr int kUnits = 256;     // compute units
 
 // Waves of a SIMD, which is workgroups of a compute unit, that the registers allow by
-// blocks of 32 channels; the kernels' launch bounds hold them to it.
+// blocks of 32 channels; the kernels' launch bounds hold them to it. Those of the forward
+// may be fewer by their LDS (resident_forward()).
+constexpr int kLdsBytes = 160 * 1024;   // of a compute unit
 constexpr int waves_forward(int dt, int db) { return db == 1 ? 4 : db == 2 ? 3 : db == 3 || dt != BEVPOOL_F32 ? 2 : 1; }
+constexpr int waves_few(int dt, int db) { return db == 4 || (db == 3 && dt == BEVPOOL_F32) ? 1 : 2; }
 constexpr int waves_dq(int dt, int db) {
     return dt == BEVPOOL_F32 ? (db == 1 ? 3 : db == 2 ? 2 : 1) : (db == 1 ? 4 : db == 2 ? 3 : 2);
 }

@@ -42,7 +42,32 @@ struct Tile {
     // pairs of tiles, keys and values, in LDS: two where they fit
     static constexpr int kPairs = 4 * kBytes <= 128 * 1024 ? 2 : 1;
     static constexpr int kLds = 2 * kPairs * kBytes;
+    // the same waves of a SIMD, or workgroups of a compute unit, by registers, and by registers and LDS: two
+    // waves of fp32 and three blocks are faster in one's LDS with some registers spilled (4096 rows, 8192 keys, 8
+    // heads of 96: 664 us) than with accumulation registers (694)
+    static constexpr int kWaves = WR == 1 ? waves_few(DT, DB) : waves_forward(DT, DB);
+    static constexpr int kResident = kWaves * kLds <= kLdsBytes ? kWaves : kLdsBytes / kLds;
+    static_assert(kResident > 0, "no workgroup fits");
 };
+
+template <int DT>
+int resident_forward(int db, bool few) {
+    if (few) {
+        if constexpr (DT != BEVPOOL_F32) {
+            if (db == 3) return Tile<DT, 3, 1>::kResident;
+            if (db == 4) return Tile<DT, 4, 1>::kResident;
+        }
+        return db == 1 ? Tile<DT, 1, 1>::kResident : Tile<DT, 2, 1>::kResident;
+    }
+    return db == 1   ? Tile<DT, 1, 4>::kResident
+           : db == 2 ? Tile<DT, 2, 4>::kResident
+           : db == 3 ? Tile<DT, 3, 4>::kResident
+                     : Tile<DT, 4, 4>::kResident;
+}
+// Workgroups of k_attend that a compute unit holds, by blocks of 32 channels.
+int resident_forward(int dt, int db, bool few) {
+    return dt == BEVPOOL_F32 ? resident_forward<BEVPOOL_F32>(db, few) : resident_forward<BEVPOOL_BF16>(db, few);
+}
 
 // What a part of a row with this maximum and sum counts where the whole row's
 // maximum is `most`: nothing without keys; a sum that is NaN without a maximum
@@ -53,7 +78,7 @@ __device__ __forceinline__ float part_weight(float top, float sum, float most) {
 }
 
 template <int DT, int DB, bool VEC, int WR>
-__global__ __launch_bounds__(kAttendBlock, (WR == 1 ? (DB == 4 || (DB == 3 && DT == BEVPOOL_F32) ? 1 : 2) : waves_forward(DT, DB))) void k_attend(AttendArgs g) {
+__global__ __launch_bounds__(kAttendBlock, (Tile<DT, DB, WR>::kWaves)) void k_attend(AttendArgs g) {
     using S = Shape<DT, DB>;
     using T = typename S::T;
     using M = typename S::M;
@@ -365,13 +390,14 @@ int part_pitch(const bevmap_attend &a) { return (a.dim + 3) / 4 * 4; }
 
 // Rows, row tiles and parts of the keys, a rule on the sizes alone, and on whether
 // samples have lengths: unequal ones need more workgroups to even out, and do less
-// work by the row. Few rows are bound by reading, two workgroups a compute unit.
+// work by the row. Parts are chosen for the workgroups that the chip holds (one query of 8
+// heads on 2 of 128 over 129600 keys in bf16: 48 us with parts for twice as many, now 39).
 void partition(const bevmap_attend &a, bool lengths, AttendArgs *g, bool *few) {
     const int64_t rows = int64_t(a.queries) * (a.heads / a.key_heads);
     // (fp32 tiles of 128 keys and more than 64 channels do not fit LDS)
     *few = rows <= kFewRows && (a.dtype != BEVPOOL_F32 || a.dim <= 64);
     g->n_tiles = attend_ceil(rows, *few ? kFewRows : kAttendTile);
-    int slots = kUnits * (*few ? 2 : waves_forward(a.dtype, (a.dim + 31) / 32));
+    int slots = kUnits * resident_forward(a.dtype, attend_ceil(a.dim, 32), *few);
     if (lengths) slots += slots / 2;
     g->n_split = pick_split(int64_t(a.batch) * a.key_heads * g->n_tiles, slots, a.keys,
                             attend_ceil(a.keys, *few ? 256 : 128), lengths ? 1200.0 : 600.0, a.dtype);

@@ -77,6 +77,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dq(DT, DB)) void k_attend_dq(At
     using T = typename S::T;
     using M = typename S::M;
     using W = Walk<DT, DB>;
+    static_assert(W::kLds * waves_dq(DT, DB) <= kLdsBytes, "workgroups that partition_q() counts");
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][k, v][tile]
     const int n_bh = g.a.batch * g.a.key_heads;
     int bh, tile;
@@ -257,6 +258,7 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
     using T = typename S::T;
     using M = typename S::M;
     using W = Walk<DT, DB>;
+    static_assert(W::kLds * waves_dkv(DT, DB) <= kLdsBytes, "workgroups that partition_k() counts");
     extern __shared__ __attribute__((aligned(16))) char lds[];       // [2][q, dout][tile], then [2][lse, delta][row]
     float *stats = reinterpret_cast<float *>(lds + 4 * W::kBytes);
     const int n_bh = g.a.batch * g.a.key_heads;

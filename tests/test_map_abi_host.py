@@ -111,6 +111,18 @@ def test_attention_refuses(lib, mb, over, code):
     assert lib.bevmap_attention_backward(a, P, P, P, P, None, None, P, P, P, P, P, P, P, 1 << 40, None) == code
 
 
+@pytest.mark.parametrize("dtype,dim,resident", [
+    (0, 32, 1), (0, 64, 1), (1, 32, 2), (1, 64, 2), (2, 96, 1), (1, 128, 1)])
+def test_attention_parts_go_by_the_workgroups_that_fit(lib, mb, dtype, dim, resident):
+    """One query over many keys is cut into as many parts as workgroups run at once on 256 compute units, or
+    half as many again for samples of unequal length, which the workspace has to hold: by the kernel's LDS, of
+    160 KB, one or two to a unit."""
+    a = _attend(mb, batch=1, queries=1, keys=1 << 20, heads=8, key_heads=2, dim=dim, dtype=dtype, q_row=8 * dim,
+                q_head=dim, k_row=2 * dim, k_head=dim, v_row=2 * dim, v_head=dim)
+    parts = lib.bevmap_attention_workspace(a, 0) / (8 * (4 * dim + 8))
+    assert 0.5 * 256 * resident < 2 * parts <= 1.5 * 256 * resident * 1.01
+
+
 def test_attention_refuses_more_tiles_than_a_launch_has(lib, mb):
     """By the call that asks for the workspace already: 2048 x 8 problems of 547 tiles each."""
     size = dict(batch=2048, heads=8, key_heads=8, dim=4)
