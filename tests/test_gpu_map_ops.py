@@ -402,6 +402,38 @@ def test_cross_attention_large_scores(torch, bev, dt):
         assert got.isfinite().all()
         _check("out", got, ref[0], ref[1] * (1 + 16 * U32) + _u(dt) * (ref[0].abs() + ref[1]) + _tiny(dt))
 
+def _check_step(torch, bev, q, k, v, dout, scale, lengths, mask, dt):
+    """Outputs and gradients of a step against the reference's bounds, as in test_cross_attention."""
+    ref = _attend_reference(torch, q, k, v, scale, lengths, mask, dout, dt)
+    q, k, v = (t.detach().requires_grad_() for t in (q, k, v))
+    out = bev.cross_attention(q, k, v, scale=scale, key_lengths=lengths, key_mask=mask)
+    grads = torch.autograd.grad(out, (q, k, v), dout)
+    with torch.no_grad():
+        for name, got in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+            r, tol = ref[name]
+            _check(name, got, r, tol * (1 + 16 * U32) + _u(dt) * (r.abs() + tol) + _tiny(dt) + 1e-30)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,M", [(4, 333), (70, 333), (150, 2100)])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, -2.0 ** -20])
+def test_cross_attention_of_other_scales(torch, bev, scale, N, M, dt):
+    """Scales that are negative or 0: all keys in use count alike then, and q and k have no gradient."""
+    print(f"[scale] {scale} N={N} M={M} {dt}", flush=True)
+    q, k, v, dout, lengths, mask = _attend_inputs(torch, 2, N, M, 4, 2, 48, dt, "packed", [M, M // 2], "random")
+    _check_step(torch, bev, q, k, v, dout, scale, lengths, mask, dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N", [6, 40])
+def test_gradients_of_large_scores(torch, bev, N, dt):
+    """The backward forms the probabilities again from an lse of some hundreds, of either sign."""
+    for shift in (0.0, -8.0, 8.0):
+        q, k, v, dout, _, _ = _attend_inputs(torch, 1, N, 200, 2, 2, 32, dt, "plain", None, None, sharp=30.0)
+        if shift:
+            q[..., 0], k[..., 0] = 100.0, shift     # adds 100 * shift / sqrt(32) to every score
+        _check_step(torch, bev, q, k, v, dout, 32 ** -0.5, None, None, dt)
+
 
 @pytest.mark.parametrize("copies", [1, 40])
 def test_cross_attention_products_of_fp32(torch, bev, copies):
@@ -700,6 +732,63 @@ def test_in_a_graph(torch, bev):
         got = out.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, _layer(torch, bev, *args, 3, 1)), f"replay {i}"
+
+
+def _step_inputs(torch):
+    """A layer's inputs as leaves, and the gradient of its output; the products between the operators are views."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda")
+
+    return ([normal(2, 40, 21, 64), 1 + 0.1 * normal(64), 0.1 * normal(64), normal(2, 45, 4, 16).bfloat16()],
+            torch.rand((2, 840), generator=gen, device="cuda") < 0.8, normal(2, 45, 64).bfloat16())
+
+
+def _step(torch, bev, args, seen, dy):
+    x, w, b, q = (t.detach().requires_grad_() for t in args)
+    states = bev.group_norm_act(x, 4, w, b, act="gelu", out_dtype=torch.bfloat16).view(2, 840, 4, 16)
+    heard = bev.cross_attention(q, states, states, key_mask=seen).flatten(2)
+    y = bev.dropout_add(heard, 0.2, 3, 1, residual=q.flatten(2))
+    return [y.detach(), *torch.autograd.grad(y, (x, w, b, q), dy)]
+
+
+def test_a_step_on_another_stream(torch, bev):
+    """Forward and backward on a side stream, on inputs made there, with nothing else to order them."""
+    args, seen, dy = _step_inputs(torch)
+    ref = _step(torch, bev, args, seen, dy)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        mine, there, grad = [torch.empty_like(t) for t in args], torch.empty_like(seen), torch.empty_like(dy)
+        big = torch.randn(1 << 26, device="cuda")
+        for _ in range(8):
+            big = big * 1.5                     # keeps the stream busy
+        for t, a in zip((*mine, there, grad), (*args, seen, dy)):
+            t.copy_(a)
+        got = _step(torch, bev, mine, there, grad)
+    side.synchronize()
+    assert all(torch.equal(a, r) for a, r in zip(got, ref))
+
+
+def test_a_step_in_a_graph(torch, bev):
+    args, seen, dy = _step_inputs(torch)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        _step(torch, bev, args, seen, dy)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _step(torch, bev, args, seen, dy)
+    for i in range(4):
+        gen = torch.Generator(device="cuda").manual_seed(60 + i)
+        for t in (args[0], args[3], dy):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        graph.replay()
+        got = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        ref = _step(torch, bev, args, seen, dy)
+        assert all(torch.equal(a, r) for a, r in zip(got, ref)), f"replay {i}"
 
 
 def test_refusals(torch, bev):
