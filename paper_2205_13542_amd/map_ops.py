@@ -307,6 +307,9 @@ def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
     use. States not in use may hold anything, NaN too; they do not reach the
     output, and their gradients are 0. A query without a state in use gets 0.
     Queries and states in use must be finite.
+    Scores, statistics and sums are fp32. With bf16 and fp16 the probabilities of
+    more than 32 queries to a key head (N * H // K) are rounded to the type for
+    their product with v; with fewer, in the backward and with fp32 they are not.
     Few queries over many states (one token in serving) are split over the
     states. Differentiable in q, k and v, bitwise reproducible."""
     if _learns(q, k, v):
