@@ -94,7 +94,7 @@ def _first_order_only():
 
 
 def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
-    """y, a buffer that starts with mean and rstd [2][B][groups], and the description."""
+    """y, mean and rstd [2][B][groups], and the description."""
     if x.dim() < 2:
         _refuse("x must have a batch and a channel dimension")
     index = _device(x, weight, bias)
@@ -121,23 +121,23 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
                                     _binding.BEVPOOL_F32 if w_like is None else _code(w_like.dtype))
     size = _map_binding.bevmap_group_norm_workspace(norm, False)
     y = x.new_empty(shape, dtype=out_dtype)
-    stats = B * groups * 4
-    start = (2 * stats + 15) // 16 * 16       # of the workspace behind the statistics
-    space = x.new_empty(start + size, dtype=torch.uint8)
-    mean = space.data_ptr()
+    # kept for the backward, which has no use for the workspace
+    stats = x.new_empty((2, B, groups), dtype=torch.float32)
+    space = x.new_empty(size, dtype=torch.uint8) if size else None
+    mean = stats.data_ptr()
     _call(_map_binding.bevmap_group_norm, index, norm, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean,
-          mean + stats, mean + start, size)
-    return y, space, norm
+          mean + 4 * B * groups, _ptr(space), size)
+    return y, stats, norm
 
 
-def _norm_backward(norm, space, dy, x, weight, bias, want_weight, want_bias):
+def _norm_backward(norm, stats, dy, x, weight, bias, want_weight, want_bias):
     dy = dy.contiguous()
     size = _map_binding.bevmap_group_norm_workspace(norm, True)
     dx = _empty_like(x)
     dw = torch.empty_like(weight) if want_weight else None
     db = torch.empty_like(bias) if want_bias else None
-    temp = space.new_empty(size) if size else None
-    mean = space.data_ptr()
+    temp = stats.new_empty(size, dtype=torch.uint8) if size else None
+    mean = stats.data_ptr()
     _call(_map_binding.bevmap_group_norm_backward, x.get_device(), norm, dy.data_ptr(), x.data_ptr(), _ptr(weight),
           _ptr(bias), mean, mean + 4 * norm.batch * norm.groups, dx.data_ptr(), _ptr(dw), _ptr(db), _ptr(temp), size)
     return dx, dw, db
@@ -220,16 +220,16 @@ def _dropout(x, threshold, seed, offset, residual):
 class _GroupNormAct(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
-        y, space, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
-        ctx.save_for_backward(x, weight, bias, space)
+        y, stats, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
+        ctx.save_for_backward(x, weight, bias, stats)
         return y
 
     @staticmethod
     def backward(ctx, dy):
         _first_order_only()
-        x, weight, bias, space = ctx.saved_tensors
+        x, weight, bias, stats = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dw, db = _norm_backward(ctx.norm, space, dy, x, weight, bias, need[1], need[2])
+        dx, dw, db = _norm_backward(ctx.norm, stats, dy, x, weight, bias, need[1], need[2])
         return dx if need[0] else None, dw, db, None, None, None, None
 
 

@@ -204,6 +204,14 @@ def test_group_norm_empty_and_nonfinite(torch, bev):
     assert torch.equal(got, clean)
 
 
+def test_group_norm_keeps_its_statistics_alone(torch, bev):
+    """For the backward: the input, the weights and two floats a sample and group, not the workspace."""
+    x = torch.zeros((2, 3000, 256), device="cuda", requires_grad=True)
+    w, b = (torch.ones(256, device="cuda", requires_grad=True) for _ in range(2))
+    y = bev.group_norm_act(x, 64, w, b)
+    assert sum(t.numel() * t.element_size() for t in y.grad_fn.saved_tensors[3:]) == 2 * 2 * 64 * 4
+
+
 def test_group_norm_of_a_constant_group(torch, bev):
     """Zero variance: x - mean is 0 and y is act(bias)."""
     x = torch.full((1, 20, 20, 8), 3.0, device="cuda")
