@@ -42,9 +42,9 @@ struct Tile {
     // pairs of tiles, keys and values, in LDS: two where they fit
     static constexpr int kPairs = 4 * kBytes <= 128 * 1024 ? 2 : 1;
     static constexpr int kLds = 2 * kPairs * kBytes;
-    // the same waves of a SIMD, or workgroups of a compute unit, by registers, and by registers and LDS: two
-    // waves of fp32 and three blocks are faster in one's LDS with some registers spilled (4096 rows, 8192 keys, 8
-    // heads of 96: 664 us) than with accumulation registers (694)
+    // Waves of a SIMD, or workgroups of a compute unit: by the registers, which the launch bound holds them to, and by
+    // the LDS as well. fp32 of three blocks has one by its LDS, but in the registers of two it is faster (4096 rows,
+    // 8192 keys, 8 heads of 96: 646 us) than with accumulation registers to move to and from (694).
     static constexpr int kWaves = WR == 1 ? waves_few(DT, DB) : waves_forward(DT, DB);
     static constexpr int kResident = kWaves * kLds <= kLdsBytes ? kWaves : kLdsBytes / kLds;
     static_assert(kResident > 0, "no workgroup fits");
