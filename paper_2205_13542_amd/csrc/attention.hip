@@ -7,14 +7,18 @@
 // and sum joins the tiles in one pass over the keys. Few rows leave the chip idle,
 // so the keys are then split over workgroups, and a second kernel joins the parts.
 //
-// A block of 32 rows and 32 keys takes a SIMD 252, 345 and 647 ns for 32, 64 and 128
-// channels of bf16 (530, 770 and 850 TFLOP/s; a library product of 8192^3 reaches
-// 1100). 32 channels are bound by the vector unit: 16 exponentials of 3.5 ns and 47
-// other instructions of 1.3 to 2 ns against 4 matrix instructions of 16 ns that mostly
-// overlap; 128 by the matrix cores and the LDS reads that feed them. Scores of the next
+// A block of 32 rows and 32 keys takes a SIMD 278, 377 and 645 ns for 32, 64 and 128
+// channels of bf16 (4096 rows, 8192 keys, 8 heads: 480, 710 and 830 TFLOP/s; a library
+// product of 8192^3 reaches 1100), and 222 ns for 32 channels at 32400 rows and 16896
+// keys. Of that 16 exponentials of 3.5 ns and 47 other vector instructions of 1.3 to 2 ns
+// fill 117 to 150 ns, and beside them 4 matrix instructions of 16 ns; the rest is waiting,
+// for LDS, at barriers and for each other (28% of the waves' cycles). 128 channels are
+// bound by the matrix cores and the LDS reads that feed them. Scores of the next
 // block formed ahead of a block's exponentials, the usual order and one block held
-// back were within 5% of each other. One query over 129600 keys (46 MB in use) takes
-// 17 us and its joining 5; 32400 queries over 16896 keys, 4 heads of 32: 457.
+// back were within 5% of each other. One query over 129600 keys in bf16, 8 heads on 2:
+// 17 us of 64 channels, whether all 66 MB are in use or, by a mask, 46; 30 us of 128,
+// 133 MB (4.0 and 4.5 TB/s; joining 5 each); of fp32 37 and 123. 32400 queries over
+// 16896 keys, 4 heads of 32: 464.
 #include "attention.h"
 
 namespace bevmap {

@@ -19,9 +19,13 @@
 // left dq, dk and dv of bf16 up to 1.55 times as far off as gradients in fp32 rounded
 // at the end; the pieces cost a quarter of the pair of kernels at large sizes.
 //
-// 4 x 600 queries of 8 heads over 8100 masked keys, ragged, 64 channels: dq 61 us and
-// its joining 9, dk and dv 74, two waves a SIMD that wait for LDS and for each other; of large sizes in bf16 a pair of kernels
-// reaches 360, 450 and 380 TFLOP/s at 32, 64 and 128 channels, five products counted.
+// 4 x 600 queries of 8 heads over 8100 masked keys, ragged, 64 channels: dq 62 us and
+// its joining 9, dk and dv 75, two waves a SIMD that wait for LDS and for each other. 4096
+// rows, 8192 keys, 8 heads of 32, 64 and 128 channels: bf16 105 + 150, 149 + 216 and 260 +
+// 539 us (340, 470 and 430 TFLOP/s, five products counted), fp16 6 to 11% more, fp32
+// 316 + 455, 540 + 837 and 1126 + 2491 (111, 125 and 95). dk and dv of 128 channels hold both
+// sums and both operands: one wave a SIMD, and in fp32 166 to 170 registers spilled (of
+// three blocks in 16 bits 6 to 17, and up to 6 of dq).
 #include "attention.h"
 
 namespace bevmap {
@@ -394,10 +398,10 @@ __global__ __launch_bounds__(kAttendBlock, waves_dkv(DT, DB)) void k_attend_dkv(
 // The same for few rows, one block of them: nothing is walked, so the sums of dv and dk
 // are formed and written one after the other in half the registers, and with two or
 // three waves to a SIMD where k_attend_dkv has one, the memory, which bounds it, is kept
-// busy: 2 x 40000 keys of 8 heads, bf16, 64 channels 72 us, now 62, 128 channels 220, now
-// 136 (656 MB read and written, 4.8 TB/s); fp32 220, now 152, and 552, now 368.
-// 16-bit rows that do not start on 16 bytes go through LDS both ways (84 channels: 400,
-// now 258).
+// busy: 2 x 4 queries over 40000 keys of 8 heads in bf16, 64 channels 61 us, 128 channels 137
+// (656 MB read and written, 4.8 TB/s; k_attend_dkv took 72 and 220); fp32 153 and 379 (220
+// and 552). 16-bit rows that do not start on 16 bytes go through LDS both ways (84
+// channels: 262 us, 400 without).
 constexpr int kFewRows = 32;
 template <int DT, int DB>
 struct Few {
