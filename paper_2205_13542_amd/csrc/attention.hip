@@ -128,8 +128,8 @@ __global__ __launch_bounds__(kAttendBlock, (Tile<DT, DB, WR>::kWaves)) void k_at
     // Probabilities of 16-bit types are rounded to the type for their product with v, and their sum is that of the
     // rounded ones, so that the weights add up to one: out is 1.3 times as far off as fp32 rounded once (32400 x
     // 16896, 4 heads of 32, bf16: 2.25e-3 of its norm, 1.66e-3). What the rounding leaves as a second piece would
-    // end that, for a quarter to a third of the time again (4096 rows, 8192 keys, 8 heads of 32, 64 and 128 channels
-    // of bf16: 72, 106 and 181 us, with it 98, 137 and 229). Few rows, bound by reading, take it.
+    // end that, for 25 to 45% of the time again (4096 rows, 8192 keys, 8 heads of 32, 64 and 128 channels of bf16:
+    // 72, 106 and 181 us, with it 98, 137 and 229; the former case 475 and 690). Few rows, bound by reading, take it.
     constexpr bool kTwo = WR == 1 && DT != BEVPOOL_F32;
     typename M::Rows p, p_low;
     // p and this lane's sum of the exponentials of a block's scores relative to base
