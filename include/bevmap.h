@@ -2,12 +2,18 @@
  * bevmap.h -- C ABI of libbevpool.so: operators of the model that reads a pooled
  * BEV map, on MI355X (gfx950). The pooling itself is in bevpool.h.
  *
- * Three operators, each with its gradients, channels last throughout:
+ * Channels last throughout. With gradients:
  *  - bevmap_group_norm: group norm with an activation;
  *  - bevmap_attention: queries attend to an encoder's states of another length
  *    (the cells of a map, the pixels of the cameras);
  *  - bevmap_dropout: residual + dropout(x), the mask from a counter-based
- *    generator and never stored.
+ *    generator and never stored;
+ *  - bevmap_rms_norm: root-mean-square norm of rows, of x + residual;
+ *  - bevmap_rotary: pairs of channels turned by angles that go with a position;
+ *  - bevmap_gated_act: act(gate) * value, what the backward needs kept in 8 bits.
+ * For serving, in 8-bit integers:
+ *  - bevmap_rms_norm_int8, bevmap_quantize_int8: rows as integers and a scale;
+ *  - bevmap_linear_int8: their product with weights of a scale for each channel.
  *
  * The conventions of bevpool.h hold: return codes and bevpool_last_error, device
  * pointers on the current device, buffers owned by the caller, hip_stream a
@@ -184,6 +190,194 @@ BEVPOOL_API int bevmap_dropout(const void *x, int64_t x_stride, const void *resi
                                int64_t residual_stride, void *y, int64_t rows, int64_t columns,
                                int32_t dtype, int32_t threshold, uint64_t seed, uint64_t offset,
                                void *hip_stream);
+
+/*
+ * Root-mean-square norm of rows. Row s starts at x + s * x_stride elements and holds
+ * `channels` elements; residual alike. With h = x + residual (x without one):
+ *   rstd = 1 / sqrt(mean of h^2 + eps),  y = weight[c] * h * rstd.
+ * The sum is handed on rounded to x_dtype; y is formed from it before that.
+ * Squares are summed in fp32, rows whose squares leave its range after a power of two is
+ * taken out, so a row of any finite size is normed. An infinity or a NaN reaches its row
+ * alone.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t channels;
+    int32_t x_dtype;       /* of x, residual, sum and their gradients */
+    int32_t y_dtype;       /* of y and grad_y */
+    int32_t weight_dtype;  /* of weight and grad_weight */
+    int64_t x_stride, residual_stride;   /* elements from row to row, >= channels */
+    float eps;             /* >= 0 */
+} bevmap_rms;
+
+/*
+ *  residual: NULL for none; sum is then not written (and may be NULL).
+ *  weight:   device [channels] of weight_dtype; NULL for ones.
+ *  sum:      device [rows][channels] of x_dtype, overwritten with x + residual.
+ *  y:        device [rows][channels] of y_dtype, overwritten.
+ *  rstd:     device float [rows], or NULL; overwritten: what the backward reads.
+ * rows of 0 is a call that does nothing.
+ * Errors: INVALID_ARG (null pointer, rows below 0, channels below 1, a stride <
+ * channels, eps negative or not finite), UNSUPPORTED_DTYPE, OVERFLOW (rows or a stride
+ * reaching 2^31, channels above 8192), HIP (launch failure).
+ */
+BEVPOOL_API int bevmap_rms_norm(const bevmap_rms *norm, const void *x, const void *residual, const void *weight,
+                                void *sum, void *y, float *rstd, void *hip_stream);
+
+/* Bytes of workspace of bevmap_rms_norm_backward; a negative error code if the
+ * description is refused. Host only. */
+BEVPOOL_API int64_t bevmap_rms_norm_backward_workspace(const bevmap_rms *norm);
+
+/*
+ * Gradients of bevmap_rms_norm, with the rstd that it wrote:
+ *  grad_y:      device [rows][channels] of y_dtype.
+ *  grad_sum:    device [rows][channels] of x_dtype: the gradient of sum, or NULL.
+ *  x:           what was normed: sum, or x where there was no residual (rows x_stride
+ *               apart; residual_stride is not used).
+ *  grad_x:      device [rows][channels] of x_dtype, overwritten: the gradient of x, which
+ *               is the residual's as well.
+ *  grad_weight: device [channels] of weight_dtype, overwritten (zeros for no rows); NULL
+ *               to skip.
+ * Errors: those of bevmap_rms_norm, and INVALID_ARG for a workspace that is too small or
+ * not 16-byte aligned.
+ */
+BEVPOOL_API int bevmap_rms_norm_backward(const bevmap_rms *norm, const void *grad_y, const void *grad_sum,
+                                         const void *x, const void *weight, const float *rstd, void *grad_x,
+                                         void *grad_weight, void *workspace, int64_t workspace_bytes,
+                                         void *hip_stream);
+
+/*
+ * The norm's result in 8 bits, for a product that reads it: with top the largest
+ * |weight * h| of a row,
+ *   held = round(weight * h * (127 / top)), scale = top * rstd / 127,
+ * so that held * scale is y to within half a scale; halves go to the even neighbour. A
+ * row of zeros has scale 0 (eps of 0: NaN), one with an infinity or a NaN has scale NaN
+ * and zeros.
+ *  held:  device int8 [rows][channels], overwritten.  scale: device float [rows],
+ *         overwritten.  The rest as for bevmap_rms_norm; y_dtype is not used.
+ * Errors: those of bevmap_rms_norm.
+ */
+BEVPOOL_API int bevmap_rms_norm_int8(const bevmap_rms *norm, const void *x, const void *residual,
+                                     const void *weight, void *sum, int8_t *held, float *scale, void *hip_stream);
+
+/*
+ * Rows as 8-bit integers: held = round(x * (127 / top)), scale = top / 127 with top the
+ * row's largest |x|; rows of zeros, infinities and NaN as above.
+ *  x: device, rows x_stride elements apart (>= columns).
+ *  held: device int8 [rows][columns], scale: device float [rows], overwritten.
+ * Errors: INVALID_ARG (null pointer, a size below 0, x_stride < columns),
+ * UNSUPPORTED_DTYPE, OVERFLOW (rows or x_stride reaching 2^31, columns above 131071),
+ * HIP (launch failure).
+ */
+BEVPOOL_API int bevmap_quantize_int8(const void *x, int64_t x_stride, int8_t *held, float *scale, int64_t rows,
+                                     int32_t columns, int32_t dtype, void *hip_stream);
+
+/*
+ * Product of 8-bit integers with a scale for each row (token) and each feature:
+ *   y[m][n] = x_scale[m] * w_scale[n] * (sum over k of x[m][k] * w[n][k]) + bias[n].
+ * Sums are 32-bit integers, exact for all values of int8 up to 131071 channels; fp32
+ * follows, and one rounding to y_dtype.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t channels, features;          /* of the sum; of the result */
+    int64_t x_stride, w_stride;          /* bytes from row to row, >= channels */
+    int32_t y_dtype;
+} bevmap_linear;
+
+/*
+ *  x: device int8, rows x_stride apart; x_scale: device float [rows].
+ *  w: device int8 [features], rows w_stride apart; w_scale: device float [features].
+ *  bias: device float [features], or NULL.
+ *  y: device [rows][features] of y_dtype, overwritten.
+ * Rows of 16-byte aligned addresses with channels a multiple of 16 are read past the
+ * registers. rows or features of 0 is a call that does nothing.
+ * Errors: INVALID_ARG (null pointer, rows or features below 0, channels below 1, a
+ * stride < channels), UNSUPPORTED_DTYPE, OVERFLOW (channels above 131071, rows reaching
+ * 2^30, a stride reaching 2^31, features above 2^20, rows * features reaching 2^37), HIP
+ * (launch failure).
+ */
+BEVPOOL_API int bevmap_linear_int8(const bevmap_linear *linear, const int8_t *x, const float *x_scale,
+                                   const int8_t *w, const float *w_scale, const float *bias, void *y,
+                                   void *hip_stream);
+
+/* Types of the positions of bevmap_rotary. */
+typedef enum { BEVMAP_POSITION_I32 = 0, BEVMAP_POSITION_I64 = 1, BEVMAP_POSITION_F32 = 2 } bevmap_position;
+
+/*
+ * Rotary positions: the first 2 * pairs channels of each head are pairs (a, b), pair p
+ * being channels (2 p, 2 p + 1) if interleaved, (p, p + pairs) otherwise, and
+ *   (a, b) -> amplitude * (a cos t - b sin t, a sin t + b cos t),
+ *   t = positions[token][p / (pairs / axes)] * frequencies[p].
+ * Later channels keep their values. Positions have `axes` numbers a token: with two axes
+ * the first half of the pairs turns with the first. Angles are formed and reduced in 64
+ * bits; the turn is fp32, and its result is rounded once.
+ * Element (b, n, h, c) of x is at x + b * x_batch + n * x_row + h * x_head + c, strides in
+ * elements.
+ */
+typedef struct {
+    int32_t batch, tokens, heads, dim, pairs, axes;
+    int32_t interleaved;
+    int32_t positions_type;              /* bevmap_position */
+    int32_t dtype;                       /* of x and out */
+    float amplitude;
+    int64_t x_batch, x_row, x_head;
+} bevmap_turn;
+
+/*
+ *  positions:   device [batch][tokens][axes] of positions_type. An infinity or a NaN gives
+ *               NaN in the channels that turn with it.
+ *  frequencies: device double [pairs], radians to a unit of position.
+ *  out:         device [batch][tokens][heads][dim] of dtype, overwritten.
+ *  backward:    not 0 turns by the negative angles: x is then the gradient of out, and out
+ *               the gradient of x.
+ * A size of 0 is a call that does nothing.
+ * Errors: INVALID_ARG (null pointer, batch or tokens below 0, heads, dim, pairs or axes
+ * below 1, 2 * pairs above dim, pairs not a multiple of axes, unknown position type,
+ * amplitude not finite, a stride below 0), UNSUPPORTED_DTYPE, OVERFLOW (batch * tokens
+ * reaching 2^31, heads above 65535, dim above 4096), HIP (launch failure).
+ */
+BEVPOOL_API int bevmap_rotary(const bevmap_turn *turn, const void *x, const void *positions,
+                              const double *frequencies, void *out, int32_t backward, void *hip_stream);
+
+/*
+ * Gated activation: a row of x holds `features` gates and then as many values,
+ *   y[f] = act(gate[f]) * value[f].
+ */
+typedef struct {
+    int64_t rows;
+    int32_t features;
+    int32_t act;           /* bevmap_act */
+    int32_t dtype;         /* of x, y and their gradients */
+    int64_t x_stride;      /* elements from row to row of x, >= 2 * features */
+} bevmap_gate;
+
+/*
+ *  x:     device [rows], rows x_stride apart.
+ *  y:     device [rows][features], overwritten.
+ *  held, exponents: NULL, or device int8 [rows][2][features] and uint8
+ *         [rows][2][ceil(features / 32)], overwritten with x in 8 bits for the backward:
+ *         32 neighbouring channels of a half share the least power of two 2^e whose 127-fold
+ *         reaches their largest magnitude (e at least -127), held = round(x / 2^e) with
+ *         halves to the even neighbour, exponents = e + 127; 255 and zeros for channels with
+ *         an infinity or a NaN among them, which the backward takes as NaN.
+ * rows of 0 is a call that does nothing.
+ * Errors: INVALID_ARG (null pointer, one of held and exponents without the other, rows
+ * below 0, features below 1, x_stride < 2 * features, unknown act), UNSUPPORTED_DTYPE,
+ * OVERFLOW (rows or x_stride reaching 2^31, features reaching 2^24), HIP (launch failure).
+ */
+BEVPOOL_API int bevmap_gated_act(const bevmap_gate *gate, const void *x, void *y, int8_t *held, uint8_t *exponents,
+                                 void *hip_stream);
+
+/*
+ * Gradients of bevmap_gated_act, from x (held and exponents NULL), or from what it held of
+ * x (x may then be NULL):
+ *  grad_y: device [rows][features].  grad_x: device [rows][2 * features], overwritten.
+ * Errors: those of bevmap_gated_act.
+ */
+BEVPOOL_API int bevmap_gated_act_backward(const bevmap_gate *gate, const void *grad_y, const void *x,
+                                          const int8_t *held, const uint8_t *exponents, void *grad_x,
+                                          void *hip_stream);
 
 #ifdef __cplusplus
 }

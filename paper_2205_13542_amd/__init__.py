@@ -8,7 +8,9 @@ the points of each cell are summed. The work runs in libbevpool.so
 package is the thin binding: ``_binding`` mirrors the C calls one to one, and
 ``Plan`` adds torch tensor plumbing (device memory and the current stream
 only). ``group_norm_act``, ``cross_attention`` and ``dropout_add`` are the
-operators of a model that reads the pooled map (``map_ops``, include/bevmap.h).
+operators of a model that reads the pooled map (``map_ops``, include/bevmap.h);
+``rms_norm``, ``rotary``, ``gated_act``, ``linear_int8`` and their kin are those
+around attention (``layer_ops``).
 There is no CPU fallback. A missing library raises ImportError. torch is
 imported where a call needs it, not before.
 """
@@ -35,6 +37,8 @@ __all__ = [
     "bevpool_geometry", "geometry_of", "BEVPOOL_F32", "BEVPOOL_BF16", "BEVPOOL_F16",
     "bevpool_associate_noalloc", "associate_noalloc", "bevpool_plan_slabs",
     "group_norm_act", "cross_attention", "dropout_add",
+    "rms_norm", "rms_norm_add", "rms_norm_int8", "rms_norm_add_int8", "quantize_int8", "linear_int8",
+    "rotary", "rotary_frequencies", "gated_act",
 ]
 
 _GEOM_FIELDS = [f for f, _ in bevpool_geometry._fields_]
@@ -362,3 +366,60 @@ def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
 def dropout_add(x, p, seed, offset=0, residual=None):
     """residual + dropout(x), the mask drawn where it is used: ``map_ops.dropout_add``."""
     return _map_ops().dropout_add(x, p, seed, offset, residual)
+
+
+_LAYER_OPS = None
+
+
+def _layer_ops():
+    global _LAYER_OPS
+    if _LAYER_OPS is None:
+        from . import layer_ops
+        _LAYER_OPS = layer_ops
+    return _LAYER_OPS
+
+
+def rms_norm(x, weight=None, eps=1e-6, out_dtype=None):
+    """Root-mean-square norm of every row: ``layer_ops.rms_norm``."""
+    return _layer_ops().rms_norm(x, weight, eps, out_dtype)
+
+
+def rms_norm_add(x, residual, weight=None, eps=1e-6, out_dtype=None):
+    """The norm of x + residual, and that sum: ``layer_ops.rms_norm_add``."""
+    return _layer_ops().rms_norm_add(x, residual, weight, eps, out_dtype)
+
+
+def rms_norm_int8(x, weight=None, eps=1e-6):
+    """The norm as 8-bit integers and a scale for each row: ``layer_ops.rms_norm_int8``."""
+    return _layer_ops().rms_norm_int8(x, weight, eps)
+
+
+def rms_norm_add_int8(x, residual, weight=None, eps=1e-6):
+    """The norm of x + residual in 8 bits, and that sum: ``layer_ops.rms_norm_add_int8``."""
+    return _layer_ops().rms_norm_add_int8(x, residual, weight, eps)
+
+
+def quantize_int8(x):
+    """Rows as 8-bit integers and a scale for each: ``layer_ops.quantize_int8``."""
+    return _layer_ops().quantize_int8(x)
+
+
+def linear_int8(x, x_scale, weight, weight_scale, bias=None, out_dtype=None):
+    """Product of 8-bit integers with token and channel scales: ``layer_ops.linear_int8``."""
+    return _layer_ops().linear_int8(x, x_scale, weight, weight_scale, bias, out_dtype)
+
+
+def rotary(x, positions, frequencies, interleaved=False, amplitude=1.0):
+    """Pairs of channels turned by a token's position: ``layer_ops.rotary``."""
+    return _layer_ops().rotary(x, positions, frequencies, interleaved, amplitude)
+
+
+def rotary_frequencies(pairs, base=10000.0, axes=1, scaling=None, factor=1.0, context=None, fast=32.0, slow=1.0,
+                       device=None):
+    """Frequencies of ``rotary``, scaled for long contexts: ``layer_ops.rotary_frequencies``."""
+    return _layer_ops().rotary_frequencies(pairs, base, axes, scaling, factor, context, fast, slow, device)
+
+
+def gated_act(x, act="silu", checkpoint=None):
+    """act(gate) * value, kept for the backward in 8 bits if asked: ``layer_ops.gated_act``."""
+    return _layer_ops().gated_act(x, act, checkpoint)

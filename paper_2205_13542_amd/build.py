@@ -19,7 +19,8 @@ FLOOR_SOURCE = "floor.hip"
 FLOOR_LIB_PATH = os.path.join(HERE, "libbevpool_floor.so")
 SOURCES = ["bevpool.hip", "plan.hip", "forward.hip", "backward.hip", "layout.hip",
            "mapops.hip", "norm.hip", "dropout.hip", "attention.hip",
-           "attention_backward.hip"]
+           "attention_backward.hip", "layerops.hip", "rms_norm.hip", "rotary.hip",
+           "gated.hip", "linear_int8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

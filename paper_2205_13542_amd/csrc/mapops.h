@@ -1,5 +1,6 @@
 // Declarations and device helpers shared by the map operators (include/bevmap.h):
-// norm.hip, attention.hip and dropout.hip launch, mapops.hip checks.
+// norm.hip, attention.hip, dropout.hip, rms_norm.hip, rotary.hip, gated.hip and
+// linear_int8.hip launch, mapops.hip and layerops.hip check.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -9,7 +10,9 @@
 #include "internal.h"
 
 // Limits that the kernels assume.
-constexpr int kNormMaxChannels = 8192;  // two floats a channel in LDS
+constexpr int kNormMaxChannels = 8192;  // two floats a channel in LDS; a row in a workgroup's registers
+constexpr int kInt8MaxChannels = 131071;        // 128 * 128 * this stays below 2^31
+constexpr int kTurnMaxDim = 4096;
 constexpr int kAttendMaxDim = 128;
 constexpr int kAttendTile = 128;        // rows or keys that a workgroup owns
 constexpr int64_t kAttendMaxTiles = int64_t(1) << 23;   // workgroups of a launch; more are never needed to split an axis
@@ -33,6 +36,22 @@ int bevmap_launch_attention_backward(const bevmap_attend &a, const void *grad_ou
 int bevmap_launch_dropout(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, void *y,
                           int64_t rows, int64_t columns, int32_t dtype, int32_t threshold, uint64_t seed,
                           uint64_t offset, hipStream_t stream);
+// q, scale: the result in 8 bits, instead of y and rstd.
+int bevmap_launch_rms_norm(const bevmap_rms &n, const void *x, const void *residual, const void *weight, void *sum,
+                           void *y, float *rstd, int8_t *q, float *scale, hipStream_t stream);
+int64_t bevmap_rms_workspace_bytes(const bevmap_rms &n);
+int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, const void *grad_sum, const void *x,
+                                    const void *weight, const float *rstd, void *grad_x, void *grad_weight,
+                                    void *workspace, hipStream_t stream);
+int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *scale, int64_t rows, int32_t columns,
+                           int32_t dtype, hipStream_t stream);
+int bevmap_launch_linear_int8(const bevmap_linear &n, const int8_t *x, const float *x_scale, const int8_t *w,
+                              const float *w_scale, const float *bias, void *y, hipStream_t stream);
+int bevmap_launch_rotary(const bevmap_turn &n, const void *x, const void *positions, const double *frequencies,
+                         void *out, bool backward, hipStream_t stream);
+int bevmap_launch_gate(const bevmap_gate &n, const void *x, void *y, int8_t *q, uint8_t *e, hipStream_t stream);
+int bevmap_launch_gate_backward(const bevmap_gate &n, const void *grad_y, const void *x, const int8_t *q,
+                                const uint8_t *e, void *grad_x, hipStream_t stream);
 
 namespace bevmap {
 namespace {

@@ -16,6 +16,7 @@
 // what it reads is still there.
 // Eight frames of 360x360x80 in bf16 take 33 + 56 us forward and 80-84 + 94 backward: the
 // 1.33 GB that two passes move, at 4.8 TB/s, what a large copy reaches.
+#include "activation.h"
 #include "mapops.h"
 
 namespace bevmap {
@@ -44,42 +45,6 @@ struct NormArgs {
     bool stream;                    // results past the caches
     float eps;
 };
-
-template <int ACT>
-__device__ __forceinline__ float activate(float z) {
-    if constexpr (ACT == BEVMAP_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if constexpr (ACT == BEVMAP_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-    if constexpr (ACT == BEVMAP_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    return z;
-}
-
-template <int ACT>
-__device__ __forceinline__ float slope(float z) {
-    if constexpr (ACT == BEVMAP_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if constexpr (ACT == BEVMAP_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    if constexpr (ACT == BEVMAP_ACT_GELU)
-        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * __expf(-0.5f * z * z) * 0.39894228f;
-    return 1.0f;
-}
-
-// body(constant) with the activation as a constant: one uniform branch for a batch
-// of rows instead of one for an element.
-template <int V>
-struct Constant {
-    static constexpr int value = V;
-};
-template <class F>
-__device__ __forceinline__ void with_act(int act, F body) {
-    switch (act) {
-        case BEVMAP_ACT_RELU: body(Constant<BEVMAP_ACT_RELU>()); break;
-        case BEVMAP_ACT_SILU: body(Constant<BEVMAP_ACT_SILU>()); break;
-        case BEVMAP_ACT_GELU: body(Constant<BEVMAP_ACT_GELU>()); break;
-        default: body(Constant<BEVMAP_ACT_NONE>()); break;
-    }
-}
 
 __device__ __forceinline__ float weight_at(const void *w, int c, int dtype, float none) {
     float v = none;

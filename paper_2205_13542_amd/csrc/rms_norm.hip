@@ -1,0 +1,533 @@
+// Root-mean-square norm of rows, of x + residual where there is one, with its gradients
+// (bevmap_rms_norm, bevmap_rms_norm_backward), and rows held in 8-bit integers
+// (bevmap_rms_norm_int8, bevmap_quantize_int8).
+//
+//   h = x + residual,  r = 1 / sqrt(mean h^2 + eps),  y = w h r
+//   u = h r, e = dy w:  dh = dsum + r (e - u mean(e u)),  dw = sum over rows of dy u
+//   z = h w, top = max |z|:  q = round(z (127 / top)),  scale = top r / 127
+// r cancels in q, so the integers do not depend on the order in which the squares are
+// summed, and one pass over the row in registers gives both.
+//
+// Bound by memory: a row stays in the registers of the lanes that share it, and each
+// tensor is read or written once. Lanes: the least power of two that holds a row at V
+// elements a lane, up to a wave; longer rows take several accesses a lane, or a whole
+// workgroup. Workgroups stay and walk the rows, so that the weights are read once into
+// registers and the backward sums dw there; its parts are joined in a fixed order by a
+// small kernel.
+#include "mapops.h"
+
+namespace bevmap {
+namespace {
+
+constexpr int kRmsBlock = 256;
+constexpr int kRmsWave = 64;
+constexpr int kRmsJoinChannels = 16;   // channels of a workgroup that joins parts of dw
+constexpr int kRmsJoinBlock = 1024;
+
+struct RmsArgs {
+    const void *x, *residual, *weight, *dy, *dsum;
+    void *sum, *y;                  // backward: sum is dx
+    int8_t *q;
+    float *rstd, *scale, *parts;    // parts: [workgroups][C]
+    int64_t ldx, ldr, rows, chunk;  // chunk: rows of a workgroup of the backward
+    int32_t C, y_dtype, w_dtype;
+    float eps;
+};
+
+enum { kFloat, kInt8Norm, kInt8 };      // what a forward kernel writes
+
+// Sum, or the largest of unsigned numbers, over the LANES lanes that share a row. Over a
+// workgroup: through LDS, two slots in turn, so that one barrier a row is enough.
+template <class F, class T>
+__device__ __forceinline__ T over_wave(T v, int lanes, F f) {
+#pragma unroll
+    for (int m = 1; m < lanes; m <<= 1) v = f(v, __shfl_xor(v, m));
+    return v;
+}
+template <int LANES, class F, class T>
+__device__ __forceinline__ T over_lanes(T v, F f, T *slots, int turn) {
+    if constexpr (LANES <= kRmsWave) return over_wave(v, LANES, f);
+    constexpr int kWaves = kRmsBlock / kRmsWave;
+    v = over_wave(v, kRmsWave, f);
+    T *s = slots + (turn & 1) * kWaves;
+    if (threadIdx.x % kRmsWave == 0) s[threadIdx.x / kRmsWave] = v;
+    __syncthreads();
+    return f(f(s[0], s[1]), f(s[2], s[3]));
+}
+
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+// |v| as an unsigned number: in the order of magnitudes, with NaN above infinity
+__device__ __forceinline__ uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// How z becomes q: q = round(z * up * mul), scale = top * rstd / 127.
+struct Steps {
+    float up, mul, scale;
+    bool none;      // a row with an infinity or a NaN: q = 0, scale NaN
+};
+__device__ __forceinline__ Steps steps_of(uint32_t top_bits, float rstd) {
+    const float top = __uint_as_float(top_bits);
+    Steps s;
+    s.none = top_bits >= kInfBits;
+    s.up = top < 0x1p-100f ? 0x1p64f : 1.0f;            // 127 / top would be infinite
+    s.mul = top > 0.0f && !s.none ? 127.0f / (top * s.up) : 0.0f;
+    s.scale = s.none ? __uint_as_float(0x7FC00000u) : top * rstd / 127.0f;
+    return s;
+}
+__device__ __forceinline__ int8_t held(float z, const Steps &s) {
+    return int8_t(s.none ? 0.0f : rintf(z * s.up * s.mul));
+}
+
+template <int V>
+__device__ __forceinline__ void store_held(int8_t *p, const int8_t *v) {
+    struct alignas(V) Bytes {
+        int8_t v[V];
+    } b;
+#pragma unroll
+    for (int i = 0; i < V; ++i) b.v[i] = v[i];
+    *reinterpret_cast<Bytes *>(p) = b;
+}
+
+template <int DT, int V, int LANES, int ITER, int OUT>
+__global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
+    using T = typename Num<DT>::T;
+    constexpr int kRows = kRmsBlock / LANES;
+    __shared__ float add[8];
+    __shared__ uint32_t most[8];
+    const int lane = threadIdx.x % LANES, n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
+    T *sum = static_cast<T *>(a.sum);
+    float w[ITER][V];
+#pragma unroll
+    for (int k = 0; k < ITER; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[k][i] = 1.0f;
+        if (OUT != kInt8 && a.weight && lane + k * LANES < n_vec)
+            load_any<V>(a.weight, int64_t(lane + k * LANES) * V, a.w_dtype, w[k]);
+    }
+    const float per = 1.0f / float(a.C);
+    int turn = 0;
+    for (int64_t first = int64_t(blockIdx.x) * kRows; first < a.rows; first += int64_t(gridDim.x) * kRows, ++turn) {
+        const int64_t row = first + threadIdx.x / LANES;
+        const bool live = row < a.rows;
+        float h[ITER][V];
+#pragma unroll
+        for (int k = 0; k < ITER; ++k) {
+            const int at = lane + k * LANES;
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[k][i] = 0.0f;
+            if (live && at < n_vec) {
+                load_n<T, V>(x + row * a.ldx + at * V, h[k]);
+                if (OUT != kInt8 && res) {
+                    float r[V];
+                    load_n<T, V>(res + row * a.ldr + at * V, r);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[k][i] += r[i];
+                    store_n<T, V>(sum + row * a.C + at * V, h[k]);
+                }
+            }
+        }
+        float rstd = 1.0f;
+        if constexpr (OUT != kInt8) {
+            float ss = 0.0f;
+#pragma unroll
+            for (int k = 0; k < ITER; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) ss = fmaf(h[k][i], h[k][i], ss);
+            ss = over_lanes<LANES>(ss, plus, add, turn);
+            // Squares that leave fp32's range: the row's numbers times a power of two, squared again.
+            // (A sum of 0 is a row of zeros, or of numbers so small that only an eps of nothing shows them.)
+            const bool large = !(ss < 0x1p120f), small = ss < 0x1p-90f && a.eps < 0x1p-60f;
+            float s = 1.0f;
+            if (LANES > kRmsWave ? large || small : __any(large || small)) {
+                s = large ? 0x1p-80f : small ? 0x1p93f : 1.0f;
+                float again = 0.0f;
+#pragma unroll
+                for (int k = 0; k < ITER; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) again = fmaf(h[k][i] * s, h[k][i] * s, again);
+                if constexpr (LANES > kRmsWave) __syncthreads();    // the slots are read
+                ss = over_lanes<LANES>(again, plus, add, turn);
+            }
+            rstd = s / sqrtf(ss * per + a.eps * s * s);
+        }
+        if constexpr (OUT == kFloat) {
+            if (a.rstd && live && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+            for (int k = 0; k < ITER; ++k) {
+                const int at = lane + k * LANES;
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * rstd * w[k][i];
+                if (live && at < n_vec) store_any<V>(a.y, row * a.C + at * V, a.y_dtype, h[k]);
+            }
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < ITER; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if constexpr (OUT == kInt8Norm) h[k][i] *= w[k][i];
+                    if (lane + k * LANES < n_vec) top = larger(top, size_bits(h[k][i]));
+                }
+            top = over_lanes<LANES>(top, larger, most, turn);
+            const Steps steps = steps_of(top, rstd);
+            if (live && lane == 0) a.scale[row] = steps.scale;
+#pragma unroll
+            for (int k = 0; k < ITER; ++k) {
+                const int at = lane + k * LANES;
+                int8_t q[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) q[i] = held(h[k][i], steps);
+                if (live && at < n_vec) store_held<V>(a.q + row * a.C + at * V, q);
+            }
+        }
+    }
+}
+
+// Rows too long for registers, a workgroup to a row: read twice, the second time from cache.
+template <int DT, int V>
+__global__ __launch_bounds__(kRmsBlock) void k_quantize_long(RmsArgs a) {
+    using T = typename Num<DT>::T;
+    __shared__ uint32_t most[8];
+    const int n_vec = a.C / V;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
+        const T *x = static_cast<const T *>(a.x) + row * a.ldx;
+        uint32_t top = 0;
+        for (int at = threadIdx.x; at < n_vec; at += kRmsBlock) {
+            float v[V];
+            load_n<T, V>(x + int64_t(at) * V, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = larger(top, size_bits(v[i]));
+        }
+        const Steps steps = steps_of(over_lanes<kRmsBlock>(top, larger, most, turn), 1.0f);
+        if (threadIdx.x == 0) a.scale[row] = steps.scale;
+        for (int at = threadIdx.x; at < n_vec; at += kRmsBlock) {
+            float v[V];
+            int8_t q[V];
+            load_n<T, V>(x + int64_t(at) * V, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) q[i] = held(v[i], steps);
+            store_held<V>(a.q + row * a.C + int64_t(at) * V, q);
+        }
+    }
+}
+
+template <int DT, int V, int LANES, int ITER>
+__global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
+    using T = typename Num<DT>::T;
+    constexpr int kRows = kRmsBlock / LANES;
+    extern __shared__ float joined[];       // [C], rows shared by a wave or less
+    __shared__ float add[8];
+    const int lane = threadIdx.x % LANES, n_vec = a.C / V;
+    const T *x = static_cast<const T *>(a.x), *dsum = static_cast<const T *>(a.dsum);
+    T *dx = static_cast<T *>(a.sum);
+    float w[ITER][V], dw[ITER][V];
+#pragma unroll
+    for (int k = 0; k < ITER; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[k][i] = 1.0f;
+            dw[k][i] = 0.0f;
+        }
+        if (a.weight && lane + k * LANES < n_vec)
+            load_any<V>(a.weight, int64_t(lane + k * LANES) * V, a.w_dtype, w[k]);
+    }
+    const float per = 1.0f / float(a.C);
+    const int64_t begin = int64_t(blockIdx.x) * a.chunk, end = min(begin + a.chunk, a.rows);
+    int turn = 0;
+    for (int64_t first = begin; first < end; first += kRows, ++turn) {
+        const int64_t row = first + threadIdx.x / LANES;
+        const bool live = row < end;
+        const float rstd = live ? a.rstd[row] : 0.0f;
+        float u[ITER][V], e[ITER][V], more[ITER][V], dot = 0.0f;
+#pragma unroll
+        for (int k = 0; k < ITER; ++k) {
+            const int at = lane + k * LANES;
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[k][i] = e[k][i] = more[k][i] = 0.0f;
+            if (live && at < n_vec) {
+                load_n<T, V>(x + row * a.ldx + at * V, u[k]);
+                load_any<V>(a.dy, row * a.C + at * V, a.y_dtype, e[k]);
+                if (dsum) load_n<T, V>(dsum + row * a.C + at * V, more[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ITER; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                u[k][i] *= rstd;
+                dw[k][i] = fmaf(e[k][i], u[k][i], dw[k][i]);
+                e[k][i] *= w[k][i];
+                dot = fmaf(e[k][i], u[k][i], dot);
+            }
+        const float mean = over_lanes<LANES>(dot, plus, add, turn) * per;
+#pragma unroll
+        for (int k = 0; k < ITER; ++k) {
+            const int at = lane + k * LANES;
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[k][i] = fmaf(rstd, fmaf(-u[k][i], mean, e[k][i]), more[k][i]);
+            if (live && at < n_vec) store_n<T, V>(dx + row * a.C + at * V, e[k]);
+        }
+    }
+    if (!a.parts) return;
+    float *part = a.parts + int64_t(blockIdx.x) * a.C;
+    if constexpr (LANES > kRmsWave) {
+#pragma unroll
+        for (int k = 0; k < ITER; ++k)
+            if (lane + k * LANES < n_vec) store_n<float, V>(part + (lane + k * LANES) * V, dw[k]);
+    } else {
+        // over the rows of a wave, then one wave after the other
+#pragma unroll
+        for (int k = 0; k < ITER; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int m = LANES; m < kRmsWave; m <<= 1) dw[k][i] += __shfl_xor(dw[k][i], m);
+        constexpr int kWaves = kRmsBlock / kRmsWave;
+        const int wave = threadIdx.x / kRmsWave;
+        for (int turns = 0; turns < kWaves; ++turns) {
+            if (wave == turns && threadIdx.x % kRmsWave < LANES)
+#pragma unroll
+                for (int k = 0; k < ITER; ++k) {
+                    const int at = lane + k * LANES;
+                    if (at >= n_vec) continue;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (turns > 0) dw[k][i] += joined[at * V + i];
+                        joined[at * V + i] = dw[k][i];
+                    }
+                    if (turns == kWaves - 1) store_n<float, V>(part + at * V, dw[k]);
+                }
+            __syncthreads();
+        }
+    }
+}
+
+// dw = the sum of the parts, in halves over the lanes that share a channel.
+__global__ __launch_bounds__(kRmsJoinBlock) void k_rms_join(const float *parts, int n, int C, void *dw, int dtype) {
+    constexpr int kLanes = kRmsJoinBlock / kRmsJoinChannels;
+    __shared__ float th[kLanes][kRmsJoinChannels + 1];
+    const int i = threadIdx.x % kRmsJoinChannels, lane = threadIdx.x / kRmsJoinChannels;
+    const int c = blockIdx.x * kRmsJoinChannels + i;
+    float sum = 0.0f;
+    if (c < C)
+#pragma unroll 8
+        for (int p = lane; p < n; p += kLanes) sum += parts[int64_t(p) * C + c];
+    th[lane][i] = sum;
+    for (int half = kLanes / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (lane < half) th[lane][i] += th[lane + half][i];
+    }
+    if (lane == 0 && c < C) store_any<1>(dw, c, dtype, &th[0][i]);
+}
+
+// A form: elements of an access, lanes that share a row, accesses of a lane.
+struct Form {
+    int v, lanes, iter;
+};
+
+constexpr int64_t kRmsGroups = 2048;    // workgroups that stay: eight to a compute unit
+
+// Elements of an access: as many as 16 bytes hold where the rows allow it, two, or one.
+int access(int32_t dtype, int32_t C, const void *const *p, const int64_t *stride, int n) {
+    for (int v : {dtype == BEVPOOL_F32 ? 4 : 8, 2}) {
+        bool fits = C % v == 0;
+        for (int i = 0; i < n; ++i) fits = fits && aligned_for(p[i], stride[i], dtype, v);
+        if (fits) return v;
+    }
+    return 1;
+}
+
+// Few rows are spread over as many lanes as there are; many rows take the fewest lanes
+// that keep a row in at most eight accesses.
+Form form_of(int v, int32_t C, int64_t rows) {
+    const int n = (C + v - 1) / v;
+    const int few = rows < 4 * kRmsGroups;
+    if (n <= 64) return {v, n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
+    if (!few && n <= 512) return {v, 64, n <= 128 ? 2 : n <= 256 ? 4 : 8};
+    return {v, 256, n <= 256 ? 1 : n <= 512 ? 2 : n <= 1024 ? 4 : n <= 2048 ? 8 : 32};
+}
+
+// body(constants V, LANES, ITER) of a form
+template <int V>
+struct Int {
+    static constexpr int value = V;
+};
+template <int WIDE, class F>
+void with_form(const Form &f, F body) {
+    auto lanes = [&](auto v) {
+        if (f.lanes == 8) return body(v, Int<8>(), Int<1>());
+        if (f.lanes == 16) return body(v, Int<16>(), Int<1>());
+        if (f.lanes == 32) return body(v, Int<32>(), Int<1>());
+        if (f.lanes == 64) {
+            if (f.iter == 1) return body(v, Int<64>(), Int<1>());
+            if (f.iter == 2) return body(v, Int<64>(), Int<2>());
+            if (f.iter == 4) return body(v, Int<64>(), Int<4>());
+            return body(v, Int<64>(), Int<8>());
+        }
+        if (f.iter == 1) return body(v, Int<256>(), Int<1>());
+        if (f.iter == 2) return body(v, Int<256>(), Int<2>());
+        if (f.iter == 4) return body(v, Int<256>(), Int<4>());
+        if constexpr (decltype(v)::value <= 4)
+            if (f.iter == 8) return body(v, Int<256>(), Int<8>());
+        if constexpr (decltype(v)::value <= 2) return body(v, Int<256>(), Int<32>());
+    };
+    if (f.v == WIDE) return lanes(Int<WIDE>());
+    if (f.v == 2) return lanes(Int<2>());
+    lanes(Int<1>());
+}
+
+template <int OUT>
+int launch_rows(RmsArgs a, int32_t dtype, const Form &f, hipStream_t stream) {
+    const int64_t each = kRmsBlock / f.lanes, all = (a.rows + each - 1) / each;
+    const dim3 grid{uint32_t(all < kRmsGroups ? all : kRmsGroups)}, wg(kRmsBlock);
+    auto go = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        with_form<DT == BEVPOOL_F32 ? 4 : 8>(f, [&](auto v, auto lanes, auto iter) {
+            hipLaunchKernelGGL((k_rms<DT, decltype(v)::value, decltype(lanes)::value, decltype(iter)::value, OUT>),
+                               grid, wg, 0, stream, a);
+        });
+    };
+    if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
+    else if (dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
+    else go(Int<BEVPOOL_F16>());
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+// Rows of a workgroup of the backward, a multiple of those it takes at once.
+int64_t chunk_of(int64_t rows, int64_t each) {
+    // eight rows or more to a lane, so that parts of dw cost little beside the rows, if that
+    // leaves two workgroups to a compute unit
+    const int64_t share = (rows + kRmsGroups - 1) / kRmsGroups, half = (rows + 511) / 512;
+    int64_t chunk = half < 8 * each ? half : 8 * each;
+    if (share > chunk) chunk = share;
+    return (chunk + each - 1) / each * each;
+}
+
+}  // namespace
+}  // namespace bevmap
+
+using namespace bevmap;
+
+// Parts of dw: as many as any form of these sizes makes.
+int64_t bevmap_rms_workspace_bytes(const bevmap_rms &n) {
+    if (n.rows == 0) return 0;
+    int64_t most = 0;
+    for (int64_t each : {1, 4, 8, 16, 32}) {
+        const int64_t chunk = chunk_of(n.rows, each), groups = (n.rows + chunk - 1) / chunk;
+        if (groups > most) most = groups;
+    }
+    return most * n.channels * int64_t(sizeof(float));
+}
+
+int bevmap_launch_rms_norm(const bevmap_rms &n, const void *x, const void *residual, const void *weight, void *sum,
+                           void *y, float *rstd, int8_t *q, float *scale, hipStream_t stream) {
+    if (n.rows == 0) return BEVPOOL_OK;
+    RmsArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.sum = sum;
+    a.y = y;
+    a.rstd = rstd;
+    a.q = q;
+    a.scale = scale;
+    a.ldx = n.x_stride;
+    a.ldr = n.residual_stride;
+    a.rows = n.rows;
+    a.C = n.channels;
+    a.y_dtype = n.y_dtype;
+    a.w_dtype = n.weight_dtype;
+    a.eps = n.eps;
+    const bool one = n.rows == 1;
+    const void *p[] = {x, residual, sum};
+    const int64_t s[] = {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride, 0};
+    int v = access(n.x_dtype, n.channels, p, s, 3);
+    if (weight && !aligned_for(weight, 0, n.weight_dtype, v)) v = 1;
+    if (!q && !aligned_for(y, 0, n.y_dtype, v)) v = 1;
+    if (q && reinterpret_cast<uintptr_t>(q) % uintptr_t(v)) v = 1;
+    const Form f = form_of(v, n.channels, n.rows);
+    return q ? launch_rows<kInt8Norm>(a, n.x_dtype, f, stream) : launch_rows<kFloat>(a, n.x_dtype, f, stream);
+}
+
+int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *scale, int64_t rows, int32_t columns,
+                           int32_t dtype, hipStream_t stream) {
+    if (rows == 0) return BEVPOOL_OK;
+    RmsArgs a{};
+    a.x = x;
+    a.q = q;
+    a.scale = scale;
+    a.ldx = x_stride;
+    a.rows = rows;
+    a.C = columns;
+    const void *p[] = {x};
+    const int64_t s[] = {rows == 1 ? 0 : x_stride};
+    int v = access(dtype, columns, p, s, 1);
+    if (reinterpret_cast<uintptr_t>(q) % uintptr_t(v)) v = 1;
+    if (columns <= kNormMaxChannels) return launch_rows<kInt8>(a, dtype, form_of(v, columns, rows), stream);
+    const dim3 grid{uint32_t(rows < kRmsGroups ? rows : kRmsGroups)}, wg(kRmsBlock);
+    auto go = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value, kWide = DT == BEVPOOL_F32 ? 4 : 8;
+        if (v == kWide) hipLaunchKernelGGL((k_quantize_long<DT, kWide>), grid, wg, 0, stream, a);
+        else hipLaunchKernelGGL((k_quantize_long<DT, 1>), grid, wg, 0, stream, a);
+    };
+    if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
+    else if (dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
+    else go(Int<BEVPOOL_F16>());
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, const void *grad_sum, const void *x,
+                                    const void *weight, const float *rstd, void *grad_x, void *grad_weight,
+                                    void *workspace, hipStream_t stream) {
+    int64_t groups = 0;
+    float *parts = grad_weight ? static_cast<float *>(workspace) : nullptr;
+    if (n.rows > 0) {
+        RmsArgs a{};
+        a.x = x;
+        a.weight = weight;
+        a.dy = grad_y;
+        a.dsum = grad_sum;
+        a.sum = grad_x;
+        a.rstd = const_cast<float *>(rstd);
+        a.parts = parts;
+        a.ldx = n.x_stride;
+        a.rows = n.rows;
+        a.C = n.channels;
+        a.y_dtype = n.y_dtype;
+        a.w_dtype = n.weight_dtype;
+        const void *p[] = {x, grad_sum, grad_x};
+        const int64_t s[] = {n.rows == 1 ? 0 : n.x_stride, 0, 0};
+        int v = access(n.x_dtype, n.channels, p, s, 3);
+        if ((weight && !aligned_for(weight, 0, n.weight_dtype, v)) || !aligned_for(grad_y, 0, n.y_dtype, v)) v = 1;
+        const Form f = form_of(v, n.channels, n.rows);
+        const int64_t each = kRmsBlock / f.lanes;
+        a.chunk = chunk_of(n.rows, each);
+        groups = (n.rows + a.chunk - 1) / a.chunk;
+        const dim3 grid{uint32_t(groups)}, wg(kRmsBlock);
+        const size_t lds = f.lanes <= kRmsWave ? size_t(n.channels) * sizeof(float) : 0;
+        auto go = [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            with_form<DT == BEVPOOL_F32 ? 4 : 8>(f, [&](auto v, auto lanes, auto iter) {
+                hipLaunchKernelGGL((k_rms_grad<DT, decltype(v)::value, decltype(lanes)::value, decltype(iter)::value>),
+                                   grid, wg, lds, stream, a);
+            });
+        };
+        if (n.x_dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
+        else if (n.x_dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
+        else go(Int<BEVPOOL_F16>());
+        BEVPOOL_HIP(hipGetLastError());
+    }
+    if (grad_weight) {
+        const dim3 grid{uint32_t((n.channels + kRmsJoinChannels - 1) / kRmsJoinChannels)}, wg(kRmsJoinBlock);
+        hipLaunchKernelGGL(k_rms_join, grid, wg, 0, stream, parts, int(groups), n.channels, grad_weight,
+                           n.weight_dtype);
+        BEVPOOL_HIP(hipGetLastError());
+    }
+    return BEVPOOL_OK;
+}

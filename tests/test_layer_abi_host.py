@@ -1,0 +1,276 @@
+"""Host-side checks of the operators around attention (no GPU needed): refusals before
+any device work, and the frequencies of rotary positions."""
+import ctypes
+import inspect
+import math
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2205_13542_amd import _binding, _map_binding, build
+    if not os.path.exists(_binding.LIB_PATH):
+        build.build()
+    return _map_binding.load()
+
+
+@pytest.fixture(scope="module")
+def mb(lib):
+    from paper_2205_13542_amd import _map_binding
+    return _map_binding
+
+
+P = ctypes.c_void_p(16)     # a pointer that no refused call follows
+INVALID, DTYPE, OVERFLOW = -1, -3, -4
+
+
+def _rms(mb, **over):
+    vals = dict(rows=9, channels=12, x_dtype=0, y_dtype=0, weight_dtype=0, x_stride=12, residual_stride=12, eps=1e-6)
+    vals.update(over)
+    return mb.bevmap_rms(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(rows=-1), INVALID), (dict(channels=0), INVALID), (dict(channels=-3), INVALID), (dict(x_stride=11), INVALID),
+    (dict(eps=-1.0), INVALID), (dict(eps=math.nan), INVALID), (dict(eps=math.inf), INVALID), (dict(x_dtype=3), DTYPE),
+    (dict(y_dtype=-1), DTYPE), (dict(weight_dtype=9), DTYPE), (dict(rows=1 << 31), OVERFLOW),
+    (dict(channels=8193, x_stride=8193, residual_stride=8193), OVERFLOW), (dict(x_stride=1 << 31), OVERFLOW)])
+def test_rms_norm_refuses(lib, mb, over, code):
+    n = _rms(mb, **over)
+    assert lib.bevmap_rms_norm_backward_workspace(n) == code
+    assert lib.bevmap_rms_norm(n, P, P, P, P, P, P, None) == code
+    assert lib.bevmap_rms_norm_int8(n, P, P, P, P, P, P, None) == code
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, 1 << 40, None) == code
+
+
+def test_rms_norm_refuses_pointers_strides_and_workspaces(lib, mb):
+    n = _rms(mb)
+    need = lib.bevmap_rms_norm_backward_workspace(n)
+    assert need > 0 and need % 48 == 0
+    for args in ((None, P, P, P, P, P), (P, P, P, None, P, P), (P, None, P, None, None, P)):
+        assert lib.bevmap_rms_norm(n, *args, None) == INVALID
+    for args in ((None, P, P, P, P, P), (P, P, P, None, P, P), (P, None, P, None, None, P), (P, None, P, None, P, None)):
+        assert lib.bevmap_rms_norm_int8(n, *args, None) == INVALID
+    for k in (0, 2, 4, 5):
+        args = [P] * 8
+        args[k] = None
+        assert lib.bevmap_rms_norm_backward(n, *args, need, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, need - 1, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, None, need, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, ctypes.c_void_p(8), need, None) == INVALID
+    assert lib.bevmap_rms_norm(None, P, P, P, P, P, P, None) == INVALID
+    short = _rms(mb, residual_stride=11)
+    assert lib.bevmap_rms_norm(short, P, P, P, P, P, P, None) == INVALID
+    empty = _rms(mb, rows=0)
+    assert lib.bevmap_rms_norm_backward_workspace(empty) == 0
+    assert lib.bevmap_rms_norm(empty, None, None, None, None, None, None, None) == 0
+    assert lib.bevmap_rms_norm_int8(empty, None, None, None, None, None, None, None) == 0
+    assert lib.bevmap_rms_norm_backward(empty, None, None, None, None, None, None, None, None, 0, None) == 0
+
+
+def test_rms_norm_workspace_stays_below_the_rows(lib, mb):
+    """Parts of the weights' gradient, at most a row of fp32 for each row, and at most 2048 of them."""
+    for rows in (1, 3, 600, 5000, 518400, 1 << 30):
+        for channels in (1, 80, 1030, 8192):
+            n = _rms(mb, rows=rows, channels=channels, x_stride=channels)
+            size = lib.bevmap_rms_norm_backward_workspace(n)
+            assert 0 < size <= 4 * channels * min(rows, 2048)
+
+
+@pytest.mark.parametrize("args,code", [
+    ((P, 8, P, P, -1, 8, 0), INVALID), ((P, 8, P, P, 4, -8, 0), INVALID), ((P, 7, P, P, 4, 8, 0), INVALID),
+    ((None, 8, P, P, 4, 8, 0), INVALID), ((P, 8, None, P, 4, 8, 0), INVALID), ((P, 8, P, None, 4, 8, 0), INVALID),
+    ((P, 8, P, P, 4, 8, 3), DTYPE), ((P, 1 << 17, P, P, 4, 1 << 17, 0), OVERFLOW),
+    ((P, 1 << 31, P, P, 4, 8, 0), OVERFLOW), ((P, 8, P, P, 1 << 31, 8, 0), OVERFLOW),
+    ((None, 8, None, None, 0, 8, 0), 0)])
+def test_quantize_refuses(lib, args, code):
+    assert lib.bevmap_quantize_int8(*args, None) == code
+
+
+def _linear(mb, **over):
+    vals = dict(rows=5, channels=16, features=7, x_stride=16, w_stride=16, y_dtype=1)
+    vals.update(over)
+    return mb.bevmap_linear(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(rows=-1), INVALID), (dict(features=-1), INVALID), (dict(channels=0), INVALID), (dict(x_stride=15), INVALID),
+    (dict(w_stride=15), INVALID), (dict(y_dtype=3), DTYPE), (dict(rows=1 << 30), OVERFLOW),
+    (dict(channels=131072, x_stride=131072, w_stride=131072), OVERFLOW), (dict(x_stride=1 << 31), OVERFLOW),
+    (dict(w_stride=1 << 31), OVERFLOW), (dict(features=(1 << 20) + 1), OVERFLOW),
+    (dict(rows=1 << 20, features=1 << 17), OVERFLOW)])
+def test_linear_refuses(lib, mb, over, code):
+    assert lib.bevmap_linear_int8(_linear(mb, **over), P, P, P, P, P, P, None) == code
+
+
+def test_linear_refuses_pointers(lib, mb):
+    for k in (0, 1, 2, 3, 5):
+        args = [P] * 6
+        args[k] = None
+        assert lib.bevmap_linear_int8(_linear(mb), *args, None) == INVALID
+    assert lib.bevmap_linear_int8(None, P, P, P, P, P, P, None) == INVALID
+    for empty in (dict(rows=0), dict(features=0)):
+        assert lib.bevmap_linear_int8(_linear(mb, **empty), None, None, None, None, None, None, None) == 0
+
+
+def _turn(mb, **over):
+    vals = dict(batch=2, tokens=3, heads=4, dim=16, pairs=6, axes=2, interleaved=0, positions_type=0, dtype=0,
+                amplitude=1.0, x_batch=192, x_row=64, x_head=16)
+    vals.update(over)
+    return mb.bevmap_turn(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(batch=-1), INVALID), (dict(tokens=-1), INVALID), (dict(heads=0), INVALID), (dict(dim=0), INVALID),
+    (dict(pairs=0), INVALID), (dict(axes=0), INVALID), (dict(pairs=9, axes=1), INVALID), (dict(axes=4), INVALID),
+    (dict(positions_type=3), INVALID), (dict(positions_type=-1), INVALID), (dict(amplitude=math.inf), INVALID),
+    (dict(amplitude=math.nan), INVALID), (dict(x_row=-1), INVALID), (dict(x_batch=-1), INVALID),
+    (dict(x_head=-1), INVALID), (dict(dtype=3), DTYPE), (dict(batch=1 << 16, tokens=1 << 15), OVERFLOW),
+    (dict(heads=65536), OVERFLOW), (dict(dim=4097), OVERFLOW), (dict(pairs=(1 << 30) + 2, axes=1), INVALID)])
+def test_rotary_refuses(lib, mb, over, code):
+    for backward in (0, 1):
+        assert lib.bevmap_rotary(_turn(mb, **over), P, P, P, P, backward, None) == code
+
+
+def test_rotary_refuses_pointers(lib, mb):
+    for k in range(4):
+        args = [P] * 4
+        args[k] = None
+        assert lib.bevmap_rotary(_turn(mb), *args, 0, None) == INVALID
+    assert lib.bevmap_rotary(None, P, P, P, P, 0, None) == INVALID
+    assert lib.bevmap_rotary(_turn(mb, tokens=0), None, None, None, None, 0, None) == 0
+
+
+def _gate(mb, **over):
+    vals = dict(rows=5, features=7, act=2, dtype=0, x_stride=14)
+    vals.update(over)
+    return mb.bevmap_gate(**vals)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(rows=-1), INVALID), (dict(features=0), INVALID), (dict(x_stride=13), INVALID), (dict(act=4), INVALID),
+    (dict(act=-1), INVALID), (dict(dtype=3), DTYPE), (dict(rows=1 << 31), OVERFLOW), (dict(x_stride=1 << 31), OVERFLOW),
+    (dict(features=1 << 24, x_stride=1 << 26), OVERFLOW)])
+def test_gated_act_refuses(lib, mb, over, code):
+    g = _gate(mb, **over)
+    assert lib.bevmap_gated_act(g, P, P, P, P, None) == code
+    assert lib.bevmap_gated_act_backward(g, P, P, P, P, P, None) == code
+
+
+def test_gated_act_refuses_pointers(lib, mb):
+    g = _gate(mb)
+    for args in ((None, P, P, P), (P, None, P, P), (P, P, None, P), (P, P, P, None)):
+        assert lib.bevmap_gated_act(g, *args, None) == INVALID
+    for args in ((None, P, P, P, P), (P, None, None, None, P), (P, P, P, P, None), (P, P, P, None, P),
+                 (P, P, None, P, P)):
+        assert lib.bevmap_gated_act_backward(g, *args, None) == INVALID
+    assert lib.bevmap_gated_act(None, P, P, P, P, None) == INVALID
+    assert lib.bevmap_gated_act(_gate(mb, rows=0), None, None, None, None, None) == 0
+    assert lib.bevmap_gated_act_backward(_gate(mb, rows=0), None, None, None, None, None, None) == 0
+
+
+def test_python_entries_refuse():
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    x, q, s = torch.zeros(2, 8), torch.zeros(2, 8, dtype=torch.int8), torch.zeros(2)
+    f = bev.rotary_frequencies(2)
+    for call in (lambda: bev.rms_norm(x), lambda: bev.rms_norm_add(x, x), lambda: bev.rms_norm_int8(x),
+                 lambda: bev.rms_norm_add_int8(x, x), lambda: bev.quantize_int8(x),
+                 lambda: bev.linear_int8(q, s, q, s), lambda: bev.rotary(x.view(1, 2, 2, 4), s.view(1, 2), f),
+                 lambda: bev.gated_act(x)):
+        with pytest.raises(bev.BevpoolError, match="device tensors"):
+            call()
+    with pytest.raises(bev.BevpoolError, match="checkpoint"):
+        bev.gated_act(x, checkpoint="fp8")
+
+
+def test_forward_mode_is_refused(monkeypatch):
+    """An input with a tangent is refused, with gradients enabled or not; the launches are stubs."""
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import layer_ops
+    from torch.autograd import forward_ad
+    monkeypatch.setattr(layer_ops, "_rms_forward",
+                        lambda x, r, *a: (x.clone(), x.clone(), x.clone(), layer_ops._map_binding.bevmap_rms()))
+    monkeypatch.setattr(layer_ops, "_rotary_of", lambda *a: (0, None))
+    monkeypatch.setattr(layer_ops, "_turn", lambda index, turn, x, *a: x.clone())
+    monkeypatch.setattr(layer_ops, "_gate_forward", lambda x, act, hold: (x.clone(), None, None, None))
+    monkeypatch.setattr(layer_ops, "_rms_int8", lambda x, *a: (x, x, x))
+    x, f = torch.ones(2, 8), torch.ones(2, dtype=torch.float64)
+    with forward_ad.dual_level():
+        xd, fd = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, f))
+        for call in (lambda: bev.rms_norm(xd), lambda: bev.rms_norm(x, xd[0]), lambda: bev.rms_norm_add(x, xd),
+                     lambda: bev.rotary(xd.view(1, 2, 2, 4), x, f), lambda: bev.rotary(x.view(1, 2, 2, 4), x, fd),
+                     lambda: bev.gated_act(xd)):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+        for call in (lambda: bev.rms_norm_int8(xd), lambda: bev.rms_norm_add_int8(x, xd), lambda: bev.quantize_int8(xd),
+                     lambda: bev.linear_int8(x, xd[0], x, x)):
+            with torch.no_grad(), pytest.raises(bev.BevpoolError, match="no gradient"):
+                call()
+        # inputs without a tangent work
+        assert torch.equal(bev.rms_norm(x), x) and bev.rms_norm_int8(x)[0] is x
+
+
+def test_rotary_frequencies():
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    plain = bev.rotary_frequencies(8)
+    assert plain.dtype == torch.float64
+    assert torch.allclose(plain, torch.tensor([10.0 ** (-i / 2) for i in range(8)], dtype=torch.float64), rtol=1e-14)
+    axes = bev.rotary_frequencies(6, base=64.0, axes=2)
+    assert torch.allclose(axes, torch.tensor([1, 0.25, 0.0625] * 2, dtype=torch.float64), rtol=1e-14)
+    assert torch.allclose(bev.rotary_frequencies(8, scaling="linear", factor=4.0), plain / 4, rtol=1e-15)
+    based = bev.rotary_frequencies(8, scaling="base", factor=4.0)
+    assert based[0] == 1 and torch.allclose(based[-1], plain[-1] / 4, rtol=1e-13)
+    assert ((based <= plain) & (based >= plain / 4 * (1 - 1e-12))).all()
+    parts = bev.rotary_frequencies(8, scaling="parts", factor=4.0, context=2000)
+    turns = plain * 2000 / (2 * math.pi)
+    assert torch.equal(parts[turns >= 32], plain[turns >= 32]) and (turns >= 32).any()
+    assert torch.allclose(parts[turns <= 1], plain[turns <= 1] / 4, rtol=1e-15) and (turns <= 1).any()
+    middle = (turns > 1) & (turns < 32)
+    share = (turns[middle] - 1) / 31
+    assert middle.any() and torch.allclose(parts[middle], plain[middle] * (share + (1 - share) / 4), rtol=1e-13)
+    for bad in (dict(pairs=0), dict(pairs=5, axes=2), dict(pairs=4, axes=0), dict(pairs=4, base=0.0),
+                dict(pairs=4, base=math.inf), dict(pairs=4, factor=0.5), dict(pairs=4, scaling="cubic"),
+                dict(pairs=4, scaling="parts"), dict(pairs=4, scaling="parts", context=100, fast=1.0, slow=1.0),
+                dict(pairs=2, axes=2, scaling="base", factor=2.0)):
+        with pytest.raises(bev.BevpoolError):
+            bev.rotary_frequencies(**bad)
+
+
+def test_star_import_needs_no_torch():
+    code = """
+import sys
+sys.modules["torch"] = None            # an import of torch raises ImportError
+from paper_2205_13542_amd import *
+for call in (lambda: rms_norm(None), lambda: rms_norm_add(None, None), lambda: rms_norm_int8(None),
+             lambda: rms_norm_add_int8(None, None), lambda: quantize_int8(None),
+             lambda: linear_int8(None, None, None, None), lambda: rotary(None, None, None),
+             lambda: rotary_frequencies(4), lambda: gated_act(None)):
+    try:
+        call()
+    except ImportError:
+        continue
+    raise SystemExit("an operator ran without torch")
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
+
+
+def test_package_names_are_the_operators():
+    pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import layer_ops
+    for name in ("rms_norm", "rms_norm_add", "rms_norm_int8", "rms_norm_add_int8", "quantize_int8", "linear_int8",
+                 "rotary", "rotary_frequencies", "gated_act"):
+        assert name in bev.__all__
+        assert inspect.signature(getattr(bev, name)) == inspect.signature(getattr(layer_ops, name))
