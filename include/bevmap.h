@@ -232,8 +232,8 @@ BEVPOOL_API int64_t bevmap_rms_norm_backward_workspace(const bevmap_rms *norm);
  * Gradients of bevmap_rms_norm, with the rstd that it wrote:
  *  grad_y:      device [rows][channels] of y_dtype.
  *  grad_sum:    device [rows][channels] of x_dtype: the gradient of sum, or NULL.
- *  x:           what was normed: sum, or x where there was no residual (rows x_stride
- *               apart; residual_stride is not used).
+ *  x, residual: those of bevmap_rms_norm. Its sum in the place of x, with a NULL
+ *               residual, does as well, but for what rounding it to x_dtype took away.
  *  grad_x:      device [rows][channels] of x_dtype, overwritten: the gradient of x, which
  *               is the residual's as well.
  *  grad_weight: device [channels] of weight_dtype, overwritten (zeros for no rows); NULL
@@ -242,9 +242,9 @@ BEVPOOL_API int64_t bevmap_rms_norm_backward_workspace(const bevmap_rms *norm);
  * not 16-byte aligned.
  */
 BEVPOOL_API int bevmap_rms_norm_backward(const bevmap_rms *norm, const void *grad_y, const void *grad_sum,
-                                         const void *x, const void *weight, const float *rstd, void *grad_x,
-                                         void *grad_weight, void *workspace, int64_t workspace_bytes,
-                                         void *hip_stream);
+                                         const void *x, const void *residual, const void *weight,
+                                         const float *rstd, void *grad_x, void *grad_weight, void *workspace,
+                                         int64_t workspace_bytes, void *hip_stream);
 
 /*
  * The norm's result in 8 bits, for a product that reads it: with top the largest

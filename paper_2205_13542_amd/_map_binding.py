@@ -75,7 +75,7 @@ def load():
         lib.bevmap_rms_norm.argtypes = [rms] + [_vp] * 7
         lib.bevmap_rms_norm_backward_workspace.argtypes = [rms]
         lib.bevmap_rms_norm_backward_workspace.restype = _i64
-        lib.bevmap_rms_norm_backward.argtypes = [rms] + [_vp] * 8 + [_i64, _vp]
+        lib.bevmap_rms_norm_backward.argtypes = [rms] + [_vp] * 9 + [_i64, _vp]
         lib.bevmap_rms_norm_int8.argtypes = [rms] + [_vp] * 7
         lib.bevmap_quantize_int8.argtypes = [_vp, _i64, _vp, _vp, _i64, _i32, _i32, _vp]
         lib.bevmap_linear_int8.argtypes = [linear] + [_vp] * 7
@@ -141,11 +141,11 @@ def bevmap_rms_norm_backward_workspace(norm: bevmap_rms) -> int:
     return _check(load().bevmap_rms_norm_backward_workspace(norm))
 
 
-def bevmap_rms_norm_backward(norm: bevmap_rms, grad_y: int, grad_sum: int, x: int, weight: int, rstd: int,
-                             grad_x: int, grad_weight: int, workspace: int, workspace_bytes: int,
+def bevmap_rms_norm_backward(norm: bevmap_rms, grad_y: int, grad_sum: int, x: int, residual: int, weight: int,
+                             rstd: int, grad_x: int, grad_weight: int, workspace: int, workspace_bytes: int,
                              hip_stream: int = 0) -> None:
-    _check(load().bevmap_rms_norm_backward(norm, grad_y, grad_sum, x, weight, rstd, grad_x, grad_weight, workspace,
-                                           workspace_bytes, hip_stream))
+    _check(load().bevmap_rms_norm_backward(norm, grad_y, grad_sum, x, residual, weight, rstd, grad_x, grad_weight,
+                                           workspace, workspace_bytes, hip_stream))
 
 
 def bevmap_rms_norm_int8(norm: bevmap_rms, x: int, residual: int, weight: int, sum: int, held: int, scale: int,

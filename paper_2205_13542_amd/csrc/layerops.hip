@@ -102,9 +102,9 @@ int64_t bevmap_rms_norm_backward_workspace(const bevmap_rms *norm) {
 }
 
 int bevmap_rms_norm_backward(const bevmap_rms *norm, const void *grad_y, const void *grad_sum, const void *x,
-                             const void *weight, const float *rstd, void *grad_x, void *grad_weight, void *workspace,
-                             int64_t workspace_bytes, void *hip_stream) {
-    if (int rc = check(norm, false)) return rc;
+                             const void *residual, const void *weight, const float *rstd, void *grad_x,
+                             void *grad_weight, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (int rc = check(norm, residual != nullptr)) return rc;
     if (norm->rows > 0 && (!grad_y || !x || !rstd || !grad_x)) return null_pointer();
     const int64_t need = grad_weight ? bevmap_rms_workspace_bytes(*norm) : 0;
     if (need > 0 && (!workspace || workspace_bytes < need))
@@ -112,8 +112,8 @@ int bevmap_rms_norm_backward(const bevmap_rms *norm, const void *grad_y, const v
                             workspace ? (long long)workspace_bytes : 0ll, (long long)need);
     if (reinterpret_cast<uintptr_t>(workspace) % 16)
         return bevpool_fail(BEVPOOL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-    return bevmap_launch_rms_norm_backward(*norm, grad_y, grad_sum, x, weight, rstd, grad_x, grad_weight, workspace,
-                                           static_cast<hipStream_t>(hip_stream));
+    return bevmap_launch_rms_norm_backward(*norm, grad_y, grad_sum, x, residual, weight, rstd, grad_x, grad_weight,
+                                           workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 int bevmap_rms_norm_int8(const bevmap_rms *norm, const void *x, const void *residual, const void *weight, void *sum,

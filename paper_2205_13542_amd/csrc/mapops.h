@@ -41,8 +41,8 @@ int bevmap_launch_rms_norm(const bevmap_rms &n, const void *x, const void *resid
                            void *y, float *rstd, int8_t *q, float *scale, hipStream_t stream);
 int64_t bevmap_rms_workspace_bytes(const bevmap_rms &n);
 int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, const void *grad_sum, const void *x,
-                                    const void *weight, const float *rstd, void *grad_x, void *grad_weight,
-                                    void *workspace, hipStream_t stream);
+                                    const void *residual, const void *weight, const float *rstd, void *grad_x,
+                                    void *grad_weight, void *workspace, hipStream_t stream);
 int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *scale, int64_t rows, int32_t columns,
                            int32_t dtype, hipStream_t stream);
 int bevmap_launch_linear_int8(const bevmap_linear &n, const int8_t *x, const float *x_scale, const int8_t *w,

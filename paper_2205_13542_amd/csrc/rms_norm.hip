@@ -222,7 +222,8 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
     extern __shared__ float joined[];       // [C], rows shared by a wave or less
     __shared__ float add[8];
     const int lane = threadIdx.x % LANES, n_vec = a.C / V;
-    const T *x = static_cast<const T *>(a.x), *dsum = static_cast<const T *>(a.dsum);
+    const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
+    const T *dsum = static_cast<const T *>(a.dsum);
     T *dx = static_cast<T *>(a.sum);
     float w[ITER][V], dw[ITER][V];
 #pragma unroll
@@ -242,14 +243,15 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
         const int64_t row = first + threadIdx.x / LANES;
         const bool live = row < end;
         const float rstd = live ? a.rstd[row] : 0.0f;
-        float u[ITER][V], e[ITER][V], more[ITER][V], dot = 0.0f;
+        float u[ITER][V], other[ITER][V], e[ITER][V], more[ITER][V], dot = 0.0f;
 #pragma unroll
         for (int k = 0; k < ITER; ++k) {
             const int at = lane + k * LANES;
 #pragma unroll
-            for (int i = 0; i < V; ++i) u[k][i] = e[k][i] = more[k][i] = 0.0f;
+            for (int i = 0; i < V; ++i) u[k][i] = other[k][i] = e[k][i] = more[k][i] = 0.0f;
             if (live && at < n_vec) {
                 load_n<T, V>(x + row * a.ldx + at * V, u[k]);
+                if (res) load_n<T, V>(res + row * a.ldr + at * V, other[k]);
                 load_any<V>(a.dy, row * a.C + at * V, a.y_dtype, e[k]);
                 if (dsum) load_n<T, V>(dsum + row * a.C + at * V, more[k]);
             }
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
         for (int k = 0; k < ITER; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                u[k][i] *= rstd;
+                u[k][i] = (u[k][i] + other[k][i]) * rstd;
                 dw[k][i] = fmaf(e[k][i], u[k][i], dw[k][i]);
                 e[k][i] *= w[k][i];
                 dot = fmaf(e[k][i], u[k][i], dot);
@@ -483,13 +485,14 @@ int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *sc
 }
 
 int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, const void *grad_sum, const void *x,
-                                    const void *weight, const float *rstd, void *grad_x, void *grad_weight,
-                                    void *workspace, hipStream_t stream) {
+                                    const void *residual, const void *weight, const float *rstd, void *grad_x,
+                                    void *grad_weight, void *workspace, hipStream_t stream) {
     int64_t groups = 0;
     float *parts = grad_weight ? static_cast<float *>(workspace) : nullptr;
     if (n.rows > 0) {
         RmsArgs a{};
         a.x = x;
+        a.residual = residual;
         a.weight = weight;
         a.dy = grad_y;
         a.dsum = grad_sum;
@@ -497,13 +500,15 @@ int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, con
         a.rstd = const_cast<float *>(rstd);
         a.parts = parts;
         a.ldx = n.x_stride;
+        a.ldr = n.residual_stride;
         a.rows = n.rows;
         a.C = n.channels;
         a.y_dtype = n.y_dtype;
         a.w_dtype = n.weight_dtype;
-        const void *p[] = {x, grad_sum, grad_x};
-        const int64_t s[] = {n.rows == 1 ? 0 : n.x_stride, 0, 0};
-        int v = access(n.x_dtype, n.channels, p, s, 3);
+        const bool one = n.rows == 1;
+        const void *p[] = {x, residual, grad_sum, grad_x};
+        const int64_t s[] = {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride, 0, 0};
+        int v = access(n.x_dtype, n.channels, p, s, 4);
         if ((weight && !aligned_for(weight, 0, n.weight_dtype, v)) || !aligned_for(grad_y, 0, n.y_dtype, v)) v = 1;
         const Form f = form_of(v, n.channels, n.rows);
         const int64_t each = kRmsBlock / f.lanes;

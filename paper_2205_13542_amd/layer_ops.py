@@ -86,7 +86,7 @@ def _rms_forward(x, residual, weight, eps, out_dtype, train):
     return y, total, rstd, norm
 
 
-def _rms_backward(norm, dy, dtotal, x, weight, rstd, want_weight):
+def _rms_backward(norm, dy, dtotal, x, residual, weight, rstd, want_weight):
     dy = dy.contiguous()
     if dtotal is not None:
         dtotal = dtotal.contiguous()
@@ -95,7 +95,7 @@ def _rms_backward(norm, dy, dtotal, x, weight, rstd, want_weight):
     size = _map_binding.bevmap_rms_norm_backward_workspace(norm) if want_weight else 0
     space = x.new_empty(size, dtype=torch.uint8) if size else None
     _call(_map_binding.bevmap_rms_norm_backward, x.get_device(), norm, dy.data_ptr(), _ptr(dtotal), x.data_ptr(),
-          _ptr(weight), rstd.data_ptr(), dx.data_ptr(), _ptr(dw), _ptr(space), size)
+          _ptr(residual), _ptr(weight), rstd.data_ptr(), dx.data_ptr(), _ptr(dw), _ptr(space), size)
     return dx, dw
 
 
@@ -111,7 +111,7 @@ class _RmsNorm(torch.autograd.Function):
         _first_order_only()
         x, weight, rstd = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dw = _rms_backward(ctx.norm, dy, None, x, weight, rstd, need[1])
+        dx, dw = _rms_backward(ctx.norm, dy, None, x, None, weight, rstd, need[1])
         return dx if need[0] else None, dw, None, None
 
 
@@ -119,19 +119,22 @@ class _RmsNormAdd(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, weight, eps, out_dtype):
         y, total, rstd, ctx.norm = _rms_forward(x, residual, weight, eps, out_dtype, True)
-        ctx.norm.x_stride = ctx.norm.channels       # the backward reads the sum
-        ctx.save_for_backward(total, weight, rstd)
+        if x.dtype == torch.float32:
+            ctx.norm.x_stride = ctx.norm.channels
+            ctx.save_for_backward(total, None, weight, rstd)
+        else:       # the sum of 16-bit numbers, rounded, would take its 2^-9 into the weight's gradient
+            ctx.save_for_backward(x, residual, weight, rstd)
         ctx.set_materialize_grads(False)
         return y, total
 
     @staticmethod
     def backward(ctx, dy, dtotal):
         _first_order_only()
-        total, weight, rstd = ctx.saved_tensors
+        x, residual, weight, rstd = ctx.saved_tensors
         need = ctx.needs_input_grad
         if dy is None:          # y was not used: the gradient of a sum
             return dtotal, dtotal, torch.zeros_like(weight) if need[2] else None, None, None
-        dx, dw = _rms_backward(ctx.norm, dy, dtotal, total, weight, rstd, need[2])
+        dx, dw = _rms_backward(ctx.norm, dy, dtotal, x, residual, weight, rstd, need[2])
         return dx if need[0] else None, dx if need[1] else None, dw, None, None
 
 

@@ -84,9 +84,7 @@ def _rms_reference(torch, x, residual, w, eps, dy, dsum, x_type, y_type, w_type)
     if dy is None:
         return out
     dy = dy.double()
-    # the backward reads the sum as it was rounded
-    du = u.abs() * (rel + (0 if residual is None else 1.01 * _u(x_type))) + \
-        (0 if residual is None else _tiny(x_type) * rstd)
+    du = rel * u.abs()
     e = dy * w
     m = (e * u).mean(-1, keepdim=True)
     dm = (e.abs() * du + (ROW + 3) * U32 * (e * u).abs()).mean(-1, keepdim=True) + 2 * U32 * m.abs()

@@ -46,7 +46,7 @@ def test_rms_norm_refuses(lib, mb, over, code):
     assert lib.bevmap_rms_norm_backward_workspace(n) == code
     assert lib.bevmap_rms_norm(n, P, P, P, P, P, P, None) == code
     assert lib.bevmap_rms_norm_int8(n, P, P, P, P, P, P, None) == code
-    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, 1 << 40, None) == code
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, P, 1 << 40, None) == code
 
 
 def test_rms_norm_refuses_pointers_strides_and_workspaces(lib, mb):
@@ -57,21 +57,22 @@ def test_rms_norm_refuses_pointers_strides_and_workspaces(lib, mb):
         assert lib.bevmap_rms_norm(n, *args, None) == INVALID
     for args in ((None, P, P, P, P, P), (P, P, P, None, P, P), (P, None, P, None, None, P), (P, None, P, None, P, None)):
         assert lib.bevmap_rms_norm_int8(n, *args, None) == INVALID
-    for k in (0, 2, 4, 5):
-        args = [P] * 8
+    for k in (0, 2, 5, 6):
+        args = [P] * 9
         args[k] = None
         assert lib.bevmap_rms_norm_backward(n, *args, need, None) == INVALID
-    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, need - 1, None) == INVALID
-    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, None, need, None) == INVALID
-    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, ctypes.c_void_p(8), need, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, P, need - 1, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, None, need, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(n, P, P, P, P, P, P, P, P, ctypes.c_void_p(8), need, None) == INVALID
     assert lib.bevmap_rms_norm(None, P, P, P, P, P, P, None) == INVALID
     short = _rms(mb, residual_stride=11)
     assert lib.bevmap_rms_norm(short, P, P, P, P, P, P, None) == INVALID
+    assert lib.bevmap_rms_norm_backward(short, P, P, P, P, P, P, P, P, P, need, None) == INVALID
     empty = _rms(mb, rows=0)
     assert lib.bevmap_rms_norm_backward_workspace(empty) == 0
     assert lib.bevmap_rms_norm(empty, None, None, None, None, None, None, None) == 0
     assert lib.bevmap_rms_norm_int8(empty, None, None, None, None, None, None, None) == 0
-    assert lib.bevmap_rms_norm_backward(empty, None, None, None, None, None, None, None, None, 0, None) == 0
+    assert lib.bevmap_rms_norm_backward(empty, None, None, None, None, None, None, None, None, None, 0, None) == 0
 
 
 def test_rms_norm_workspace_stays_below_the_rows(lib, mb):
