@@ -22,8 +22,9 @@ namespace {
 using i32x4 = int32_t __attribute__((ext_vector_type(4)));
 using i32x16 = int32_t __attribute__((ext_vector_type(16)));
 
-constexpr int kStep = 128;              // bytes of k in a stage
-constexpr int kChunks = kStep / 16;     // 16-byte chunks of a row in a stage
+constexpr int kRun = 128;               // bytes of k that a wave of the form for few tokens takes at once
+constexpr int kUnits = 256;             // compute units
+constexpr int kGroup = 4;               // tiles of tokens that are walked before the next tile of features
 
 struct LinearArgs {
     const int8_t *x, *w;
@@ -55,11 +56,16 @@ __device__ __forceinline__ float scaled(int32_t sum, float xs, float ws, float b
     return fmaf(float(sum) * xs, ws, bias);
 }
 
-// MW x NW waves of BM x BN blocks of 32 x 32. DIRECT: every row starts on 16 bytes and K
-// is a multiple of 16.
-template <int MW, int NW, int BM, int BN, bool DIRECT>
+// MW x NW waves of BM x BN blocks of 32 x 32, kStep bytes of k in a stage. DIRECT: every
+// row starts on 16 bytes and K is a multiple of 16.
+template <int MW, int NW, int BM, int BN, int KS, bool DIRECT>
 struct Tile {
+    static constexpr int kStep = KS, kChunks = KS / 16;         // 16-byte chunks of a row in a stage
+    // Row r of a stage holds chunk c of its bytes at place c ^ bank_of(r): the sixteen lanes
+    // that read at once, each 16 bytes of a row of its own, then cover all banks.
+    static __device__ __forceinline__ int bank_of(int r) { return r / (256 / kStep) % kChunks; }
     static constexpr int kThreads = 64 * MW * NW;
+    static_assert(kThreads / kChunks % 16 == 0, "a thread's rows of a stage share their bank_of");
     static constexpr int kM = 32 * MW * BM, kN = 32 * NW * BN;
     static constexpr int kStage = (kM + kN) * kStep;            // tokens, then channels
     static constexpr int kLoads = (kM + kN) * kChunks / kThreads;   // chunks of a thread
@@ -72,6 +78,18 @@ struct Tile {
     }
 };
 
+template <int V>
+struct Int {
+    static constexpr int value = V;
+};
+// body(constant) with the type of y
+template <class F>
+__device__ __forceinline__ void with_dtype(int dtype, F body) {
+    if (dtype == BEVPOOL_F32) body(Int<BEVPOOL_F32>());
+    else if (dtype == BEVPOOL_BF16) body(Int<BEVPOOL_BF16>());
+    else body(Int<BEVPOOL_F16>());
+}
+
 // The channel that row r of a wave's 32 * BN rows of weights stands for: lane l of a
 // block holds rows 8 (i / 4) + 4 (l / 32) + i % 4, and these are to be neighbours, over
 // the wave's blocks too.
@@ -81,30 +99,19 @@ __device__ __forceinline__ int channel_of(int r) {
     return half * 16 * BN + block * 16 + g * 4 + r % 4;
 }
 
-template <int MW, int NW, int BM, int BN, bool DIRECT>
-__global__ __launch_bounds__(64 * MW * NW) void k_linear(LinearArgs a) {
-    using G = Tile<MW, NW, BM, BN, DIRECT>;
-    extern __shared__ __align__(16) char lds[];
+// A tile of the product, its first token and channel m0 and n0.
+template <int MW, int NW, int BM, int BN, int KS, bool DIRECT>
+__device__ __forceinline__ void multiply_tile(const LinearArgs &a, char *lds, int m0, int n0) {
+    using G = Tile<MW, NW, BM, BN, KS, DIRECT>;
+    constexpr int kStep = G::kStep, kChunks = G::kChunks;
     float *xs = reinterpret_cast<float *>(lds), *ws = xs + G::kM, *bias = ws + G::kN;
     char *stages = lds + G::kScales;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    // neighbouring workgroups go to different XCDs: each gets a run of tiles of its own,
-    // which share their rows in its cache
-    const int tiles = a.m_tiles * a.n_tiles, xcd = blockIdx.x % 8, at = blockIdx.x / 8;
-    const int tile = xcd * (tiles / 8) + (xcd < tiles % 8 ? xcd : tiles % 8) + at;
-    const int m0 = tile / a.n_tiles * G::kM, n0 = tile % a.n_tiles * G::kN;
     const int steps = (a.K + kStep - 1) / kStep;
-
-    for (int i = tid; i < G::kM; i += G::kThreads) xs[i] = a.x_scale[min(m0 + i, a.M - 1)];
-    for (int i = tid; i < G::kN; i += G::kThreads) {
-        const int n = min(n0 + i, a.N - 1);
-        ws[i] = a.w_scale[n];
-        bias[i] = a.bias ? a.bias[n] : 0.0f;
-    }
 
     // A thread's chunks: row i * (threads / 8) + tid / 8 of the stage, its place tid % 8
     // holding the chunk of k that makes lanes of a column read different banks.
-    const int place = tid % kChunks, k_at = (place ^ (tid / kChunks % kChunks)) * 16;
+    const int place = tid % kChunks, k_at = (place ^ G::bank_of(tid / kChunks)) * 16;
     const int8_t *from[G::kLoads];
 #pragma unroll
     for (int i = 0; i < G::kLoads; ++i) {
@@ -117,19 +124,23 @@ __global__ __launch_bounds__(64 * MW * NW) void k_linear(LinearArgs a) {
         }
     }
     i32x4 held[DIRECT ? 1 : G::kLoads];
-    auto fetch = [&](int step, char *stage) {
+    // Chunks i0 .. i1 - 1 of a thread for a step, on their way to the stage or into registers.
+    auto fetch = [&](int step, char *stage, int i0, int i1) {
         const int k = step * kStep + k_at;
+        if constexpr (DIRECT) {
+            const bool whole = (step + 1) * kStep <= a.K;
 #pragma unroll
-        for (int i = 0; i < G::kLoads; ++i) {
-            if constexpr (DIRECT) {
-                const void *p = k < a.K ? static_cast<const void *>(from[i] + k) : static_cast<const void *>(&kNothing);
+            for (int i = i0; i < i1; ++i) {
+                const void *p = from[i] + k;
+                if (!whole && k >= a.K) p = &kNothing;
                 // lands at the wave's first place and 16 bytes further for each lane
                 __builtin_amdgcn_global_load_lds(
                     (const __attribute__((address_space(1))) void *)p,
                     (__attribute__((address_space(3))) void *)(stage + (i * G::kThreads + wave * 64) * 16), 16, 0, 0);
-            } else {
-                held[i] = load_chunk(from[i], k, a.K);
             }
+        } else {
+#pragma unroll
+            for (int i = i0; i < i1; ++i) held[i] = load_chunk(from[i], k, a.K);
         }
     };
     auto place_held = [&](char *stage) {
@@ -148,86 +159,179 @@ __global__ __launch_bounds__(64 * MW * NW) void k_linear(LinearArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-    fetch(0, stages);
+    // Operands of a quarter of a stage, 32 bytes of k, for all of the wave's blocks. Two sets in
+    // turn: while one is multiplied the next is on its way.
+    struct Operands {
+        i32x4 x[BM], w[BN];
+    } set[2];
+    const int x_row = (wm * BM * 32 + col) * kStep, w_row = (G::kM + wn * BN * 32 + col) * kStep;
+    auto read = [&](const char *stage, int k, Operands &o) {
+        const int chunk = ((2 * k + half) ^ G::bank_of(col)) * 16;
+#pragma unroll
+        for (int j = 0; j < BM; ++j) o.x[j] = *reinterpret_cast<const i32x4 *>(stage + x_row + j * 32 * kStep + chunk);
+#pragma unroll
+        for (int i = 0; i < BN; ++i) o.w[i] = *reinterpret_cast<const i32x4 *>(stage + w_row + i * 32 * kStep + chunk);
+    };
+    // between(i) runs after the products of the i-th blocks of channels: reads that are begun
+    // there have the other products' time, and wait for nothing that is still to be multiplied.
+    auto multiply = [&](const Operands &o, auto between) {
+#pragma unroll
+        for (int i = 0; i < BN; ++i) {
+#pragma unroll
+            for (int j = 0; j < BM; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[i], o.x[j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    constexpr int kQuarters = kStep / 32, kSpread = BN > 1 ? BN - 1 : 1;
+
+    fetch(0, stages, 0, G::kLoads);
+    for (int i = tid; i < G::kM; i += G::kThreads) xs[i] = a.x_scale[min(m0 + i, a.M - 1)];
+    for (int i = tid; i < G::kN; i += G::kThreads) {
+        const int n = min(n0 + i, a.N - 1);
+        ws[i] = a.w_scale[n];
+        bias[i] = a.bias ? a.bias[n] : 0.0f;
+    }
     place_held(stages);
     __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-        const char *now = stages + (s & 1) * G::kStage;
-        char *next = stages + ((s + 1) & 1) * G::kStage;
-        if (s + 1 < steps) fetch(s + 1, next);
-        const char *xt = now + (wm * BM * 32 + col) * kStep, *wt = now + (G::kM + wn * BN * 32 + col) * kStep;
+    read(stages, 0, set[0]);
+    if (steps > 1) fetch(1, stages + G::kStage, 0, G::kLoads);
+    for (int s = 0; s + 1 < steps; ++s) {
+        char *now = stages + (s & 1) * G::kStage, *next = stages + ((s + 1) & 1) * G::kStage;
 #pragma unroll
-        for (int k = 0; k < kStep / 32; ++k) {
-            if (s * kStep + k * 32 >= a.K) break;
-            const int chunk = ((2 * k + half) ^ (col % kChunks)) * 16;
-            i32x4 xv[BM], wv[BN];
-#pragma unroll
-            for (int j = 0; j < BM; ++j) xv[j] = *reinterpret_cast<const i32x4 *>(xt + j * 32 * kStep + chunk);
-#pragma unroll
-            for (int i = 0; i < BN; ++i) wv[i] = *reinterpret_cast<const i32x4 *>(wt + i * 32 * kStep + chunk);
-#pragma unroll
-            for (int i = 0; i < BN; ++i)
-#pragma unroll
-                for (int j = 0; j < BM; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
-        }
-        if (s + 1 < steps) place_held(next);
+        for (int k = 0; k + 1 < kQuarters; ++k)
+            multiply(set[k & 1], [&](int i) {
+                if (i == 0) read(now, k + 1, set[(k + 1) & 1]);
+            });
+        // all that this stage holds is in registers: the one after next may overwrite it
+        place_held(next);
         __syncthreads();
+        multiply(set[(kQuarters - 1) & 1], [&](int i) {
+            if (i == 0) read(next, 0, set[0]);
+            if (s + 2 < steps && (i > 0 || BN == 1)) {
+                const int at = BN == 1 ? 0 : i - 1;
+                fetch(s + 2, now, G::kLoads * at / kSpread, G::kLoads * (at + 1) / kSpread);
+            }
+        });
     }
+    const char *last = stages + ((steps - 1) & 1) * G::kStage;
+    const int left = a.K - (steps - 1) * kStep;
+#pragma unroll
+    for (int k = 0; k < kQuarters; ++k) {
+        if (k * 32 >= left) break;
+        multiply(set[k & 1], [&](int i) {
+            if (i == 0 && k + 1 < kQuarters) read(last, k + 1, set[(k + 1) & 1]);
+        });
+    }
+    __syncthreads();
 
-    // Results go through LDS, 32 tokens of a wave at a time, so that whole rows are written.
+    // Sums go through LDS, 32 tokens of a wave at a time, so that whole rows are written. A
+    // lane then keeps to its channels, whose scales stay in registers.
     char *mine = stages + wave * 32 * G::kOutPitch;
-    constexpr int kCols = 32 * BN;
-    const int nw = n0 + wn * kCols;         // the wave's first channel
+    constexpr int kCols = 32 * BN, kPer = kCols / 8;    // lanes of a row, eight channels each
+    const int nw = n0 + wn * kCols, mw = wm * BM * 32, mine_at = lane % kPer * 8;
+    float w_scale[8], b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        w_scale[e] = ws[wn * kCols + mine_at + e];
+        b[e] = bias[wn * kCols + mine_at + e];
+    }
 #pragma unroll
     for (int j = 0; j < BM; ++j) {
-        const int m_first = m0 + (wm * BM + j) * 32;
-        const float scale = xs[(wm * BM + j) * 32 + col];
 #pragma unroll
         for (int i = 0; i < BN; ++i)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int c = half * 16 * BN + i * 16 + g * 4;
-                float4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    (&v.x)[e] = scaled(acc[i][j][4 * g + e], scale, ws[wn * kCols + c + e], bias[wn * kCols + c + e]);
-                *reinterpret_cast<float4 *>(mine + col * G::kOutPitch + c * 4) = v;
+                *reinterpret_cast<i32x4 *>(mine + col * G::kOutPitch + c * 4) =
+                    i32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
             }
         // a wave's own rows: no other wave to wait for
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (a.wide) {
-            constexpr int kPer = kCols / 8;     // lanes of a row, eight channels each
-            for (int r = lane / kPer; r < 32; r += 64 / kPer) {
-                const int m = m_first + r, n = nw + lane % kPer * 8;
-                if (m < a.M && n < a.N) {
+        const int m_first = m0 + mw + j * 32;
+        with_dtype(a.y_dtype, [&](auto dt) {
+            using T = typename Num<decltype(dt)::value>::T;
+            T *y = static_cast<T *>(a.y);
+            if (a.wide) {
+                const int n = nw + mine_at;
+#pragma unroll 4
+                for (int r = lane / kPer; r < 32; r += 64 / kPer) {
+                    const i32x4 *p = reinterpret_cast<const i32x4 *>(mine + r * G::kOutPitch + mine_at * 4);
+                    const i32x4 low = p[0], high = p[1];
+                    const float scale = xs[mw + j * 32 + r];
                     float v[8];
-                    const float4 *p = reinterpret_cast<const float4 *>(mine + r * G::kOutPitch + lane % kPer * 32);
-                    *reinterpret_cast<float4 *>(v) = p[0];
-                    *reinterpret_cast<float4 *>(v + 4) = p[1];
-                    store_any<8>(a.y, int64_t(m) * a.N + n, a.y_dtype, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = scaled(e < 4 ? low[e] : high[e - 4], scale, w_scale[e], b[e]);
+                    if (m_first + r < a.M && n < a.N) store_n<T, 8>(y + int64_t(m_first + r) * a.N + n, v);
+                }
+                return;
+            }
+            constexpr int kAcross = kCols < 64 ? kCols : 64;    // lanes of a row, a channel each
+#pragma unroll
+            for (int c = lane % kAcross; c < kCols; c += kAcross) {
+                const float one = ws[wn * kCols + c], add = bias[wn * kCols + c];
+#pragma unroll 4
+                for (int r = lane / kAcross; r < 32; r += 64 / kAcross) {
+                    const int32_t sum = *reinterpret_cast<const int32_t *>(mine + r * G::kOutPitch + c * 4);
+                    if (m_first + r < a.M && nw + c < a.N)
+                        y[int64_t(m_first + r) * a.N + nw + c] = T(scaled(sum, xs[mw + j * 32 + r], one, add));
                 }
             }
-        } else {
-            for (int t = lane; t < 32 * kCols; t += 64) {
-                const int m = m_first + t / kCols, n = nw + t % kCols;
-                if (m < a.M && n < a.N)
-                    store_any<1>(a.y, int64_t(m) * a.N + n, a.y_dtype,
-                                 reinterpret_cast<const float *>(mine + t / kCols * G::kOutPitch) + t % kCols);
-            }
-        }
+        });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
 }
 
+// Tiles in the order in which they are taken: kGroup down before the next of the features,
+// so that those that run at a time share their rows in a cache.
+__device__ __forceinline__ void place_of(int tile, int m_tiles, int n_tiles, int *m, int *n) {
+    const int group = tile / (kGroup * n_tiles), in = tile - group * kGroup * n_tiles;
+    const int tall = min(kGroup, m_tiles - group * kGroup);
+    *m = group * kGroup + in % tall;
+    *n = in / tall;
+}
+// Neighbouring workgroups go to different XCDs: each XCD gets a run of tiles of its own
+// (8192^3: 564 us, with tiles row by row 596).
+__device__ __forceinline__ int run_of(int block, int tiles) {
+    const int xcd = block % 8;
+    return xcd * (tiles / 8) + min(xcd, tiles % 8) + block / 8;
+}
+
+template <int MW, int NW, int BM, int BN, int KS, bool DIRECT>
+__global__ __launch_bounds__(64 * MW * NW) void k_linear(LinearArgs a) {
+    using G = Tile<MW, NW, BM, BN, KS, DIRECT>;
+    extern __shared__ __align__(16) char lds[];
+    int m, n;
+    place_of(run_of(blockIdx.x, gridDim.x), a.m_tiles, a.n_tiles, &m, &n);
+    multiply_tile<MW, NW, BM, BN, KS, DIRECT>(a, lds, m * G::kM, n * G::kN);
+}
+
+// Tiles of 256 x 256, the last ones in eighths: a few tiles that are left over a whole
+// round of workgroups would take as long as a round.
+template <bool DIRECT>
+__global__ __launch_bounds__(512) void k_linear_eighths(LinearArgs a, int whole) {
+    extern __shared__ __align__(16) char lds[];
+    const int block = blockIdx.x, left = a.m_tiles * a.n_tiles - whole;
+    int m, n;
+    if (block < whole) {
+        place_of(run_of(block, whole), a.m_tiles, a.n_tiles, &m, &n);
+        multiply_tile<4, 2, 2, 4, 128, DIRECT>(a, lds, m * 256, n * 256);
+        return;
+    }
+    const int part = (block - whole) / left;
+    place_of(whole + (block - whole) % left, a.m_tiles, a.n_tiles, &m, &n);
+    multiply_tile<4, 2, 1, 1, 128, DIRECT>(a, lds, m * 256 + part / 4 * 128, n * 256 + part % 4 * 64);
+}
+
 // Few tokens: 16 channels and 16 * MB tokens of a workgroup, whose waves share out k in
-// runs of kStep bytes.
-constexpr int kFewWaves = 8;
-template <int MB, bool DIRECT>
-__global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(LinearArgs a) {
-    __shared__ i32x4 sums[kFewWaves][MB][64];
+// runs of kRun bytes. A wave's next run is on its way while one is multiplied.
+template <int MB, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearArgs a) {
+    __shared__ i32x4 sums[WAVES][MB][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, quarter = lane / 16, col = lane % 16;
     const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MB;
     const int8_t *w = a.w + int64_t(min(n0 + col, a.N - 1)) * a.ldw, *x[MB];
@@ -242,45 +346,68 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(LinearArgs a) {
             return load_chunk(row, k, a.K);
         }
     };
+    struct Run {
+        i32x4 w[kRun / 64], x[kRun / 64][MB];
+    };
+    auto load_run = [&](int first, Run &r) {
+#pragma unroll
+        for (int s = 0; s < kRun / 64; ++s) {
+            const int k = first + 64 * s + 16 * quarter;
+            r.w[s] = load(w, k);
+#pragma unroll
+            for (int j = 0; j < MB; ++j) r.x[s][j] = load(x[j], k);
+        }
+    };
     i32x4 acc[MB];
 #pragma unroll
     for (int j = 0; j < MB; ++j) acc[j] = i32x4{0, 0, 0, 0};
-    for (int first = wave * kStep; first < a.K; first += kFewWaves * kStep) {
-        i32x4 wv[kStep / 64], xv[kStep / 64][MB];
+    auto multiply = [&](const Run &r) {
 #pragma unroll
-        for (int s = 0; s < kStep / 64; ++s) {
-            const int k = first + 64 * s + 16 * quarter;
-            wv[s] = load(w, k);
+        for (int s = 0; s < kRun / 64; ++s)
 #pragma unroll
-            for (int j = 0; j < MB; ++j) xv[s][j] = load(x[j], k);
-        }
-#pragma unroll
-        for (int s = 0; s < kStep / 64; ++s)
-#pragma unroll
-            for (int j = 0; j < MB; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[s], xv[s][j], acc[j], 0, 0, 0);
+            for (int j = 0; j < MB; ++j)
+                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(r.w[s], r.x[s][j], acc[j], 0, 0, 0);
+    };
+    Run one, two;
+    int first = wave * kRun;
+    load_run(first, one);
+    for (; first < a.K; first += 2 * WAVES * kRun) {
+        load_run(first + WAVES * kRun, two);
+        multiply(one);
+        load_run(first + 2 * WAVES * kRun, one);
+        multiply(two);
     }
 #pragma unroll
     for (int j = 0; j < MB; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
     // sums[..][j][l][e]: token 16 j + l % 16, channel 4 (l / 16) + e
-    for (int t = threadIdx.x; t < 256 * MB; t += 64 * kFewWaves) {
+    for (int t = threadIdx.x; t < 256 * MB; t += 64 * WAVES) {
         const int c = t % 16, row = t / 16, m = m0 + row, n = n0 + c;
         if (m >= a.M || n >= a.N) continue;
         int32_t sum = 0;
 #pragma unroll
-        for (int v = 0; v < kFewWaves; ++v) sum += sums[v][row / 16][c / 4 * 16 + row % 16][c % 4];
+        for (int v = 0; v < WAVES; ++v) sum += sums[v][row / 16][c / 4 * 16 + row % 16][c % 4];
         const float y = scaled(sum, a.x_scale[m], a.w_scale[n], a.bias ? a.bias[n] : 0.0f);
         store_any<1>(a.y, int64_t(m) * a.N + n, a.y_dtype, &y);
     }
 }
 
-template <int MW, int NW, int BM, int BN, bool DIRECT>
+template <int MB, int WAVES, bool DIRECT>
+int launch_few(const LinearArgs &a, hipStream_t stream) {
+    hipLaunchKernelGGL((k_linear_few<MB, WAVES, DIRECT>),
+                       dim3(uint32_t((a.N + 15) / 16), uint32_t((a.M + 16 * MB - 1) / (16 * MB))), dim3(64 * WAVES), 0,
+                       stream, a);
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+template <int MW, int NW, int BM, int BN, int KS, bool DIRECT>
 int launch_tiles(LinearArgs a, hipStream_t stream) {
-    using G = Tile<MW, NW, BM, BN, DIRECT>;
+    using G = Tile<MW, NW, BM, BN, KS, DIRECT>;
     a.m_tiles = (a.M + G::kM - 1) / G::kM;
     a.n_tiles = (a.N + G::kN - 1) / G::kN;
-    const int lds = G::lds((a.K + kStep - 1) / kStep);
-    auto kernel = k_linear<MW, NW, BM, BN, DIRECT>;
+    const int lds = G::lds((a.K + KS - 1) / KS);
+    auto kernel = k_linear<MW, NW, BM, BN, KS, DIRECT>;
     if (lds > 65536)
         BEVPOOL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                         hipFuncAttributeMaxDynamicSharedMemorySize, lds));
@@ -290,23 +417,40 @@ int launch_tiles(LinearArgs a, hipStream_t stream) {
 }
 
 template <bool DIRECT>
+int launch_eighths(LinearArgs a, int left, hipStream_t stream) {
+    using G = Tile<4, 2, 2, 4, 128, DIRECT>;
+    a.m_tiles = (a.M + 255) / 256;
+    a.n_tiles = (a.N + 255) / 256;
+    const int tiles = a.m_tiles * a.n_tiles, lds = G::lds((a.K + 127) / 128);
+    BEVPOOL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_linear_eighths<DIRECT>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL((k_linear_eighths<DIRECT>), dim3(uint32_t(tiles + 7 * left)), dim3(512), lds, stream, a,
+                       tiles - left);
+    BEVPOOL_HIP(hipGetLastError());
+    return BEVPOOL_OK;
+}
+
+template <bool DIRECT>
 int launch(const LinearArgs &a, hipStream_t stream) {
     auto tiles = [&](int m, int n) { return int64_t((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
-    if (a.M <= 16) {
-        hipLaunchKernelGGL((k_linear_few<1, DIRECT>), dim3(uint32_t((a.N + 15) / 16)), dim3(64 * kFewWaves), 0, stream,
-                           a);
-        BEVPOOL_HIP(hipGetLastError());
-        return BEVPOOL_OK;
-    }
-    if (tiles(64, 64) < 128) {
-        hipLaunchKernelGGL((k_linear_few<4, DIRECT>), dim3(uint32_t((a.N + 15) / 16), uint32_t((a.M + 63) / 64)),
-                           dim3(64 * kFewWaves), 0, stream, a);
-        BEVPOOL_HIP(hipGetLastError());
-        return BEVPOOL_OK;
-    }
-    if (tiles(128, 128) < 512) return launch_tiles<2, 2, 1, 1, DIRECT>(a, stream);
-    if (tiles(256, 256) < 512 || a.K <= 512) return launch_tiles<2, 2, 2, 2, DIRECT>(a, stream);
-    return launch_tiles<4, 2, 2, 4, DIRECT>(a, stream);
+    // Few tokens. The time of this form goes with its workgroups and with k, that of tiles of
+    // 64 x 64 that all run at once with k alone, and the two meet at about 560 workgroups
+    // (K 1024: 300 x 1024, 640 of them, 6.8 against 5.5 us; 517 x 512, 544, 4.5 against 5.8).
+    // One block of tokens instead of two where those leave compute units without work and k
+    // is short (64 x 1024, K 1024: 3.3 against 3.7 us; 300 x 256, K 4096: 9.1 against 7.5).
+    if (a.M <= 16) return launch_few<1, 8, DIRECT>(a, stream);
+    if (const int64_t groups = tiles(32, 16); groups <= 560)
+        return groups < kUnits && a.K <= 1024 ? launch_few<1, 8, DIRECT>(a, stream)
+                                              : launch_few<2, 8, DIRECT>(a, stream);
+    if (tiles(128, 128) < kUnits) return launch_tiles<2, 2, 1, 1, 128, DIRECT>(a, stream);
+    // Rounds of workgroups, in units of a round of 256 x 256 tiles, one to a compute unit (38
+    // us at K 2048): a round of 128 x 128, two to a unit, takes 22 us, one of eighths 10.
+    const int64_t big = tiles(256, 256), left = big % kUnits;
+    const bool eighths = big >= kUnits && left > 0 && left <= kUnits / 4;
+    const double big_time = double(big / kUnits) + (left == 0 ? 0.0 : eighths ? 0.27 * double((8 * left + kUnits - 1) / kUnits) : 1.0);
+    const double small_time = 0.58 * double((tiles(128, 128) + 2 * kUnits - 1) / (2 * kUnits));
+    if (a.K < 512 || small_time < big_time) return launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream);
+    return eighths ? launch_eighths<DIRECT>(a, int(left), stream) : launch_tiles<4, 2, 2, 4, 128, DIRECT>(a, stream);
 }
 
 }  // namespace

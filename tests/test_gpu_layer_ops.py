@@ -270,6 +270,15 @@ LINEAR_CASES = [
     (9000, 640, 2056, 0, 0, True, "bf16"),
     (9000, 640, 2049, 0, 0, False, "f32"),
     (8500, 700, 4100, 1, 0, True, "bf16"),
+    # the largest tiles, all of them whole and the last ones in eighths
+    (16384, 640, 1024, 0, 0, True, "bf16"),
+    (16300, 515, 1020, 0, 2, False, "f16"),
+    (16500, 528, 1000, 0, 0, True, "bf16"),
+    (16390, 513, 1021, 3, 0, True, "f32"),
+    # few tokens: one block of them and two, k shorter and longer than the waves' runs
+    (32, 1040, 4096, 0, 0, True, "bf16"),
+    (100, 3000, 300, 0, 0, False, "f32"),
+    (40, 5000, 2000, 0, 0, True, "bf16"),
 ]
 
 
