@@ -1,4 +1,5 @@
-"""Build libbevpool.so for gfx950 with hipcc, in-tree.
+"""Build libbevpool.so for gfx950 with hipcc, in-tree, and, where there is a torch, the
+native module _layer_native.so that calls it on torch tensors.
 
 ``python -m paper_2205_13542_amd.build`` (or ``build()``) always recompiles,
 so a stale library never survives a source change.
@@ -6,6 +7,7 @@ so a stale library never survives a source change.
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 
@@ -17,11 +19,15 @@ LIB_PATH = os.path.join(HERE, "libbevpool.so")
 # measurement probe for bench.py --floor (not part of the pooling library)
 FLOOR_SOURCE = "floor.hip"
 FLOOR_LIB_PATH = os.path.join(HERE, "libbevpool_floor.so")
+# calls of libbevpool.so on torch tensors, for layer_ops.py; host code alone
+TORCH_SOURCE = "layer_torch.cpp"
+TORCH_LIB_PATH = os.path.join(HERE, "_layer_native.so")
 SOURCES = ["bevpool.hip", "plan.hip", "forward.hip", "backward.hip", "layout.hip",
            "mapops.hip", "norm.hip", "dropout.hip", "attention.hip",
            "attention_backward.hip", "layerops.hip", "rms_norm.hip", "rotary.hip",
            "gated.hip", "linear_int8.hip"]
 
+CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
@@ -32,6 +38,27 @@ FLAGS = [
     "-Wall", "-Wno-unused-function",
     "-fvisibility=hidden",
 ]
+
+
+def _torch_commands(lib_dir: str, tmp: str) -> list:
+    """Compile and link commands of the native module, for the torch that is installed; none without one."""
+    import importlib.util
+    import sysconfig
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return []
+    torch_dir = os.path.dirname(spec.origin)
+    obj = tmp + ".o"
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))
+    system = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+              os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+    compile_ = [CXX, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+                "-DUSE_ROCM=1", "-I", INCLUDE, *(a for d in system for a in ("-isystem", d)), "-c",
+                os.path.join(CSRC, TORCH_SOURCE), "-o", obj]
+    link = [CXX, "-shared", obj, "-o", tmp, "-L", lib_dir, "-lbevpool", "-L", os.path.join(torch_dir, "lib"),
+            *("-l" + name for name in ("c10", "c10_hip", "torch_cpu", "torch_hip", "torch", "torch_python")),
+            "-Wl,-rpath,$ORIGIN"]
+    return [compile_, link]
 
 
 def build(verbose: bool = False) -> str:
@@ -45,6 +72,9 @@ def build(verbose: bool = False) -> str:
                  os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
         floor_tmp = FLOOR_LIB_PATH + ".tmp"
         cmds.append([HIPCC, *FLAGS, os.path.join(CSRC, FLOOR_SOURCE), "-o", floor_tmp])
+        lib_tmp, torch_tmp = os.path.join(tmpdir, "libbevpool.so"), os.path.join(tmpdir, "_layer_native.so")
+        torch_cmds = _torch_commands(tmpdir, torch_tmp)
+        cmds.extend(torch_cmds[:1])
         if verbose:
             for c in cmds:
                 print(" ".join(c), flush=True)
@@ -53,11 +83,14 @@ def build(verbose: bool = False) -> str:
             for r in ex.map(lambda c: subprocess.run(c, capture_output=True, text=True), cmds):
                 if r.returncode != 0:
                     raise subprocess.CalledProcessError(r.returncode, r.args, r.stdout, r.stderr)
-        tmp = LIB_PATH + ".tmp"
-        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp],
-                       check=True)
+        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", lib_tmp], check=True)
+        if torch_cmds:
+            subprocess.run(torch_cmds[1], check=True)
         os.replace(floor_tmp, FLOOR_LIB_PATH)
-    os.replace(tmp, LIB_PATH)
+        for made, path in ((lib_tmp, LIB_PATH), (torch_tmp, TORCH_LIB_PATH)):
+            if os.path.exists(made):        # the folder may be on another file system
+                shutil.copy(made, path + ".tmp")
+                os.replace(path + ".tmp", path)
     return LIB_PATH
 
 

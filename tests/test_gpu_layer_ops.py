@@ -529,7 +529,7 @@ def test_checkpoint_in_8_bits(torch, bev, features, dtype):
         x[7], x[8] = 3e38, 2.0 ** -125
         x[9] = 2.0 ** -130
     with torch.no_grad():
-        y, held, exponents, _ = layer_ops._gate_forward(x, "none", True)
+        y, held, exponents = layer_ops._native.gated_act_held(x, 0)
     rest = [i for i in range(20) if i != 6]
     ref, e = _held_reference(torch, x[rest], features)
     assert torch.equal(held[rest], ref) and torch.equal(exponents[rest], e)

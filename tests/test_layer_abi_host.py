@@ -191,34 +191,43 @@ def test_python_entries_refuse():
         bev.gated_act(x, checkpoint="fp8")
 
 
-def test_forward_mode_is_refused(monkeypatch):
-    """An input with a tangent is refused, with gradients enabled or not; the launches are stubs."""
+def test_forward_mode_is_refused():
+    """An input with a tangent is refused before anything else, with gradients enabled or not; inputs
+    without one get as far as the refusal of tensors that no GPU holds."""
     torch = pytest.importorskip("torch")
     import paper_2205_13542_amd as bev
-    from paper_2205_13542_amd import layer_ops
     from torch.autograd import forward_ad
-    monkeypatch.setattr(layer_ops, "_rms_forward",
-                        lambda x, r, *a: (x.clone(), x.clone(), x.clone(), layer_ops._map_binding.bevmap_rms()))
-    monkeypatch.setattr(layer_ops, "_rotary_of", lambda *a: (0, None))
-    monkeypatch.setattr(layer_ops, "_turn", lambda index, turn, x, *a: x.clone())
-    monkeypatch.setattr(layer_ops, "_gate_forward", lambda x, act, hold: (x.clone(), None, None, None))
-    monkeypatch.setattr(layer_ops, "_rms_int8", lambda x, *a: (x, x, x))
-    x, f = torch.ones(2, 8), torch.ones(2, dtype=torch.float64)
+    x, f, q, s = torch.ones(2, 8), torch.ones(2, dtype=torch.float64), torch.ones(2, 8, dtype=torch.int8), torch.ones(2)
     with forward_ad.dual_level():
-        xd, fd = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, f))
+        xd, fd, sd = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, f, s))
         for call in (lambda: bev.rms_norm(xd), lambda: bev.rms_norm(x, xd[0]), lambda: bev.rms_norm_add(x, xd),
-                     lambda: bev.rotary(xd.view(1, 2, 2, 4), x, f), lambda: bev.rotary(x.view(1, 2, 2, 4), x, fd),
-                     lambda: bev.gated_act(xd)):
+                     lambda: bev.rotary(xd.view(1, 2, 2, 4), s[None], f),
+                     lambda: bev.rotary(x.view(1, 2, 2, 4), s[None], fd), lambda: bev.gated_act(xd),
+                     lambda: bev.rms_norm_int8(xd), lambda: bev.rms_norm_add_int8(x, xd), lambda: bev.quantize_int8(xd),
+                     lambda: bev.linear_int8(q, s, q, sd)):
             with pytest.raises(NotImplementedError, match="forward mode"):
                 call()
             with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):
                 call()
-        for call in (lambda: bev.rms_norm_int8(xd), lambda: bev.rms_norm_add_int8(x, xd), lambda: bev.quantize_int8(xd),
-                     lambda: bev.linear_int8(x, xd[0], x, x)):
-            with torch.no_grad(), pytest.raises(bev.BevpoolError, match="no gradient"):
+        for call in (lambda: bev.rms_norm(x), lambda: bev.rms_norm_int8(x), lambda: bev.gated_act(x)):
+            with pytest.raises(bev.BevpoolError, match="device tensors"):
                 call()
-        # inputs without a tangent work
-        assert torch.equal(bev.rms_norm(x), x) and bev.rms_norm_int8(x)[0] is x
+
+
+def test_calls_with_other_things_than_tensors():
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    x, q, s = torch.zeros(2, 8), torch.zeros(2, 8, dtype=torch.int8), torch.zeros(2)
+    for call in (lambda: bev.rms_norm([1.0]), lambda: bev.rms_norm(x, 2.0), lambda: bev.rms_norm(x, eps="small"),
+                 lambda: bev.rms_norm(x, out_dtype="bf16"), lambda: bev.rms_norm_add(x, None),
+                 lambda: bev.rms_norm_add_int8(x, None), lambda: bev.quantize_int8(None),
+                 lambda: bev.linear_int8(q, None, q, s), lambda: bev.linear_int8(q, s, q, s, bias=0.0),
+                 lambda: bev.rotary(x, s, None), lambda: bev.gated_act(3)):
+        with pytest.raises(bev.BevpoolError, match="must be") as caught:
+            call()
+        assert caught.value.code == INVALID
+    with pytest.raises(RuntimeError, match="has no gradient"):
+        bev.quantize_int8(x.clone().requires_grad_())
 
 
 def test_rotary_frequencies():
