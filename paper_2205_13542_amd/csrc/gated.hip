@@ -96,7 +96,7 @@ __device__ __forceinline__ Place place_of(int64_t n, int32_t blocks) {
     return p;
 }
 
-template <int DT, int V>
+template <int DT, int V, bool STREAM>
 __global__ __launch_bounds__(kGateBlock) void k_gate(GateArgs a) {
     using T = typename Num<DT>::T;
     const T *x = static_cast<const T *>(a.x);
@@ -124,11 +124,11 @@ __global__ __launch_bounds__(kGateBlock) void k_gate(GateArgs a) {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] *= activate<act.value>(g[i]);
         });
-        if (live) store_n<T, V>(y + p.row * a.F + p.c, v);
+        if (live) store_n<T, V, STREAM>(y + p.row * a.F + p.c, v);
     }
 }
 
-template <int DT, int V, bool HELD>
+template <int DT, int V, bool HELD, bool STREAM>
 __global__ __launch_bounds__(kGateBlock) void k_gate_grad(GateArgs a) {
     using T = typename Num<DT>::T;
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
@@ -156,8 +156,8 @@ __global__ __launch_bounds__(kGateBlock) void k_gate_grad(GateArgs a) {
                 v[i] = d[i] * activate<act.value>(gate);
             }
         });
-        store_n<T, V>(dx + p.row * 2 * a.F + p.c, g);
-        store_n<T, V>(dx + p.row * 2 * a.F + a.F + p.c, v);
+        store_n<T, V, STREAM>(dx + p.row * 2 * a.F + p.c, g);
+        store_n<T, V, STREAM>(dx + p.row * 2 * a.F + a.F + p.c, v);
     }
 }
 
@@ -218,9 +218,11 @@ int bevmap_launch_gate(const bevmap_gate &n, const void *x, void *y, int8_t *q, 
     a.q = q;
     a.e = e;
     a.held = q != nullptr;
+    const bool past = past_caches(n.rows * n.features * dtype_bytes(n.dtype));
     with_type(n.dtype, v, [&](auto dt, auto width) {
-        hipLaunchKernelGGL((k_gate<decltype(dt)::value, decltype(width)::value>), grid_of(a), dim3(kGateBlock), 0,
-                           stream, a);
+        constexpr int DT = decltype(dt)::value, V = decltype(width)::value;
+        if (V > 2 && past) hipLaunchKernelGGL((k_gate<DT, V, (V > 2)>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+        else hipLaunchKernelGGL((k_gate<DT, V, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
     });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
@@ -236,10 +238,18 @@ int bevmap_launch_gate_backward(const bevmap_gate &n, const void *grad_y, const 
     a.dx = grad_x;
     a.q = const_cast<int8_t *>(q);
     a.e = const_cast<uint8_t *>(e);
+    const bool past = past_caches(n.rows * 2 * n.features * dtype_bytes(n.dtype));
     with_type(n.dtype, v, [&](auto dt, auto width) {
         constexpr int DT = decltype(dt)::value, V = decltype(width)::value;
-        if (q) hipLaunchKernelGGL((k_gate_grad<DT, V, true>), grid_of(a), dim3(kGateBlock), 0, stream, a);
-        else hipLaunchKernelGGL((k_gate_grad<DT, V, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+        auto go = [&](auto held) {
+            constexpr bool kHeldRow = decltype(held)::value != 0;
+            if (V > 2 && past)
+                hipLaunchKernelGGL((k_gate_grad<DT, V, kHeldRow, (V > 2)>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+            else
+                hipLaunchKernelGGL((k_gate_grad<DT, V, kHeldRow, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+        };
+        if (q) go(Int<1>());
+        else go(Int<0>());
     });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;

@@ -90,7 +90,7 @@ __device__ __forceinline__ void store_held(int8_t *p, const int8_t *v) {
     *reinterpret_cast<Bytes *>(p) = b;
 }
 
-template <int DT, int V, int LANES, int ITER, int OUT>
+template <int DT, int V, int LANES, int ITER, int OUT, bool STREAM>
 __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
     using T = typename Num<DT>::T;
     constexpr int kRows = kRmsBlock / LANES;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                     load_n<T, V>(res + row * a.ldr + at * V, r);
 #pragma unroll
                     for (int i = 0; i < V; ++i) h[k][i] += r[i];
-                    store_n<T, V>(sum + row * a.C + at * V, h[k]);
+                    store_n<T, V, STREAM>(sum + row * a.C + at * V, h[k]);
                 }
             }
         }
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 const int at = lane + k * LANES;
 #pragma unroll
                 for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * rstd * w[k][i];
-                if (live && at < n_vec) store_any<V>(a.y, row * a.C + at * V, a.y_dtype, h[k]);
+                if (live && at < n_vec) store_any<V, STREAM>(a.y, row * a.C + at * V, a.y_dtype, h[k]);
             }
         } else {
             uint32_t top = 0;
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_quantize_long(RmsArgs a) {
     }
 }
 
-template <int DT, int V, int LANES, int ITER>
+template <int DT, int V, int LANES, int ITER, bool STREAM>
 __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
     using T = typename Num<DT>::T;
     constexpr int kRows = kRmsBlock / LANES;
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
             const int at = lane + k * LANES;
 #pragma unroll
             for (int i = 0; i < V; ++i) e[k][i] = fmaf(rstd, fmaf(-u[k][i], mean, e[k][i]), more[k][i]);
-            if (live && at < n_vec) store_n<T, V>(dx + row * a.C + at * V, e[k]);
+            if (live && at < n_vec) store_n<T, V, STREAM>(dx + row * a.C + at * V, e[k]);
         }
     }
     if (!a.parts) return;
@@ -343,13 +343,15 @@ int access(int32_t dtype, int32_t C, const void *const *p, const int64_t *stride
     return 1;
 }
 
-// Few rows are spread over as many lanes as there are; many rows take the fewest lanes
-// that keep a row in at most eight accesses.
+// A row of up to a wave's accesses takes the fewest lanes; a longer one a wave, two accesses
+// a lane, where rows are many, else a workgroup. (Four and eight accesses of a wave were
+// slower than a workgroup: steps of 16896 x 2048 157 us against 115, of 8192 x 4096 172
+// against 137; two were not: 33000 x 1024 129 against 136.)
 Form form_of(int v, int32_t C, int64_t rows) {
     const int n = (C + v - 1) / v;
     const int few = rows < 4 * kRmsGroups;
     if (n <= 64) return {v, n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
-    if (!few && n <= 512) return {v, 64, n <= 128 ? 2 : n <= 256 ? 4 : 8};
+    if (!few && n <= 128) return {v, 64, 2};
     return {v, 256, n <= 256 ? 1 : n <= 512 ? 2 : n <= 1024 ? 4 : n <= 2048 ? 8 : 32};
 }
 
@@ -366,9 +368,7 @@ void with_form(const Form &f, F body) {
         if (f.lanes == 32) return body(v, Int<32>(), Int<1>());
         if (f.lanes == 64) {
             if (f.iter == 1) return body(v, Int<64>(), Int<1>());
-            if (f.iter == 2) return body(v, Int<64>(), Int<2>());
-            if (f.iter == 4) return body(v, Int<64>(), Int<4>());
-            return body(v, Int<64>(), Int<8>());
+            return body(v, Int<64>(), Int<2>());
         }
         if (f.iter == 1) return body(v, Int<256>(), Int<1>());
         if (f.iter == 2) return body(v, Int<256>(), Int<2>());
@@ -384,13 +384,19 @@ void with_form(const Form &f, F body) {
 
 template <int OUT>
 int launch_rows(RmsArgs a, int32_t dtype, const Form &f, hipStream_t stream) {
+    const bool past = past_caches(a.rows * a.C * dtype_bytes(dtype));
     const int64_t each = kRmsBlock / f.lanes, all = (a.rows + each - 1) / each;
     const dim3 grid{uint32_t(all < kRmsGroups ? all : kRmsGroups)}, wg(kRmsBlock);
     auto go = [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        with_form<DT == BEVPOOL_F32 ? 4 : 8>(f, [&](auto v, auto lanes, auto iter) {
-            hipLaunchKernelGGL((k_rms<DT, decltype(v)::value, decltype(lanes)::value, decltype(iter)::value, OUT>),
-                               grid, wg, 0, stream, a);
+        constexpr int kWide = DT == BEVPOOL_F32 ? 4 : 8;
+        with_form<kWide>(f, [&](auto v, auto lanes, auto iter) {
+            constexpr int V = decltype(v)::value, L = decltype(lanes)::value, I = decltype(iter)::value;
+            constexpr bool kMay = V == kWide && OUT != kInt8;   // write whole 16 bytes
+            if (kMay && past)
+                hipLaunchKernelGGL((k_rms<DT, V, L, I, OUT, kMay>), grid, wg, 0, stream, a);
+            else
+                hipLaunchKernelGGL((k_rms<DT, V, L, I, OUT, false>), grid, wg, 0, stream, a);
         });
     };
     if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
@@ -419,7 +425,7 @@ using namespace bevmap;
 int64_t bevmap_rms_workspace_bytes(const bevmap_rms &n) {
     if (n.rows == 0) return 0;
     int64_t most = 0;
-    for (int64_t each : {1, 4, 8, 16, 32}) {
+    for (int64_t each : {1, 4, 8, 16, 32}) {    // rows that the forms take at once
         const int64_t chunk = chunk_of(n.rows, each), groups = (n.rows + chunk - 1) / chunk;
         if (groups > most) most = groups;
     }
@@ -515,12 +521,17 @@ int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, con
         a.chunk = chunk_of(n.rows, each);
         groups = (n.rows + a.chunk - 1) / a.chunk;
         const dim3 grid{uint32_t(groups)}, wg(kRmsBlock);
+        const bool past = past_caches(n.rows * n.channels * dtype_bytes(n.x_dtype));
         const size_t lds = f.lanes <= kRmsWave ? size_t(n.channels) * sizeof(float) : 0;
         auto go = [&](auto dt) {
             constexpr int DT = decltype(dt)::value;
-            with_form<DT == BEVPOOL_F32 ? 4 : 8>(f, [&](auto v, auto lanes, auto iter) {
-                hipLaunchKernelGGL((k_rms_grad<DT, decltype(v)::value, decltype(lanes)::value, decltype(iter)::value>),
-                                   grid, wg, lds, stream, a);
+            constexpr int kWide = DT == BEVPOOL_F32 ? 4 : 8;
+            with_form<kWide>(f, [&](auto v, auto lanes, auto iter) {
+                constexpr int V = decltype(v)::value, L = decltype(lanes)::value, I = decltype(iter)::value;
+                if (V == kWide && past)
+                    hipLaunchKernelGGL((k_rms_grad<DT, V, L, I, V == kWide>), grid, wg, lds, stream, a);
+                else
+                    hipLaunchKernelGGL((k_rms_grad<DT, V, L, I, false>), grid, wg, lds, stream, a);
             });
         };
         if (n.x_dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());

@@ -16,6 +16,7 @@ namespace bevmap {
 namespace {
 
 constexpr int kTurnBlock = 256;
+constexpr int kTurnAhead = 2;           // units of a thread that are on their way at once
 constexpr int kTurnEntries = 2048;      // (cos, sin) of a tile, 16 KB
 constexpr int64_t kTurnGroups = 1 << 16;
 
@@ -57,72 +58,97 @@ __device__ __forceinline__ float2 turn_of(double position, double frequency) {
 
 // V: elements of an access. A unit is V pairs in halves (two accesses), V / 2 pairs
 // interleaved (one access; with V = 1 one pair in two), or V channels that keep their place.
-template <int DT, int V, bool MIXED>
+template <int DT, int V, bool MIXED, bool STREAM>
 __global__ __launch_bounds__(kTurnBlock) void k_turn(TurnArgs a) {
     using T = typename Num<DT>::T;
     extern __shared__ float2 turns[];            // [tile][pairs]
     const T *x = static_cast<const T *>(a.x);
     T *out = static_cast<T *>(a.out);
     constexpr int kEach = MIXED ? (V > 1 ? V / 2 : 1) : V;      // pairs of a unit
+    constexpr bool kOne = MIXED && V > 1;                       // one access to a unit
     const int turned = a.pairs / kEach, units = turned + (a.dim - 2 * a.pairs) / V;
+    const int apart = MIXED ? 1 : a.pairs;
     for (int64_t first = int64_t(blockIdx.x) * a.tile; first < a.tokens; first += int64_t(gridDim.x) * a.tile) {
-        const int n = int(min(int64_t(a.tile), a.tokens - first));
-        for (int i = threadIdx.x; i < n * a.pairs; i += kTurnBlock) {
-            const uint32_t t = bevpool::fdiv(i, a.by_pairs), p = i - t * a.pairs;
-            const int64_t at = (first + t) * a.axes + bevpool::fdiv(p, a.by_axis);
-            const float2 cs = turn_of(position_at(a, at), a.frequencies[p]);
-            turns[i] = make_float2(cs.x * a.amplitude, cs.y * a.amplitude * a.sign);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < n * a.heads * units; i += kTurnBlock) {
-            const uint32_t th = bevpool::fdiv(i, a.by_units), u = i - th * units;
-            const uint32_t t = bevpool::fdiv(th, a.by_head), head = th - t * a.heads;
-            const uint32_t token = uint32_t(first + t), b = bevpool::fdiv(token, a.by_sample);
-            const T *from = x + int64_t(b) * a.x_batch + int64_t(token - b * a.per_sample) * a.x_row + head * a.x_head;
-            T *to = out + (int64_t(token) * a.heads + head) * a.dim;
-            float v[V];
-            if (int(u) >= turned) {
-                const int c = 2 * a.pairs + (u - turned) * V;
-                load_n<T, V>(from + c, v);
-                store_n<T, V>(to + c, v);
-                continue;
+        const int n = int(min(int64_t(a.tile), a.tokens - first)), all = n * a.heads * units;
+        for (int begin = 0; begin < all; begin += kTurnAhead * kTurnBlock) {
+            // a thread's units are on their way while it forms the tile's sines and cosines
+            Pack<T, V> low[kTurnAhead], high[kTurnAhead];
+            T *to[kTurnAhead];
+            int turn[kTurnAhead];           // first of the unit's pairs among the tile's; -1: channels that stay
+#pragma unroll
+            for (int j = 0; j < kTurnAhead; ++j) {
+                const int i = begin + j * kTurnBlock + threadIdx.x;
+                to[j] = nullptr;
+                if (i >= all) continue;
+                const uint32_t th = bevpool::fdiv(i, a.by_units), u = i - th * units;
+                const uint32_t t = bevpool::fdiv(th, a.by_head), head = th - t * a.heads;
+                const uint32_t token = uint32_t(first + t), b = bevpool::fdiv(token, a.by_sample);
+                const bool turns_it = int(u) < turned;
+                const int c = !turns_it ? 2 * a.pairs + int(u - turned) * V : MIXED && V == 1 ? 2 * u : u * V;
+                const T *from = x + int64_t(b) * a.x_batch + int64_t(token - b * a.per_sample) * a.x_row +
+                                head * a.x_head + c;
+                low[j] = *reinterpret_cast<const Pack<T, V> *>(from);
+                if (!kOne && turns_it) high[j] = *reinterpret_cast<const Pack<T, V> *>(from + apart);
+                turn[j] = turns_it ? int(t * a.pairs + u * kEach) : -1;
+                to[j] = out + (int64_t(token) * a.heads + head) * a.dim + c;
             }
-            const float2 *cs = turns + t * a.pairs + u * kEach;
-            if constexpr (MIXED && V > 1) {
-                load_n<T, V>(from + u * V, v);
-#pragma unroll
-                for (int j = 0; j < V / 2; ++j) {
-                    const float p = v[2 * j], q = v[2 * j + 1];
-                    v[2 * j] = fmaf(p, cs[j].x, -q * cs[j].y);
-                    v[2 * j + 1] = fmaf(p, cs[j].y, q * cs[j].x);
+            if (begin == 0) {
+                for (int i = threadIdx.x; i < n * a.pairs; i += kTurnBlock) {
+                    const uint32_t t = bevpool::fdiv(i, a.by_pairs), p = i - t * a.pairs;
+                    const int64_t at = (first + t) * a.axes + bevpool::fdiv(p, a.by_axis);
+                    const float2 cs = turn_of(position_at(a, at), a.frequencies[p]);
+                    turns[i] = make_float2(cs.x * a.amplitude, cs.y * a.amplitude * a.sign);
                 }
-                store_n<T, V>(to + u * V, v);
-            } else {
-                const int c = MIXED ? 2 * u : u * V, apart = MIXED ? 1 : a.pairs;
-                float w[V];
-                load_n<T, V>(from + c, v);
-                load_n<T, V>(from + c + apart, w);
+                __syncthreads();
+            }
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float p = v[j], q = w[j];
-                    v[j] = fmaf(p, cs[j].x, -q * cs[j].y);
-                    w[j] = fmaf(p, cs[j].y, q * cs[j].x);
+            for (int j = 0; j < kTurnAhead; ++j) {
+                if (!to[j]) continue;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = float(low[j].v[e]);
+                if (turn[j] >= 0) {
+                    const float2 *cs = turns + turn[j];
+                    if constexpr (kOne) {
+#pragma unroll
+                        for (int e = 0; e < V / 2; ++e) {
+                            const float p = v[2 * e], q = v[2 * e + 1];
+                            v[2 * e] = fmaf(p, cs[e].x, -q * cs[e].y);
+                            v[2 * e + 1] = fmaf(p, cs[e].y, q * cs[e].x);
+                        }
+                    } else {
+                        float w[V];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const float p = v[e], q = float(high[j].v[e]);
+                            v[e] = fmaf(p, cs[e].x, -q * cs[e].y);
+                            w[e] = fmaf(p, cs[e].y, q * cs[e].x);
+                        }
+                        store_n<T, V, STREAM>(to[j] + apart, w);
+                    }
                 }
-                store_n<T, V>(to + c, v);
-                store_n<T, V>(to + c + apart, w);
+                store_n<T, V, STREAM>(to[j], v);
             }
         }
         __syncthreads();
     }
 }
 
-template <int DT, int V>
-void launch(const TurnArgs &a, bool mixed, hipStream_t stream) {
+template <int DT, int V, bool MIXED>
+void launch(const TurnArgs &a, hipStream_t stream) {
     const int64_t all = (a.tokens + a.tile - 1) / a.tile;
     const dim3 grid{uint32_t(all < kTurnGroups ? all : kTurnGroups)}, wg(kTurnBlock);
     const size_t lds = size_t(a.tile) * a.pairs * sizeof(float2);
-    if (mixed) hipLaunchKernelGGL((k_turn<DT, V, true>), grid, wg, lds, stream, a);
-    else hipLaunchKernelGGL((k_turn<DT, V, false>), grid, wg, lds, stream, a);
+    if (V > 2 && past_caches(a.tokens * a.heads * a.dim * dtype_bytes(DT)))
+        hipLaunchKernelGGL((k_turn<DT, V, MIXED, (V > 2)>), grid, wg, lds, stream, a);
+    else
+        hipLaunchKernelGGL((k_turn<DT, V, MIXED, false>), grid, wg, lds, stream, a);
+}
+
+template <int DT, int V>
+void launch(const TurnArgs &a, bool mixed, hipStream_t stream) {
+    if (mixed) launch<DT, V, true>(a, stream);
+    else launch<DT, V, false>(a, stream);
 }
 
 template <int DT>
@@ -173,10 +199,12 @@ int bevmap_launch_rotary(const bevmap_turn &n, const void *x, const void *positi
     }
     const int each = mixed ? (v > 1 ? v / 2 : 1) : v;
     const int units = n.pairs / each + (n.dim - 2 * n.pairs) / v;
-    // tokens of a tile: about four units to a thread, less where that leaves compute units without work
-    int64_t tile = kTurnEntries / n.pairs;
-    const int64_t enough = (int64_t(4) * kTurnBlock + int64_t(n.heads) * units - 1) / (int64_t(n.heads) * units);
-    if (tile > enough) tile = enough;
+    // Tokens of a tile: a unit and a pair to every thread, less where that leaves compute units
+    // without work. (129600 tokens, 4 heads of 32: 36 us a step; two units to a thread 44, four 52.)
+    auto per = [](int64_t of, int64_t each) { return (of + each - 1) / each; };
+    const int64_t by_unit = per(kTurnBlock, int64_t(n.heads) * units), by_pair = per(kTurnBlock, n.pairs);
+    int64_t tile = by_unit > by_pair ? by_unit : by_pair;
+    if (tile > kTurnEntries / n.pairs) tile = kTurnEntries / n.pairs;
     const int64_t spread = (a.tokens + 1023) / 1024;
     if (tile > spread) tile = spread;
     a.tile = int32_t(tile < 1 ? 1 : tile);
