@@ -43,6 +43,19 @@ __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int K) {
     i32x4 v = {0, 0, 0, 0};
     if (k + 16 <= K) {
         __builtin_memcpy(&v, row + k, 16);
+    } else if (k < K && K >= 16) {
+        // the row's last 16 bytes, moved down by those before k
+        uint64_t part[2];
+        __builtin_memcpy(part, row + K - 16, 16);
+        const int down = 8 * (16 - (K - k));
+        if (down >= 64) {
+            part[0] = part[1] >> (down - 64);
+            part[1] = 0;
+        } else {
+            part[0] = part[0] >> down | part[1] << (64 - down);
+            part[1] >>= down;
+        }
+        __builtin_memcpy(&v, part, 16);
     } else if (k < K) {
         int8_t b[16];
 #pragma unroll
@@ -328,7 +341,9 @@ __global__ __launch_bounds__(512) void k_linear_eighths(LinearArgs a, int whole)
 }
 
 // Few tokens: 16 channels and 16 * MB tokens of a workgroup, whose waves share out k in
-// runs of kRun bytes. A wave's next run is on its way while one is multiplied.
+// runs of kRun bytes. Bound by the loads of 16 rows each, some 70 cycles of a compute unit
+// (64 x 4096 x 2048: 7.8 us; the next run on its way, or four at once, change nothing, nor
+// do workgroups that start at different k).
 template <int MB, int WAVES, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearArgs a) {
     __shared__ i32x4 sums[WAVES][MB][64];
@@ -346,36 +361,22 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearArgs a) {
             return load_chunk(row, k, a.K);
         }
     };
-    struct Run {
-        i32x4 w[kRun / 64], x[kRun / 64][MB];
-    };
-    auto load_run = [&](int first, Run &r) {
-#pragma unroll
-        for (int s = 0; s < kRun / 64; ++s) {
-            const int k = first + 64 * s + 16 * quarter;
-            r.w[s] = load(w, k);
-#pragma unroll
-            for (int j = 0; j < MB; ++j) r.x[s][j] = load(x[j], k);
-        }
-    };
     i32x4 acc[MB];
 #pragma unroll
     for (int j = 0; j < MB; ++j) acc[j] = i32x4{0, 0, 0, 0};
-    auto multiply = [&](const Run &r) {
+    for (int first = wave * kRun; first < a.K; first += WAVES * kRun) {
+        i32x4 wv[kRun / 64], xv[kRun / 64][MB];
+#pragma unroll
+        for (int s = 0; s < kRun / 64; ++s) {
+            const int k = first + 64 * s + 16 * quarter;
+            wv[s] = load(w, k);
+#pragma unroll
+            for (int j = 0; j < MB; ++j) xv[s][j] = load(x[j], k);
+        }
 #pragma unroll
         for (int s = 0; s < kRun / 64; ++s)
 #pragma unroll
-            for (int j = 0; j < MB; ++j)
-                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(r.w[s], r.x[s][j], acc[j], 0, 0, 0);
-    };
-    Run one, two;
-    int first = wave * kRun;
-    load_run(first, one);
-    for (; first < a.K; first += 2 * WAVES * kRun) {
-        load_run(first + WAVES * kRun, two);
-        multiply(one);
-        load_run(first + 2 * WAVES * kRun, one);
-        multiply(two);
+            for (int j = 0; j < MB; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[s], xv[s][j], acc[j], 0, 0, 0);
     }
 #pragma unroll
     for (int j = 0; j < MB; ++j) sums[wave][j][lane] = acc[j];
@@ -435,13 +436,13 @@ int launch(const LinearArgs &a, hipStream_t stream) {
     auto tiles = [&](int m, int n) { return int64_t((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
     // Few tokens. The time of this form goes with its workgroups and with k, that of tiles of
     // 64 x 64 that all run at once with k alone, and the two meet at about 560 workgroups
-    // (K 1024: 300 x 1024, 640 of them, 6.8 against 5.5 us; 517 x 512, 544, 4.5 against 5.8).
+    // (K 1024: 300 x 1024, 640 of them, 6.6 against 5.5 us; 517 x 512, 544, 4.1 against 5.8).
     // One block of tokens instead of two where those leave compute units without work and k
-    // is short (64 x 1024, K 1024: 3.3 against 3.7 us; 300 x 256, K 4096: 9.1 against 7.5).
+    // is short (64 x 1024, K 1024: 3.1 against 3.8 us; 300 x 256, K 4096: 9.2 against 7.9).
     if (a.M <= 16) return launch_few<1, 8, DIRECT>(a, stream);
     if (const int64_t groups = tiles(32, 16); groups <= 560)
         return groups < kUnits && a.K <= 1024 ? launch_few<1, 8, DIRECT>(a, stream)
-                                              : launch_few<2, 8, DIRECT>(a, stream);
+                                              : launch_few<2, 4, DIRECT>(a, stream);
     if (tiles(128, 128) < kUnits) return launch_tiles<2, 2, 1, 1, 128, DIRECT>(a, stream);
     // Rounds of workgroups, in units of a round of 256 x 256 tiles, one to a compute unit (38
     // us at K 2048): a round of 128 x 128, two to a unit, takes 22 us, one of eighths 10.
