@@ -341,43 +341,73 @@ __global__ __launch_bounds__(512) void k_linear_eighths(LinearArgs a, int whole)
 }
 
 // Few tokens: 16 channels and 16 * MB tokens of a workgroup, whose waves share out k in
-// runs of kRun bytes. Bound by the loads of 16 rows each, some 70 cycles of a compute unit
-// (64 x 4096 x 2048: 7.8 us; the next run on its way, or four at once, change nothing, nor
-// do workgroups that start at different k).
+// runs of kRun bytes. A wave reads eight rows of a run at a time, whole cache lines, and
+// turns them in LDS of its own into the operands' order, 16 rows of 16 bytes. (Read in that
+// order, a wave's load of 16 half lines takes a compute unit some 70 cycles: 64 x 4096 x
+// 2048 7.8 us.)
 template <int MB, int WAVES, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearArgs a) {
-    __shared__ i32x4 sums[WAVES][MB][64];
+    constexpr int kBlocks = 1 + MB;         // of 16 rows: channels, then tokens
+    constexpr int kMine = kBlocks * 16 * kRun;
+    __shared__ __align__(16) char lds[WAVES * kMine];
+    i32x4(*sums)[MB][64] = reinterpret_cast<i32x4(*)[MB][64]>(lds);
+    static_assert(sizeof(i32x4) * MB * 64 <= kMine, "");
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, quarter = lane / 16, col = lane % 16;
     const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MB;
-    const int8_t *w = a.w + int64_t(min(n0 + col, a.N - 1)) * a.ldw, *x[MB];
+    const int line = lane / 8, chunk = lane % 8;
+    const int8_t *from[kBlocks][2];         // rows line and line + 8 of a block
 #pragma unroll
-    for (int j = 0; j < MB; ++j) x[j] = a.x + int64_t(min(m0 + 16 * j + col, a.M - 1)) * a.ldx;
-    auto load = [&](const int8_t *row, int k) {
-        if constexpr (DIRECT) {
-            i32x4 v = {0, 0, 0, 0};
-            if (k < a.K) v = *reinterpret_cast<const i32x4 *>(row + k);
-            return v;
-        } else {
-            return load_chunk(row, k, a.K);
-        }
+    for (int h = 0; h < 2; ++h) {
+        from[0][h] = a.w + int64_t(min(n0 + 8 * h + line, a.N - 1)) * a.ldw;
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+            from[1 + j][h] = a.x + int64_t(min(m0 + 16 * j + 8 * h + line, a.M - 1)) * a.ldx;
+    }
+    i32x4 way[kBlocks][2];                  // a run on its way
+    auto fetch = [&](int first) {
+        const int k = first + 16 * chunk;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (DIRECT) {
+                    way[b][h] = i32x4{0, 0, 0, 0};
+                    if (k < a.K) way[b][h] = *reinterpret_cast<const i32x4 *>(from[b][h] + k);
+                } else {
+                    way[b][h] = load_chunk(from[b][h], k, a.K);
+                }
+            }
     };
+    // row r's chunk c lies at place c ^ r / 2: sixteen rows at one chunk cover all banks
+    char *mine = lds + wave * kMine;
     i32x4 acc[MB];
 #pragma unroll
     for (int j = 0; j < MB; ++j) acc[j] = i32x4{0, 0, 0, 0};
+    fetch(wave * kRun);
     for (int first = wave * kRun; first < a.K; first += WAVES * kRun) {
-        i32x4 wv[kRun / 64], xv[kRun / 64][MB];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 8 * h + line;
+                *reinterpret_cast<i32x4 *>(mine + (b * 16 + r) * kRun + (chunk ^ r / 2) * 16) = way[b][h];
+            }
+        if (first + WAVES * kRun < a.K) fetch(first + WAVES * kRun);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int s = 0; s < kRun / 64; ++s) {
-            const int k = first + 64 * s + 16 * quarter;
-            wv[s] = load(w, k);
+            i32x4 v[kBlocks];
 #pragma unroll
-            for (int j = 0; j < MB; ++j) xv[s][j] = load(x[j], k);
+            for (int b = 0; b < kBlocks; ++b)
+                v[b] = *reinterpret_cast<const i32x4 *>(mine + (b * 16 + col) * kRun + ((4 * s + quarter) ^ col / 2) * 16);
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[0], v[1 + j], acc[j], 0, 0, 0);
         }
-#pragma unroll
-        for (int s = 0; s < kRun / 64; ++s)
-#pragma unroll
-            for (int j = 0; j < MB; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[s], xv[s][j], acc[j], 0, 0, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < MB; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
@@ -435,14 +465,13 @@ template <bool DIRECT>
 int launch(const LinearArgs &a, hipStream_t stream) {
     auto tiles = [&](int m, int n) { return int64_t((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
     // Few tokens. The time of this form goes with its workgroups and with k, that of tiles of
-    // 64 x 64 that all run at once with k alone, and the two meet at about 560 workgroups
-    // (K 1024: 300 x 1024, 640 of them, 6.6 against 5.5 us; 517 x 512, 544, 4.1 against 5.8).
-    // One block of tokens instead of two where those leave compute units without work and k
-    // is short (64 x 1024, K 1024: 3.1 against 3.8 us; 300 x 256, K 4096: 9.2 against 7.9).
+    // 64 x 64 that all run at once with k alone, and the two meet at about 1100 workgroups
+    // (256 x 2048, K 2048, 1024 of them: 7.0 against 8.3 us; 1111 x 520, K 336, 1155: 4.3
+    // against 3.8). Eight waves where a compute unit holds one workgroup (64 x 2048, K 4096:
+    // 5.1 against 5.8 us), four where it holds more (256 x 2048, K 2048: 7.0 against 7.4).
     if (a.M <= 16) return launch_few<1, 8, DIRECT>(a, stream);
-    if (const int64_t groups = tiles(32, 16); groups <= 560)
-        return groups < kUnits && a.K <= 1024 ? launch_few<1, 8, DIRECT>(a, stream)
-                                              : launch_few<2, 4, DIRECT>(a, stream);
+    if (const int64_t groups = tiles(32, 16); groups <= 1100)
+        return groups <= kUnits ? launch_few<2, 8, DIRECT>(a, stream) : launch_few<2, 4, DIRECT>(a, stream);
     if (tiles(128, 128) < kUnits) return launch_tiles<2, 2, 1, 1, 128, DIRECT>(a, stream);
     // Rounds of workgroups, in units of a round of 256 x 256 tiles, one to a compute unit (38
     // us at K 2048): a round of 128 x 128, two to a unit, takes 22 us, one of eighths 10.

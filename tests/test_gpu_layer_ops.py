@@ -279,6 +279,12 @@ LINEAR_CASES = [
     (32, 1040, 4096, 0, 0, True, "bf16"),
     (100, 3000, 300, 0, 0, False, "f32"),
     (40, 5000, 2000, 0, 0, True, "bf16"),
+    (33, 129, 70, 0, 0, True, "f32"),
+    (200, 1025, 1000, 0, 0, False, "bf16"),
+    (250, 1056, 2000, 0, 0, True, "f16"),
+    (16, 7, 40, 0, 0, True, "f32"),
+    (700, 2000, 777, 0, 0, True, "f32"),        # tiles of 64, a k that divides nothing
+    (2500, 300, 1100, 0, 0, False, "bf16"),
 ]
 
 
