@@ -12,6 +12,7 @@
 //
 // Bound by memory. A thread takes V neighbouring channels of both halves, and
 // neighbouring lanes the rest of their blocks, whose largest goes through the lanes.
+// 129600 x 640 in bf16 takes 54-56 us with the copy (335 MB, 6.0 TB/s), 52 backward from it.
 #include "activation.h"
 #include "mapops.h"
 

@@ -1,8 +1,8 @@
 // The operators around attention as calls from Python on torch tensors: the module
 // _layer_native, which layer_ops.py documents and wraps. Argument checks, allocations,
 // the C ABI's calls and the autograd nodes are here and not in Python because a call on a
-// few rows costs its host time: one token's rotary positions take 5 us a call here, 9
-// through ctypes; a training step of the norm 60 instead of 110.
+// few rows costs its host time: one token's rotary positions take 4.9 us a call here, 8.7
+// through ctypes; a training step of the norm of 600 rows 66 instead of 110.
 //
 // Everything runs on the current stream of its inputs' device, with temporaries from
 // torch's allocator. A refusal is a BevpoolError (its class comes from Python), an input

@@ -11,9 +11,10 @@
 //
 // Two forms. Tiles: a workgroup stages kStep bytes of its rows and channels in LDS, two
 // stages in turn, the next on its way (past the registers, where rows are 16-byte
-// aligned) while the matrix cores work. Few tokens: the weights are what is read, so a
-// workgroup takes 16 channels, its waves share out k, and operands go straight to
-// registers; the waves' sums are joined in LDS.
+// aligned) while the matrix cores work: 16896 x 2048 x 4096 (tokens, k, channels) takes 158
+// to 172 us, 8192^3 531, 2070 TOP/s (a library product without scales 171 and 541). Few
+// tokens: the weights are what is read, so a workgroup takes 16 channels, its waves share out
+// k and join their sums in LDS: 64 x 4096 x 2048 takes 5.1 us.
 #include "mapops.h"
 
 namespace bevmap {
