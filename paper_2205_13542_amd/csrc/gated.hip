@@ -34,11 +34,6 @@ struct GateArgs {
     bool held;                  // write q and e
 };
 
-template <int V>
-struct alignas(V) Bytes {
-    int8_t v[V];
-};
-
 // The largest magnitude's bits over the lanes that share a block.
 template <int V>
 __device__ __forceinline__ uint32_t block_top(const float *v) {
@@ -63,24 +58,26 @@ __device__ __forceinline__ int exponent_of(uint32_t top) {
     return e > -127 ? e : -127;
 }
 
-template <int V>
-__device__ __forceinline__ void hold(const float *v, int8_t *q, uint8_t *e, bool live, bool first) {
+// count: channels of the unit, 0 of one past the row's end.
+template <int V, int ROWS>
+__device__ __forceinline__ void hold(const float *v, int8_t *q, uint8_t *e, int count, bool first) {
     const uint32_t top = block_top<V>(v);
     const bool none = top >= 0x7F800000u;
     const int ex = exponent_of(top);
-    Bytes<V> b;
+    int8_t b[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) b.v[i] = int8_t(none ? 0.0f : rintf(ldexpf(v[i], -ex)));
-    if (live) *reinterpret_cast<Bytes<V> *>(q) = b;
+    for (int i = 0; i < V; ++i) b[i] = int8_t(none ? 0.0f : rintf(ldexpf(v[i], -ex)));
+    if (count > 0) store_bytes<V, ROWS>(q, count, b);
     if (first) *e = uint8_t(none ? kNanExponent : ex + 127);
 }
 
-template <int V>
-__device__ __forceinline__ void release(const int8_t *q, uint8_t e, float *v) {
-    const Bytes<V> b = *reinterpret_cast<const Bytes<V> *>(q);
+template <int V, int ROWS>
+__device__ __forceinline__ void release(const int8_t *q, uint8_t e, int count, float *v) {
+    int8_t b[V];
+    load_bytes<V, ROWS>(q, count, b);
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        v[i] = e == kNanExponent ? __uint_as_float(0x7FC00000u) : ldexpf(float(b.v[i]), int(e) - 127);
+        v[i] = e == kNanExponent ? __uint_as_float(0x7FC00000u) : ldexpf(float(b[i]), int(e) - 127);
 }
 
 // Unit n of a pass: row and first channel; whole blocks of kHeld / V units each.
@@ -97,57 +94,60 @@ __device__ __forceinline__ Place place_of(int64_t n, int32_t blocks) {
     return p;
 }
 
-template <int DT, int V, bool STREAM>
+template <int DT, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kGateBlock) void k_gate(GateArgs a) {
     using T = typename Num<DT>::T;
+    constexpr int V = kWide<DT>;
     const T *x = static_cast<const T *>(a.x);
     T *y = static_cast<T *>(a.y);
     // whole waves stay together, for the lanes that share a block
     for (int64_t n0 = int64_t(blockIdx.x) * kGateBlock; n0 < a.units; n0 += int64_t(gridDim.x) * kGateBlock) {
         const int64_t n = n0 + threadIdx.x;
         const Place p = place_of<V>(n, a.blocks);
-        const bool live = n < a.units && p.c < a.F;
+        const int count = n < a.units && p.c < a.F ? a.F - p.c : 0;
         float g[V], v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) g[i] = v[i] = 0.0f;
-        if (live) {
-            load_n<T, V>(x + p.row * a.ldx + p.c, g);
-            load_n<T, V>(x + p.row * a.ldx + a.F + p.c, v);
+        if (count > 0) {
+            load_part<T, V, ROWS>(x + p.row * a.ldx + p.c, count, g);
+            load_part<T, V, ROWS>(x + p.row * a.ldx + a.F + p.c, count, v);
         }
         if (a.held) {
             int8_t *q = a.q + p.row * 2 * a.F + p.c;
             uint8_t *e = a.e + p.row * 2 * a.blocks + p.c / kHeld;
-            const bool first = live && p.c % kHeld == 0;
-            hold<V>(g, q, e, live, first);
-            hold<V>(v, q + a.F, e + a.blocks, live, first);
+            const bool first = count > 0 && p.c % kHeld == 0;
+            hold<V, ROWS>(g, q, e, count, first);
+            hold<V, ROWS>(v, q + a.F, e + a.blocks, count, first);
         }
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] *= activate<act.value>(g[i]);
         });
-        if (live) store_n<T, V, STREAM>(y + p.row * a.F + p.c, v);
+        if (count > 0) store_part<T, V, ROWS, STREAM>(y + p.row * a.F + p.c, count, v);
     }
 }
 
-template <int DT, int V, bool HELD, bool STREAM>
+template <int DT, int ROWS, bool HELD, bool STREAM>
 __global__ __launch_bounds__(kGateBlock) void k_gate_grad(GateArgs a) {
     using T = typename Num<DT>::T;
+    constexpr int V = kWide<DT>;
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
     T *dx = static_cast<T *>(a.dx);
     for (int64_t n = int64_t(blockIdx.x) * kGateBlock + threadIdx.x; n < a.units;
          n += int64_t(gridDim.x) * kGateBlock) {
         const Place p = place_of<V>(n, a.blocks);
-        if (p.c >= a.F) continue;
+        const int count = a.F - p.c;
+        if (count <= 0) continue;
         float g[V], v[V], d[V];
-        load_n<T, V>(dy + p.row * a.F + p.c, d);
+        load_part<T, V, ROWS>(dy + p.row * a.F + p.c, count, d);
         if constexpr (HELD) {
             const int8_t *q = a.q + p.row * 2 * a.F + p.c;
             const uint8_t *e = a.e + p.row * 2 * a.blocks + p.c / kHeld;
-            release<V>(q, e[0], g);
-            release<V>(q + a.F, e[a.blocks], v);
+            release<V, ROWS>(q, e[0], count, g);
+            release<V, ROWS>(q + a.F, e[a.blocks], count, v);
         } else {
-            load_n<T, V>(x + p.row * a.ldx + p.c, g);
-            load_n<T, V>(x + p.row * a.ldx + a.F + p.c, v);
+            load_part<T, V, ROWS>(x + p.row * a.ldx + p.c, count, g);
+            load_part<T, V, ROWS>(x + p.row * a.ldx + a.F + p.c, count, v);
         }
         with_act(a.act, [&](auto act) {
 #pragma unroll
@@ -157,45 +157,28 @@ __global__ __launch_bounds__(kGateBlock) void k_gate_grad(GateArgs a) {
                 v[i] = d[i] * activate<act.value>(gate);
             }
         });
-        store_n<T, V, STREAM>(dx + p.row * 2 * a.F + p.c, g);
-        store_n<T, V, STREAM>(dx + p.row * 2 * a.F + a.F + p.c, v);
+        store_part<T, V, ROWS, STREAM>(dx + p.row * 2 * a.F + p.c, count, g);
+        store_part<T, V, ROWS, STREAM>(dx + p.row * 2 * a.F + a.F + p.c, count, v);
     }
 }
 
-// Elements of an access: as many as 16 bytes hold where both halves of every row allow it, two, or one.
-int access(const bevmap_gate &n, const void *x, const void *y, const void *dx, const void *q) {
-    for (int v : {n.dtype == BEVPOOL_F32 ? 4 : 8, 2})
-        if (n.features % v == 0 && (!x || aligned_for(x, n.rows == 1 ? 0 : n.x_stride, n.dtype, v)) &&
-            aligned_for(y, 0, n.dtype, v) && aligned_for(dx, 0, n.dtype, v) &&
-            reinterpret_cast<uintptr_t>(q) % uintptr_t(v) == 0)
-            return v;
-    return 1;
+// How the halves of rows lie.
+int halves_lie(const bevmap_gate &n, const void *x, const void *y, const void *dx, const void *q) {
+    const int v = n.dtype == BEVPOOL_F32 ? 4 : 8;
+    if (n.features < v) return kShort;
+    const bool even = n.features % v == 0 && aligned_for(x, n.rows == 1 ? 0 : n.x_stride, n.dtype, v) &&
+                      aligned_for(y, 0, n.dtype, v) && aligned_for(dx, 0, n.dtype, v) &&
+                      reinterpret_cast<uintptr_t>(q) % 8 == 0;
+    return even ? kEven : kUneven;
 }
 
-template <int V>
-struct Int {
-    static constexpr int value = V;
-};
-template <class F>
-void with_type(int32_t dtype, int v, F body) {
-    auto go = [&](auto dt) {
-        constexpr int kWide = decltype(dt)::value == BEVPOOL_F32 ? 4 : 8;
-        if (v == kWide) body(dt, Int<kWide>());
-        else if (v == 2) body(dt, Int<2>());
-        else body(dt, Int<1>());
-    };
-    if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
-    else if (dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
-    else go(Int<BEVPOOL_F16>());
-}
-
-GateArgs args_of(const bevmap_gate &n, int v) {
+GateArgs args_of(const bevmap_gate &n) {
     GateArgs a{};
     a.ldx = n.x_stride;
     a.rows = n.rows;
     a.F = n.features;
     a.blocks = (n.features + kHeld - 1) / kHeld;
-    a.units = n.rows * a.blocks * (kHeld / v);
+    a.units = n.rows * a.blocks * (kHeld / (n.dtype == BEVPOOL_F32 ? 4 : 8));
     a.act = n.act;
     return a;
 }
@@ -212,18 +195,18 @@ using namespace bevmap;
 
 int bevmap_launch_gate(const bevmap_gate &n, const void *x, void *y, int8_t *q, uint8_t *e, hipStream_t stream) {
     if (n.rows == 0) return BEVPOOL_OK;
-    const int v = access(n, x, y, nullptr, q);
-    GateArgs a = args_of(n, v);
+    GateArgs a = args_of(n);
     a.x = x;
     a.y = y;
     a.q = q;
     a.e = e;
     a.held = q != nullptr;
     const bool past = past_caches(n.rows * n.features * dtype_bytes(n.dtype));
-    with_type(n.dtype, v, [&](auto dt, auto width) {
-        constexpr int DT = decltype(dt)::value, V = decltype(width)::value;
-        if (V > 2 && past) hipLaunchKernelGGL((k_gate<DT, V, (V > 2)>), grid_of(a), dim3(kGateBlock), 0, stream, a);
-        else hipLaunchKernelGGL((k_gate<DT, V, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+    with_type_and_rows(n.dtype, halves_lie(n, x, y, nullptr, q), [&](auto dt, auto how) {
+        constexpr int DT = decltype(dt)::value;
+        constexpr int ROWS = decltype(how)::value;
+        if (ROWS == kEven && past) hipLaunchKernelGGL((k_gate<DT, ROWS, ROWS == kEven>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+        else hipLaunchKernelGGL((k_gate<DT, ROWS, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
     });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
@@ -232,22 +215,22 @@ int bevmap_launch_gate(const bevmap_gate &n, const void *x, void *y, int8_t *q, 
 int bevmap_launch_gate_backward(const bevmap_gate &n, const void *grad_y, const void *x, const int8_t *q,
                                 const uint8_t *e, void *grad_x, hipStream_t stream) {
     if (n.rows == 0) return BEVPOOL_OK;
-    const int v = access(n, q ? nullptr : x, grad_y, grad_x, q);
-    GateArgs a = args_of(n, v);
+    GateArgs a = args_of(n);
     a.x = x;
     a.dy = grad_y;
     a.dx = grad_x;
     a.q = const_cast<int8_t *>(q);
     a.e = const_cast<uint8_t *>(e);
     const bool past = past_caches(n.rows * 2 * n.features * dtype_bytes(n.dtype));
-    with_type(n.dtype, v, [&](auto dt, auto width) {
-        constexpr int DT = decltype(dt)::value, V = decltype(width)::value;
+    with_type_and_rows(n.dtype, halves_lie(n, q ? nullptr : x, grad_y, grad_x, q), [&](auto dt, auto how) {
+        constexpr int DT = decltype(dt)::value;
+        constexpr int ROWS = decltype(how)::value;
         auto go = [&](auto held) {
-            constexpr bool kHeldRow = decltype(held)::value != 0;
-            if (V > 2 && past)
-                hipLaunchKernelGGL((k_gate_grad<DT, V, kHeldRow, (V > 2)>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+            constexpr bool kHeldRow = decltype(held)::value;
+            if (ROWS == kEven && past)
+                hipLaunchKernelGGL((k_gate_grad<DT, ROWS, kHeldRow, ROWS == kEven>), grid_of(a), dim3(kGateBlock), 0, stream, a);
             else
-                hipLaunchKernelGGL((k_gate_grad<DT, V, kHeldRow, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
+                hipLaunchKernelGGL((k_gate_grad<DT, ROWS, kHeldRow, false>), grid_of(a), dim3(kGateBlock), 0, stream, a);
         };
         if (q) go(Int<1>());
         else go(Int<0>());

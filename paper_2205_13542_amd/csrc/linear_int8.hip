@@ -92,10 +92,6 @@ struct Tile {
     }
 };
 
-template <int V>
-struct Int {
-    static constexpr int value = V;
-};
 // body(constant) with the type of y
 template <class F>
 __device__ __forceinline__ void with_dtype(int dtype, F body) {

@@ -15,6 +15,8 @@
 // registers and the backward sums dw there; its parts are joined in a fixed order by a
 // small kernel. 518400 x 80 in bf16 takes 58 us forward with a residual (332 MB, 5.7 TB/s;
 // a copy of 4 GiB reaches 4.75), 84 + 6 backward (415 MB); 129600 x 80 in 8 bits 15.9.
+#include <initializer_list>
+
 #include "mapops.h"
 
 namespace bevmap {
@@ -81,23 +83,13 @@ __device__ __forceinline__ int8_t held(float z, const Steps &s) {
     return int8_t(s.none ? 0.0f : rintf(z * s.up * s.mul));
 }
 
-template <int V>
-__device__ __forceinline__ void store_held(int8_t *p, const int8_t *v) {
-    struct alignas(V) Bytes {
-        int8_t v[V];
-    } b;
-#pragma unroll
-    for (int i = 0; i < V; ++i) b.v[i] = v[i];
-    *reinterpret_cast<Bytes *>(p) = b;
-}
-
-template <int DT, int V, int LANES, int ITER, int OUT, bool STREAM>
+template <int DT, int LANES, int ITER, int OUT, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
     using T = typename Num<DT>::T;
-    constexpr int kRows = kRmsBlock / LANES;
+    constexpr int V = kWide<DT>, kRows = kRmsBlock / LANES;
     __shared__ float add[8];
     __shared__ uint32_t most[8];
-    const int lane = threadIdx.x % LANES, n_vec = a.C / V;
+    const int lane = threadIdx.x % LANES, n_vec = (a.C + V - 1) / V;
     const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
     T *sum = static_cast<T *>(a.sum);
     float w[ITER][V];
@@ -106,7 +98,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) w[k][i] = 1.0f;
         if (OUT != kInt8 && a.weight && lane + k * LANES < n_vec)
-            load_any<V>(a.weight, int64_t(lane + k * LANES) * V, a.w_dtype, w[k]);
+            load_any_part<V, ROWS>(a.weight, (lane + k * LANES) * V, a.w_dtype, a.C - (lane + k * LANES) * V, w[k]);
     }
     const float per = 1.0f / float(a.C);
     int turn = 0;
@@ -120,13 +112,14 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
 #pragma unroll
             for (int i = 0; i < V; ++i) h[k][i] = 0.0f;
             if (live && at < n_vec) {
-                load_n<T, V>(x + row * a.ldx + at * V, h[k]);
+                const int count = a.C - at * V;
+                load_part<T, V, ROWS>(x + row * a.ldx + at * V, count, h[k]);
                 if (OUT != kInt8 && res) {
                     float r[V];
-                    load_n<T, V>(res + row * a.ldr + at * V, r);
+                    load_part<T, V, ROWS>(res + row * a.ldr + at * V, count, r);
 #pragma unroll
                     for (int i = 0; i < V; ++i) h[k][i] += r[i];
-                    store_n<T, V, STREAM>(sum + row * a.C + at * V, h[k]);
+                    store_part<T, V, ROWS, STREAM>(sum + row * a.C + at * V, count, h[k]);
                 }
             }
         }
@@ -161,7 +154,8 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 const int at = lane + k * LANES;
 #pragma unroll
                 for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * rstd * w[k][i];
-                if (live && at < n_vec) store_any<V, STREAM>(a.y, row * a.C + at * V, a.y_dtype, h[k]);
+                if (live && at < n_vec)
+                    store_any_part<V, ROWS, STREAM>(a.y, row * a.C + at * V, a.y_dtype, a.C - at * V, h[k]);
             }
         } else {
             uint32_t top = 0;
@@ -181,25 +175,26 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 int8_t q[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) q[i] = held(h[k][i], steps);
-                if (live && at < n_vec) store_held<V>(a.q + row * a.C + at * V, q);
+                if (live && at < n_vec) store_bytes<V, ROWS>(a.q + row * a.C + at * V, a.C - at * V, q);
             }
         }
     }
 }
 
 // Rows too long for registers, a workgroup to a row: read twice, the second time from cache.
-template <int DT, int V>
+template <int DT, int ROWS>
 __global__ __launch_bounds__(kRmsBlock) void k_quantize_long(RmsArgs a) {
     using T = typename Num<DT>::T;
+    constexpr int V = kWide<DT>;
     __shared__ uint32_t most[8];
-    const int n_vec = a.C / V;
+    const int n_vec = (a.C + V - 1) / V;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
         const T *x = static_cast<const T *>(a.x) + row * a.ldx;
         uint32_t top = 0;
         for (int at = threadIdx.x; at < n_vec; at += kRmsBlock) {
             float v[V];
-            load_n<T, V>(x + int64_t(at) * V, v);
+            load_part<T, V, ROWS>(x + int64_t(at) * V, a.C - at * V, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) top = larger(top, size_bits(v[i]));
         }
@@ -208,21 +203,21 @@ __global__ __launch_bounds__(kRmsBlock) void k_quantize_long(RmsArgs a) {
         for (int at = threadIdx.x; at < n_vec; at += kRmsBlock) {
             float v[V];
             int8_t q[V];
-            load_n<T, V>(x + int64_t(at) * V, v);
+            load_part<T, V, ROWS>(x + int64_t(at) * V, a.C - at * V, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) q[i] = held(v[i], steps);
-            store_held<V>(a.q + row * a.C + int64_t(at) * V, q);
+            store_bytes<V, ROWS>(a.q + row * a.C + int64_t(at) * V, a.C - at * V, q);
         }
     }
 }
 
-template <int DT, int V, int LANES, int ITER, bool STREAM>
+template <int DT, int LANES, int ITER, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
     using T = typename Num<DT>::T;
-    constexpr int kRows = kRmsBlock / LANES;
-    extern __shared__ float joined[];       // [C], rows shared by a wave or less
+    constexpr int V = kWide<DT>, kRows = kRmsBlock / LANES;
+    extern __shared__ float joined[];       // [n_vec * V], rows shared by a wave or less
     __shared__ float add[8];
-    const int lane = threadIdx.x % LANES, n_vec = a.C / V;
+    const int lane = threadIdx.x % LANES, n_vec = (a.C + V - 1) / V;
     const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
     const T *dsum = static_cast<const T *>(a.dsum);
     T *dx = static_cast<T *>(a.sum);
@@ -235,7 +230,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
             dw[k][i] = 0.0f;
         }
         if (a.weight && lane + k * LANES < n_vec)
-            load_any<V>(a.weight, int64_t(lane + k * LANES) * V, a.w_dtype, w[k]);
+            load_any_part<V, ROWS>(a.weight, (lane + k * LANES) * V, a.w_dtype, a.C - (lane + k * LANES) * V, w[k]);
     }
     const float per = 1.0f / float(a.C);
     const int64_t begin = int64_t(blockIdx.x) * a.chunk, end = min(begin + a.chunk, a.rows);
@@ -251,10 +246,11 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
 #pragma unroll
             for (int i = 0; i < V; ++i) u[k][i] = other[k][i] = e[k][i] = more[k][i] = 0.0f;
             if (live && at < n_vec) {
-                load_n<T, V>(x + row * a.ldx + at * V, u[k]);
-                if (res) load_n<T, V>(res + row * a.ldr + at * V, other[k]);
-                load_any<V>(a.dy, row * a.C + at * V, a.y_dtype, e[k]);
-                if (dsum) load_n<T, V>(dsum + row * a.C + at * V, more[k]);
+                const int count = a.C - at * V;
+                load_part<T, V, ROWS>(x + row * a.ldx + at * V, count, u[k]);
+                if (res) load_part<T, V, ROWS>(res + row * a.ldr + at * V, count, other[k]);
+                load_any_part<V, ROWS>(a.dy, row * a.C + at * V, a.y_dtype, count, e[k]);
+                if (dsum) load_part<T, V, ROWS>(dsum + row * a.C + at * V, count, more[k]);
             }
         }
 #pragma unroll
@@ -272,7 +268,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
             const int at = lane + k * LANES;
 #pragma unroll
             for (int i = 0; i < V; ++i) e[k][i] = fmaf(rstd, fmaf(-u[k][i], mean, e[k][i]), more[k][i]);
-            if (live && at < n_vec) store_n<T, V, STREAM>(dx + row * a.C + at * V, e[k]);
+            if (live && at < n_vec) store_part<T, V, ROWS, STREAM>(dx + row * a.C + at * V, a.C - at * V, e[k]);
         }
     }
     if (!a.parts) return;
@@ -280,7 +276,8 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
     if constexpr (LANES > kRmsWave) {
 #pragma unroll
         for (int k = 0; k < ITER; ++k)
-            if (lane + k * LANES < n_vec) store_n<float, V>(part + (lane + k * LANES) * V, dw[k]);
+            if (lane + k * LANES < n_vec)
+                store_part<float, V, ROWS>(part + (lane + k * LANES) * V, a.C - (lane + k * LANES) * V, dw[k]);
     } else {
         // over the rows of a wave, then one wave after the other
 #pragma unroll
@@ -298,11 +295,11 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms_grad(RmsArgs a) {
                     const int at = lane + k * LANES;
                     if (at >= n_vec) continue;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
+                    for (int i = 0; i < V; ++i) {       // of whole vectors: joined has their room
                         if (turns > 0) dw[k][i] += joined[at * V + i];
                         joined[at * V + i] = dw[k][i];
                     }
-                    if (turns == kWaves - 1) store_n<float, V>(part + at * V, dw[k]);
+                    if (turns == kWaves - 1) store_part<float, V, ROWS>(part + at * V, a.C - at * V, dw[k]);
                 }
             __syncthreads();
         }
@@ -327,82 +324,70 @@ __global__ __launch_bounds__(kRmsJoinBlock) void k_rms_join(const float *parts, 
     if (lane == 0 && c < C) store_any<1>(dw, c, dtype, &th[0][i]);
 }
 
-// A form: elements of an access, lanes that share a row, accesses of a lane.
+// A form: lanes that share a row, accesses of a lane.
 struct Form {
-    int v, lanes, iter;
+    int lanes, iter;
 };
 
 constexpr int64_t kRmsGroups = 2048;    // workgroups that stay: eight to a compute unit
 
-// Elements of an access: as many as 16 bytes hold where the rows allow it, two, or one.
-int access(int32_t dtype, int32_t C, const void *const *p, const int64_t *stride, int n) {
-    for (int v : {dtype == BEVPOOL_F32 ? 4 : 8, 2}) {
-        bool fits = C % v == 0;
-        for (int i = 0; i < n; ++i) fits = fits && aligned_for(p[i], stride[i], dtype, v);
-        if (fits) return v;
-    }
-    return 1;
+// How rows of C elements lie that start at p and are so many elements apart.
+int rows_lie(int32_t dtype, int32_t C, std::initializer_list<const void *> p, std::initializer_list<int64_t> strides) {
+    const int v = dtype == BEVPOOL_F32 ? 4 : 8;
+    if (C < v) return kShort;
+    bool even = C % v == 0;
+    for (const void *q : p) even = even && aligned_for(q, 0, dtype, v);
+    for (int64_t s : strides) even = even && aligned_for(nullptr, s, dtype, v);
+    return even ? kEven : kUneven;
 }
+// The same where something of another type, which starts at p, has rows beside them.
+int beside(int lie, int32_t dtype, const void *p) {
+    return lie == kEven && !aligned_for(p, 0, dtype, 8) ? kUneven : lie;
+}
+int beside_bytes(int lie, const void *p) { return lie == kEven && reinterpret_cast<uintptr_t>(p) % 8 ? kUneven : lie; }
 
 // A row of up to a wave's accesses takes the fewest lanes; a longer one a wave, two accesses
 // a lane, where rows are many, else a workgroup. (Four and eight accesses of a wave were
 // slower than a workgroup: steps of 16896 x 2048 157 us against 115, of 8192 x 4096 172
 // against 137; two were not: 33000 x 1024 129 against 136.)
-Form form_of(int v, int32_t C, int64_t rows) {
-    const int n = (C + v - 1) / v;
-    const int few = rows < 4 * kRmsGroups;
-    if (n <= 64) return {v, n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
-    if (!few && n <= 128) return {v, 64, 2};
-    return {v, 256, n <= 256 ? 1 : n <= 512 ? 2 : n <= 1024 ? 4 : n <= 2048 ? 8 : 32};
+Form form_of(int32_t dtype, int32_t C, int64_t rows) {
+    const int v = dtype == BEVPOOL_F32 ? 4 : 8, n = (C + v - 1) / v;
+    if (n <= 64) return {n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
+    if (n <= 128 && rows >= 4 * kRmsGroups) return {64, 2};
+    return {256, n <= 256 ? 1 : n <= 512 ? 2 : n <= 1024 ? 4 : 8};
 }
 
-// body(constants V, LANES, ITER) of a form
-template <int V>
-struct Int {
-    static constexpr int value = V;
-};
-template <int WIDE, class F>
+// body(constants LANES, ITER) of a form
+template <int DT, int ROWS, class F>
 void with_form(const Form &f, F body) {
-    auto lanes = [&](auto v) {
-        if (f.lanes == 8) return body(v, Int<8>(), Int<1>());
-        if (f.lanes == 16) return body(v, Int<16>(), Int<1>());
-        if (f.lanes == 32) return body(v, Int<32>(), Int<1>());
-        if (f.lanes == 64) {
-            if (f.iter == 1) return body(v, Int<64>(), Int<1>());
-            return body(v, Int<64>(), Int<2>());
-        }
-        if (f.iter == 1) return body(v, Int<256>(), Int<1>());
-        if (f.iter == 2) return body(v, Int<256>(), Int<2>());
-        if (f.iter == 4) return body(v, Int<256>(), Int<4>());
-        if constexpr (decltype(v)::value <= 4)
-            if (f.iter == 8) return body(v, Int<256>(), Int<8>());
-        if constexpr (decltype(v)::value <= 2) return body(v, Int<256>(), Int<32>());
-    };
-    if (f.v == WIDE) return lanes(Int<WIDE>());
-    if (f.v == 2) return lanes(Int<2>());
-    lanes(Int<1>());
+    if (ROWS == kShort || f.lanes == 8) return body(Int<8>(), Int<1>());
+    if constexpr (ROWS != kShort) {
+        if (f.lanes == 16) return body(Int<16>(), Int<1>());
+        if (f.lanes == 32) return body(Int<32>(), Int<1>());
+        if (f.lanes == 64) return f.iter == 1 ? body(Int<64>(), Int<1>()) : body(Int<64>(), Int<2>());
+        if (f.iter == 1) return body(Int<256>(), Int<1>());
+        if (f.iter == 2) return body(Int<256>(), Int<2>());
+        if (f.iter == 4) return body(Int<256>(), Int<4>());
+        if constexpr (kWide<DT> == 4) body(Int<256>(), Int<8>());
+    }
 }
 
 template <int OUT>
-int launch_rows(RmsArgs a, int32_t dtype, const Form &f, hipStream_t stream) {
-    const bool past = past_caches(a.rows * a.C * dtype_bytes(dtype));
+int launch_rows(const RmsArgs &a, int32_t dtype, int lie, hipStream_t stream) {
+    const Form f = form_of(dtype, a.C, a.rows);
+    const bool past = OUT != kInt8 && past_caches(a.rows * a.C * dtype_bytes(dtype));
     const int64_t each = kRmsBlock / f.lanes, all = (a.rows + each - 1) / each;
     const dim3 grid{uint32_t(all < kRmsGroups ? all : kRmsGroups)}, wg(kRmsBlock);
-    auto go = [&](auto dt) {
+    with_type_and_rows(dtype, lie, [&](auto dt, auto how) {
         constexpr int DT = decltype(dt)::value;
-        constexpr int kWide = DT == BEVPOOL_F32 ? 4 : 8;
-        with_form<kWide>(f, [&](auto v, auto lanes, auto iter) {
-            constexpr int V = decltype(v)::value, L = decltype(lanes)::value, I = decltype(iter)::value;
-            constexpr bool kMay = V == kWide && OUT != kInt8;   // write whole 16 bytes
-            if (kMay && past)
-                hipLaunchKernelGGL((k_rms<DT, V, L, I, OUT, kMay>), grid, wg, 0, stream, a);
-            else
-                hipLaunchKernelGGL((k_rms<DT, V, L, I, OUT, false>), grid, wg, 0, stream, a);
+        constexpr int ROWS = decltype(how)::value;
+        constexpr bool kMay = ROWS == kEven && OUT != kInt8;    // writes whole 16 bytes
+        with_form<DT, ROWS>(f, [&](auto lanes, auto iter) {
+            constexpr int L = decltype(lanes)::value, I = decltype(iter)::value;
+            if (kMay && past) hipLaunchKernelGGL((k_rms<DT, L, I, OUT, ROWS, kMay>), grid, wg, 0, stream, a);
+            else hipLaunchKernelGGL((k_rms<DT, L, I, OUT, ROWS, false>), grid, wg, 0, stream, a);
         });
-    };
-    if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
-    else if (dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
-    else go(Int<BEVPOOL_F16>());
+    });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -453,14 +438,11 @@ int bevmap_launch_rms_norm(const bevmap_rms &n, const void *x, const void *resid
     a.w_dtype = n.weight_dtype;
     a.eps = n.eps;
     const bool one = n.rows == 1;
-    const void *p[] = {x, residual, sum};
-    const int64_t s[] = {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride, 0};
-    int v = access(n.x_dtype, n.channels, p, s, 3);
-    if (weight && !aligned_for(weight, 0, n.weight_dtype, v)) v = 1;
-    if (!q && !aligned_for(y, 0, n.y_dtype, v)) v = 1;
-    if (q && reinterpret_cast<uintptr_t>(q) % uintptr_t(v)) v = 1;
-    const Form f = form_of(v, n.channels, n.rows);
-    return q ? launch_rows<kInt8Norm>(a, n.x_dtype, f, stream) : launch_rows<kFloat>(a, n.x_dtype, f, stream);
+    int lie = rows_lie(n.x_dtype, n.channels, {x, residual, sum},
+                       {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride});
+    lie = beside(lie, n.weight_dtype, weight);
+    if (q) return launch_rows<kInt8Norm>(a, n.x_dtype, beside_bytes(lie, q), stream);
+    return launch_rows<kFloat>(a, n.x_dtype, beside(lie, n.y_dtype, y), stream);
 }
 
 int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *scale, int64_t rows, int32_t columns,
@@ -473,20 +455,12 @@ int bevmap_launch_quantize(const void *x, int64_t x_stride, int8_t *q, float *sc
     a.ldx = x_stride;
     a.rows = rows;
     a.C = columns;
-    const void *p[] = {x};
-    const int64_t s[] = {rows == 1 ? 0 : x_stride};
-    int v = access(dtype, columns, p, s, 1);
-    if (reinterpret_cast<uintptr_t>(q) % uintptr_t(v)) v = 1;
-    if (columns <= kNormMaxChannels) return launch_rows<kInt8>(a, dtype, form_of(v, columns, rows), stream);
+    const int lie = beside_bytes(rows_lie(dtype, columns, {x}, {rows == 1 ? 0 : x_stride}), q);
+    if (columns <= kNormMaxChannels) return launch_rows<kInt8>(a, dtype, lie, stream);
     const dim3 grid{uint32_t(rows < kRmsGroups ? rows : kRmsGroups)}, wg(kRmsBlock);
-    auto go = [&](auto dt) {
-        constexpr int DT = decltype(dt)::value, kWide = DT == BEVPOOL_F32 ? 4 : 8;
-        if (v == kWide) hipLaunchKernelGGL((k_quantize_long<DT, kWide>), grid, wg, 0, stream, a);
-        else hipLaunchKernelGGL((k_quantize_long<DT, 1>), grid, wg, 0, stream, a);
-    };
-    if (dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
-    else if (dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
-    else go(Int<BEVPOOL_F16>());
+    with_type_and_rows(dtype, lie, [&](auto dt, auto how) {
+        hipLaunchKernelGGL((k_quantize_long<decltype(dt)::value, decltype(how)::value>), grid, wg, 0, stream, a);
+    });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
@@ -513,31 +487,25 @@ int bevmap_launch_rms_norm_backward(const bevmap_rms &n, const void *grad_y, con
         a.y_dtype = n.y_dtype;
         a.w_dtype = n.weight_dtype;
         const bool one = n.rows == 1;
-        const void *p[] = {x, residual, grad_sum, grad_x};
-        const int64_t s[] = {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride, 0, 0};
-        int v = access(n.x_dtype, n.channels, p, s, 4);
-        if ((weight && !aligned_for(weight, 0, n.weight_dtype, v)) || !aligned_for(grad_y, 0, n.y_dtype, v)) v = 1;
-        const Form f = form_of(v, n.channels, n.rows);
+        int lie = rows_lie(n.x_dtype, n.channels, {x, residual, grad_sum, grad_x},
+                           {one ? 0 : n.x_stride, one || !residual ? 0 : n.residual_stride});
+        lie = beside(beside(lie, n.weight_dtype, weight), n.y_dtype, grad_y);
+        const Form f = form_of(n.x_dtype, n.channels, n.rows);
         const int64_t each = kRmsBlock / f.lanes;
         a.chunk = chunk_of(n.rows, each);
         groups = (n.rows + a.chunk - 1) / a.chunk;
         const dim3 grid{uint32_t(groups)}, wg(kRmsBlock);
         const bool past = past_caches(n.rows * n.channels * dtype_bytes(n.x_dtype));
-        const size_t lds = f.lanes <= kRmsWave ? size_t(n.channels) * sizeof(float) : 0;
-        auto go = [&](auto dt) {
+        with_type_and_rows(n.x_dtype, lie, [&](auto dt, auto how) {
             constexpr int DT = decltype(dt)::value;
-            constexpr int kWide = DT == BEVPOOL_F32 ? 4 : 8;
-            with_form<kWide>(f, [&](auto v, auto lanes, auto iter) {
-                constexpr int V = decltype(v)::value, L = decltype(lanes)::value, I = decltype(iter)::value;
-                if (V == kWide && past)
-                    hipLaunchKernelGGL((k_rms_grad<DT, V, L, I, V == kWide>), grid, wg, lds, stream, a);
-                else
-                    hipLaunchKernelGGL((k_rms_grad<DT, V, L, I, false>), grid, wg, lds, stream, a);
+            constexpr int ROWS = decltype(how)::value;
+            with_form<DT, ROWS>(f, [&](auto lanes, auto iter) {
+                constexpr int L = decltype(lanes)::value, I = decltype(iter)::value;
+                const size_t lds = L <= kRmsWave ? size_t(L) * I * kWide<DT> * sizeof(float) : 0;
+                if (ROWS == kEven && past) hipLaunchKernelGGL((k_rms_grad<DT, L, I, ROWS, ROWS == kEven>), grid, wg, lds, stream, a);
+                else hipLaunchKernelGGL((k_rms_grad<DT, L, I, ROWS, false>), grid, wg, lds, stream, a);
             });
-        };
-        if (n.x_dtype == BEVPOOL_F32) go(Int<BEVPOOL_F32>());
-        else if (n.x_dtype == BEVPOOL_BF16) go(Int<BEVPOOL_BF16>());
-        else go(Int<BEVPOOL_F16>());
+        });
         BEVPOOL_HIP(hipGetLastError());
     }
     if (grad_weight) {

@@ -57,24 +57,25 @@ __device__ __forceinline__ float2 turn_of(double position, double frequency) {
     return make_float2(k == 1 || k == 2 ? -c : c, k >= 2 ? -d : d);
 }
 
-// V: elements of an access. A unit is V pairs in halves (two accesses), V / 2 pairs
-// interleaved (one access; with V = 1 one pair in two), or V channels that keep their place.
-template <int DT, int V, bool MIXED, bool STREAM>
+// An access has V elements. A unit is V pairs in halves (two accesses), V / 2 pairs
+// interleaved (one access), or V channels that keep their place. Short rows (kShort) go pair
+// by pair.
+template <int DT, bool MIXED, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kTurnBlock) void k_turn(TurnArgs a) {
     using T = typename Num<DT>::T;
+    constexpr int V = ROWS != kShort ? kWide<DT> : MIXED ? 2 : 1;
     extern __shared__ float2 turns[];            // [tile][pairs]
     const T *x = static_cast<const T *>(a.x);
     T *out = static_cast<T *>(a.out);
-    constexpr int kEach = MIXED ? (V > 1 ? V / 2 : 1) : V;      // pairs of a unit
-    constexpr bool kOne = MIXED && V > 1;                       // one access to a unit
-    const int turned = a.pairs / kEach, units = turned + (a.dim - 2 * a.pairs) / V;
-    const int apart = MIXED ? 1 : a.pairs;
+    constexpr int kEach = MIXED ? V / 2 : V;                    // pairs of a unit
+    const int turned = (a.pairs + kEach - 1) / kEach, rest = a.dim - 2 * a.pairs, units = turned + (rest + V - 1) / V;
     for (int64_t first = int64_t(blockIdx.x) * a.tile; first < a.tokens; first += int64_t(gridDim.x) * a.tile) {
         const int n = int(min(int64_t(a.tile), a.tokens - first)), all = n * a.heads * units;
         for (int begin = 0; begin < all; begin += kTurnAhead * kTurnBlock) {
             // a thread's units are on their way while it forms the tile's sines and cosines
-            Pack<T, V> low[kTurnAhead], high[kTurnAhead];
+            float low[kTurnAhead][V], high[kTurnAhead][V];
             T *to[kTurnAhead];
+            int count[kTurnAhead];          // elements of an access
             int turn[kTurnAhead];           // first of the unit's pairs among the tile's; -1: channels that stay
 #pragma unroll
             for (int j = 0; j < kTurnAhead; ++j) {
@@ -85,11 +86,18 @@ __global__ __launch_bounds__(kTurnBlock) void k_turn(TurnArgs a) {
                 const uint32_t t = bevpool::fdiv(th, a.by_head), head = th - t * a.heads;
                 const uint32_t token = uint32_t(first + t), b = bevpool::fdiv(token, a.by_sample);
                 const bool turns_it = int(u) < turned;
-                const int c = !turns_it ? 2 * a.pairs + int(u - turned) * V : MIXED && V == 1 ? 2 * u : u * V;
+                const int c = turns_it ? u * V : 2 * a.pairs + int(u - turned) * V;
                 const T *from = x + int64_t(b) * a.x_batch + int64_t(token - b * a.per_sample) * a.x_row +
                                 head * a.x_head + c;
-                low[j] = *reinterpret_cast<const Pack<T, V> *>(from);
-                if (!kOne && turns_it) high[j] = *reinterpret_cast<const Pack<T, V> *>(from + apart);
+                count[j] = !turns_it ? a.dim - c : MIXED ? 2 * a.pairs - c : a.pairs - c;
+                if constexpr (ROWS == kShort) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) low[j][e] = e < count[j] ? float(from[e]) : 0.0f;
+                    if (!MIXED && turns_it) high[j][0] = float(from[a.pairs]);
+                } else {        // a window over the end of the channels that stay begins among the others
+                    load_part<T, V, ROWS>(from, count[j], low[j]);
+                    if (!MIXED && turns_it) load_part<T, V, ROWS>(from + a.pairs, count[j], high[j]);
+                }
                 turn[j] = turns_it ? int(t * a.pairs + u * kEach) : -1;
                 to[j] = out + (int64_t(token) * a.heads + head) * a.dim + c;
             }
@@ -105,12 +113,11 @@ __global__ __launch_bounds__(kTurnBlock) void k_turn(TurnArgs a) {
 #pragma unroll
             for (int j = 0; j < kTurnAhead; ++j) {
                 if (!to[j]) continue;
-                float v[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = float(low[j].v[e]);
+                float(&v)[V] = low[j];
                 if (turn[j] >= 0) {
+                    // (an uneven unit's last angles are another's, for elements that are not written)
                     const float2 *cs = turns + turn[j];
-                    if constexpr (kOne) {
+                    if constexpr (MIXED) {
 #pragma unroll
                         for (int e = 0; e < V / 2; ++e) {
                             const float p = v[2 * e], q = v[2 * e + 1];
@@ -118,46 +125,42 @@ __global__ __launch_bounds__(kTurnBlock) void k_turn(TurnArgs a) {
                             v[2 * e + 1] = fmaf(p, cs[e].y, q * cs[e].x);
                         }
                     } else {
-                        float w[V];
+                        float(&w)[V] = high[j];
 #pragma unroll
                         for (int e = 0; e < V; ++e) {
-                            const float p = v[e], q = float(high[j].v[e]);
+                            const float p = v[e], q = w[e];
                             v[e] = fmaf(p, cs[e].x, -q * cs[e].y);
                             w[e] = fmaf(p, cs[e].y, q * cs[e].x);
                         }
-                        store_n<T, V, STREAM>(to[j] + apart, w);
+                        if constexpr (ROWS == kShort) to[j][a.pairs] = T(w[0]);
+                        else store_part<T, V, ROWS, STREAM>(to[j] + a.pairs, count[j], w);
                     }
                 }
-                store_n<T, V, STREAM>(to[j], v);
+                if constexpr (ROWS == kShort) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (e < count[j]) to[j][e] = T(v[e]);
+                } else {
+                    store_part<T, V, ROWS, STREAM>(to[j], count[j], v);
+                }
             }
         }
         __syncthreads();
     }
 }
 
-template <int DT, int V, bool MIXED>
+template <int DT, bool MIXED, int ROWS>
 void launch(const TurnArgs &a, hipStream_t stream) {
     const int64_t all = (a.tokens + a.tile - 1) / a.tile;
     const dim3 grid{uint32_t(all < kTurnGroups ? all : kTurnGroups)}, wg(kTurnBlock);
-    const size_t lds = size_t(a.tile) * a.pairs * sizeof(float2);
-    if (V > 2 && past_caches(a.tokens * a.heads * a.dim * dtype_bytes(DT)))
-        hipLaunchKernelGGL((k_turn<DT, V, MIXED, (V > 2)>), grid, wg, lds, stream, a);
+    // room for the angles that an uneven unit reads and does not use
+    const size_t lds = (size_t(a.tile) * a.pairs + kWide<DT>) * sizeof(float2);
+    // (not in halves: their accesses write parts of cache lines, which only a cache joins: 50000 x 8
+    // heads of 64 with 20 pairs, fp32, 81 us past the caches and 44 through them)
+    if (MIXED && ROWS == kEven && past_caches(a.tokens * a.heads * a.dim * dtype_bytes(DT)))
+        hipLaunchKernelGGL((k_turn<DT, MIXED, ROWS, MIXED && ROWS == kEven>), grid, wg, lds, stream, a);
     else
-        hipLaunchKernelGGL((k_turn<DT, V, MIXED, false>), grid, wg, lds, stream, a);
-}
-
-template <int DT, int V>
-void launch(const TurnArgs &a, bool mixed, hipStream_t stream) {
-    if (mixed) launch<DT, V, true>(a, stream);
-    else launch<DT, V, false>(a, stream);
-}
-
-template <int DT>
-void launch(const TurnArgs &a, int v, bool mixed, hipStream_t stream) {
-    constexpr int kWide = DT == BEVPOOL_F32 ? 4 : 8;
-    if (v == kWide) launch<DT, kWide>(a, mixed, stream);
-    else if (v == 2) launch<DT, 2>(a, mixed, stream);
-    else launch<DT, 1>(a, mixed, stream);
+        hipLaunchKernelGGL((k_turn<DT, MIXED, ROWS, false>), grid, wg, lds, stream, a);
 }
 
 }  // namespace
@@ -186,20 +189,18 @@ int bevmap_launch_rotary(const bevmap_turn &n, const void *x, const void *positi
     a.amplitude = n.amplitude;
     a.sign = backward ? -1.0f : 1.0f;
     const bool mixed = n.interleaved != 0;
-    int v = 1;
-    for (int wide : {n.dtype == BEVPOOL_F32 ? 4 : 8, 2}) {
-        const bool fits = n.dim % wide == 0 && (mixed ? 2 * n.pairs : n.pairs) % wide == 0 &&
-                          aligned_for(x, n.heads > 1 ? n.x_head : 0, n.dtype, wide) &&
-                          aligned_for(x, n.tokens > 1 ? n.x_row : 0, n.dtype, wide) &&
-                          aligned_for(x, n.batch > 1 ? n.x_batch : 0, n.dtype, wide) &&
-                          aligned_for(out, 0, n.dtype, wide);
-        if (fits) {
-            v = wide;
-            break;
-        }
-    }
-    const int each = mixed ? (v > 1 ? v / 2 : 1) : v;
-    const int units = n.pairs / each + (n.dim - 2 * n.pairs) / v;
+    int v = n.dtype == BEVPOOL_F32 ? 4 : 8;
+    const int part = mixed ? 2 * n.pairs : n.pairs, rest = n.dim - 2 * n.pairs;     // what is read as a row
+    const bool even = rest % v == 0 && part % v == 0 && aligned_for(x, n.heads > 1 ? n.x_head : 0, n.dtype, v) &&
+                      aligned_for(x, n.tokens > 1 ? n.x_row : 0, n.dtype, v) &&
+                      aligned_for(x, n.batch > 1 ? n.x_batch : 0, n.dtype, v) && aligned_for(out, 0, n.dtype, v);
+    // Pair by pair where an access is longer than a row, and where few accesses of a half are whole
+    // (129600 x 4 x 32 with 15 pairs in halves: bf16 26 us against 34, fp32 27 against 36; 42 of
+    // 84 channels: bf16 24 by wide accesses).
+    const bool few = !mixed && (n.dtype == BEVPOOL_F32 || part < 2 * v);
+    const int lie = even ? kEven : part < v || few ? kShort : kUneven;
+    if (lie == kShort) v = mixed ? 2 : 1;
+    const int each = mixed ? v / 2 : v, units = (n.pairs + each - 1) / each + (rest + v - 1) / v;
     // Tokens of a tile: a unit and a pair to every thread, less where that leaves compute units
     // without work. (129600 tokens, 4 heads of 32: 36 us a step; two units to a thread 44, four 52.)
     auto per = [](int64_t of, int64_t each) { return (of + each - 1) / each; };
@@ -214,9 +215,11 @@ int bevmap_launch_rotary(const bevmap_turn &n, const void *x, const void *positi
     a.by_axis = bevpool::make_fastdiv(uint32_t(n.pairs / n.axes));
     a.by_head = bevpool::make_fastdiv(uint32_t(n.heads));
     a.by_units = bevpool::make_fastdiv(uint32_t(units));
-    if (n.dtype == BEVPOOL_F32) launch<BEVPOOL_F32>(a, v, mixed, stream);
-    else if (n.dtype == BEVPOOL_BF16) launch<BEVPOOL_BF16>(a, v, mixed, stream);
-    else launch<BEVPOOL_F16>(a, v, mixed, stream);
+    with_type_and_rows(n.dtype, lie, [&](auto dt, auto how) {
+        constexpr int DT = decltype(dt)::value, ROWS = decltype(how)::value;
+        if (mixed) launch<DT, true, ROWS>(a, stream);
+        else launch<DT, false, ROWS>(a, stream);
+    });
     BEVPOOL_HIP(hipGetLastError());
     return BEVPOOL_OK;
 }
