@@ -122,6 +122,13 @@ RMS_CASES = [
     ((5, 8192), 0, True, "f32", "f32", "f32"),              # the most channels
     ((5, 8190), 0, True, "f16", "f16", "f32"),
     ((3, 8191), 2, False, "bf16", "bf16", "f32"),
+    # rows shorter than an access, and of one and a bit
+    ((50, 5), 0, True, "bf16", "f32", "f32"),
+    ((2000, 3), 1, True, "f32", "bf16", "bf16"),
+    ((1500, 9), 0, True, "f16", "f32", "f32"),
+    ((70, 5), 0, False, "f32", "f16", "f32"),
+    ((1025, 100), 0, True, "bf16", "bf16", "f32"),
+    ((1024, 2047), 3, True, "f16", "f32", "bf16"),
 ]
 
 
@@ -342,6 +349,57 @@ def test_linear_int8_leaves_the_rest_alone(torch, bev):
         y = bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32)
         assert torch.equal(buffer[17:17 + rows * features].view(rows, features), y)
         assert (buffer[:17] == 7).all() and (buffer[17 + rows * features:] == 7).all()
+
+
+def test_uneven_results_leave_the_rest_alone(torch, bev):
+    """Through the C ABI, rows of sizes that divide nothing into the middle of buffers, at odd addresses."""
+    mb = bev._map_binding
+    normal = _normal(torch, 8)
+    for rows, C in ((7, 5), (33, 331), (9, 1027), (5, 77)):
+        x, r, w = normal(rows, C).bfloat16(), normal(rows, C).bfloat16(), normal(C)
+        out = [torch.full((rows * n + 64,), 7, device="cuda", dtype=t)
+               for n, t in ((C, torch.bfloat16), (C, torch.bfloat16), (C, torch.int8), (C, torch.bfloat16), (C, torch.float32))]
+        total, y, held, dx, wide = out
+        scale = torch.empty(rows, device="cuda")
+        at = [t.data_ptr() + 17 * t.element_size() for t in out]
+        n = mb.bevmap_rms(rows, C, 1, 1, 0, C, C, 1e-6)
+        rstd = torch.empty(rows, device="cuda")
+        mb.bevmap_rms_norm(n, x.data_ptr(), r.data_ptr(), w.data_ptr(), at[0], at[1], rstd.data_ptr())
+        mb.bevmap_rms_norm_int8(n, x.data_ptr(), 0, w.data_ptr(), 0, at[2], scale.data_ptr())
+        mb.bevmap_rms_norm_backward(n, r.data_ptr(), 0, x.data_ptr(), 0, w.data_ptr(), rstd.data_ptr(), at[3], 0, 0, 0)
+        n = mb.bevmap_rms(rows, C, 1, 0, 0, C, C, 1e-6)
+        mb.bevmap_rms_norm(n, x.data_ptr(), 0, w.data_ptr(), 0, at[4], 0)
+        torch.cuda.synchronize()
+        ref = [*reversed(bev.rms_norm_add(x, r, w)), bev.rms_norm_int8(x, w)[0], None,
+               bev.rms_norm(x, w, out_dtype=torch.float32)]
+        for t, expect in zip(out, ref):
+            assert (t[:17] == 7).all() and (t[17 + rows * C:] == 7).all(), (rows, C)
+            assert expect is None or torch.equal(t[17:17 + rows * C].view(rows, C), expect), (rows, C)
+    for rows, F in ((9, 3), (21, 65), (5, 331)):
+        x, dy = normal(rows, 2 * F).half(), normal(rows, F).half()
+        y, dx = (torch.full((rows * n + 64,), 7.0, device="cuda", dtype=torch.float16) for n in (F, 2 * F))
+        held = torch.full((rows * 2 * F + 64,), 7, device="cuda", dtype=torch.int8)
+        e = torch.full((rows * 2 * -(-F // 32) + 64,), 7, device="cuda", dtype=torch.uint8)
+        g = mb.bevmap_gate(rows, F, 2, 2, 2 * F)
+        mb.bevmap_gated_act(g, x.data_ptr(), y.data_ptr() + 34, held.data_ptr() + 17, e.data_ptr() + 17)
+        mb.bevmap_gated_act_backward(g, dy.data_ptr(), 0, held.data_ptr() + 17, e.data_ptr() + 17, dx.data_ptr() + 34)
+        torch.cuda.synchronize()
+        leaf = x.clone().requires_grad_()
+        ref = bev.gated_act(leaf, "silu", "int8")
+        grad, = torch.autograd.grad(ref, leaf, dy)
+        for t, n, expect in ((y, F, ref), (dx, 2 * F, grad), (held, 2 * F, None), (e, 2 * -(-F // 32), None)):
+            assert (t[:17] == 7).all() and (t[17 + rows * n:] == 7).all(), (rows, F)
+            assert expect is None or torch.equal(t[17:17 + rows * n].view(rows, n), expect), (rows, F)
+    for tokens, H, D, P, mixed in ((5, 3, 31, 15, 0), (5, 3, 31, 15, 1), (7, 1, 84, 42, 0), (7, 2, 9, 4, 1), (7, 2, 9, 4, 0),
+                                   (3, 3, 45, 20, 0)):
+        x = normal(1, tokens, H, D).bfloat16()
+        f, place = bev.rotary_frequencies(P, device="cuda"), torch.arange(tokens, device="cuda")[None]
+        out = torch.full((x.numel() + 64,), 7.0, device="cuda", dtype=torch.bfloat16)
+        mb.bevmap_rotary(mb.bevmap_turn(1, tokens, H, D, P, 1, mixed, 1, 1, 1.0, 0, H * D, D), x.data_ptr(),
+                         place.data_ptr(), f.data_ptr(), out.data_ptr() + 34, False)
+        torch.cuda.synchronize()
+        assert (out[:17] == 7).all() and (out[17 + x.numel():] == 7).all(), (D, P)
+        assert torch.equal(out[17:17 + x.numel()].view_as(x), bev.rotary(x, place, f, bool(mixed))), (D, P)
 
 
 # ---------------------------------------------------------------- rotary positions
