@@ -12,7 +12,9 @@
 // Two forms. Tiles: a workgroup stages kStep bytes of its rows and channels in LDS, two
 // stages in turn, the next on its way (past the registers, where rows are 16-byte
 // aligned) while the matrix cores work: 16896 x 2048 x 4096 (tokens, k, channels) takes 158
-// to 172 us, 8192^3 531, 2070 TOP/s (a library product without scales 171 and 541). Few
+// to 172 us, 8192^3 531, 2070 TOP/s (a library product without scales 171 and 541). Rows of
+// any other alignment go through the registers, with no branch of a lane's own on the way, so
+// that all loads of a stage are under way at a time: 16390 x 1025 x 1021 takes 49 us. Few
 // tokens: the weights are what is read, so a workgroup takes 16 channels, its waves share out
 // k and join their sums in LDS: 64 x 4096 x 2048 takes 5.1 us.
 #include "mapops.h"
@@ -39,30 +41,32 @@ struct LinearArgs {
 
 __device__ const uint4 kNothing = {0, 0, 0, 0};     // what lies past the end of k
 
-// 16 bytes of a row of K from k on, zeros past its end; any alignment.
+// 16 bytes of a row of K from k on, at any alignment; where the row ends before them, its
+// last 16 (all of a row shorter than that, and zeros), which settle_chunk then moves.
 __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int K) {
     i32x4 v = {0, 0, 0, 0};
-    if (k + 16 <= K) {
-        __builtin_memcpy(&v, row + k, 16);
-    } else if (k < K && K >= 16) {
-        // the row's last 16 bytes, moved down by those before k
-        uint64_t part[2];
-        __builtin_memcpy(part, row + K - 16, 16);
-        const int down = 8 * (16 - (K - k));
-        if (down >= 64) {
-            part[0] = part[1] >> (down - 64);
-            part[1] = 0;
-        } else {
-            part[0] = part[0] >> down | part[1] << (64 - down);
-            part[1] >>= down;
-        }
-        __builtin_memcpy(&v, part, 16);
-    } else if (k < K) {
+    if (K >= 16) {
+        __builtin_memcpy(&v, row + min(k, K - 16), 16);
+    } else {
         int8_t b[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) b[i] = k + i < K ? row[k + i] : int8_t(0);
+        for (int i = 0; i < 16; ++i) b[i] = i < K ? row[i] : int8_t(0);
         __builtin_memcpy(&v, b, 16);
     }
+    return v;
+}
+// What load_chunk brought, moved down by the bytes before k, zeros behind it.
+__device__ __forceinline__ i32x4 settle_chunk(i32x4 v, int k, int K) {
+    const int down = 8 * (k - max(K - 16, 0));
+    if (down <= 0) return v;
+    uint64_t part[2];
+    __builtin_memcpy(part, &v, 16);
+    const bool far = down >= 64;
+    const uint64_t low = far ? part[1] : part[0], high = far ? 0 : part[1];
+    const int by = down % 64;
+    part[0] = down >= 128 ? 0 : low >> by | high << 1 << (63 - by);
+    part[1] = high >> by;
+    __builtin_memcpy(&v, part, 16);
     return v;
 }
 
@@ -153,11 +157,15 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs &a, char *lds, in
             for (int i = i0; i < i1; ++i) held[i] = load_chunk(from[i], k, a.K);
         }
     };
-    auto place_held = [&](char *stage) {
-        if constexpr (!DIRECT)
+    auto place_held = [&](int step, char *stage) {
+        if constexpr (!DIRECT) {
+            if ((step + 1) * kStep > a.K)
+#pragma unroll
+                for (int i = 0; i < G::kLoads; ++i) held[i] = settle_chunk(held[i], step * kStep + k_at, a.K);
 #pragma unroll
             for (int i = 0; i < G::kLoads; ++i)
                 *reinterpret_cast<i32x4 *>(stage + (i * G::kThreads + tid) * 16) = held[i];
+        }
     };
 
     const int wm = wave % MW, wn = wave / MW, half = lane / 32, col = lane % 32;
@@ -204,7 +212,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs &a, char *lds, in
         ws[i] = a.w_scale[n];
         bias[i] = a.bias ? a.bias[n] : 0.0f;
     }
-    place_held(stages);
+    place_held(0, stages);
     __syncthreads();
     read(stages, 0, set[0]);
     if (steps > 1) fetch(1, stages + G::kStage, 0, G::kLoads);
@@ -216,7 +224,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs &a, char *lds, in
                 if (i == 0) read(now, k + 1, set[(k + 1) & 1]);
             });
         // all that this stage holds is in registers: the one after next may overwrite it
-        place_held(next);
+        place_held(s + 1, next);
         __syncthreads();
         multiply(set[(kQuarters - 1) & 1], [&](int i) {
             if (i == 0) read(next, 0, set[0]);
@@ -382,6 +390,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearArgs a) {
     for (int j = 0; j < MB; ++j) acc[j] = i32x4{0, 0, 0, 0};
     fetch(wave * kRun);
     for (int first = wave * kRun; first < a.K; first += WAVES * kRun) {
+        if (!DIRECT && first + kRun > a.K)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) way[b][h] = settle_chunk(way[b][h], first + 16 * chunk, a.K);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -476,7 +489,12 @@ int launch(const LinearArgs &a, hipStream_t stream) {
     const bool eighths = big >= kUnits && left > 0 && left <= kUnits / 4;
     const double big_time = double(big / kUnits) + (left == 0 ? 0.0 : eighths ? 0.27 * double((8 * left + kUnits - 1) / kUnits) : 1.0);
     const double small_time = 0.58 * double((tiles(128, 128) + 2 * kUnits - 1) / (2 * kUnits));
-    if (a.K < 512 || small_time < big_time) return launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream);
+    // Rows that go through the registers: 128 x 64 by eight waves, whose stores of single
+    // channels overlap better than those of four (33000 x 509, K 443: 35.6 against 40.2 us;
+    // with aligned rows, 33000 x 512, K 448, 21.9 against 21.7).
+    if (a.K < 512 || small_time < big_time)
+        return DIRECT ? launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream)
+                      : launch_tiles<4, 2, 1, 1, 128, DIRECT>(a, stream);
     return eighths ? launch_eighths<DIRECT>(a, int(left), stream) : launch_tiles<4, 2, 2, 4, 128, DIRECT>(a, stream);
 }
 

@@ -292,6 +292,9 @@ LINEAR_CASES = [
     (16, 7, 40, 0, 0, True, "f32"),
     (700, 2000, 777, 0, 0, True, "f32"),        # tiles of 64, a k that divides nothing
     (2500, 300, 1100, 0, 0, False, "bf16"),
+    (33000, 443, 509, 0, 0, True, "bf16"),      # 128 x 64 of rows that go through the registers
+    (16400, 715, 1001, 0, 1, True, "f16"),
+    (2100, 9, 2000, 0, 0, True, "f32"),         # rows shorter than an access, in tiles of 128 x 64
 ]
 
 
@@ -308,6 +311,20 @@ def test_linear_int8(torch, bev, rows, channels, features, left, w_left, bias, y
     ref = product + b.double() if bias else product
     _check("y", y, ref, 3 * U32 * product.abs() + (U32 + _u(y_type)) * ref.abs() + _tiny(y_type))
     assert torch.equal(y, bev.linear_int8(x, xs, w, ws, b, out_dtype=_dtype(torch, y_type)))
+
+
+@pytest.mark.parametrize("rows,features", [(16400, 1001), (16384, 1024), (3000, 2000), (700, 1000), (60, 400)])
+@pytest.mark.parametrize("channels", [530, 545, 560, 592, 597, 607, 624, 637, 715, 720, 331, 333])
+def test_linear_int8_ends_of_k(torch, bev, rows, features, channels):
+    """k that ends in every quarter of a stage, in rows of any alignment, for every form; and
+    the same again and again."""
+    x, xs = _held(torch, 6, rows, channels)
+    w, ws = _held(torch, 7, features, channels)
+    y = bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32)
+    ref = (x.double() @ w.double().t().contiguous()) * xs.double()[:, None] * ws.double()
+    _check("y", y, ref, 3 * U32 * ref.abs())
+    for _ in range(5):
+        assert torch.equal(y, bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32))
 
 
 def test_linear_int8_of_the_largest_sums(torch, bev):
