@@ -65,7 +65,10 @@ template <class... Ts>
 void one_device(const Tensor &first, const Ts &...others) {
     if (!first.is_cuda()) refuse("inputs must be device tensors");
     for (const Tensor *t : {&others..., &first})
-        if (t->defined() && t->device() != first.device()) refuse("all tensors must be on one device");
+        if (t->defined()) {
+            if (t->device() != first.device()) refuse("all tensors must be on one device");
+            if (t->is_neg()) refuse("a view that negates what lies in memory: resolve_neg() first");
+        }
 }
 
 // Whether a gradient is asked for through a call on these; a tangent among them ends it.
@@ -138,6 +141,8 @@ void check_vector(const Tensor &t, int64_t n, const char *name) {
 void first_order_only() {
     if (c10::GradMode::is_enabled()) throw std::runtime_error("the map operators have no second derivatives");
 }
+
+Tensor whole(const Tensor &gradient) { return gradient.resolve_neg().contiguous(); }
 
 // A description kept from a forward for its backward.
 template <class T>
@@ -231,12 +236,12 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
             const variable_list saved = ctx->get_saved_variables();
             const Tensor &x = saved[0], &residual = saved[1], &weight = saved[2], &rstd = saved[3];
             const bool want = ctx->saved_data["w"].toBool(), added = grads.size() > 1;
-            const Tensor dtotal = added && grads[1].defined() ? grads[1].contiguous() : Tensor();
+            const Tensor dtotal = added && grads[1].defined() ? whole(grads[1]) : Tensor();
             if (!grads[0].defined())        // y was not used: the gradient of a sum
                 return {dtotal, dtotal, want ? at::zeros_like(weight) : Tensor(), Tensor(), Tensor()};
             const On on(x);
             const bevmap_rms n = kept<bevmap_rms>(ctx);
-            const Tensor dy = grads[0].contiguous();
+            const Tensor dy = whole(grads[0]);
             const Tensor dx = empty(x.sizes(), x.scalar_type(), x);
             Tensor dw, space;
             int64_t size = 0;
@@ -386,7 +391,7 @@ struct Rotary : torch::autograd::Function<Rotary> {
     static variable_list backward(AutogradContext *ctx, variable_list grads) {
         return in_backward([&]() -> variable_list {
             const variable_list saved = ctx->get_saved_variables();
-            const Tensor dy = grads[0].stride(3) == 1 ? grads[0] : grads[0].contiguous();
+            const Tensor dy = grads[0].stride(3) == 1 ? grads[0].resolve_neg() : whole(grads[0]);
             return {turn(kept<bevmap_turn>(ctx), dy, saved[0], saved[1], true), Tensor(), Tensor(), Tensor(), Tensor()};
         });
     }
@@ -442,7 +447,7 @@ struct GatedAct : torch::autograd::Function<GatedAct> {
         return in_backward([&]() -> variable_list {
             const variable_list saved = ctx->get_saved_variables();
             const bevmap_gate n = kept<bevmap_gate>(ctx);
-            const Tensor dy = grads[0].contiguous();
+            const Tensor dy = whole(grads[0]);
             const On on(dy);
             at::DimVector sizes(dy.sizes());
             sizes.back() = 2 * int64_t(n.features);

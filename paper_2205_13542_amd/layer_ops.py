@@ -16,6 +16,10 @@ the current stream of its inputs' device, with temporaries from torch's allocato
 and with tensors elsewhere, types and layouts that a call does not take refused
 with a BevpoolError. Checks, allocations and autograd nodes are native too
 (csrc/layer_torch.cpp): a call on a few rows costs its host time.
+
+All of them may be captured into a graph. Before a training step is, let go of what
+earlier eager steps on the same leaves returned: while such a result lives, torch
+forms the leaves' gradients on that step's stream, which a capture must not enter.
 """
 from __future__ import annotations
 

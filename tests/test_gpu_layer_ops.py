@@ -882,6 +882,24 @@ def test_empty_inputs(torch, bev):
     assert bev.rms_norm_int8(x.detach())[0].shape == (0, 8) and bev.quantize_int8(x.detach())[1].shape == (0,)
 
 
+def test_views_that_negate(torch, bev):
+    """A view that negates what lies in memory is refused as an input and resolved as a gradient."""
+    x, dy = _normal(torch, 1)(6, 16), _normal(torch, 2)(6, 16)
+    place, f = torch.arange(6, device="cuda")[None], bev.rotary_frequencies(4, device="cuda")
+    calls = [bev.rms_norm, lambda t: bev.rms_norm_add(t, t)[1],
+             lambda t: bev.gated_act(torch.cat((t, t), -1), checkpoint="int8"),
+             lambda t: bev.rotary(t.view(1, 6, 1, 16), place, f).view(6, 16)]
+    for call in calls:
+        leaf = x.clone().requires_grad_()
+        got, = torch.autograd.grad(call(leaf), leaf, torch._neg_view(dy))
+        ref, = torch.autograd.grad(call(leaf), leaf, -dy)
+        assert torch.equal(got, ref)
+    for call in (bev.rms_norm, bev.quantize_int8, bev.gated_act,
+                 lambda t: bev.rotary(t.view(1, 6, 1, 16), place, f), lambda t: bev.rms_norm(x, t[0])):
+        with pytest.raises(bev.BevpoolError, match="resolve_neg"):
+            call(torch._neg_view(x))
+
+
 def test_refusals(torch, bev):
     x = torch.zeros(6, 5, 8, device="cuda")
     q, s = torch.zeros(6, 8, dtype=torch.int8, device="cuda"), torch.ones(6, device="cuda")
