@@ -14,7 +14,7 @@
 // aligned) while the matrix cores work: 16896 x 2048 x 4096 (tokens, k, channels) takes 158
 // to 172 us, 8192^3 531, 2070 TOP/s (a library product without scales 171 and 541). Rows of
 // any other alignment go through the registers, with no branch of a lane's own on the way, so
-// that all loads of a stage are under way at a time: 16390 x 1025 x 1021 takes 49 us. Few
+// that all loads of a stage are under way at a time: 16390 x 1025 x 1021 takes 42 us. Few
 // tokens: the weights are what is read, so a workgroup takes 16 channels, its waves share out
 // k and join their sums in LDS: 64 x 4096 x 2048 takes 5.1 us.
 #include "mapops.h"
@@ -36,7 +36,7 @@ struct LinearArgs {
     int64_t ldx, ldw;
     int32_t M, N, K;
     int32_t m_tiles, n_tiles, y_dtype;
-    bool wide;                          // rows of y can be written 16 bytes at a time
+    bool wide;                          // rows of y lie at 16 bytes, in whole accesses
 };
 
 __device__ const uint4 kNothing = {0, 0, 0, 0};     // what lies past the end of k
@@ -273,30 +273,19 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs &a, char *lds, in
         with_dtype(a.y_dtype, [&](auto dt) {
             using T = typename Num<decltype(dt)::value>::T;
             T *y = static_cast<T *>(a.y);
-            if (a.wide) {
-                const int n = nw + mine_at;
+            const int n = nw + mine_at;
 #pragma unroll 4
-                for (int r = lane / kPer; r < 32; r += 64 / kPer) {
-                    const i32x4 *p = reinterpret_cast<const i32x4 *>(mine + r * G::kOutPitch + mine_at * 4);
-                    const i32x4 low = p[0], high = p[1];
-                    const float scale = xs[mw + j * 32 + r];
-                    float v[8];
+            for (int r = lane / kPer; r < 32; r += 64 / kPer) {
+                const i32x4 *p = reinterpret_cast<const i32x4 *>(mine + r * G::kOutPitch + mine_at * 4);
+                const i32x4 low = p[0], high = p[1];
+                const float scale = xs[mw + j * 32 + r];
+                float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = scaled(e < 4 ? low[e] : high[e - 4], scale, w_scale[e], b[e]);
-                    if (m_first + r < a.M && n < a.N) store_n<T, 8>(y + int64_t(m_first + r) * a.N + n, v);
-                }
-                return;
-            }
-            constexpr int kAcross = kCols < 64 ? kCols : 64;    // lanes of a row, a channel each
-#pragma unroll
-            for (int c = lane % kAcross; c < kCols; c += kAcross) {
-                const float one = ws[wn * kCols + c], add = bias[wn * kCols + c];
-#pragma unroll 4
-                for (int r = lane / kAcross; r < 32; r += 64 / kAcross) {
-                    const int32_t sum = *reinterpret_cast<const int32_t *>(mine + r * G::kOutPitch + c * 4);
-                    if (m_first + r < a.M && nw + c < a.N)
-                        y[int64_t(m_first + r) * a.N + nw + c] = T(scaled(sum, xs[mw + j * 32 + r], one, add));
-                }
+                for (int e = 0; e < 8; ++e) v[e] = scaled(e < 4 ? low[e] : high[e - 4], scale, w_scale[e], b[e]);
+                if (m_first + r >= a.M || n >= a.N) continue;
+                T *to = y + int64_t(m_first + r) * a.N + n;
+                if (a.wide) store_n<T, 8>(to, v);
+                else store_part<T, 8, kUneven>(to, a.N - n, v);
             }
         });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -489,12 +478,12 @@ int launch(const LinearArgs &a, hipStream_t stream) {
     const bool eighths = big >= kUnits && left > 0 && left <= kUnits / 4;
     const double big_time = double(big / kUnits) + (left == 0 ? 0.0 : eighths ? 0.27 * double((8 * left + kUnits - 1) / kUnits) : 1.0);
     const double small_time = 0.58 * double((tiles(128, 128) + 2 * kUnits - 1) / (2 * kUnits));
-    // Rows that go through the registers: 128 x 64 by eight waves, whose stores of single
-    // channels overlap better than those of four (33000 x 509, K 443: 35.6 against 40.2 us;
-    // with aligned rows, 33000 x 512, K 448, 21.9 against 21.7).
-    if (a.K < 512 || small_time < big_time)
-        return DIRECT ? launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream)
-                      : launch_tiles<4, 2, 1, 1, 128, DIRECT>(a, stream);
+    // Short rows that go through the registers: 128 x 64 by eight waves (100000 x 250, K 120:
+    // 19.2 us against 20.6 by 128 x 128; 3000 x 2000, K 331: 11.6 against 12.7; 33000 x 509, K
+    // 443: 33.3 against 31.5).
+    if constexpr (!DIRECT)
+        if (a.K <= 384) return launch_tiles<4, 2, 1, 1, 128, DIRECT>(a, stream);
+    if (a.K < 512 || small_time < big_time) return launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream);
     return eighths ? launch_eighths<DIRECT>(a, int(left), stream) : launch_tiles<4, 2, 2, 4, 128, DIRECT>(a, stream);
 }
 

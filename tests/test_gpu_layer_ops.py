@@ -292,8 +292,17 @@ LINEAR_CASES = [
     (16, 7, 40, 0, 0, True, "f32"),
     (700, 2000, 777, 0, 0, True, "f32"),        # tiles of 64, a k that divides nothing
     (2500, 300, 1100, 0, 0, False, "bf16"),
-    (33000, 443, 509, 0, 0, True, "bf16"),      # 128 x 64 of rows that go through the registers
+    (33000, 443, 509, 0, 0, True, "bf16"),      # 128 x 128 and 128 x 64 of rows that go through the registers
+    (33000, 203, 509, 0, 0, True, "f16"),
+    (16400, 512, 1001, 0, 0, True, "f16"),      # rows of y at any alignment, the last of it in part
+    (16400, 512, 1023, 0, 0, False, "f32"),
+    (9000, 300, 1026, 0, 0, False, "f32"),
+    (4100, 80, 1027, 0, 0, True, "bf16"),
+    (700, 80, 1005, 0, 0, True, "bf16"),
     (16400, 715, 1001, 0, 1, True, "f16"),
+    (40000, 64, 7, 0, 0, True, "bf16"),         # rows of y shorter than an access
+    (140000, 64, 3, 0, 0, True, "f32"),
+    (70000, 33, 1, 0, 0, False, "f16"),
     (2100, 9, 2000, 0, 0, True, "f32"),         # rows shorter than an access, in tiles of 128 x 64
 ]
 
@@ -364,6 +373,22 @@ def test_linear_int8_leaves_the_rest_alone(torch, bev):
                               xs.data_ptr(), w.data_ptr(), ws.data_ptr(), 0, buffer.data_ptr() + 4 * 17)
         torch.cuda.synchronize()
         y = bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32)
+        assert torch.equal(buffer[17:17 + rows * features].view(rows, features), y)
+        assert (buffer[:17] == 7).all() and (buffer[17 + rows * features:] == 7).all()
+
+
+def test_linear_int8_of_uneven_rows_leaves_the_rest_alone(torch, bev):
+    """The same of 16-bit rows of any length at odd addresses, in every size of tile."""
+    mb = bev._map_binding
+    for rows, channels, features in ((16400, 512, 1001), (33000, 100, 259), (1111, 64, 517), (8300, 64, 1035), (40000, 64, 7)):
+        x, xs = _held(torch, 6, rows, channels)
+        w, ws = _held(torch, 7, features, channels)
+        ws = ws * 2.0 ** -10
+        buffer = torch.full((rows * features + 64,), 7.0, device="cuda", dtype=torch.bfloat16)
+        mb.bevmap_linear_int8(mb.bevmap_linear(rows, channels, features, channels, channels, 1), x.data_ptr(),
+                              xs.data_ptr(), w.data_ptr(), ws.data_ptr(), 0, buffer.data_ptr() + 2 * 17)
+        torch.cuda.synchronize()
+        y = bev.linear_int8(x, xs, w, ws)
         assert torch.equal(buffer[17:17 + rows * features].view(rows, features), y)
         assert (buffer[:17] == 7).all() and (buffer[17 + rows * features:] == 7).all()
 
