@@ -896,6 +896,21 @@ def test_serving_in_two_graphs(torch, bev):
             assert all(torch.equal(a, r) for a, r in zip(out, ref)), f"replay {i}"
 
 
+@pytest.mark.parametrize("rows,channels,features", [(16500, 592, 1000), (16390, 597, 1021), (4096, 80, 2056),
+                                                    (3000, 331, 2000), (700, 2000, 777), (60, 400, 400)])
+def test_linear_int8_in_a_graph(torch, bev, rows, channels, features):
+    """Every size of tile, first called while it is captured."""
+    x, xs = _held(torch, 8, rows, channels)
+    w, ws = _held(torch, 9, features, channels)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32)
+    for i in range(3):
+        x.copy_(_held(torch, 10 + i, rows, channels)[0])
+        graph.replay()
+        assert torch.equal(y, bev.linear_int8(x, xs, w, ws, out_dtype=torch.float32)), f"replay {i}"
+
+
 def test_empty_inputs(torch, bev):
     x = torch.zeros(0, 8, device="cuda", requires_grad=True)
     w = torch.ones(8, device="cuda", requires_grad=True)
