@@ -54,6 +54,10 @@ int code_of(at::ScalarType type) {
     refuse(c10::str("dtype ", type), BEVPOOL_ERR_UNSUPPORTED_DTYPE);
 }
 
+at::ScalarType type_of(int32_t code) {
+    return code == BEVPOOL_F32 ? at::kFloat : code == BEVPOOL_BF16 ? at::kBFloat16 : at::kHalf;
+}
+
 void done(int64_t rc) {
     if (rc < 0) throw Refused{int(rc), bevpool_last_error()};
 }
@@ -107,28 +111,31 @@ struct Rows {
     int64_t rows, columns, stride;
 };
 
-// Rows, columns and the row stride of t, its last dimension the columns: rows must be
+// Rows, columns and the row stride of t, its last dimension the columns; whether rows are
 // evenly spaced and their elements adjacent.
-Rows rows_of(const Tensor &t, const char *name) {
+bool even_rows(const Tensor &t, Rows &r) {
     const int64_t dims = t.dim();
-    if (dims < 1) refuse(c10::str(name, " must have a channel dimension"), BEVPOOL_ERR_SHAPE_MISMATCH);
-    Rows r{1, t.size(-1), t.size(-1)};
+    r = {1, t.size(-1), t.size(-1)};
     for (int64_t i = 0; i + 1 < dims; ++i) r.rows *= t.size(i);
-    if (!t.is_contiguous()) {
-        bool even = t.stride(-1) == 1 || r.columns <= 1;
-        int64_t step = -1, expect = 0;
-        for (int64_t i = dims - 2; even && i >= 0; --i) {
-            if (t.size(i) == 1) continue;
-            if (step < 0) step = t.stride(i);
-            else even = t.stride(i) == expect;
-            expect = t.stride(i) * t.size(i);
-        }
-        if (step >= 0) {
-            even = even && step >= r.columns;
-            r.stride = step;
-        }
-        if (!even) refuse(c10::str("rows of ", name, " must be evenly spaced, their channels adjacent"));
+    if (t.is_contiguous()) return true;
+    bool even = t.stride(-1) == 1 || r.columns <= 1;
+    int64_t step = -1, expect = 0;
+    for (int64_t i = dims - 2; even && i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (step < 0) step = t.stride(i);
+        else even = t.stride(i) == expect;
+        expect = t.stride(i) * t.size(i);
     }
+    if (step >= 0) {
+        even = even && step >= r.columns;
+        r.stride = step;
+    }
+    return even;
+}
+Rows rows_of(const Tensor &t, const char *name) {
+    if (t.dim() < 1) refuse(c10::str(name, " must have a channel dimension"), BEVPOOL_ERR_SHAPE_MISMATCH);
+    Rows r;
+    if (!even_rows(t, r)) refuse(c10::str("rows of ", name, " must be evenly spaced, their channels adjacent"));
     if (r.rows > kMost || r.columns > kMost) refuse(c10::str(name, " ", shape_of(t), ": too large"), BEVPOOL_ERR_OVERFLOW);
     return r;
 }
@@ -142,7 +149,8 @@ void first_order_only() {
     if (c10::GradMode::is_enabled()) throw std::runtime_error("the map operators have no second derivatives");
 }
 
-Tensor whole(const Tensor &gradient) { return gradient.resolve_neg().contiguous(); }
+// t, contiguous and as its memory says.
+Tensor whole(const Tensor &t) { return t.is_contiguous() && !t.is_neg() ? t : t.resolve_neg().contiguous(); }
 
 // A description kept from a forward for its backward.
 template <class T>
@@ -155,6 +163,24 @@ T kept(AutogradContext *ctx) {
     const std::string &bytes = ctx->saved_data["d"].toStringRef();
     memcpy(&description, bytes.data(), sizeof(T));
     return description;
+}
+
+// What a forward saved, as the backward gets it: a hook on saved tensors may have brought it
+// back with other strides, or as something else.
+[[noreturn]] void changed() { refuse("a saved tensor came back with another size, dtype or device", BEVPOOL_ERR_SHAPE_MISMATCH); }
+Tensor saved_whole(const Tensor &t, int64_t numel, at::ScalarType type, const Tensor &gradient) {
+    if (!t.defined()) return t;
+    if (t.numel() != numel || t.scalar_type() != type || t.device() != gradient.device()) changed();
+    return whole(t);
+}
+Tensor saved_rows(const Tensor &t, int64_t rows, int64_t columns, int32_t dtype, const Tensor &gradient, int64_t *stride) {
+    if (!t.defined()) return t;
+    Rows r;
+    if (t.dim() < 1 || t.device() != gradient.device() || code_of(t.scalar_type()) != dtype) changed();
+    const bool even = even_rows(t, r) && !t.is_neg();
+    if (r.rows != rows || r.columns != columns) changed();
+    *stride = even ? r.stride : columns;
+    return even ? t : whole(t);
 }
 
 // A refusal inside a backward, where no caller of ours catches it.
@@ -211,7 +237,7 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
     static variable_list forward(AutogradContext *ctx, const Tensor &x, const std::optional<Tensor> &maybe_residual,
                                  const std::optional<Tensor> &maybe_weight, double eps, int64_t out_type) {
         const Tensor residual = maybe_residual.value_or(Tensor()), weight = maybe_weight.value_or(Tensor());
-        bevmap_rms n = describe_rms(x, residual, weight, eps, at::ScalarType(out_type));
+        const bevmap_rms n = describe_rms(x, residual, weight, eps, at::ScalarType(out_type));
         const Normed r = rms_forward(n, x, residual, weight, at::ScalarType(out_type), true);
         ctx->set_materialize_grads(false);
         ctx->saved_data["w"] = weight.defined() && weight.requires_grad();
@@ -221,7 +247,6 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
             return {r.y};
         }
         if (x.scalar_type() == at::kFloat) {
-            n.x_stride = n.channels;
             ctx->save_for_backward({r.total, Tensor(), weight, r.rstd});
         } else {
             // the sum of 16-bit numbers, rounded, would take its rounding into the weight's gradient
@@ -234,14 +259,17 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
     static variable_list backward(AutogradContext *ctx, variable_list grads) {
         return in_backward([&]() -> variable_list {
             const variable_list saved = ctx->get_saved_variables();
-            const Tensor &x = saved[0], &residual = saved[1], &weight = saved[2], &rstd = saved[3];
             const bool want = ctx->saved_data["w"].toBool(), added = grads.size() > 1;
             const Tensor dtotal = added && grads[1].defined() ? whole(grads[1]) : Tensor();
             if (!grads[0].defined())        // y was not used: the gradient of a sum
-                return {dtotal, dtotal, want ? at::zeros_like(weight) : Tensor(), Tensor(), Tensor()};
-            const On on(x);
-            const bevmap_rms n = kept<bevmap_rms>(ctx);
+                return {dtotal, dtotal, want ? at::zeros_like(saved[2]) : Tensor(), Tensor(), Tensor()};
+            bevmap_rms n = kept<bevmap_rms>(ctx);
             const Tensor dy = whole(grads[0]);
+            const On on(dy);
+            const Tensor x = saved_rows(saved[0], n.rows, n.channels, n.x_dtype, dy, &n.x_stride);
+            const Tensor residual = saved_rows(saved[1], n.rows, n.channels, n.x_dtype, dy, &n.residual_stride);
+            const Tensor weight = saved_whole(saved[2], n.channels, type_of(n.weight_dtype), dy);
+            const Tensor rstd = saved_whole(saved[3], n.rows, at::kFloat, dy);
             const Tensor dx = empty(x.sizes(), x.scalar_type(), x);
             Tensor dw, space;
             int64_t size = 0;
@@ -392,7 +420,13 @@ struct Rotary : torch::autograd::Function<Rotary> {
         return in_backward([&]() -> variable_list {
             const variable_list saved = ctx->get_saved_variables();
             const Tensor dy = grads[0].stride(3) == 1 ? grads[0].resolve_neg() : whole(grads[0]);
-            return {turn(kept<bevmap_turn>(ctx), dy, saved[0], saved[1], true), Tensor(), Tensor(), Tensor(), Tensor()};
+            const bevmap_turn n = kept<bevmap_turn>(ctx);
+            const at::ScalarType type = n.positions_type == BEVMAP_POSITION_I32   ? at::kInt
+                                        : n.positions_type == BEVMAP_POSITION_I64 ? at::kLong
+                                                                                  : at::kFloat;
+            const Tensor positions = saved_whole(saved[0], int64_t(n.batch) * n.tokens * n.axes, type, dy);
+            const Tensor frequencies = saved_whole(saved[1], n.pairs, at::kDouble, dy);
+            return {turn(n, dy, positions, frequencies, true), Tensor(), Tensor(), Tensor(), Tensor()};
         });
     }
 };
@@ -446,14 +480,18 @@ struct GatedAct : torch::autograd::Function<GatedAct> {
     static variable_list backward(AutogradContext *ctx, variable_list grads) {
         return in_backward([&]() -> variable_list {
             const variable_list saved = ctx->get_saved_variables();
-            const bevmap_gate n = kept<bevmap_gate>(ctx);
+            bevmap_gate n = kept<bevmap_gate>(ctx);
             const Tensor dy = whole(grads[0]);
             const On on(dy);
+            const int64_t halves = n.rows * 2, blocks = (n.features + kHeldBlock - 1) / kHeldBlock;
+            const Tensor x = saved_rows(saved[0], n.rows, 2 * int64_t(n.features), n.dtype, dy, &n.x_stride);
+            const Tensor held = saved_whole(saved[1], halves * n.features, at::kChar, dy);
+            const Tensor exponents = saved_whole(saved[2], halves * blocks, at::kByte, dy);
             at::DimVector sizes(dy.sizes());
             sizes.back() = 2 * int64_t(n.features);
             const Tensor dx = empty(sizes, dy.scalar_type(), dy);
-            done(bevmap_gated_act_backward(&n, ptr(dy), ptr(saved[0]), static_cast<const int8_t *>(ptr(saved[1])),
-                                           static_cast<const uint8_t *>(ptr(saved[2])), out(dx), on.stream));
+            done(bevmap_gated_act_backward(&n, ptr(dy), ptr(x), static_cast<const int8_t *>(ptr(held)),
+                                           static_cast<const uint8_t *>(ptr(exponents)), out(dx), on.stream));
             return {dx, Tensor(), Tensor()};
         });
     }

@@ -922,6 +922,64 @@ def test_empty_inputs(torch, bev):
     assert bev.rms_norm_int8(x.detach())[0].shape == (0, 8) and bev.quantize_int8(x.detach())[1].shape == (0,)
 
 
+def test_hooks_on_saved_tensors(torch, bev):
+    """Saved tensors that come back with other strides, from the host or another layout, give
+    the same gradients; another size or dtype is refused."""
+    normal = _normal(torch, 3)
+    place = torch.arange(20, device="cuda").view(2, 10)
+    f = bev.rotary_frequencies(3, device="cuda")
+    w = normal(24)
+    packed = normal(20, 3 * 24)
+    wide = packed[:, 24:48]                          # rows 72 elements apart
+    half = packed.bfloat16()[:, 24:48]
+
+    def spread(t):                                   # each row followed by a row of something else
+        if t.dim() != 2:
+            return t
+        room = torch.full((t.shape[0], 2 * t.shape[1]), 9, dtype=t.dtype, device=t.device)
+        room[:, ::2] = t
+        return room[:, ::2]
+
+    hooks = [
+        lambda: torch.autograd.graph.save_on_cpu(),
+        lambda: torch.autograd.graph.saved_tensors_hooks(spread, lambda t: t),
+        lambda: torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.clone(memory_format=torch.contiguous_format)),
+    ]
+    calls = [
+        (lambda x, w: bev.rms_norm(x, w), wide),
+        (lambda x, w: bev.rms_norm(x, w), half),
+        (lambda x, w: torch.cat(bev.rms_norm_add(x, x.detach(), w)), wide),
+        (lambda x, w: torch.cat(bev.rms_norm_add(x.detach(), x, w)), half),
+        (lambda x, w: bev.gated_act(x) * w[:12], wide),
+        (lambda x, w: bev.gated_act(x, "gelu", checkpoint="int8") * w[:12], half),
+        (lambda x, w: bev.rotary(x.unflatten(0, (2, 10)).unflatten(-1, (3, 8)), place, f).flatten(-2) * w, wide),
+    ]
+    for call, x in calls:
+        leaf, weight = x.detach().requires_grad_(), w.clone().requires_grad_()
+        dy = None
+        grads = []
+        for hook in [None, *hooks]:
+            if hook is None:
+                y = call(leaf, weight)
+                dy = _normal(torch, 4)(*y.shape).to(y.dtype)
+            else:
+                with hook():
+                    y = call(leaf, weight)
+            grads.append(torch.autograd.grad(y, (leaf, weight), dy))
+        for other in grads[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(grads[0], other))
+
+    def changes(t):
+        return t[..., :1].clone() if t.dtype != torch.float64 else t.float()
+
+    for call, x in (*calls[:4], *((lambda x, w, c=c: c(x, torch.ones_like(w.detach())), x) for c, x in calls[4:])):
+        leaf = x.detach().requires_grad_()
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, changes):
+            y = call(leaf, w)
+            with pytest.raises(RuntimeError):
+                torch.autograd.grad(y.float().sum(), leaf)
+
+
 def test_views_that_negate(torch, bev):
     """A view that negates what lies in memory is refused as an input and resolved as a gradient."""
     x, dy = _normal(torch, 1)(6, 16), _normal(torch, 2)(6, 16)
