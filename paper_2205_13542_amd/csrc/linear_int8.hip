@@ -468,10 +468,15 @@ int launch(const LinearArgs &a, hipStream_t stream) {
     // (256 x 2048, K 2048, 1024 of them: 7.0 against 8.3 us; 1111 x 520, K 336, 1155: 4.3
     // against 3.8). Eight waves where a compute unit holds one workgroup (64 x 2048, K 4096:
     // 5.1 against 5.8 us), four where it holds more (256 x 2048, K 2048: 7.0 against 7.4).
-    if (a.M <= 16) return launch_few<1, 8, DIRECT>(a, stream);
+    // Blocks of 16 tokens where they make no more workgroups than there are compute units (32 x
+    // 1024, K 4096: 3.8 against 4.4 us; 64 x 2048, twice as many: 5.6 against 5.1).
+    if (a.M <= 16 || tiles(16, 16) <= kUnits) return launch_few<1, 8, DIRECT>(a, stream);
     if (const int64_t groups = tiles(32, 16); groups <= 1100)
         return groups <= kUnits ? launch_few<2, 8, DIRECT>(a, stream) : launch_few<2, 4, DIRECT>(a, stream);
-    if (tiles(128, 128) < kUnits) return launch_tiles<2, 2, 1, 1, 128, DIRECT>(a, stream);
+    // Tiles of 64 x 64 where those of 128 x 128 leave compute units without work, and, two to a
+    // unit, for the shortest k, whose rows are not read often enough to repay larger tiles
+    // (5120 x 1024, K 128: 5.9 against 7.0 us, K 512: 10.8 against 10.0).
+    if (tiles(128, 128) < (a.K < 256 ? 2 * kUnits : kUnits)) return launch_tiles<2, 2, 1, 1, 128, DIRECT>(a, stream);
     // Rounds of workgroups, in units of a round of 256 x 256 tiles, one to a compute unit (38
     // us at K 2048): a round of 128 x 128, two to a unit, takes 22 us, one of eighths 10.
     const int64_t big = tiles(256, 256), left = big % kUnits;
