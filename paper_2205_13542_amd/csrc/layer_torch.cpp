@@ -12,12 +12,15 @@
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <algorithm>
 #include <optional>
@@ -44,6 +47,19 @@ struct Refused {
 [[noreturn]] void refuse(const std::string &message, int code = BEVPOOL_ERR_INVALID_ARG) { throw Refused{code, message}; }
 
 struct Tangent {};
+
+// torch's dispatcher sees nothing of these calls, so that a tracer would keep the result of
+// the inputs that it traces with as a constant: refused, under torch.jit.trace, and under
+// make_fx (whose mode is on the dispatcher's stack, or on one of its own ahead of autograd,
+// which this key stands for).
+void not_traced() {
+    using c10::impl::TorchDispatchModeKey;
+    using c10::impl::TorchDispatchModeTLS;
+    if (torch::jit::tracer::isTracing() ||
+        (TorchDispatchModeTLS::any_modes_set() && TorchDispatchModeTLS::get_mode(TorchDispatchModeKey::PROXY)) ||
+        c10::impl::tls_local_dispatch_key_set().included_.has(c10::DispatchKey::PreDispatch))
+        refuse("the operators around attention cannot be traced: the result would be recorded as a constant");
+}
 
 std::string shape_of(const Tensor &t) { return c10::str("[", c10::Join(", ", t.sizes()), "]"); }
 
@@ -510,6 +526,7 @@ PyObject *g_error = nullptr;    // BevpoolError
 template <class F>
 PyObject *guarded(F body) {
     try {
+        not_traced();
         return body();
     } catch (const Refused &r) {
         PyObject *e = PyObject_CallFunction(g_error ? g_error : PyExc_RuntimeError, "is", r.code, r.message.c_str());

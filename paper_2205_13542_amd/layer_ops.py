@@ -17,6 +17,9 @@ and with tensors elsewhere, types and layouts that a call does not take refused
 with a BevpoolError. Checks, allocations and autograd nodes are native too
 (csrc/layer_torch.cpp): a call on a few rows costs its host time.
 
+A call that is being traced (torch.jit.trace, make_fx) is refused too: a tracer
+cannot see it and would record its result as a constant.
+
 All of them may be captured into a graph. Before a training step is, let go of what
 earlier eager steps on the same leaves returned: while such a result lives, torch
 forms the leaves' gradients on that step's stream, which a capture must not enter.

@@ -214,6 +214,34 @@ def test_forward_mode_is_refused():
                 call()
 
 
+@pytest.mark.parametrize("tracer", ["jit", "real", "symbolic", "pre_dispatch"])
+def test_tracing_is_refused(tracer):
+    """A tracer does not see these calls and would keep their results as constants: refused before the
+    refusal of tensors that no GPU holds, which a call gets again once nothing is traced."""
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from torch.fx.experimental.proxy_tensor import make_fx
+    x, q, s = torch.ones(2, 8), torch.ones(2, 8, dtype=torch.int8), torch.ones(2)
+    place, f = s.view(1, 2), bev.rotary_frequencies(2)
+
+    def trace(call):
+        if tracer == "jit":
+            return torch.jit.trace(call, (x,))
+        if tracer == "pre_dispatch":
+            return make_fx(call, tracing_mode="real", pre_dispatch=True)(x)
+        return make_fx(call, tracing_mode=tracer)(x)
+
+    for call in (lambda x: bev.rms_norm(x), lambda x: bev.rms_norm_add(x, x), lambda x: bev.rms_norm_int8(x),
+                 lambda x: bev.rms_norm_add_int8(x, x), lambda x: bev.quantize_int8(x),
+                 lambda x: bev.linear_int8(q, x[:, 0], q, s), lambda x: bev.rotary(x.view(1, 2, 2, 4), place, f),
+                 lambda x: bev.gated_act(x), lambda x: bev.gated_act(x, checkpoint="int8")):
+        for enabled in (True, False):
+            with torch.set_grad_enabled(enabled), pytest.raises(bev.BevpoolError, match="cannot be traced"):
+                trace(call)
+        with pytest.raises(bev.BevpoolError, match="device tensors"):
+            call(x)
+
+
 def test_calls_with_other_things_than_tensors():
     torch = pytest.importorskip("torch")
     import paper_2205_13542_amd as bev
