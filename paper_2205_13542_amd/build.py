@@ -1,5 +1,5 @@
-"""Build libbevpool.so for gfx950 with hipcc, in-tree, and, where there is a torch, the
-native module _layer_native.so that calls it on torch tensors.
+"""Build libbevpool.so for gfx950 with hipcc, in-tree, and, where there is a ROCm build of
+torch, the native module _layer_native.so that calls it on torch tensors.
 
 ``python -m paper_2205_13542_amd.build`` (or ``build()``) always recompiles,
 so a stale library never survives a source change.
@@ -41,17 +41,26 @@ FLAGS = [
 
 
 def _torch_commands(lib_dir: str, tmp: str) -> list:
-    """Compile and link commands of the native module, for the torch that is installed; none without one."""
+    """Compile and link commands of the native module; none where there is no ROCm build of torch, or no
+    compiler or Python headers, which only the module needs."""
     import importlib.util
     import sysconfig
+    import warnings
     spec = importlib.util.find_spec("torch")
-    if spec is None:
+    if spec is None or spec.origin is None:
         return []
     torch_dir = os.path.dirname(spec.origin)
+    if not os.path.exists(os.path.join(torch_dir, "lib", "libtorch_hip.so")):
+        return []
+    python = sysconfig.get_paths()["include"]
+    missing = CXX if shutil.which(CXX) is None else "Python.h"
+    if missing == CXX or not os.path.exists(os.path.join(python, "Python.h")):
+        warnings.warn(f"no {missing}: {os.path.basename(TORCH_LIB_PATH)} is left out, which layer_ops needs")
+        return []
     obj = tmp + ".o"
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))
     system = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
-              os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+              os.path.join(rocm, "include"), python]
     compile_ = [CXX, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
                 "-DUSE_ROCM=1", "-I", INCLUDE, *(a for d in system for a in ("-isystem", d)), "-c",
                 os.path.join(CSRC, TORCH_SOURCE), "-o", obj]
@@ -61,8 +70,22 @@ def _torch_commands(lib_dir: str, tmp: str) -> list:
     return [compile_, link]
 
 
+def _run(command) -> None:
+    done = subprocess.run(command, capture_output=True, text=True)
+    if done.returncode != 0:
+        raise subprocess.CalledProcessError(done.returncode, done.args, done.stdout, done.stderr)
+
+
+def _install(made: str, path: str) -> None:
+    shutil.copy(made, path + ".tmp")        # the folders may be on two file systems
+    os.replace(path + ".tmp", path)
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source to an object in parallel, then link the library."""
+    """Compile every source to an object in parallel, then link and install the library, then the module.
+
+    Where the module is not built, or fails to, the library is installed all the same and no
+    older module is left beside it; a failure is raised then."""
     import concurrent.futures
     import tempfile
     compile_flags = [f for f in FLAGS if f != "-shared"]
@@ -70,27 +93,29 @@ def build(verbose: bool = False) -> str:
         objs = [os.path.join(tmpdir, os.path.splitext(s)[0] + ".o") for s in SOURCES]
         cmds = [[HIPCC, *compile_flags, "-I", INCLUDE, "-I", CSRC, "-c",
                  os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
-        floor_tmp = FLOOR_LIB_PATH + ".tmp"
+        floor_tmp, lib_tmp, torch_tmp = (os.path.join(tmpdir, os.path.basename(p))
+                                         for p in (FLOOR_LIB_PATH, LIB_PATH, TORCH_LIB_PATH))
         cmds.append([HIPCC, *FLAGS, os.path.join(CSRC, FLOOR_SOURCE), "-o", floor_tmp])
-        lib_tmp, torch_tmp = os.path.join(tmpdir, "libbevpool.so"), os.path.join(tmpdir, "_layer_native.so")
         torch_cmds = _torch_commands(tmpdir, torch_tmp)
-        cmds.extend(torch_cmds[:1])
         if verbose:
-            for c in cmds:
+            for c in cmds + torch_cmds[:1]:
                 print(" ".join(c), flush=True)
-        workers = max(1, min(len(cmds), os.cpu_count() or 1))
+        workers = max(1, min(len(cmds) + 1, os.cpu_count() or 1))
         with concurrent.futures.ThreadPoolExecutor(workers) as ex:
-            for r in ex.map(lambda c: subprocess.run(c, capture_output=True, text=True), cmds):
-                if r.returncode != 0:
-                    raise subprocess.CalledProcessError(r.returncode, r.args, r.stdout, r.stderr)
-        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", lib_tmp], check=True)
-        if torch_cmds:
-            subprocess.run(torch_cmds[1], check=True)
-        os.replace(floor_tmp, FLOOR_LIB_PATH)
-        for made, path in ((lib_tmp, LIB_PATH), (torch_tmp, TORCH_LIB_PATH)):
-            if os.path.exists(made):        # the folder may be on another file system
-                shutil.copy(made, path + ".tmp")
-                os.replace(path + ".tmp", path)
+            module = ex.submit(_run, torch_cmds[0]) if torch_cmds else None
+            for r in [ex.submit(_run, c) for c in cmds]:
+                r.result()
+        _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", lib_tmp])
+        _install(floor_tmp, FLOOR_LIB_PATH)
+        _install(lib_tmp, LIB_PATH)
+        try:
+            if module:
+                module.result()
+                _run(torch_cmds[1])
+                _install(torch_tmp, TORCH_LIB_PATH)
+        finally:
+            if not os.path.exists(torch_tmp) and os.path.exists(TORCH_LIB_PATH):
+                os.remove(TORCH_LIB_PATH)       # one of another library
     return LIB_PATH
 
 
