@@ -1,0 +1,90 @@
+"""Forms of the operators around attention that only large calls take, by value: results that go
+past the caches (over 16 MB, in whole 16-byte accesses), a workgroup's second turn, two accesses of
+a wave in uneven rows. References and tolerances are those of test_gpu_layer_ops."""
+import pytest
+
+from test_gpu_layer_ops import (U32, _act_reference, _check, _dtype, _held_reference, _normal, _over,  # noqa: F401
+                                _rotary_reference, _tiny, _u, _value_of, bev, test_gated_act as check_gated_act,
+                                test_rms_norm as check_rms_norm, test_rms_norm_int8 as check_rms_norm_int8,
+                                test_rotary as check_rotary, torch)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+@pytest.mark.parametrize("shape,act,dtype", [((9000, 1024), "silu", "bf16"), ((9000, 1024), "gelu", "f16"),
+                                             ((140, 100, 320), "silu", "f32"), ((70001, 128), "relu", "bf16")])
+def test_gated_act_past_the_caches(torch, bev, shape, act, dtype, checkpoint):
+    check_gated_act(torch, bev, shape, 0, act, dtype, checkpoint)
+
+
+@pytest.mark.parametrize("batch,tokens,heads,dim,pairs,axes,kind,dtype,packed", [
+    (2, 2100, 16, 128, 64, 1, "i32", "bf16", False), (2, 2100, 16, 128, 32, 2, "f32", "f16", True),
+    (1, 40000, 4, 32, 16, 1, "i64", "f32", False), (1, 70001, 1, 136, 60, 1, "i64", "bf16", True)])
+def test_interleaved_rotary_past_the_caches(torch, bev, batch, tokens, heads, dim, pairs, axes, kind, dtype, packed):
+    check_rotary(torch, bev, batch, tokens, heads, dim, pairs, axes, True, kind, dtype, packed)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_of_more_tiles_than_workgroups(torch, bev, interleaved):
+    """A tile is a token here, and the workgroups that stay are 65536: the first ones form the sines
+    and cosines of a second tile where those of the first were."""
+    tokens, heads, pairs = 66001, 4, 256
+    normal = _normal(torch, 1)
+    x, dy = (normal(1, tokens, heads, 2 * pairs).bfloat16() for _ in range(2))
+    x.requires_grad_()
+    positions = torch.arange(tokens, device="cuda")[None] * 7 - 100
+    f = bev.rotary_frequencies(pairs, device="cuda")
+    y = bev.rotary(x, positions, f, interleaved)
+    dx, = torch.autograd.grad(y, x, dy)
+    for part in (slice(0, 500), slice(65500, tokens)):
+        for got, src, backward in ((y, x, False), (dx, dy, True)):
+            ref, tol = _rotary_reference(torch, src.detach()[:, part], positions[:, part].contiguous(), f, interleaved, 1.0,
+                                         backward)
+            _check("rotary", got.detach()[:, part], ref, tol + 1.01 * _u("bf16") * ref.abs() + _tiny("bf16"))
+
+
+@pytest.mark.parametrize("rows,features,dtype", [(4200000, 32, "bf16"), (2100000, 31, "f32")])
+def test_gated_act_of_more_units_than_threads(torch, bev, rows, features, dtype):
+    """More than 2^24 units, which 65536 workgroups take in two turns; aligned rows and uneven ones."""
+    normal = _normal(torch, 2)
+    to = _dtype(torch, dtype)
+    x = normal(rows, 2 * features).to(to).requires_grad_()
+    dy = normal(rows, features).to(to)
+    second = (1 << 24) // (32 // (4 if dtype == "f32" else 8))      # row of the first unit of the second turn
+    parts = (slice(0, 1000), slice(second - 1000, second + 1000), slice(rows - 1000, rows))
+    for checkpoint in (None, "int8"):
+        y = bev.gated_act(x, "silu", checkpoint)
+        dx, = torch.autograd.grad(y, x, dy)
+        for part in parts:
+            here = x.detach()[part]
+            flat = here.double().view(-1, 2, features)
+            a, _, a_tol, _ = _act_reference(torch, flat[:, 0], "silu")
+            ref = a * flat[:, 1]
+            _check("y", y.detach()[part], ref, a_tol * flat[:, 1].abs() + (U32 + 1.01 * _u(dtype)) * ref.abs() + _tiny(dtype))
+            if checkpoint:
+                flat = _value_of(torch, *_held_reference(torch, here, features))
+            a, slope, a_tol, slope_tol = _act_reference(torch, flat[:, 0], "silu")
+            d = dy[part].double()
+            ref = torch.stack((d * flat[:, 1] * slope, d * a), 1)
+            tol = torch.stack(((d * flat[:, 1]).abs() * slope_tol, d.abs() * a_tol), 1)
+            _check("dx", dx[part].view(-1, 2, features), ref, tol + (2 * U32 + 1.01 * _u(dtype)) * ref.abs() + _tiny(dtype))
+
+
+@pytest.mark.parametrize("shape,left,residual,x_type,y_type", [
+    ((8200, 1001), 0, True, "bf16", "bf16"), ((8192, 1023), 1, False, "f16", "f32"), ((8300, 513), 0, True, "f16", "bf16"),
+    ((9000, 331), 0, True, "f32", "f32"), ((8192, 511), 2, False, "f32", "bf16"), ((70000, 520), 0, True, "bf16", "f32")])
+def test_rms_norm_of_two_accesses_of_a_wave(torch, bev, shape, left, residual, x_type, y_type):
+    """Of 8192 rows and more: uneven rows of 513 to 1023 16-bit channels, 257 to 511 of fp32."""
+    check_rms_norm(torch, bev, shape, left, residual, x_type, y_type, "f32")
+    check_rms_norm_int8(torch, bev, shape, left, residual, x_type, y_type, "f32")
+
+
+@pytest.mark.parametrize("shape,x_type", [((2100, 8200), "bf16"), ((2050, 8193), "f16"), ((2049, 9001), "f32"),
+                                          ((5000, 5000), "bf16"), ((40001, 331), "f16")])
+def test_quantize_int8_of_more_rows_than_workgroups(torch, bev, shape, x_type):
+    x = _normal(torch, 5)(*shape).to(_dtype(torch, x_type))
+    held, scale = bev.quantize_int8(x)
+    top = x.float().abs().amax(-1, keepdim=True)
+    assert torch.equal(held, torch.round(x.float() * _over(torch, 127, top)).to(torch.int8))
+    assert torch.equal(scale, (top / torch.full_like(top, 127)).squeeze(-1))
