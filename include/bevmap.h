@@ -343,6 +343,8 @@ BEVPOOL_API int bevmap_rotary(const bevmap_turn *turn, const void *x, const void
 /*
  * Gated activation: a row of x holds `features` gates and then as many values,
  *   y[f] = act(gate[f]) * value[f].
+ * act is formed in fp32 to within 2^-15 of its value, far below 0 too (there silu is taken as
+ * 0 where it is under 2^-118 in magnitude), and near 0 and above to within some 2^-22.
  */
 typedef struct {
     int64_t rows;

@@ -161,7 +161,9 @@ def rotary_frequencies(pairs, base=10000.0, axes=1, scaling=None, factor=1.0, co
 def gated_act(x, act="silu", checkpoint=None):
     """Gated activation: act(gate) * value, the halves of every row of x [...][2 F]
     (fp32, bf16 or fp16; contiguous or with evenly spaced rows). Returns [...][F],
-    contiguous, rounded once; act "none", "relu", "silu" or "gelu" (through erf).
+    contiguous; act "none", "relu", "silu" or "gelu" (through erf), in fp32 to within
+    2^-15 of its value in the tail far below 0 and some 2^-22 elsewhere, and the product
+    rounded once.
 
     checkpoint: what the backward reads. None keeps x; "int8" keeps a copy in 8.25
     bits an element (32 neighbouring channels of a half share a power of two, and

@@ -1,6 +1,8 @@
 """Forms of the operators around attention that only large calls take, by value: results that go
 past the caches (over 16 MB, in whole 16-byte accesses), a workgroup's second turn, two accesses of
 a wave in uneven rows. References and tolerances are those of test_gpu_layer_ops."""
+import math
+
 import pytest
 
 from test_gpu_layer_ops import (U32, _act_reference, _check, _dtype, _held_reference, _normal, _over,  # noqa: F401
@@ -88,3 +90,54 @@ def test_quantize_int8_of_more_rows_than_workgroups(torch, bev, shape, x_type):
     top = x.float().abs().amax(-1, keepdim=True)
     assert torch.equal(held, torch.round(x.float() * _over(torch, 127, top)).to(torch.int8))
     assert torch.equal(scale, (top / torch.full_like(top, 127)).squeeze(-1))
+
+
+def _tails(torch, g, act):
+    """act(g), its slope, and bounds of both that shrink with them. exp(v) is off by 2 |v| U32 of itself
+    through its argument's two roundings, and some more, the square of g by another |v| U32; exponentials
+    below 2^-126 are 0, which takes up to 2^-118 away where g is below -87. What multiplies exp(-g^2 / 2) in
+    the normal distribution's tail is a polynomial of nine terms of one to two roundings each."""
+    z = g.abs()
+    if act == "silu":
+        s = torch.sigmoid(g)
+        rel = (2.5 * z * (1 - s) + 8) * U32
+        a, slope = g * s, s * (1 + g * (1 - s))
+        a_tol = rel * a.abs() + 2.0 ** -118
+        slope_tol = rel * slope.abs() + s * (z * s * rel + 3 * U32 * (1 + z * (1 - s))) + 2.0 ** -118
+    else:
+        phi, share = torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi), 0.5 * torch.erfc(-g / math.sqrt(2))
+        a, slope = g * share, share + g * phi
+        tail = torch.minimum(share, 1 - share)
+        share_tol = (2 * g * g + 20) * U32 * tail + U32 * share
+        a_tol = z * share_tol + 2 * U32 * a.abs() + 2.0 ** -118
+        slope_tol = share_tol + (2 * g * g + 10) * U32 * (g * phi).abs() + 2 * U32 * slope.abs() + 2.0 ** -118
+    return a, slope, a_tol, slope_tol
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_tails_of_activations(torch, bev, act, dtype):
+    """Gates from far below 0, where an activation is small, to some above it: right to within some
+    units of the value itself, so that bf16 and fp16 results are the rounded values."""
+    to = _dtype(torch, dtype)
+    g = torch.linspace(-105, 20, 1 << 16, device="cuda").to(to)
+    v = _normal(torch, 1)(g.numel()).to(to)
+    x = torch.cat((g.view(-1, 64), v.view(-1, 64)), 1).requires_grad_()
+    dy = _normal(torch, 2)(g.numel() // 64, 64).to(to)
+    y = bev.gated_act(x, act)
+    dx, = torch.autograd.grad(y, x, dy)
+    g, v, d = g.double().view(-1, 64), v.double().view(-1, 64), dy.double()
+    a, slope, a_tol, slope_tol = _tails(torch, g, act)
+    u, tiny = 1.01 * _u(dtype) + 2 * U32, _tiny(dtype)
+    _check("y", y.detach(), a * v, a_tol * v.abs() + u * (a * v).abs() + tiny)
+    ref = torch.cat((d * v * slope, d * a), 1)
+    tol = torch.cat(((d * v).abs() * slope_tol, d.abs() * a_tol), 1)
+    _check("dx", dx, ref, tol + u * ref.abs() + tiny)
+
+
+def test_activations_of_infinities(torch, bev):
+    inf = math.inf
+    x = torch.tensor([[inf, -inf, math.nan, 3e38, -3e38, 0.0] + [1.0] * 6], device="cuda")
+    for act in ("silu", "gelu"):
+        y = bev.gated_act(x, act)[0]
+        assert y[0] == inf and y[2].isnan() and y[3] == x[0, 3] and y[4] == 0 and y[5] == 0
