@@ -198,7 +198,8 @@ BEVPOOL_API int bevmap_dropout(const void *x, int64_t x_stride, const void *resi
  * The sum is handed on rounded to x_dtype; y is formed from it before that.
  * Squares are summed in fp32, rows whose squares leave its range after a power of two is
  * taken out, so a row of any finite size is normed. An infinity or a NaN reaches its row
- * alone.
+ * alone. (Gradients read rstd: through a row whose rstd is past fp32's range, of numbers below
+ * 2^-127 with an eps of 0, they are not finite, and the weight's neither.)
  */
 typedef struct {
     int64_t rows;

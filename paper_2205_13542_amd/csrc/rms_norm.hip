@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 }
             }
         }
-        float rstd = 1.0f;
+        float rstd = 1.0f, s = 1.0f;        // y = w h rstd, h times s by then
         if constexpr (OUT != kInt8) {
             float ss = 0.0f;
 #pragma unroll
@@ -131,24 +131,27 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) ss = fmaf(h[k][i], h[k][i], ss);
             ss = over_lanes<LANES>(ss, plus, add, turn);
-            // Squares that leave fp32's range: the row's numbers times a power of two, squared again.
+            // Squares that leave fp32's range: the row's numbers times a power of two, squared again, and
+            // normed as they are then (1 / rms itself may be no fp32 number).
             // (A sum of 0 is a row of zeros, or of numbers so small that only an eps of nothing shows them.)
             const bool large = !(ss < 0x1p120f), small = ss < 0x1p-90f && a.eps < 0x1p-60f;
-            float s = 1.0f;
             if (LANES > kRmsWave ? large || small : __any(large || small)) {
                 s = large ? 0x1p-80f : small ? 0x1p93f : 1.0f;
                 float again = 0.0f;
 #pragma unroll
                 for (int k = 0; k < ITER; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) again = fmaf(h[k][i] * s, h[k][i] * s, again);
+                    for (int i = 0; i < V; ++i) {
+                        h[k][i] *= s;
+                        again = fmaf(h[k][i], h[k][i], again);
+                    }
                 if constexpr (LANES > kRmsWave) __syncthreads();    // the slots are read
                 ss = over_lanes<LANES>(again, plus, add, turn);
             }
-            rstd = s / sqrtf(ss * per + a.eps * s * s);
+            rstd = 1.0f / sqrtf(ss * per + a.eps * s * s);
         }
         if constexpr (OUT == kFloat) {
-            if (a.rstd && live && lane == 0) a.rstd[row] = rstd;
+            if (a.rstd && live && lane == 0) a.rstd[row] = rstd * s;
 #pragma unroll
             for (int k = 0; k < ITER; ++k) {
                 const int at = lane + k * LANES;

@@ -141,3 +141,28 @@ def test_activations_of_infinities(torch, bev):
     for act in ("silu", "gelu"):
         y = bev.gated_act(x, act)[0]
         assert y[0] == inf and y[2].isnan() and y[3] == x[0, 3] and y[4] == 0 and y[5] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("channels", [1, 24, 331, 1030, 8192])
+def test_rms_norm_at_the_ends_of_the_range(torch, bev, channels, dtype):
+    """Rows whose 1 / rms is no fp32 number, or one with few bits, with an eps of 0; their norm is of
+    order 1. The bound is that of any row: 32 roundings."""
+    x = _normal(torch, 1)(6, channels)
+    for i, size in enumerate((2.0 ** -130, 2.0 ** -140, 2.0 ** -126, 2.0 ** 125, 1.0)):
+        x[i] *= size
+    x[5] = 0
+    x[5, channels // 2] = 2.0 ** -130                       # one number alone
+    x = x.clamp(-3e38, 3e38).to(_dtype(torch, dtype))
+    x[:, 0] = torch.where(x[:, 0] == 0, 2.0 ** -130, x[:, 0])   # no row of zeros
+    ref = x.double() / x.double().square().mean(1, keepdim=True).sqrt()
+    w = 1 + _normal(torch, 2)(channels, s=0.2)
+    y = bev.rms_norm(x, w, eps=0.0, out_dtype=torch.float32)
+    _check("y", y, ref * w.double(), 32 * U32 * (ref * w.double()).abs())
+    y, total = bev.rms_norm_add(x, torch.zeros_like(x), w, eps=0.0, out_dtype=torch.float32)
+    _check("y", y, ref * w.double(), 32 * U32 * (ref * w.double()).abs())
+    assert torch.equal(total, x)
+    held, scale = bev.rms_norm_int8(x, w, eps=0.0)
+    step = scale.double()[:, None]
+    assert scale.isfinite().all() and (held.abs().amax(1) == 127).all()
+    _check("held", held.double() * step, ref * w.double(), 0.5 * step + 64 * U32 * 127 * step)
