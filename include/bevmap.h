@@ -252,8 +252,8 @@ BEVPOOL_API int bevmap_rms_norm_backward(const bevmap_rms *norm, const void *gra
  * |weight * h| of a row,
  *   held = round(weight * h * (127 / top)), scale = top * rstd / 127,
  * so that held * scale is y to within half a scale; halves go to the even neighbour. A
- * row of zeros has scale 0 (eps of 0: NaN), one with an infinity or a NaN has scale NaN
- * and zeros.
+ * row of zeros has scale 0 (eps of 0: NaN), one with an infinity or a NaN, its own, a
+ * weight's or y's, has scale NaN and zeros.
  *  held:  device int8 [rows][channels], overwritten.  scale: device float [rows],
  *         overwritten.  The rest as for bevmap_rms_norm; y_dtype is not used.
  * Errors: those of bevmap_rms_norm.

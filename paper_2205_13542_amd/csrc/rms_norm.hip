@@ -83,8 +83,14 @@ __device__ __forceinline__ int8_t held(float z, const Steps &s) {
     return int8_t(s.none ? 0.0f : rintf(z * s.up * s.mul));
 }
 
+// Waves of a SIMD that the registers are to leave room for, where they are next to that: all
+// of the workgroups that stay then run at a time (8 bits of 100003 x 331: 48 us, by seven 54).
+constexpr int rms_waves(int lanes, int iter, int out, int rows) {
+    return out == kInt8Norm && lanes <= kRmsWave && (iter == 1 || rows == kEven) ? 8 : 1;
+}
+
 template <int DT, int LANES, int ITER, int OUT, int ROWS, bool STREAM>
-__global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
+__global__ __launch_bounds__(kRmsBlock, rms_waves(LANES, ITER, OUT, ROWS)) void k_rms(RmsArgs a) {
     using T = typename Num<DT>::T;
     constexpr int V = kWide<DT>, kRows = kRmsBlock / LANES;
     __shared__ float add[8];
@@ -123,9 +129,8 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 }
             }
         }
-        float rstd = 1.0f, s = 1.0f;        // y = w h rstd, h times s by then
+        float rstd = 1.0f, s = 1.0f, ss = 0.0f;     // y = w h rstd, h times s by then
         if constexpr (OUT != kInt8) {
-            float ss = 0.0f;
 #pragma unroll
             for (int k = 0; k < ITER; ++k)
 #pragma unroll
@@ -161,15 +166,32 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                     store_any_part<V, ROWS, STREAM>(a.y, row * a.C + at * V, a.y_dtype, a.C - at * V, h[k]);
             }
         } else {
-            uint32_t top = 0;
+            auto largest = [&] {
+                uint32_t top = 0;
 #pragma unroll
-            for (int k = 0; k < ITER; ++k)
+                for (int k = 0; k < ITER; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if constexpr (OUT == kInt8Norm) h[k][i] *= w[k][i];
-                    if (lane + k * LANES < n_vec) top = larger(top, size_bits(h[k][i]));
+                    for (int i = 0; i < V; ++i)
+                        if (lane + k * LANES < n_vec) top = larger(top, size_bits(OUT == kInt8Norm ? h[k][i] * w[k][i] : h[k][i]));
+                return over_lanes<LANES>(top, larger, most, turn);
+            };
+            uint32_t top = largest();
+            if constexpr (OUT == kInt8Norm) {
+                // Products with the weights that leave fp32's range where the norm does not: once more, of
+                // the row times the power of two next to 1 / rms, which leaves q as it would be.
+                const bool far = top >= kInfBits || (top < __float_as_uint(0x1p-100f) && ss > 0.0f);
+                if (LANES > kRmsWave ? far : __any(far)) {
+                    const uint32_t power = __float_as_uint(rstd) & kInfBits;
+                    const float p = far && power > 0 && power < kInfBits ? __uint_as_float(power) : 1.0f;
+                    rstd /= p;
+#pragma unroll
+                    for (int k = 0; k < ITER; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) h[k][i] *= p;
+                    if constexpr (LANES > kRmsWave) __syncthreads();    // the slots are read
+                    top = largest();
                 }
-            top = over_lanes<LANES>(top, larger, most, turn);
+            }
             const Steps steps = steps_of(top, rstd);
             if (live && lane == 0) a.scale[row] = steps.scale;
 #pragma unroll
@@ -177,7 +199,7 @@ __global__ __launch_bounds__(kRmsBlock) void k_rms(RmsArgs a) {
                 const int at = lane + k * LANES;
                 int8_t q[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) q[i] = held(h[k][i], steps);
+                for (int i = 0; i < V; ++i) q[i] = held(OUT == kInt8Norm ? h[k][i] * w[k][i] : h[k][i], steps);
                 if (live && at < n_vec) store_bytes<V, ROWS>(a.q + row * a.C + at * V, a.C - at * V, q);
             }
         }

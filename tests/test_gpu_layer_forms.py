@@ -166,3 +166,29 @@ def test_rms_norm_at_the_ends_of_the_range(torch, bev, channels, dtype):
     step = scale.double()[:, None]
     assert scale.isfinite().all() and (held.abs().amax(1) == 127).all()
     _check("held", held.double() * step, ref * w.double(), 0.5 * step + 64 * U32 * 127 * step)
+
+
+@pytest.mark.parametrize("channels", [24, 331, 1030, 8192])
+def test_rms_norm_int8_with_weights_of_any_size(torch, bev, channels):
+    """Rows whose products with the weights are past fp32's range, or below it, where the norm is not:
+    the integers are those of the same row and weights a power of two away, and the scale is the norm's."""
+    x = _normal(torch, 1)(7, channels)
+    ordinary = 1 + _normal(torch, 2)(channels, s=0.2)
+    rows = torch.tensor([0, 100, -100, 50, -50, 126, -120], device="cuda")
+    x = (x.double().clamp(-1.9, 1.9) * 2.0 ** rows[:, None].double()).float()
+    for power in (0, 100, -100, 40, -40):
+        w = ordinary * 2.0 ** power
+        held, scale = bev.rms_norm_int8(x, w, eps=0.0)
+        near = (x.double() * 2.0 ** -rows[:, None].double()).float() * ordinary     # exact but for the last product
+        top = near.abs().amax(1, keepdim=True)
+        assert torch.equal(held, torch.round(near * _over(torch, 127, top)).to(torch.int8)), power
+        y = x.double() / x.double().square().mean(1, keepdim=True).sqrt() * w.double()
+        _check("scale", scale, y.abs().amax(1) / 127, 32 * U32 * y.abs().amax(1) / 127)
+    x[3] = 0
+    x[4, 5], x[5, 6] = math.inf, math.nan
+    for power in (0, 100, -100):
+        held, scale = bev.rms_norm_int8(x, ordinary * 2.0 ** power, eps=1e-6)
+        assert scale[3] == 0 and scale[4:6].isnan().all() and not held[3:6].any()
+        # (row 2 with the smallest weights: a norm of 2^-180, which is 0 in fp32, and so is its scale)
+        fine = slice(0, 2 if power < 0 else 3)
+        assert scale[:3].isfinite().all() and (held[fine].abs().amax(1) == 127).all()
