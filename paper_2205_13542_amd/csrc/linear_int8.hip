@@ -460,6 +460,9 @@ int launch_eighths(LinearArgs a, int left, hipStream_t stream) {
     return BEVPOOL_OK;
 }
 
+// A launch has fewer than 2^32 threads.
+bool fits(int64_t tiles, int threads) { return tiles * threads < int64_t(1) << 32; }
+
 template <bool DIRECT>
 int launch(const LinearArgs &a, hipStream_t stream) {
     auto tiles = [&](int m, int n) { return int64_t((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
@@ -487,7 +490,7 @@ int launch(const LinearArgs &a, hipStream_t stream) {
     // 19.2 us against 20.6 by 128 x 128; 3000 x 2000, K 331: 11.6 against 12.7; 33000 x 509, K
     // 443: 33.3 against 31.5).
     if constexpr (!DIRECT)
-        if (a.K <= 384) return launch_tiles<4, 2, 1, 1, 128, DIRECT>(a, stream);
+        if (a.K <= 384 && fits(tiles(128, 64), 512)) return launch_tiles<4, 2, 1, 1, 128, DIRECT>(a, stream);
     if (a.K < 512 || small_time < big_time) return launch_tiles<2, 2, 2, 2, 128, DIRECT>(a, stream);
     return eighths ? launch_eighths<DIRECT>(a, int(left), stream) : launch_tiles<4, 2, 2, 4, 128, DIRECT>(a, stream);
 }

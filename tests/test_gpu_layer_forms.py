@@ -192,3 +192,16 @@ def test_rms_norm_int8_with_weights_of_any_size(torch, bev, channels):
         # (row 2 with the smallest weights: a norm of 2^-180, which is 0 in fp32, and so is its scale)
         fine = slice(0, 2 if power < 0 else 3)
         assert scale[:3].isfinite().all() and (held[fine].abs().amax(1) == 127).all()
+
+
+def test_linear_int8_of_the_most_rows(torch, bev):
+    """As many rows as a call takes, of a few unaligned channels: a launch of fewer than 2^32 threads."""
+    rows, channels = (1 << 30) - 1, 3
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randint(-128, 128, (rows, channels), generator=gen, device="cuda", dtype=torch.int8)
+    xs = torch.rand(rows, generator=gen, device="cuda")
+    w, ws = torch.tensor([[3, -100, 127]], dtype=torch.int8, device="cuda"), torch.tensor([0.25], device="cuda")
+    y = bev.linear_int8(x, xs, w, ws)
+    for part in (slice(0, 1 << 20), slice(1 << 29, (1 << 29) + (1 << 20)), slice(rows - (1 << 20), rows)):
+        ref = (x[part].double() * w.double()).sum(1, keepdim=True) * xs[part].double()[:, None] * 0.25
+        _check("y", y[part], ref, (3 * U32 + _u("bf16")) * ref.abs())
