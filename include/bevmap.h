@@ -277,7 +277,8 @@ BEVPOOL_API int bevmap_quantize_int8(const void *x, int64_t x_stride, int8_t *he
  * Product of 8-bit integers with a scale for each row (token) and each feature:
  *   y[m][n] = x_scale[m] * w_scale[n] * (sum over k of x[m][k] * w[n][k]) + bias[n].
  * Sums are 32-bit integers, exact for all values of int8 up to 131071 channels; fp32
- * follows, and one rounding to y_dtype.
+ * follows, in an order in which only results past its range are infinite, and one rounding
+ * to y_dtype.
  */
 typedef struct {
     int64_t rows;

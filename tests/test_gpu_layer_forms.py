@@ -5,7 +5,7 @@ import math
 
 import pytest
 
-from test_gpu_layer_ops import (U32, _act_reference, _check, _dtype, _held_reference, _normal, _over,  # noqa: F401
+from test_gpu_layer_ops import (U32, _act_reference, _check, _dtype, _held, _held_reference, _normal, _over,  # noqa: F401
                                 _rotary_reference, _tiny, _u, _value_of, bev, test_gated_act as check_gated_act,
                                 test_rms_norm as check_rms_norm, test_rms_norm_int8 as check_rms_norm_int8,
                                 test_rotary as check_rotary, torch)
@@ -205,3 +205,23 @@ def test_linear_int8_of_the_most_rows(torch, bev):
     for part in (slice(0, 1 << 20), slice(1 << 29, (1 << 29) + (1 << 20)), slice(rows - (1 << 20), rows)):
         ref = (x[part].double() * w.double()).sum(1, keepdim=True) * xs[part].double()[:, None] * 0.25
         _check("y", y[part], ref, (3 * U32 + _u("bf16")) * ref.abs())
+
+
+@pytest.mark.parametrize("rows,channels,features", [(3, 700, 40), (100, 320, 300), (1200, 331, 517), (5000, 640, 512),
+                                                    (16500, 592, 1000), (16390, 597, 1021)])
+def test_linear_int8_of_scales_of_any_size(torch, bev, rows, channels, features):
+    """Scales whose product with a sum alone leaves fp32's range where the result does not, either way,
+    among rows and channels of ordinary ones; in every form."""
+    x, xs = _held(torch, 1, rows, channels)
+    w, ws = _held(torch, 2, features, channels)
+    power = torch.tensor([0, 120, -120, 90, 60, -90], device="cuda", dtype=torch.float64)
+    xp, wp = power[torch.arange(rows, device="cuda") % 6], power[torch.arange(features, device="cuda") % 6]
+    xs, ws = (xs.double() * 2 ** xp).float(), (ws.double() * 2 ** wp).float()
+    b = _normal(torch, 3)(features, s=100.0)
+    y = bev.linear_int8(x, xs, w, ws, b, out_dtype=torch.float32)
+    product = (x.double() @ w.double().t().contiguous()) * xs.double()[:, None] * ws.double()
+    ref = product + b.double()
+    # from where the scales' product is no fp32 number on, nothing is said
+    fine = (xp[:, None] + wp).abs() <= 100
+    tol = 3 * U32 * product.abs() + 2 * U32 * ref.abs() + 2.0 ** -126
+    _check("y", torch.where(fine, y, 0), torch.where(fine, ref, 0), tol)
