@@ -522,6 +522,19 @@ Tensor gated_act(const Tensor &x, int64_t act, bool hold) {
 
 PyObject *g_error = nullptr;    // BevpoolError
 
+// While one lives, other Python threads run: a launch may wait for a place in the queue, an
+// allocation for the driver.
+struct Released {
+    PyThreadState *const state = PyEval_SaveThread();
+    ~Released() { PyEval_RestoreThread(state); }
+};
+// body's result, formed without the interpreter's lock
+template <class F>
+auto released(F body) {
+    const Released r;
+    return body();
+}
+
 // body's result, what it throws as a Python exception
 template <class F>
 PyObject *guarded(F body) {
@@ -536,7 +549,8 @@ PyObject *guarded(F body) {
         }
     } catch (const Tangent &) {
         PyErr_SetString(PyExc_NotImplementedError, "the operators around attention have no forward mode");
-    } catch (const python_error &) {
+    } catch (python_error &e) {
+        e.restore();
     } catch (const c10::Error &e) {
         PyErr_SetString(std::string(e.what()).find("out of memory") != std::string::npos ? PyExc_MemoryError
                                                                                          : PyExc_RuntimeError,
@@ -588,43 +602,54 @@ void expect(Py_ssize_t got, Py_ssize_t want) {
 PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 5);
-        const variable_list r = rms_norm(tensor_of(a[0], "x"), maybe_tensor(a[1], "residual"),
-                                         maybe_tensor(a[2], "weight"), number_of(a[3], "eps"), maybe_type(a[4]));
+        const Tensor x = tensor_of(a[0], "x"), residual = maybe_tensor(a[1], "residual"), weight = maybe_tensor(a[2], "weight");
+        const double eps = number_of(a[3], "eps");
+        const auto type = maybe_type(a[4]);
+        const variable_list r = released([&] { return rms_norm(x, residual, weight, eps, type); });
         return r.size() == 1 ? THPVariable_Wrap(r[0]) : wrap(r);
     });
 }
 PyObject *py_rms_norm_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 4);
-        return wrap(rms_norm_int8(tensor_of(a[0], "x"), maybe_tensor(a[1], "residual"), maybe_tensor(a[2], "weight"),
-                                  number_of(a[3], "eps")));
+        const Tensor x = tensor_of(a[0], "x"), residual = maybe_tensor(a[1], "residual"), weight = maybe_tensor(a[2], "weight");
+        const double eps = number_of(a[3], "eps");
+        return wrap(released([&] { return rms_norm_int8(x, residual, weight, eps); }));
     });
 }
 PyObject *py_quantize_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 1);
-        return wrap(quantize_int8(tensor_of(a[0], "x")));
+        const Tensor x = tensor_of(a[0], "x");
+        return wrap(released([&] { return quantize_int8(x); }));
     });
 }
 PyObject *py_linear_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 6);
-        return THPVariable_Wrap(linear_int8(tensor_of(a[0], "x"), tensor_of(a[1], "x_scale"), tensor_of(a[2], "weight"),
-                                            tensor_of(a[3], "weight_scale"), maybe_tensor(a[4], "bias"),
-                                            maybe_type(a[5])));
+        const Tensor x = tensor_of(a[0], "x"), x_scale = tensor_of(a[1], "x_scale"), weight = tensor_of(a[2], "weight"),
+                     weight_scale = tensor_of(a[3], "weight_scale"), bias = maybe_tensor(a[4], "bias");
+        const auto type = maybe_type(a[5]);
+        return THPVariable_Wrap(released([&] { return linear_int8(x, x_scale, weight, weight_scale, bias, type); }));
     });
 }
 PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 5);
-        return THPVariable_Wrap(rotary(tensor_of(a[0], "x"), tensor_of(a[1], "positions"),
-                                       tensor_of(a[2], "frequencies"), truth_of(a[3]), number_of(a[4], "amplitude")));
+        const Tensor x = tensor_of(a[0], "x"), positions = tensor_of(a[1], "positions"),
+                     frequencies = tensor_of(a[2], "frequencies");
+        const bool interleaved = truth_of(a[3]);
+        const double amplitude = number_of(a[4], "amplitude");
+        return THPVariable_Wrap(released([&] { return rotary(x, positions, frequencies, interleaved, amplitude); }));
     });
 }
 PyObject *py_gated_act(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
         expect(n, 3);
-        return THPVariable_Wrap(gated_act(tensor_of(a[0], "x"), int64_t(number_of(a[1], "act")), truth_of(a[2])));
+        const Tensor x = tensor_of(a[0], "x");
+        const int64_t act = int64_t(number_of(a[1], "act"));
+        const bool hold = truth_of(a[2]);
+        return THPVariable_Wrap(released([&] { return gated_act(x, act, hold); }));
     });
 }
 // y and the copy in 8 bits, as a training step keeps it
@@ -633,7 +658,8 @@ PyObject *py_gated_act_held(PyObject *, PyObject *const *a, Py_ssize_t n) {
         expect(n, 2);
         const Tensor x = tensor_of(a[0], "x");
         no_gradient("gated_act_held", x);
-        return wrap(gate_forward(describe_gate(x, int64_t(number_of(a[1], "act"))), x, true));
+        const int64_t act = int64_t(number_of(a[1], "act"));
+        return wrap(released([&] { return gate_forward(describe_gate(x, act), x, true); }));
     });
 }
 PyObject *py_set_error(PyObject *, PyObject *type) {

@@ -2,6 +2,9 @@
 past the caches (over 16 MB, in whole 16-byte accesses), a workgroup's second turn, two accesses of
 a wave in uneven rows. References and tolerances are those of test_gpu_layer_ops."""
 import math
+import sys
+import threading
+import time
 
 import pytest
 
@@ -225,3 +228,52 @@ def test_linear_int8_of_scales_of_any_size(torch, bev, rows, channels, features)
     fine = (xp[:, None] + wp).abs() <= 100
     tol = 3 * U32 * product.abs() + 2 * U32 * ref.abs() + 2.0 ** -126
     _check("y", torch.where(fine, y, 0), torch.where(fine, ref, 0), tol)
+
+
+def test_other_threads_run_during_calls(torch, bev):
+    """A Python thread that waits for the interpreter's lock, which nothing else here gives away (results
+    are kept: freeing one may), gets it while another one calls: a call that has to wait for the device
+    holds nobody else up."""
+    x, place = torch.randn(1, 64, device="cuda"), torch.zeros(1, 1, dtype=torch.int64, device="cuda")
+    turned, f = x.view(1, 1, 4, 16), bev.rotary_frequencies(8, device="cuda")
+    held, scale = bev.quantize_int8(x)
+    calls = [lambda: bev.rms_norm(x), lambda: bev.rms_norm_int8(x), lambda: bev.quantize_int8(x), lambda: bev.gated_act(x),
+             lambda: bev.linear_int8(held, scale, held, scale), lambda: bev.rotary(turned, place, f)]
+    interval = sys.getswitchinterval()
+    for i, call in enumerate(calls):
+        go, ran, kept = threading.Event(), [], [call()]
+
+        def run():
+            go.wait()
+            ran.append(True)
+
+        other = threading.Thread(target=run)
+        other.start()
+        time.sleep(0.01)
+        sys.setswitchinterval(1000.0)
+        try:
+            go.set()
+            end = time.monotonic() + 2
+            while not ran and time.monotonic() < end:
+                kept.append(call())
+            got = bool(ran)
+        finally:
+            sys.setswitchinterval(interval)
+            other.join()
+        torch.cuda.synchronize()
+        assert got, f"call {i}"
+
+
+def test_hooks_that_raise(torch, bev):
+    """What a hook on saved tensors raises comes out of the call."""
+    x = torch.randn(4, 16, device="cuda", requires_grad=True)
+    place, f = torch.arange(4, device="cuda")[None], bev.rotary_frequencies(2, device="cuda")
+
+    def pack(t):
+        raise KeyError("not kept")
+
+    for call in (lambda: bev.rms_norm(x), lambda: bev.gated_act(x), lambda: bev.gated_act(x, checkpoint="int8"),
+                 lambda: bev.rotary(x.view(1, 4, 2, 8), place, f)):
+        with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t), pytest.raises(KeyError, match="not kept"):
+            call()
+        call()
