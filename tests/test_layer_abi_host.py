@@ -4,8 +4,11 @@ import ctypes
 import inspect
 import math
 import os
+import re
+import struct
 import subprocess
 import sys
+import tempfile
 
 import pytest
 
@@ -288,6 +291,7 @@ def test_rotary_frequencies():
 def test_star_import_needs_no_torch():
     code = """
 import sys
+import tempfile
 sys.modules["torch"] = None            # an import of torch raises ImportError
 from paper_2205_13542_amd import *
 for call in (lambda: rms_norm(None), lambda: rms_norm_add(None, None), lambda: rms_norm_int8(None),
@@ -312,3 +316,49 @@ def test_package_names_are_the_operators():
                  "rotary", "rotary_frequencies", "gated_act"):
         assert name in bev.__all__
         assert inspect.signature(getattr(bev, name)) == inspect.signature(getattr(layer_ops, name))
+
+
+def _kernels(path):
+    """Registers, spills and scratch of the kernels in a library that was built here, from the notes of its
+    gfx950 code objects."""
+    data = open(path, "rb").read()
+    readelf = "/opt/rocm/llvm/bin/llvm-readelf"
+    magic, at, out = b"__CLANG_OFFLOAD_BUNDLE__", 0, {}
+    while (at := data.find(magic, at)) >= 0:
+        count, = struct.unpack_from("<Q", data, at + 24)
+        entry = at + 32
+        for _ in range(count):
+            offset, size, length = struct.unpack_from("<QQQ", data, entry)
+            name = data[entry + 24:entry + 24 + length].decode()
+            entry += 24 + length
+            if "gfx950" not in name or not size:
+                continue
+            with tempfile.NamedTemporaryFile(suffix=".co") as f:
+                f.write(data[at + offset:at + offset + size])
+                f.flush()
+                notes = subprocess.run([readelf, "--notes", f.name], capture_output=True, text=True, check=True).stdout
+            for kernel in re.split(r"\n  - \.", notes)[1:]:
+                name = re.search(r"\.name: +(\S+)", kernel)
+                if name:
+                    out[name.group(1)] = {k: int(v) for k, v in re.findall(r"\.(\w+): +(\d+)\n", kernel)}
+        at += len(magic)
+    return out
+
+
+def test_kernels_neither_spill_nor_use_scratch(lib):
+    """The kernels of linear_int8 whose rows go through the registers hold up to 240 of them; an earlier
+    form of these spilled and had wrong sums. (Scalar registers of other kernels may be kept in lanes of
+    vector registers.)"""
+    from paper_2205_13542_amd import _binding
+    if not os.path.exists("/opt/rocm/llvm/bin/llvm-readelf"):
+        pytest.skip("no llvm-readelf")
+    kernels = _kernels(_binding.LIB_PATH)
+    counts = dict.fromkeys(("k_linear", "k_rms", "k_quantize_long", "k_turn", "k_gate"), 0)
+    for name, held in kernels.items():
+        for part in counts:
+            if part in name:
+                counts[part] += 1
+                assert held["vgpr_spill_count"] == held["private_segment_fixed_size"] == 0, (name, held)
+                assert part != "k_linear" or held["sgpr_spill_count"] == 0, (name, held)
+                break
+    assert counts["k_linear"] >= 15 and all(counts.values()), counts
