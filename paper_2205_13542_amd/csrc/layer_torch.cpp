@@ -539,7 +539,6 @@ auto released(F body) {
 template <class F>
 PyObject *guarded(F body) {
     try {
-        not_traced();
         return body();
     } catch (const Refused &r) {
         PyObject *e = PyObject_CallFunction(g_error ? g_error : PyExc_RuntimeError, "is", r.code, r.message.c_str());
@@ -601,6 +600,7 @@ void expect(Py_ssize_t got, Py_ssize_t want) {
 
 PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 5);
         const Tensor x = tensor_of(a[0], "x"), residual = maybe_tensor(a[1], "residual"), weight = maybe_tensor(a[2], "weight");
         const double eps = number_of(a[3], "eps");
@@ -611,6 +611,7 @@ PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *py_rms_norm_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 4);
         const Tensor x = tensor_of(a[0], "x"), residual = maybe_tensor(a[1], "residual"), weight = maybe_tensor(a[2], "weight");
         const double eps = number_of(a[3], "eps");
@@ -619,6 +620,7 @@ PyObject *py_rms_norm_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *py_quantize_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 1);
         const Tensor x = tensor_of(a[0], "x");
         return wrap(released([&] { return quantize_int8(x); }));
@@ -626,6 +628,7 @@ PyObject *py_quantize_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *py_linear_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 6);
         const Tensor x = tensor_of(a[0], "x"), x_scale = tensor_of(a[1], "x_scale"), weight = tensor_of(a[2], "weight"),
                      weight_scale = tensor_of(a[3], "weight_scale"), bias = maybe_tensor(a[4], "bias");
@@ -635,6 +638,7 @@ PyObject *py_linear_int8(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 5);
         const Tensor x = tensor_of(a[0], "x"), positions = tensor_of(a[1], "positions"),
                      frequencies = tensor_of(a[2], "frequencies");
@@ -645,6 +649,7 @@ PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *py_gated_act(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 3);
         const Tensor x = tensor_of(a[0], "x");
         const int64_t act = int64_t(number_of(a[1], "act"));
@@ -655,11 +660,29 @@ PyObject *py_gated_act(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // y and the copy in 8 bits, as a training step keeps it
 PyObject *py_gated_act_held(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
+        not_traced();
         expect(n, 2);
         const Tensor x = tensor_of(a[0], "x");
         no_gradient("gated_act_held", x);
         const int64_t act = int64_t(number_of(a[1], "act"));
         return wrap(released([&] { return gate_forward(describe_gate(x, act), x, true); }));
+    });
+}
+// How tensors (or None) lie: sizes, strides, types and devices as bytes, to compare with others
+PyObject *py_layout(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        c10::SmallVector<int64_t, 96> lie;
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            if (a[i] == Py_None) {
+                lie.push_back(-1);
+                continue;
+            }
+            const Tensor t = tensor_of(a[i], "a tensor");
+            lie.append({t.dim(), int64_t(t.scalar_type()), int64_t(t.device().type()), t.device().index(), t.is_neg()});
+            lie.append(t.sizes().begin(), t.sizes().end());
+            lie.append(t.strides().begin(), t.strides().end());
+        }
+        return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(lie.data()), Py_ssize_t(lie.size() * sizeof(int64_t)));
     });
 }
 PyObject *py_set_error(PyObject *, PyObject *type) {
@@ -671,7 +694,7 @@ PyObject *py_set_error(PyObject *, PyObject *type) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(rms_norm),    FAST(rms_norm_int8), FAST(quantize_int8),    FAST(linear_int8),
-                           FAST(rotary),      FAST(gated_act),     FAST(gated_act_held),
+                           FAST(rotary),      FAST(gated_act),     FAST(gated_act_held), FAST(layout),
                            {"set_error", py_set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_layer_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

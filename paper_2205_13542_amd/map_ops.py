@@ -20,10 +20,16 @@ from torch.autograd import forward_ad
 from . import _binding, _map_binding
 from ._binding import BevpoolError
 
+try:
+    from . import _layer_native as _native
+except ImportError:             # a build without it
+    _native = None
+
 _ACTS = {"none": _map_binding.BEVMAP_ACT_NONE, "relu": _map_binding.BEVMAP_ACT_RELU,
          "silu": _map_binding.BEVMAP_ACT_SILU, "gelu": _map_binding.BEVMAP_ACT_GELU}
 _CODES = {torch.float32: _binding.BEVPOOL_F32, torch.bfloat16: _binding.BEVPOOL_BF16,
           torch.float16: _binding.BEVPOOL_F16}
+_DTYPES = {code: dtype for dtype, code in _CODES.items()}
 
 _MOST = (1 << 31) - 1       # of a size in the C descriptions, where ctypes would wrap it round
 
@@ -130,7 +136,41 @@ def _norm_forward(x, groups, weight, bias, eps, act, out_dtype):
     return y, stats, norm
 
 
-def _norm_backward(norm, stats, dy, x, weight, bias, want_weight, want_bias):
+def _layout_of(*tensors):
+    return [None if t is None else (t.shape, t.stride(), t.dtype, t.device, t.is_neg()) for t in tensors]
+
+
+# How tensors lie, to compare with how others do; native for its host time
+_layout = _layout_of if _native is None else _native.layout
+
+
+def _check_saved(index, *expected):
+    """What a forward saved, as a hook on saved tensors brought it back: other strides are looked at by the
+    callers, anything else is refused."""
+    for t, shape, dtype in expected:
+        if t is not None and (t.shape != shape or t.dtype != dtype or t.get_device() != index or t.is_neg()):
+            _refuse("a saved tensor came back with another size, dtype or device",
+                    _binding.BEVPOOL_ERR_SHAPE_MISMATCH)
+
+
+def _whole(t):
+    return t if t is None or t.is_contiguous() else t.contiguous()
+
+
+def _norm_brought_back(norm, index, shape, x, weight, bias, stats):
+    C, w_dtype = norm.channels, _DTYPES[norm.weight_dtype]
+    _check_saved(index, (x, shape, _DTYPES[norm.x_dtype]), (weight, (C,), w_dtype), (bias, (C,), w_dtype),
+                 (stats, (2, norm.batch, norm.groups), torch.float32))
+    norm = type(norm).from_buffer_copy(norm)
+    norm.row_stride = _row_stride(x)
+    if norm.row_stride is None:
+        x, norm.row_stride = x.contiguous(), C
+    return norm, x, _whole(weight), _whole(bias), _whole(stats)
+
+
+def _norm_backward(norm, layout, stats, dy, x, weight, bias, want_weight, want_bias):
+    if _layout(x, weight, bias, stats) != layout:
+        norm, x, weight, bias, stats = _norm_brought_back(norm, dy.get_device(), dy.shape, x, weight, bias, stats)
     dy = dy.contiguous()
     size = _map_binding.bevmap_group_norm_workspace(norm, True)
     dx = _empty_like(x)
@@ -189,7 +229,29 @@ def _attend_forward(q, k, v, scale, key_lengths, key_mask, train):
     return out, low, lse, attend, back_size
 
 
-def _attend_backward(attend, size, dout, q, k, v, key_lengths, key_mask, out, low, lse):
+def _attend_brought_back(attend, index, q, k, v, key_lengths, key_mask, out, low, lse):
+    B, N, M, H, K, D = attend.batch, attend.queries, attend.keys, attend.heads, attend.key_heads, attend.dim
+    dtype, asked, states = _DTYPES[attend.dtype], (B, N, H, D), (B, M, K, D)
+    _check_saved(index, (q, asked, dtype), (k, states, dtype), (v, states, dtype), (out, asked, dtype),
+                 (low, asked, dtype), (lse, (B, H, N), torch.float32), (key_lengths, (B,), torch.int32),
+                 (key_mask, (B, M), torch.bool))
+    attend = type(attend).from_buffer_copy(attend)
+    heads = []
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        heads.append(t if D <= 1 or t.stride(3) == 1 else t.contiguous())
+        for dim, part in enumerate(("batch", "row", "head")):
+            setattr(attend, f"{name}_{part}", heads[-1].stride(dim))
+    if key_mask is not None:
+        key_mask = key_mask if M <= 1 or key_mask.stride(1) == 1 else key_mask.contiguous()
+        attend.mask_batch = key_mask.stride(0)
+    size = _map_binding.bevmap_attention_workspace(attend, True)
+    return attend, size, *heads, _whole(key_lengths), key_mask, _whole(out), _whole(low), _whole(lse)
+
+
+def _attend_backward(attend, size, layout, dout, q, k, v, key_lengths, key_mask, out, low, lse):
+    if _layout(q, k, v, key_lengths, key_mask, out, low, lse) != layout:
+        attend, size, q, k, v, key_lengths, key_mask, out, low, lse = _attend_brought_back(
+            attend, dout.get_device(), q, k, v, key_lengths, key_mask, out, low, lse)
     dout = dout.contiguous()
     dq, dk, dv = _empty_like(q), _empty_like(k), _empty_like(v)
     temp = q.new_empty(size, dtype=torch.uint8)
@@ -220,7 +282,8 @@ def _dropout(x, threshold, seed, offset, residual):
 class _GroupNormAct(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
-        y, stats, ctx.norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
+        y, stats, norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
+        ctx.norm = norm, _layout(x, weight, bias, stats)
         ctx.save_for_backward(x, weight, bias, stats)
         return y
 
@@ -229,14 +292,15 @@ class _GroupNormAct(torch.autograd.Function):
         _first_order_only()
         x, weight, bias, stats = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dw, db = _norm_backward(ctx.norm, stats, dy, x, weight, bias, need[1], need[2])
+        dx, dw, db = _norm_backward(*ctx.norm, stats, dy, x, weight, bias, need[1], need[2])
         return dx if need[0] else None, dw, db, None, None, None, None
 
 
 class _CrossAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, key_lengths, key_mask):
-        out, low, lse, *ctx.attend = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
+        out, low, lse, attend, size = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
+        ctx.attend = attend, size, _layout(q, k, v, key_lengths, key_mask, out, low, lse)
         ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
         return out
 

@@ -861,3 +861,37 @@ def test_refusals_of_sizes_past_32_bits(torch, bev):
         with pytest.raises(bev.BevpoolError):
             call()
             print(f"call {i} was not refused", flush=True)
+
+
+def test_hooks_on_saved_tensors(torch, bev):
+    """Saved tensors that come back with other strides, or from the host, give the same gradients."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *shape: torch.randn(shape, generator=gen, device="cuda")    # noqa: E731
+
+    def spread(t):                                  # each row followed by a row of something else
+        room = torch.ones((*t.shape[:-1], 2 * t.shape[-1]), dtype=t.dtype, device=t.device)
+        room[..., :t.shape[-1]] = t
+        return room[..., :t.shape[-1]]
+
+    hooks = [lambda: torch.autograd.graph.save_on_cpu(),
+             lambda: torch.autograd.graph.saved_tensors_hooks(spread, lambda t: t),
+             lambda: torch.autograd.graph.saved_tensors_hooks(
+                 lambda t: t, lambda t: t.clone(memory_format=torch.contiguous_format))]
+    x, w, b = normal(2, 9, 11, 72)[..., 24:48], normal(24), normal(24)
+    q, kv = normal(2, 7, 3 * 64).bfloat16()[..., 64:128].unflatten(-1, (4, 16)), normal(2, 200, 2, 4, 16).bfloat16()
+    mask = (torch.rand(2, 300, generator=gen, device="cuda") < 0.7)[:, :200]
+    lengths = torch.tensor([200, 90], dtype=torch.int32, device="cuda")
+    calls = [(lambda x, w, b: bev.group_norm_act(x, 6, w, b, act="silu"), (x, w, b)),
+             (lambda x, w, b: bev.group_norm_act(x, 6, w, b, act="gelu"), (x.bfloat16(), w, b)),
+             (lambda q, k, v: bev.cross_attention(q, k, v, None, lengths, mask), (q, kv[:, :, 0], kv[:, :, 1])),
+             (lambda q, k, v: bev.cross_attention(q, k, v, None, None, mask),
+              (q.float(), kv[:, :, 0].float(), kv[:, :, 1].float()))]
+    for call, inputs in calls:
+        leaves = [t.detach().requires_grad_() for t in inputs]
+        y = call(*leaves)
+        dy = torch.randn(y.shape, generator=gen, device="cuda").to(y.dtype)
+        ref = torch.autograd.grad(y, leaves, dy)
+        for hook in hooks:
+            with hook():
+                y = call(*leaves)
+            assert all(torch.equal(a, r) for a, r in zip(torch.autograd.grad(y, leaves, dy), ref))

@@ -224,3 +224,66 @@ def test_package_names_are_the_map_operators():
     for name in ("group_norm_act", "cross_attention", "dropout_add"):
         assert name in bev.__all__
         assert inspect.signature(getattr(bev, name)) == inspect.signature(getattr(map_ops, name))
+
+
+def test_backward_describes_saved_tensors_as_they_come_back(monkeypatch):
+    """A hook on saved tensors may bring a strided input back contiguous, or in other rows: what the library
+    is told of it then has to be that, or it reads past its end. (Nothing runs here: calls are recorded.)"""
+    torch = pytest.importorskip("torch")
+    from paper_2205_13542_amd import map_ops
+    calls = []
+    monkeypatch.setattr(map_ops, "_device", lambda first, *others: 0)
+    monkeypatch.setattr(map_ops, "_call", lambda function, index, *args: calls.append(args))
+
+    def spread(t):                                  # each row followed by a row of something else
+        room = t.new_zeros((*t.shape[:-1], 2 * t.shape[-1]))
+        room[..., :t.shape[-1]] = t
+        return room[..., :t.shape[-1]]
+
+    keep = lambda t: t                              # noqa: E731
+    hooks = [(keep, keep), (lambda t: t.contiguous().clone(), keep), (spread, keep), (keep, lambda t: t.clone(
+        memory_format=torch.contiguous_format))]
+    q = torch.zeros(2, 6, 3 * 16)[..., 16:32].unflatten(-1, (2, 8))
+    kv = torch.zeros(2, 9, 2, 2, 8)
+    mask = torch.ones(2, 20, dtype=torch.bool)[:, :9]
+    for pack, unpack in hooks:
+        kept = {}
+
+        def back(t, unpack=unpack, kept=kept):
+            t = unpack(t)
+            kept[t.data_ptr()] = t
+            return t
+
+        x, w = torch.zeros(2, 3, 5, 24)[..., 8:16].requires_grad_(), torch.ones(8, requires_grad=True)
+        with torch.autograd.graph.saved_tensors_hooks(pack, back):
+            y = map_ops.group_norm_act(x, 2, w, w.detach(), act="silu")
+            torch.autograd.grad(y, (x, w), torch.zeros_like(y))
+        norm, _, at, *rest = calls[-1]
+        assert norm.row_stride == kept[at].stride(2) if at in kept else norm.row_stride == 8
+        for pointer in rest[:3]:                    # weight, bias, mean
+            assert pointer not in kept or kept[pointer].is_contiguous()
+
+        a, k, v = q.detach().requires_grad_(), kv[:, :, 0].requires_grad_(), kv[:, :, 1].requires_grad_()
+        kept.clear()
+        with torch.autograd.graph.saved_tensors_hooks(pack, back):
+            y = map_ops.cross_attention(a, k, v, key_mask=mask)
+            torch.autograd.grad(y, (a, k, v), torch.zeros_like(y))
+        attend, _, *at = calls[-1]
+        for name, pointer in zip("qkv", at):
+            got = tuple(getattr(attend, f"{name}_{part}") for part in ("batch", "row", "head"))
+            assert got == kept[pointer].stride()[:3] and kept[pointer].stride(3) == 1
+        assert at[4] not in kept or attend.mask_batch == kept[at[4]].stride(0)
+
+
+def test_backward_refuses_saved_tensors_of_another_kind(monkeypatch):
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import map_ops
+    monkeypatch.setattr(map_ops, "_device", lambda first, *others: 0)
+    monkeypatch.setattr(map_ops, "_call", lambda function, index, *args: None)
+    x, q = torch.zeros(2, 5, 8, requires_grad=True), torch.zeros(2, 3, 2, 8, requires_grad=True)
+    for change in (lambda t: t[..., :1].clone(), lambda t: t.double()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+            for y, leaf in ((map_ops.group_norm_act(x, 2), x), (map_ops.cross_attention(q, q, q), q)):
+                with pytest.raises(bev.BevpoolError, match="saved tensor"):
+                    torch.autograd.grad(y, leaf, torch.zeros_like(y))
