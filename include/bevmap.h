@@ -313,7 +313,8 @@ typedef enum { BEVMAP_POSITION_I32 = 0, BEVMAP_POSITION_I64 = 1, BEVMAP_POSITION
  *   t = positions[token][p / (pairs / axes)] * frequencies[p].
  * Later channels keep their values. Positions have `axes` numbers a token: with two axes
  * the first half of the pairs turns with the first. Angles are formed and reduced in 64
- * bits; the turn is fp32, and its result is rounded once.
+ * bits, as exactly for positions up to 2^53 in magnitude as for near ones; the turn is fp32,
+ * and its result is rounded once.
  * Element (b, n, h, c) of x is at x + b * x_batch + n * x_row + h * x_head + c, strides in
  * elements.
  */

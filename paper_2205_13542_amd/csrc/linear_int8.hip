@@ -11,10 +11,10 @@
 //
 // Two forms. Tiles: a workgroup stages kStep bytes of its rows and channels in LDS, two
 // stages in turn, the next on its way (past the registers, where rows are 16-byte
-// aligned) while the matrix cores work: 16896 x 2048 x 4096 (tokens, k, channels) takes 158
-// to 172 us, 8192^3 531, 2070 TOP/s (a library product without scales 171 and 541). Rows of
+// aligned) while the matrix cores work: 16896 x 2048 x 4096 (tokens, k, channels) takes 150
+// to 161 us, 8192^3 468, 2350 TOP/s (a library product without scales 170 and 445). Rows of
 // any other alignment go through the registers, with no branch of a lane's own on the way, so
-// that all loads of a stage are under way at a time: 16390 x 1025 x 1021 takes 42 us. Few
+// that all loads of a stage are under way at a time: 16390 x 1025 x 1021 takes 38 to 42 us. Few
 // tokens: the weights are what is read, so a workgroup takes 16 channels, its waves share out
 // k and join their sums in LDS: 64 x 4096 x 2048 takes 5.1 us.
 #include "mapops.h"

@@ -85,7 +85,7 @@ def rms_norm_add_int8(x, residual, weight=None, eps=1e-6):
 def quantize_int8(x):
     """Rows in 8 bits: x [...][C] (fp32, bf16 or fp16; evenly spaced rows) gives
     (held int8 [...][C], scale fp32 [...]): scale the row's largest magnitude
-    over 127, held = round(x / scale), halves to the even neighbour. A row of
+    over 127, held = round(x * (127 / that magnitude)), halves to the even neighbour. A row of
     zeros has scale 0, one with an infinity or a NaN scale NaN. For weights
     (a row is an output channel) and activations of ``linear_int8``. Has no
     gradient."""
@@ -115,8 +115,8 @@ def rotary(x, positions, frequencies, interleaved=False, amplitude=1.0):
     [B][N][axes] for places along several axes (a cell's, in a map): P is a
     multiple of axes, and each P / axes neighbouring pairs turn with one axis.
 
-    Angles are formed and reduced in 64 bits, so far positions are as exact as
-    near ones; the turn, times amplitude, is fp32 and rounded once. An infinite
+    Angles are formed and reduced in 64 bits, so far positions, up to 2^53 in
+    magnitude, are as exact as near ones; the turn, times amplitude, is fp32 and rounded once. An infinite
     position gives NaN. Differentiable in x."""
     return _native.rotary(x, positions, frequencies, interleaved, amplitude)
 
