@@ -49,16 +49,16 @@ struct Refused {
 struct Tangent {};
 
 // torch's dispatcher sees nothing of these calls, so that a tracer would keep the result of
-// the inputs that it traces with as a constant: refused, under torch.jit.trace, and under
-// make_fx (whose mode is on the dispatcher's stack, or on one of its own ahead of autograd,
+// the inputs that it traces with as a constant (of the map operators, an empty tensor that
+// nothing fills): refused, under torch.jit.trace, and under make_fx (whose mode is on the dispatcher's stack, or on one of its own ahead of autograd,
 // which this key stands for).
-void not_traced() {
+void not_traced(bool jit = true) {
     using c10::impl::TorchDispatchModeKey;
     using c10::impl::TorchDispatchModeTLS;
-    if (torch::jit::tracer::isTracing() ||
+    if ((jit && torch::jit::tracer::isTracing()) ||
         (TorchDispatchModeTLS::any_modes_set() && TorchDispatchModeTLS::get_mode(TorchDispatchModeKey::PROXY)) ||
         c10::impl::tls_local_dispatch_key_set().included_.has(c10::DispatchKey::PreDispatch))
-        refuse("the operators around attention cannot be traced: the result would be recorded as a constant");
+        refuse("the operators cannot be traced: their results would be recorded as constants, or as empty tensors");
 }
 
 std::string shape_of(const Tensor &t) { return c10::str("[", c10::Join(", ", t.sizes()), "]"); }
@@ -685,6 +685,13 @@ PyObject *py_layout(PyObject *, PyObject *const *a, Py_ssize_t n) {
         return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(lie.data()), Py_ssize_t(lie.size() * sizeof(int64_t)));
     });
 }
+// not_traced(False): by torch.jit.trace the call may be
+PyObject *py_not_traced(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        not_traced(n < 1 || truth_of(a[0]));
+        Py_RETURN_NONE;
+    });
+}
 PyObject *py_set_error(PyObject *, PyObject *type) {
     Py_XDECREF(g_error);
     Py_INCREF(type);
@@ -695,6 +702,7 @@ PyObject *py_set_error(PyObject *, PyObject *type) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(rms_norm),    FAST(rms_norm_int8), FAST(quantize_int8),    FAST(linear_int8),
                            FAST(rotary),      FAST(gated_act),     FAST(gated_act_held), FAST(layout),
+                           FAST(not_traced),
                            {"set_error", py_set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_layer_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -6,7 +6,9 @@
 
 Each runs in libbevpool.so (include/bevmap.h) on the current stream of its
 inputs' device, and is differentiable (backwards; inputs with a tangent of
-torch.autograd.forward_ad are refused). Temporaries come from torch's allocator.
+torch.autograd.forward_ad are refused). Calls that are being traced by make_fx, or
+without gradients by torch.jit.trace, are refused: their results would be recorded
+as empty tensors. Temporaries come from torch's allocator.
 There is no CPU form: tensors elsewhere are refused with a BevpoolError, as
 are types and layouts that a call does not take (nothing is copied silently).
 """
@@ -22,6 +24,7 @@ from ._binding import BevpoolError
 
 try:
     from . import _layer_native as _native
+    _native.set_error(BevpoolError)
 except ImportError:             # a build without it
     _native = None
 
@@ -74,6 +77,17 @@ def _device(first, *others) -> int:
         if t is not None and t.get_device() != index:
             _refuse("all tensors must be on one device")
     return index
+
+
+def _jit_not_traced(jit=True):
+    if jit and torch.jit.is_tracing():
+        _refuse("the operators cannot be traced: their results would be recorded as empty tensors")
+
+
+# Refuses a call that is being traced (torch.jit.trace, make_fx), which sees the allocation of a
+# result but not what fills it. An autograd function is called again by what torch.jit.trace makes
+# of it: _not_traced(False) lets that pass.
+_not_traced = _jit_not_traced if _native is None else _native.not_traced
 
 
 def _call(function, index, *args):
@@ -282,6 +296,7 @@ def _dropout(x, threshold, seed, offset, residual):
 class _GroupNormAct(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, eps, act, out_dtype):
+        _not_traced(False)
         y, stats, norm = _norm_forward(x, groups, weight, bias, eps, act, out_dtype)
         ctx.norm = norm, _layout(x, weight, bias, stats)
         ctx.save_for_backward(x, weight, bias, stats)
@@ -299,6 +314,7 @@ class _GroupNormAct(torch.autograd.Function):
 class _CrossAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, key_lengths, key_mask):
+        _not_traced(False)
         out, low, lse, attend, size = _attend_forward(q, k, v, scale, key_lengths, key_mask, True)
         ctx.attend = attend, size, _layout(q, k, v, key_lengths, key_mask, out, low, lse)
         ctx.save_for_backward(q, k, v, key_lengths, key_mask, out, low, lse)
@@ -316,6 +332,7 @@ class _CrossAttention(torch.autograd.Function):
 class _DropoutAdd(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, threshold, seed, offset):
+        _not_traced(False)
         ctx.draw = threshold, seed, offset
         return _dropout(x, threshold, seed, offset, residual)
 
@@ -354,6 +371,7 @@ def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", out_
     rounded once. Differentiable in x, weight and bias."""
     if _learns(x, weight, bias):
         return _GroupNormAct.apply(x, weight, bias, groups, eps, act, out_dtype)
+    _not_traced()
     return _norm_forward(x, groups, weight, bias, eps, act, out_dtype)[0]
 
 
@@ -378,6 +396,7 @@ def cross_attention(q, k, v, scale=None, key_lengths=None, key_mask=None):
     states. Differentiable in q, k and v, bitwise reproducible."""
     if _learns(q, k, v):
         return _CrossAttention.apply(q, k, v, scale, key_lengths, key_mask)
+    _not_traced()
     return _attend_forward(q, k, v, scale, key_lengths, key_mask, False)[0]
 
 
@@ -398,4 +417,5 @@ def dropout_add(x, p, seed, offset=0, residual=None):
     threshold = int(65536 * p + 0.5)
     if _learns(x, residual):
         return _DropoutAdd.apply(x, residual, threshold, seed, offset)
+    _not_traced()
     return _dropout(x, threshold, seed, offset, residual)

@@ -287,3 +287,39 @@ def test_backward_refuses_saved_tensors_of_another_kind(monkeypatch):
             for y, leaf in ((map_ops.group_norm_act(x, 2), x), (map_ops.cross_attention(q, q, q), q)):
                 with pytest.raises(bev.BevpoolError, match="saved tensor"):
                     torch.autograd.grad(y, leaf, torch.zeros_like(y))
+
+
+@pytest.mark.parametrize("tracer", ["jit", "real", "pre_dispatch"])
+def test_tracing_is_refused(monkeypatch, tracer):
+    """A tracer sees that a result is allocated and not what fills it. (Where a gradient is asked for,
+    what torch.jit.trace makes calls the autograd function again.)"""
+    torch = pytest.importorskip("torch")
+    import paper_2205_13542_amd as bev
+    from paper_2205_13542_amd import map_ops
+    from torch.fx.experimental.proxy_tensor import make_fx
+    monkeypatch.setattr(map_ops, "_device", lambda first, *others: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    ran = []
+    for name in ("bevmap_group_norm", "bevmap_attention", "bevmap_dropout"):
+        monkeypatch.setattr(map_ops._map_binding, name, lambda *args: ran.append(args))
+    x, leaf = torch.ones(1, 4, 2, 8), torch.ones(1, 4, 2, 8, requires_grad=True)
+
+    def trace(call, x=x):
+        if tracer == "jit":
+            return torch.jit.trace(call, (x,), check_trace=False)
+        return make_fx(call, tracing_mode="real", pre_dispatch=tracer == "pre_dispatch")(x)
+
+    for call in (lambda x: map_ops.group_norm_act(x, 2), lambda x: map_ops.cross_attention(x, x, x),
+                 lambda x: map_ops.dropout_add(x, 0.1, 3)):
+        for enabled in (True, False):
+            with torch.set_grad_enabled(enabled), pytest.raises(bev.BevpoolError, match="cannot be traced"):
+                trace(call)
+        call(x)
+        if tracer == "jit":
+            again, before = trace(call, leaf), len(ran)
+            again(leaf)
+            assert len(ran) == before + 1
+        else:
+            with pytest.raises(bev.BevpoolError, match="cannot be traced"):
+                trace(call, leaf)
