@@ -277,3 +277,40 @@ def test_hooks_that_raise(torch, bev):
         with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t), pytest.raises(KeyError, match="not kept"):
             call()
         call()
+
+
+def test_calls_of_several_threads(torch, bev):
+    """Threads that call at the same time, each on a stream of its own, steps among them."""
+    normal = _normal(torch, 1)
+    place, f = torch.arange(300, device="cuda")[None], bev.rotary_frequencies(16, device="cuda")
+    inputs = [(normal(300, 512).bfloat16(), normal(300, 512).bfloat16(), normal(300, 512).bfloat16()) for _ in range(4)]
+    w, weights = 1 + normal(512, s=0.1), bev.quantize_int8(normal(700, 512))
+
+    def work(x, r, dy):
+        x, r = x.clone().requires_grad_(), r.clone().requires_grad_()
+        y, total = bev.rms_norm_add(x, r, w)
+        z = bev.rotary(y.view(1, 300, 8, 64), place, f).view(300, 512)
+        z = bev.gated_act(torch.cat((z, total), -1), "gelu", "int8")
+        held, scale = bev.rms_norm_int8(x.detach(), w)
+        return [z.detach(), *torch.autograd.grad(z, (x, r), dy), held, bev.linear_int8(held, scale, *weights)]
+
+    refs, wrong = [work(*i) for i in inputs], []
+    torch.cuda.synchronize()
+
+    def run(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(30):
+                    got = work(*inputs[k])
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, refs[k])):
+                        wrong.append(k)
+        except Exception as e:                      # noqa: BLE001
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
